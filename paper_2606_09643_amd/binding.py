@@ -41,7 +41,8 @@ EXPORTS = ("vfm_status_string", "vfm_plan_size", "vfm_plan", "vfm_workspace_size
            "vfm_embed_series", "vfm_encoder_attach", "vfm_layer_forward_paged", "vfm_greedy_tokens",
            "vfm_pages_state_size", "vfm_pages_init", "vfm_pages_reserve", "vfm_pages_release",
            "vfm_pages_table", "vfm_pages_count", "vfm_bfq_charge",
-           "vfm_layer_forward_noalloc")
+           "vfm_layer_forward_noalloc", "vfm_kv_append", "vfm_attention_workspace", "vfm_attention_paged",
+           "vfm_workspace_size_windowed", "vfm_layer_forward_windowed", "vfm_sample_tokens")
 PROF_CLASSES = ("gemm_qkv", "gemm_o", "gemm_up", "gemm_down", "attn", "norm", "shrink", "other")
 
 
@@ -83,6 +84,15 @@ class vfm_head_table(C.Structure):
 class vfm_kv_pages(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int64), ("page_size", C.c_int32),
                 ("max_pages", C.c_int32), ("table_host", C.POINTER(C.c_int32)), ("table_dev", C.c_void_p)]
+
+
+class vfm_attn(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("window", C.c_int32), ("n_sink", C.c_int32), ("scale", C.c_float), ("rope_theta", C.c_float)]
+
+
+class vfm_sampling(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
 
 
 class vfm_pages_config(C.Structure):
@@ -153,6 +163,21 @@ def _lib_handle():
         lib.vfm_bfq_queued.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_int32)]
         lib.vfm_bfq_tags.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_double),
                                      C.POINTER(C.c_double)]
+        lib.vfm_kv_append.argtypes = [C.POINTER(vfm_attn), C.POINTER(vfm_batch), C.c_void_p, C.c_int64, C.c_void_p,
+                                      C.POINTER(vfm_kv_pages), C.c_void_p]
+        lib.vfm_attention_workspace.argtypes = [C.POINTER(vfm_attn), C.POINTER(vfm_batch), C.POINTER(C.c_size_t)]
+        lib.vfm_attention_paged.argtypes = [C.POINTER(vfm_attn), C.POINTER(vfm_batch), C.c_void_p, C.c_int64,
+                                            C.POINTER(vfm_kv_pages), C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t,
+                                            C.c_void_p]
+        lib.vfm_workspace_size_windowed.argtypes = [C.POINTER(vfm_cfg), C.POINTER(vfm_batch),
+                                                    C.POINTER(vfm_lora_table), C.c_int32, C.c_int32,
+                                                    C.POINTER(C.c_size_t)]
+        lib.vfm_layer_forward_windowed.argtypes = [C.POINTER(vfm_cfg), C.POINTER(vfm_layer_weights),
+                                                   C.POINTER(vfm_lora_table), C.POINTER(vfm_batch), C.c_void_p,
+                                                   C.POINTER(vfm_kv_pages), C.c_int32, C.c_int32, C.c_void_p,
+                                                   C.c_size_t, C.c_void_p]
+        lib.vfm_sample_tokens.argtypes = [C.POINTER(vfm_batch), C.c_void_p, C.POINTER(vfm_sampling), C.c_void_p,
+                                          C.c_void_p, C.c_void_p, C.c_void_p]
         for name in EXPORTS:
             getattr(lib, name).restype = C.c_int if name != "vfm_status_string" else C.c_char_p
         _LIB = lib
@@ -449,6 +474,126 @@ def vfm_encoder_attach(enc, task, W=None, b=None, stream=None):
 def vfm_greedy_tokens(batch, out, ids, stream=None):
     _check(_lib_handle().vfm_greedy_tokens(C.byref(batch), _ptr(out), _ptr(ids), _stream(stream)),
            "vfm_greedy_tokens")
+
+
+# ---- decoding over a bounded KV cache (include/vfm_decode.h) -----------------
+_TORCH_DTYPE = {VFM_F32: torch.float32, VFM_BF16: torch.bfloat16}
+
+
+def _operand(t, name, dtype, numel, device=None):
+    """t as the library takes it: of that type, dense, at least numel elements, on `device`."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+        raise ValueError(f"{name}: a {dtype} tensor is expected")
+    if not t.is_contiguous() or t.numel() < numel:
+        raise ValueError(f"{name}: a dense tensor of at least {numel} elements is expected")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, the other operands on {device}")
+    return t.data_ptr()
+
+
+def _rows(t, name, attn, batch, cols, device=None):
+    """(pointer, row stride) of a [T, cols or more] tensor whose rows are dense."""
+    T = batch.plan_host[2]
+    if not isinstance(t, torch.Tensor) or t.dtype != _TORCH_DTYPE[attn.dtype] or t.dim() != 2:
+        raise ValueError(f"{name}: a 2-dimensional {_TORCH_DTYPE[attn.dtype]} tensor is expected")
+    if t.shape[0] < T or t.shape[1] < cols or t.stride(1) != 1 or (T > 1 and t.stride(0) < cols):
+        raise ValueError(f"{name}: {T} dense rows of at least {cols} columns are expected")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, the other operands on {device}")
+    return t.data_ptr(), t.stride(0) if T > 1 else -(-cols // 8) * 8
+
+
+def _cache(kv, attn, device):
+    """The C struct of a PagedKV, its pools checked against the attention (a vfm_kv_pages is taken as it is)."""
+    if not isinstance(kv, PagedKV):
+        return kv
+    for t in (kv.k, kv.v):
+        if t.dtype != _TORCH_DTYPE[attn.dtype] or tuple(t.shape) != (attn.n_kv_heads, kv.c.n_pages * kv.c.page_size,
+                                                                     attn.head_dim) or not t.is_contiguous():
+            raise ValueError("the cache's pools are not [n_kv_heads, n_pages * page_size, head_dim] of the attention")
+        if t.device != device or kv.table_dev.device != device:
+            raise ValueError("the cache is on another device than the rows")
+    return kv.c
+
+
+def make_attn(dtype, n_heads, n_kv_heads, head_dim, window=0, n_sink=0, scale=0.0, rope_theta=0.0) -> vfm_attn:
+    return vfm_attn(dtype, n_heads, n_kv_heads, head_dim, window, n_sink, scale, rope_theta)
+
+
+def vfm_kv_append(attn, batch, qkv, q_out, kv, stream=None):
+    """qkv: [T, (n_heads + 2 n_kv_heads) * head_dim or more]; q_out: dense [T, n_heads * head_dim]."""
+    hd = attn.head_dim
+    p, ld = _rows(qkv, "qkv", attn, batch, (attn.n_heads + 2 * attn.n_kv_heads) * hd)
+    q = _operand(q_out, "q_out", qkv.dtype, batch.plan_host[2] * attn.n_heads * hd, qkv.device)
+    st = _lib_handle().vfm_kv_append(C.byref(attn), C.byref(batch), p, ld, q,
+                                     C.byref(_cache(kv, attn, qkv.device)), _stream(stream))
+    _check(st, "vfm_kv_append")
+
+
+def vfm_attention_workspace(attn, batch) -> int:
+    n = C.c_size_t()
+    _check(_lib_handle().vfm_attention_workspace(C.byref(attn), C.byref(batch), C.byref(n)),
+           "vfm_attention_workspace")
+    return n.value
+
+
+def vfm_attention_paged(attn, batch, q, kv, out, workspace=None, stream=None):
+    """q, out: [T, n_heads * head_dim or more], rows dense; kv: a PagedKV or a vfm_kv_pages."""
+    cols = attn.n_heads * attn.head_dim
+    pq, ldq = _rows(q, "q", attn, batch, cols)
+    po, ldo = _rows(out, "out", attn, batch, cols, q.device)
+    ws, nb = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
+    st = _lib_handle().vfm_attention_paged(C.byref(attn), C.byref(batch), pq, ldq,
+                                           C.byref(_cache(kv, attn, q.device)), po, ldo, ws, nb, _stream(stream))
+    _check(st, "vfm_attention_paged")
+
+
+def vfm_workspace_size_windowed(cfg, batch, lora=None, window=0, n_sink=0) -> int:
+    n = C.c_size_t()
+    st = _lib_handle().vfm_workspace_size_windowed(C.byref(cfg), C.byref(batch),
+                                                   C.byref(lora) if lora is not None else None, int(window),
+                                                   int(n_sink), C.byref(n))
+    _check(st, "vfm_workspace_size_windowed")
+    return n.value
+
+
+def vfm_layer_forward_windowed(cfg, weights, lora, batch, x, kv, window, n_sink, workspace, stream=None):
+    """kv: a PagedKV, or a vfm_kv_pages struct built by the caller."""
+    kvc = kv.c if isinstance(kv, PagedKV) else kv
+    st = _lib_handle().vfm_layer_forward_windowed(C.byref(cfg), C.byref(weights),
+                                                  C.byref(lora) if lora is not None else None, C.byref(batch),
+                                                  _ptr(x), C.byref(kvc), int(window), int(n_sink),
+                                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                                  _stream(stream))
+    _check(st, "vfm_layer_forward_windowed")
+
+
+class Sampling:
+    """Per-request sampling parameters on the device (original order, each
+    optional) as the C struct vfm_sampling."""
+
+    def __init__(self, temperature=None, top_k=None, top_p=None, min_p=None):
+        self.tensors = {"temperature": temperature, "top_k": top_k, "top_p": top_p, "min_p": min_p}
+        for n, t in self.tensors.items():
+            if t is not None and (t.dtype != (torch.int32 if n == "top_k" else torch.float32)
+                                  or not t.is_contiguous()):
+                raise ValueError(f"{n}: a dense {'int32' if n == 'top_k' else 'float32'} tensor is expected")
+        self.c = vfm_sampling(*[_ptr(t) for t in self.tensors.values()])
+
+
+def vfm_sample_tokens(batch, out, sampling, u, ids, logprob=None, stream=None):
+    """One token per request drawn from its head outputs; sampling: a Sampling."""
+    n = batch.plan_host[0]
+    po = _operand(out, "out", torch.float32, batch.plan_host[6])
+    for name, t in sampling.tensors.items():
+        if t is not None:
+            _operand(t, name, t.dtype, n, out.device)
+    st = _lib_handle().vfm_sample_tokens(C.byref(batch), po, C.byref(sampling.c),
+                                         _operand(u, "u", torch.float32, n, out.device),
+                                         _operand(ids, "ids", torch.int32, n, out.device),
+                                         _operand(logprob, "logprob", torch.float32, n, out.device)
+                                         if logprob is not None else None, _stream(stream))
+    _check(st, "vfm_sample_tokens")
 
 
 # ---- KV page allocator (host, include/vfm_pages.h) --------------------------

@@ -4,6 +4,7 @@
 #include <initializer_list>
 #include <mutex>
 
+#include "decode_internal.h"
 #include "vfm_internal.h"
 
 namespace {
@@ -76,7 +77,8 @@ struct LayerWs {
   int kchunks;
 };
 
-LayerWs layer_ws(const vfm_cfg& c, const Plan& pl, const vfm_lora_table* l, int max_keys) {
+// attn_bytes: the windowed attention's workspace in place of the attention's over max_keys keys.
+LayerWs layer_ws(const vfm_cfg& c, const Plan& pl, const vfm_lora_table* l, int max_keys, int64_t attn_bytes = -1) {
   const size_t es = elem_size(c.dtype);
   const size_t T = (size_t)pl.T;
   const int d = c.d_model, f = c.d_ff, rpad = rpad_of(l);
@@ -86,7 +88,7 @@ LayerWs layer_ws(const vfm_cfg& c, const Plan& pl, const vfm_lora_table* l, int 
   w.big = off;  off += align_up(T * std::max<size_t>(3 * (size_t)d, f) * es);
   w.attn = off; off += align_up(T * d * es);
   w.u = off;    off += align_up(T * 8 * rpad * es);
-  w.aws = off; off += align_up(attention_workspace(c, pl, max_keys));
+  w.aws = off; off += align_up(attn_bytes >= 0 ? (size_t)attn_bytes : attention_workspace(c, pl, max_keys));
   w.z = w.p = off;
   w.kchunks = 0;
   if (use_skinny(c, pl)) {
@@ -181,9 +183,142 @@ extern "C" int vfm_embed_forward(const vfm_cfg* cfg, const vfm_batch* batch, int
 
 namespace {
 
-// Checks shared by the two layer entry points (everything but the cache).
+// A paged cache's pool and tables.
+int check_pool(const vfm_kv_pages* kv) {
+  if (!kv || !kv->k || !kv->v || !kv->table_host || !kv->table_dev) return VFM_ERR_ARG;
+  const int ps = kv->page_size;
+  if (ps < 16 || ps > 1024 || (ps & (ps - 1))) return VFM_ERR_ARG;
+  if (kv->n_pages < 1 || kv->max_pages < 1 || kv->n_pages > ((int64_t)1 << 40) / ps) return VFM_ERR_SHAPE;
+  return VFM_OK;
+}
+
+KvPages pages_of(const vfm_kv_pages* kv) {
+  int lp = 0;
+  while ((1 << lp) < kv->page_size) ++lp;
+  return KvPages{kv->table_dev, kv->max_pages, lp};
+}
+
+// ---- decoding over a bounded cache (vfm_decode.h) ----------------------------
+constexpr int kMaxPos = 1 << 30;
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// The stream belongs to the current device (the one the kernels' code is loaded on).
+int check_stream(void* stream) {
+  if (stream == nullptr) return VFM_OK;
+  int dev = -1;
+  hipDevice_t sdev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || hipStreamGetDevice((hipStream_t)stream, &sdev) != hipSuccess)
+    return VFM_ERR_HIP;
+  return sdev == dev ? VFM_OK : VFM_ERR_ARG;
+}
+
+int check_attn(const vfm_attn* a) {
+  if (!a) return VFM_ERR_ARG;
+  if (a->dtype != VFM_F32 && a->dtype != VFM_BF16) return VFM_ERR_ARG;
+  if (a->head_dim != 64 && a->head_dim != 128) return VFM_ERR_UNSUPPORTED;
+  if (a->n_heads < 1 || a->n_heads > 1024 || a->n_kv_heads < 1 || a->n_heads % a->n_kv_heads) return VFM_ERR_SHAPE;
+  if (a->n_heads / a->n_kv_heads > 64) return VFM_ERR_UNSUPPORTED;
+  if (a->window < 0 || a->window > kMaxPos || a->n_sink < 0 || a->n_sink > kMaxPos) return VFM_ERR_ARG;
+  if (!(a->scale >= 0.f && a->scale <= 1e30f) || !(a->rope_theta >= 0.f && a->rope_theta <= 1e30f)) return VFM_ERR_ARG;
+  return VFM_OK;
+}
+
+// The pages that a step uses exist: those of each request's new positions
+// (writes) and, with `reads`, those with a position that one of its rows sees.
+int check_pages(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, const vfm_kv_pages* kv, bool reads) {
+  const int64_t ps = kv->page_size;
+  if (!aligned16(kv->k) || !aligned16(kv->v)) return VFM_ERR_ARG;
+  if (kv->n_pages * ps >= (int64_t)1 << 31) return VFM_ERR_SHAPE;
+  const PlanOffsets po = plan_offsets(pl.n_req, pl.n_tasks, pl.T);
+  const int32_t *ctx = host_arr(batch, po.ctx), *cu = host_arr(batch, po.cu_seqlens), *order = host_arr(batch, po.order);
+  for (int p = 0; p < pl.n_req; ++p) {
+    const int64_t end = (int64_t)ctx[p] + (cu[p + 1] - cu[p]);
+    if (ctx[p] < 0 || end > kMaxPos) return VFM_ERR_SHAPE;
+    const int64_t last = (end - 1) / ps;
+    if (last >= kv->max_pages) return VFM_ERR_SHAPE;
+    const int32_t* row = kv->table_host + (int64_t)order[p] * kv->max_pages;
+    int64_t first = ctx[p];                               // the window's (or the new rows') first position
+    if (reads) first = a.window > 0 ? std::max<int64_t>(0, (int64_t)ctx[p] - a.window + 1) : 0;
+    for (int64_t j = first / ps; j <= last; ++j)
+      if (row[j] < 0 || row[j] >= kv->n_pages) return VFM_ERR_SHAPE;
+    if (reads && a.window > 0) {
+      const int64_t sinks = std::min<int64_t>(a.n_sink, end);
+      for (int64_t j = 0; j * ps < sinks; ++j)
+        if (row[j] < 0 || row[j] >= kv->n_pages) return VFM_ERR_SHAPE;
+    }
+  }
+  return VFM_OK;
+}
+
+// Launch facts of the paged attention over a batch.
+struct AttnPlan {
+  int few_chunks, rows_chunks, qtiles;
+  bool few, rows;
+  int64_t bytes;             // workspace
+  int nchunk() const { return std::max(few_chunks, rows_chunks); }
+};
+
+int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, AttnPlan* out) {
+  AttnPlan ap = {1, 1, 1, false, false, 0};
+  const int G = a.n_heads / a.n_kv_heads;
+  const PlanOffsets po = plan_offsets(pl.n_req, pl.n_tasks, pl.T);
+  const int32_t *ctx = host_arr(batch, po.ctx), *cu = host_arr(batch, po.cu_seqlens);
+  for (int p = 0; p < pl.n_req; ++p) {
+    const int m = cu[p + 1] - cu[p];
+    if (ctx[p] < 0 || (int64_t)ctx[p] + m > kMaxPos) return VFM_ERR_SHAPE;
+    const int n = request_chunks(a.dtype, m, ctx[p], G, a.n_kv_heads, a.window, a.n_sink).n;
+    if (few_rows(a.dtype, m, G)) {
+      ap.few = true;
+      ap.few_chunks = std::max(ap.few_chunks, n);
+      if (a.dtype == VFM_BF16) ap.qtiles = std::max(ap.qtiles, few_qtiles(m, G));
+    } else {
+      ap.rows = true;
+      ap.rows_chunks = std::max(ap.rows_chunks, n);
+    }
+  }
+  // a launch holds at most 2^32 - 1 threads, 256 a block
+  const int64_t most = ((int64_t)1 << 24) - 1;
+  const int64_t few_tiles = a.dtype == VFM_BF16 ? (int64_t)ap.qtiles * pl.n_req : (int64_t)pl.T * G / 16 + pl.n_req;
+  const int64_t rows_tiles = (int64_t)pl.T / rows_per_block(G) + pl.n_req;
+  if ((ap.few && few_tiles * a.n_kv_heads * ap.few_chunks > most) ||
+      (ap.rows && rows_tiles * a.n_kv_heads * ap.rows_chunks > most) ||
+      (ap.nchunk() > 1 && (int64_t)pl.T * a.n_heads / 4 >= most))
+    return VFM_ERR_UNSUPPORTED;
+  if (ap.nchunk() > 1) {
+    const int64_t recs = (int64_t)pl.T * a.n_heads * ap.nchunk();
+    ap.bytes = (int64_t)align_up((size_t)recs * a.head_dim * 4) + (int64_t)align_up((size_t)recs * 8);
+  }
+  *out = ap;
+  return VFM_OK;
+}
+
+hipError_t run_attention(const vfm_attn& a, const Plan& pl, const AttnPlan& ap, const void* q, int64_t ldq, const void* k,
+                         const void* v, int64_t slots, const KvPages& kp, void* out, int64_t ldo, char* ws,
+                         hipStream_t s) {
+  PagedAttn p = {};
+  p.H = a.n_heads; p.KH = a.n_kv_heads; p.G = a.n_heads / a.n_kv_heads;
+  p.window = a.window; p.n_sink = a.window > 0 ? a.n_sink : 0;
+  p.scale_log2 = (a.scale > 0.f ? a.scale : 1.f / sqrtf((float)a.head_dim)) * 1.4426950408889634f;
+  p.q = q; p.ldq = ldq; p.k = k; p.v = v; p.slots = slots; p.kp = kp; p.out = out; p.ldo = ldo;
+  p.few_chunks = ap.few_chunks; p.rows_chunks = ap.rows_chunks; p.nchunk = ap.nchunk(); p.qtiles = ap.qtiles;
+  if (p.nchunk > 1) {
+    p.rec_o = (float*)ws;
+    p.rec_ml = (float2*)(ws + align_up((size_t)pl.T * p.H * p.nchunk * a.head_dim * 4));
+  }
+  return launch_attention_paged(a.dtype, a.head_dim, pl, p, ap.few, ap.rows, p.nchunk > 1, s);
+}
+
+vfm_attn attn_of_layer(const vfm_cfg& c, int32_t window, int32_t n_sink) {
+  vfm_attn a = {};
+  a.dtype = c.dtype; a.n_heads = a.n_kv_heads = c.n_heads; a.head_dim = c.head_dim;
+  a.window = window; a.n_sink = n_sink;
+  return a;
+}
+
+// Checks shared by the layer entry points (everything but the cache).
 int check_layer(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_table* lora,
-                const vfm_batch* batch, const float* x, bool have_cache, Plan* pl) {
+                const vfm_batch* batch, const float* x, bool have_cache, Plan* pl, bool windowed = false) {
   VFM_TRY(check_cfg(cfg));
   VFM_TRY(check_batch(batch, pl));
   VFM_TRY(check_lora(lora, *pl));
@@ -203,7 +338,7 @@ int check_layer(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_t
     for (int p = 0; p < pl->n_req; ++p)
       if (ctx[p] > 0) return VFM_ERR_UNSUPPORTED;
   }
-  if (cfg->attn == VFM_ATTN_MIXED && cfg->dtype != VFM_BF16) {   // prompt chunks after cached tokens: bf16
+  if (cfg->attn == VFM_ATTN_MIXED && cfg->dtype != VFM_BF16 && !windowed) {   // prompt chunks after cached tokens: bf16
     const int32_t* ctx = host_arr(batch, po.ctx);
     const int32_t* cu = host_arr(batch, po.cu_seqlens);
     for (int p = 0; p < pl->n_req; ++p)
@@ -212,9 +347,11 @@ int check_layer(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_t
   return VFM_OK;
 }
 
+// win: attention over the paged cache with a window and sinks (vfm_layer_forward_windowed), or NULL.
 int layer_impl(const vfm_cfg& c, const vfm_layer_weights* w, const vfm_lora_table* lora,
                const vfm_batch* batch, const Plan& pl, float* x, void* k_cache, void* v_cache,
-               int64_t kv_slots, const KvPages& kp, void* workspace, size_t ws_bytes, void* stream);
+               int64_t kv_slots, const KvPages& kp, void* workspace, size_t ws_bytes, void* stream,
+               const vfm_attn* win = nullptr);
 
 }  // namespace
 
@@ -312,10 +449,8 @@ extern "C" int vfm_layer_forward_paged(const vfm_cfg* cfg, const vfm_layer_weigh
                                        const vfm_lora_table* lora, const vfm_batch* batch, float* x,
                                        const vfm_kv_pages* kv, void* workspace, size_t ws_bytes,
                                        void* stream) {
-  if (!kv || !kv->k || !kv->v || !kv->table_host || !kv->table_dev) return VFM_ERR_ARG;
+  VFM_TRY(check_pool(kv));
   const int ps = kv->page_size;
-  if (ps < 16 || ps > 1024 || (ps & (ps - 1))) return VFM_ERR_ARG;
-  if (kv->n_pages < 1 || kv->max_pages < 1 || kv->n_pages > ((int64_t)1 << 40) / ps) return VFM_ERR_SHAPE;
   Plan pl;
   VFM_TRY(check_layer(cfg, w, lora, batch, x, true, &pl));
   if (cfg->attn == VFM_ATTN_BIDIR) return VFM_ERR_UNSUPPORTED;
@@ -331,20 +466,21 @@ extern "C" int vfm_layer_forward_paged(const vfm_cfg* cfg, const vfm_layer_weigh
     for (int64_t j = 0; j < need; ++j)
       if (row[j] < 0 || row[j] >= kv->n_pages) return VFM_ERR_SHAPE;
   }
-  int lp = 0;
-  while ((1 << lp) < ps) ++lp;
-  return layer_impl(*cfg, w, lora, batch, pl, x, kv->k, kv->v, kv->n_pages * ps,
-                    KvPages{kv->table_dev, kv->max_pages, lp}, workspace, ws_bytes, stream);
+  return layer_impl(*cfg, w, lora, batch, pl, x, kv->k, kv->v, kv->n_pages * ps, pages_of(kv), workspace, ws_bytes,
+                    stream);
 }
 
 namespace {
 
 int layer_impl(const vfm_cfg& c, const vfm_layer_weights* w, const vfm_lora_table* lora,
                const vfm_batch* batch, const Plan& pl, float* x, void* k_cache, void* v_cache,
-               int64_t kv_slots, const KvPages& kp, void* workspace, size_t ws_bytes, void* stream) {
+               int64_t kv_slots, const KvPages& kp, void* workspace, size_t ws_bytes, void* stream,
+               const vfm_attn* win) {
   const int d = c.d_model, f = c.d_ff, T = pl.T;
   const int max_keys = max_keys_of(batch, pl);
-  const LayerWs ws = layer_ws(c, pl, lora, max_keys);
+  AttnPlan ap = {};
+  if (win) VFM_TRY(plan_attention(*win, batch, pl, &ap));
+  const LayerWs ws = win ? layer_ws(c, pl, lora, 0, ap.bytes) : layer_ws(c, pl, lora, max_keys);
   if (!workspace || ws_bytes < ws.total || ((uintptr_t)workspace % ALIGN)) return VFM_ERR_WORKSPACE;
 
   hipStream_t s = (hipStream_t)stream;
@@ -509,14 +645,20 @@ int layer_impl(const vfm_cfg& c, const vfm_layer_weights* w, const vfm_lora_tabl
                                           kv_slots, kp, s));
   // a6: attention per request (and the KV-cache write)
   // (timed per kernel inside the launcher)
+  if (win) {
+    if (!rope_writes_kv)
+      VFM_TIMED(VFM_PROF_OTHER, launch_kv_append(c.dtype, pl, c.n_heads, c.n_heads, c.head_dim, 0.f, qkv, 3 * (int64_t)d,
+                                                 nullptr, k_cache, v_cache, kv_slots, kp, s));
+    VFM_HIP(run_attention(*win, pl, ap, qkv, 3 * (int64_t)d, k_cache, v_cache, kv_slots, kp, attn, d, base + ws.aws, s));
+  }
   bool chunked = false;                      // a prompt chunk after cached tokens
-  if (c.attn == VFM_ATTN_MIXED) {
+  if (!win && c.attn == VFM_ATTN_MIXED) {
     const PlanOffsets po = plan_offsets(pl.n_req, pl.n_tasks, pl.T);
     const int32_t* ctx = host_arr(batch, po.ctx);
     const int32_t* cu = host_arr(batch, po.cu_seqlens);
     for (int p = 0; p < pl.n_req && !chunked; ++p) chunked = ctx[p] > 0 && cu[p + 1] - cu[p] > 1;
   }
-  VFM_HIP(launch_attention(c.dtype, pl, c, qkv, attn, k_cache, v_cache, kv_slots, kp, rope_writes_kv, chunked,
+  if (!win) VFM_HIP(launch_attention(c.dtype, pl, c, qkv, attn, k_cache, v_cache, kv_slots, kp, rope_writes_kv, chunked,
                            base + ws.aws, ws.z - ws.aws, max_keys, s));
   // a7: output projection + LoRA_o + residual
   VFM_TRY(project(VFM_PROF_GEMM_O, attn, d, w->w_o, nullptr, w->b_o, d, EPI_RESID, x, d, {VFM_O}, d,
@@ -603,4 +745,98 @@ extern "C" int vfm_greedy_tokens(const vfm_batch* batch, const float* out, int32
   VFM_TRY(check_batch(batch, &pl));
   if (!out || !ids) return VFM_ERR_ARG;
   return hip_status(launch_greedy(pl, out, ids, (hipStream_t)stream));
+}
+
+// ---- decoding over a bounded cache (vfm_decode.h) ----------------------------
+
+extern "C" int vfm_workspace_size_windowed(const vfm_cfg* cfg, const vfm_batch* batch, const vfm_lora_table* lora,
+                                           int32_t window, int32_t n_sink, size_t* bytes) {
+  if (!bytes) return VFM_ERR_ARG;
+  VFM_TRY(check_cfg(cfg));
+  const vfm_attn a = attn_of_layer(*cfg, window, n_sink);
+  VFM_TRY(check_attn(&a));
+  Plan pl;
+  VFM_TRY(check_batch(batch, &pl));
+  VFM_TRY(check_lora(lora, pl));
+  AttnPlan ap;
+  VFM_TRY(plan_attention(a, batch, pl, &ap));
+  *bytes = std::max(layer_ws(*cfg, pl, lora, 0, ap.bytes).total, head_ws(*cfg, pl));
+  return VFM_OK;
+}
+
+extern "C" int vfm_layer_forward_windowed(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_table* lora,
+                                          const vfm_batch* batch, float* x, const vfm_kv_pages* kv, int32_t window,
+                                          int32_t n_sink, void* workspace, size_t ws_bytes, void* stream) {
+  VFM_TRY(check_pool(kv));
+  Plan pl;
+  VFM_TRY(check_layer(cfg, w, lora, batch, x, true, &pl, true));
+  if (cfg->attn == VFM_ATTN_BIDIR) return VFM_ERR_UNSUPPORTED;
+  const vfm_attn a = attn_of_layer(*cfg, window, n_sink);
+  VFM_TRY(check_attn(&a));
+  VFM_TRY(check_pages(a, batch, pl, kv, true));
+  VFM_TRY(check_stream(stream));
+  return layer_impl(*cfg, w, lora, batch, pl, x, kv->k, kv->v, kv->n_pages * kv->page_size, pages_of(kv), workspace,
+                    ws_bytes, stream, &a);
+}
+
+extern "C" int vfm_kv_append(const vfm_attn* attn, const vfm_batch* batch, const void* qkv, int64_t ld, void* q_out,
+                             const vfm_kv_pages* kv, void* stream) {
+  VFM_TRY(check_attn(attn));
+  VFM_TRY(check_pool(kv));
+  Plan pl;
+  VFM_TRY(check_batch(batch, &pl));
+  if (!qkv || !q_out || !aligned16(qkv) || !aligned16(q_out)) return VFM_ERR_ARG;
+  if (ld % 8 || ld < (int64_t)(attn->n_heads + 2 * attn->n_kv_heads) * attn->head_dim) return VFM_ERR_SHAPE;
+  VFM_TRY(check_pages(*attn, batch, pl, kv, false));
+  VFM_TRY(check_stream(stream));
+  hipStream_t s = (hipStream_t)stream;
+  VFM_TIMED(VFM_PROF_OTHER, launch_kv_append(attn->dtype, pl, attn->n_heads, attn->n_kv_heads, attn->head_dim,
+                                             attn->rope_theta, qkv, ld, q_out, kv->k, kv->v,
+                                             kv->n_pages * kv->page_size, pages_of(kv), s));
+  return VFM_OK;
+}
+
+extern "C" int vfm_attention_workspace(const vfm_attn* attn, const vfm_batch* batch, size_t* bytes) {
+  if (!bytes) return VFM_ERR_ARG;
+  VFM_TRY(check_attn(attn));
+  Plan pl;
+  VFM_TRY(check_batch(batch, &pl));
+  AttnPlan ap;
+  VFM_TRY(plan_attention(*attn, batch, pl, &ap));
+  *bytes = (size_t)ap.bytes;
+  return VFM_OK;
+}
+
+extern "C" int vfm_attention_paged(const vfm_attn* attn, const vfm_batch* batch, const void* q, int64_t ldq,
+                                   const vfm_kv_pages* kv, void* out, int64_t ldo, void* workspace, size_t ws_bytes,
+                                   void* stream) {
+  VFM_TRY(check_attn(attn));
+  VFM_TRY(check_pool(kv));
+  Plan pl;
+  VFM_TRY(check_batch(batch, &pl));
+  if (!q || !out || !aligned16(q) || !aligned16(out)) return VFM_ERR_ARG;
+  const int64_t cols = (int64_t)attn->n_heads * attn->head_dim;
+  if (ldq % 8 || ldo % 8 || ldq < cols || ldo < cols) return VFM_ERR_SHAPE;
+  VFM_TRY(check_pages(*attn, batch, pl, kv, true));
+  AttnPlan ap;
+  VFM_TRY(plan_attention(*attn, batch, pl, &ap));
+  if (ap.bytes > 0 && (!workspace || ws_bytes < (size_t)ap.bytes || ((uintptr_t)workspace % ALIGN)))
+    return VFM_ERR_WORKSPACE;
+  VFM_TRY(check_stream(stream));
+  VFM_HIP(run_attention(*attn, pl, ap, q, ldq, kv->k, kv->v, kv->n_pages * kv->page_size, pages_of(kv), out, ldo,
+                        (char*)workspace, (hipStream_t)stream));
+  return VFM_OK;
+}
+
+extern "C" int vfm_sample_tokens(const vfm_batch* batch, const float* out, const vfm_sampling* sampling, const float* u,
+                                 int32_t* ids, float* logprob, void* stream) {
+  Plan pl;
+  VFM_TRY(check_batch(batch, &pl));
+  if (!out || !sampling || !u || !ids) return VFM_ERR_ARG;
+  const PlanOffsets po = plan_offsets(pl.n_req, pl.n_tasks, pl.T);
+  const int32_t* off = host_arr(batch, po.out_off);
+  int most = 0;
+  for (int i = 0; i < pl.n_req; ++i) most = std::max(most, off[i + 1] - off[i]);
+  VFM_TRY(check_stream(stream));
+  return hip_status(launch_sample(pl, out, *sampling, u, ids, logprob, most, (hipStream_t)stream));
 }

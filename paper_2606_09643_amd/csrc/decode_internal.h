@@ -1,0 +1,94 @@
+// Declarations of the bounded-cache decoding kernels (k_paged.hip, k_sample.hip).
+#pragma once
+
+#include "vfm_decode.h"
+#include "vfm_internal.h"
+
+// One attention over a paged cache, as the kernels take it.
+struct PagedAttn {
+  int H, KH, G;                // query heads, key heads, query heads per key head
+  int window, n_sink;          // window 0: none
+  float scale_log2;            // scale * log2(e)
+  const void* q; int64_t ldq;
+  const void* k; const void* v; int64_t slots;   // slots per head
+  KvPages kp;
+  void* out; int64_t ldo;
+  float* rec_o;                // [T][H][nchunk][head_dim] partial outputs
+  float2* rec_ml;              // [T][H][nchunk] running maximum (log2 units), sum
+  int few_chunks, rows_chunks; // the largest chunk count of a few-row and of a many-row request (1 if none)
+  int nchunk;                  // the larger of the two (the records' stride)
+  int qtiles;                  // the largest query-tile count of a few-row request
+};
+
+// What one request's rows see, in runs of 2^SH positions: ns runs from position
+// 0 (the sinks), then the runs from run `base` up to the last row's own.
+struct Vis {
+  int ns, base, n;             // n: runs in all
+  __host__ __device__ int run(int i) const { return i < ns ? i : i - ns + base; }
+};
+template <int SH>
+__host__ __device__ inline Vis visible_runs(int first_pos, int last_pos, int window, int n_sink) {
+  Vis v;
+  const int end = last_pos + 1;
+  const int lo = window > 0 && first_pos - window + 1 > 0 ? first_pos - window + 1 : 0;
+  v.base = lo >> SH;
+  const int sk = n_sink < end ? n_sink : end;
+  v.ns = (sk + (1 << SH) - 1) >> SH;
+  if (v.ns >= v.base) { v.ns = 0; v.base = 0; }
+  v.n = v.ns + ((end + (1 << SH) - 1) >> SH) - v.base;
+  return v;
+}
+
+// A request's keys are cut into chunks of whole tiles, one block each, as far
+// as the request alone then fills the chip: 256 blocks with the `par` (key
+// heads x query tiles) that it has uncut, and at least min_tiles tiles each.
+// Nothing but the request's own sizes and the head layout goes into it, so a
+// row's bits do not depend on the batch.
+struct Chunks { int n, tiles; };   // chunks, tiles per chunk
+__host__ __device__ inline Chunks key_chunks(int tiles, int par, int min_tiles) {
+  int want = 256 / par;
+  const int most = (tiles + min_tiles - 1) / min_tiles;
+  if (want > most) want = most;
+  if (want < 1) want = 1;
+  Chunks c;
+  c.tiles = (tiles + want - 1) / want;
+  c.n = (tiles + c.tiles - 1) / c.tiles;
+  return c;
+}
+
+constexpr int FEW_QUERIES = 32;      // packed queries (rows x group) up to which a request takes the few-row kernel
+constexpr int FEW_MIN_TILES = 8;     // 32-key tiles
+constexpr int ROWS_QUERIES = 128;    // packed queries per block of the many-row kernel
+constexpr int ROWS_MIN_TILES = 16;   // 64-key tiles
+
+// few-row kernel (bf16; fp32: every request): 16 packed queries per block
+__host__ __device__ inline bool few_rows(int dtype, int m, int G) { return dtype != VFM_BF16 || (int64_t)m * G <= FEW_QUERIES; }
+__host__ __device__ inline int few_qtiles(int m, int G) { return (int)(((int64_t)m * G + 15) / 16); }
+__host__ __device__ inline int rows_per_block(int G) { return ROWS_QUERIES / G; }
+
+// chunks of the request with m rows after ctx cached tokens
+__host__ __device__ inline Chunks request_chunks(int dtype, int m, int ctx, int G, int KH, int window, int n_sink) {
+  if (few_rows(dtype, m, G)) {
+    const int tiles = (visible_runs<4>(ctx, ctx + m - 1, window, n_sink).n + 1) / 2;
+    return key_chunks(tiles, KH * few_qtiles(m, G) > 256 ? 256 : KH * few_qtiles(m, G), FEW_MIN_TILES);
+  }
+  const int rb = rows_per_block(G);
+  const int64_t par = (int64_t)KH * ((m + rb - 1) / rb);
+  const int m1 = m < rb ? m : rb;     // a block sees at most this many tiles more or fewer than another
+  const int tiles = visible_runs<6>(ctx + m - m1, ctx + m - 1, window, n_sink).n;
+  return key_chunks(tiles, par > 256 ? 256 : (int)par, ROWS_MIN_TILES);
+}
+
+// q_out NULL: keys and values only.
+hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv,
+                            int64_t ld, void* q_out, void* k, void* v, int64_t slots, const KvPages& kp,
+                            hipStream_t s);
+
+// need_few / need_rows: the batch has requests of that kernel (bf16).
+// split: some request has more than one chunk.
+hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, bool need_few,
+                                  bool need_rows, bool split, hipStream_t s);
+
+// max_out: the batch's longest row of head outputs.
+hipError_t launch_sample(const Plan& pl, const float* out, const vfm_sampling& sp, const float* u, int32_t* ids,
+                         float* logprob, int max_out, hipStream_t s);

@@ -1,0 +1,946 @@
+// Appending to a paged KV cache and attention of new rows over it, with a
+// sliding window and first tokens that stay visible, for any number of query
+// heads per key head.
+//
+// A request's m rows times the G query heads of one key head are its packed
+// queries (row-major: neighbours share the row, so a tile's queries see nearly
+// the same keys); all of them read the same K and V.  Every kernel computes
+// S^T = K Q^T, keys in the MFMA's A slot and packed queries in the B slot, so
+// a lane holds several keys of ONE query: the softmax's maximum and sum are
+// in-lane plus one or two lane swaps, and exp(S^T) already lies as the B operand
+// of O^T = V^T P^T.
+//
+// Unseen keys.  Scores of unseen keys become -inf by a select, so what K holds
+// there does not matter.  V rows that no query of the tile sees are staged as
+// zeros.  Where some queries of a tile see a key and others do not, a zero
+// weight would still turn an infinity or a NaN of its V row into a NaN: such
+// tiles look for those values while staging, put zeros in their place and add
+// them afterwards to the queries that see them (add_nonfinite below).
+#include <type_traits>
+
+#include "decode_internal.h"
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float NEG_BIG = -1e30f;
+
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// 2^x, x <= 0 or -inf: the hardware exponential (1 ulp; no range reduction)
+__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ bf16x8 pack8(float a, float b, float c, float d, float e, float f, float g, float h) {
+  const bf16x2 p0 = __builtin_convertvector(f32x2{a, b}, bf16x2), p1 = __builtin_convertvector(f32x2{c, d}, bf16x2);
+  const bf16x2 p2 = __builtin_convertvector(f32x2{e, f}, bf16x2), p3 = __builtin_convertvector(f32x2{g, h}, bf16x2);
+  const bf16x4 lo = __builtin_shufflevector(p0, p1, 0, 1, 2, 3), hi = __builtin_shufflevector(p2, p3, 0, 1, 2, 3);
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// v of lane ^ 32 and of lane ^ 16 combined with the lane's own (gfx950 lane swaps)
+__device__ __forceinline__ float max_x32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_x16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_x32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float sum_x16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A wave's own LDS accesses complete in order; only the compiler must keep them.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// whether the row at position j sees position k
+__device__ __forceinline__ bool sees(int j, int k, int window, int n_sink) {
+  return k <= j && (window == 0 || j - k < window || k < n_sink);
+}
+// whether any of the rows at positions j0 .. j1 sees position k
+__device__ __forceinline__ bool seen_by_any(int j0, int j1, int k, int window, int n_sink) {
+  return k <= j1 && (window == 0 || j0 - k < window || k < n_sink);
+}
+// whether all of them see every position of [k0, k1]
+__device__ __forceinline__ bool seen_by_all(int j0, int j1, int k0, int k1, int window, int n_sink) {
+  return k1 <= j0 && (window == 0 || j1 - k0 < window || k1 < n_sink);
+}
+
+// bf16 pairs with an infinity or a NaN replaced by zeros; `found` is set if any
+__device__ __forceinline__ bf16x8 drop_nonfinite(const bf16x8& v, bool& found) {
+  u32x4 w;
+  __builtin_memcpy(&w, &v, 16);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool lo = (w[i] & 0x7F80u) == 0x7F80u, hi = (w[i] & 0x7F800000u) == 0x7F800000u;
+    found = found || lo || hi;
+    w[i] &= (lo ? 0xFFFF0000u : 0xFFFFFFFFu) & (hi ? 0x0000FFFFu : 0xFFFFFFFFu);
+  }
+  bf16x8 r;
+  __builtin_memcpy(&r, &w, 16);
+  return r;
+}
+__device__ __forceinline__ bool nonfinite(float v) { return !(fabsf(v) < INFINITY); }
+
+// Slot of position k in a request's page row.
+__device__ __forceinline__ int page_slot(const int32_t* prow, int lp, int k) {
+  return (prow[k >> lp] << lp) + (k & ((1 << lp) - 1));
+}
+
+// ---------------------------------------------------------------------------
+// Append: rotate-half of the q and k heads, q to q_out, k and v to their slots.
+// One block per row; a thread takes 8 pairs (i, i + dh/2) of one head with
+// 16-byte accesses (32 for fp32).  Bound by its bytes: every element is read and
+// written once.  The row's dh/2 angles go through LDS: revolutions in fp64
+// (position times theta^(-2i/dh) / 2 pi loses nothing up to 2^30 positions),
+// their fraction in fp32.
+// ---------------------------------------------------------------------------
+template <typename T> struct Vec8;
+template <> struct Vec8<bf16> { bf16x8 v; };
+template <> struct Vec8<float> { f32x4 v[2]; };
+__device__ __forceinline__ float get(const Vec8<bf16>& x, int i) { return (float)x.v[i]; }
+__device__ __forceinline__ float get(const Vec8<float>& x, int i) { return x.v[i >> 2][i & 3]; }
+__device__ __forceinline__ void put(Vec8<bf16>& x, int i, float f) { x.v[i] = (bf16)f; }
+__device__ __forceinline__ void put(Vec8<float>& x, int i, float f) { x.v[i >> 2][i & 3] = f; }
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void kv_append_kernel(Plan pl, int H, int KH, int rotate, double log2_theta,
+                                                        const T* __restrict__ qkv, int64_t ld, T* __restrict__ q_out,
+                                                        T* __restrict__ kc, T* __restrict__ vc, int64_t slots,
+                                                        KvPages kp) {
+  constexpr int HALF = DH / 2, PER = HALF / 8;
+  __shared__ float cs[HALF], sn[HALF];
+  const int r = blockIdx.x;
+  const int pos = pl.pos[r];
+  if (rotate && (int)threadIdx.x < HALF) {
+    const double inv = exp2(-(2.0 * (double)threadIdx.x / (double)DH) * log2_theta) * 0.15915494309189535;
+    const double rev = (double)pos * inv;
+    float s, c;
+    sincospif((float)(2.0 * (rev - rint(rev))), &s, &c);
+    cs[threadIdx.x] = c;
+    sn[threadIdx.x] = s;
+  }
+  const int64_t slot = kv_slot(pl, kp, pl.row_req[r], pos);
+  __syncthreads();
+  const T* row = qkv + (int64_t)r * ld;
+  const int first = q_out != nullptr ? 0 : H * PER;
+  for (int w = first + threadIdx.x; w < (H + 2 * KH) * PER; w += 256) {
+    const int hh = w / PER, i0 = (w % PER) * 8;
+    Vec8<T> a = *reinterpret_cast<const Vec8<T>*>(row + hh * DH + i0);
+    Vec8<T> b = *reinterpret_cast<const Vec8<T>*>(row + hh * DH + HALF + i0);
+    if (rotate && hh < H + KH) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float x = get(a, j), y = get(b, j), c = cs[i0 + j], s = sn[i0 + j];
+        put(a, j, x * c - y * s);
+        put(b, j, x * s + y * c);
+      }
+    }
+    T* dst = hh < H ? q_out + ((int64_t)r * H + hh) * DH
+                    : (hh < H + KH ? kc + ((int64_t)(hh - H) * slots + slot) * DH
+                                   : vc + ((int64_t)(hh - H - KH) * slots + slot) * DH);
+    *reinterpret_cast<Vec8<T>*>(dst + i0) = a;
+    *reinterpret_cast<Vec8<T>*>(dst + HALF + i0) = b;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Where a block of the attention kernels works.
+// ---------------------------------------------------------------------------
+struct Work {
+  int h, c, qt, p;    // key head, chunk, query tile, plan position
+};
+
+// Output of packed query `qi` (of the request's first row R0): the row's head.
+__device__ __forceinline__ int64_t out_row(const PagedAttn& a, int R0, int h, int qi, int& head) {
+  const int i = qi / a.G;
+  head = h * a.G + (qi - i * a.G);
+  return (int64_t)R0 + i;
+}
+
+// ---------------------------------------------------------------------------
+// Few rows (decode and short chunks), bf16: one block per 16 packed queries of
+// one request and key head and chunk of its keys; each of the 4 waves streams
+// every 4th 32-key tile of the chunk on its own (no barrier in the loop) and
+// the waves' partial softmax sums are merged through LDS at the end.
+// Memory bound: each visible K / V row is read once per query tile.  K fragments
+// go straight to registers (lane: one key's row, 16 bytes per MFMA step), V
+// through a wave-private LDS tile that the transposing LDS read turns into the
+// V^T operand; a tile's loads are issued while the tile before is computed.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// V rows of a few-row tile in LDS, [32][DH]: the 32-byte segments of row r
+// swizzled so that the transposing reads (each 32-lane half: 8 rows, one segment
+// each) spread over all banks; a row's stores stay one contiguous run.
+template <int DH>
+__device__ __forceinline__ int few_vswz(int r) {
+  return DH == 128 ? ((r & 3) | (((r >> 3) & 1) << 2)) : (((r >> 1) & 1) | (((r >> 3) & 1) << 1));
+}
+
+template <int DH>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attn_few_bf16_kernel(Plan pl, PagedAttn a) {
+  constexpr int LPR = DH / 8;          // lanes per K / V row (16 bytes each)
+  constexpr int RPI = 64 / LPR;        // rows per wave-wide load
+  constexpr int VI = 32 / RPI;         // V loads per lane and tile
+  constexpr int KS = DH / 32;          // MFMA steps over the head dims
+  constexpr int ND = DH / 16;          // output tiles
+  __shared__ __attribute__((aligned(16))) char smem[4 * 32 * DH * 2];   // V tiles, then the waves' outputs
+  __shared__ float sm[4][16], sl[4][16];
+
+  Work w;
+  {
+    int id = blockIdx.x;
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % a.few_chunks; id /= a.few_chunks;
+    w.qt = id % a.qtiles;
+    w.p = id / a.qtiles;
+  }
+  const int R0 = pl.cu_seqlens[w.p], m = pl.cu_seqlens[w.p + 1] - R0, ctx = pl.ctx[w.p];
+  if (!few_rows(VFM_BF16, m, a.G)) return;              // block-uniform, as every exit below
+  const int qn = m * a.G;
+  if (w.qt * 16 >= qn) return;
+  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink);
+  if (w.c >= ck.n) return;
+  const Vis vis = visible_runs<4>(ctx, ctx + m - 1, a.window, a.n_sink);
+  const int t0 = w.c * ck.tiles, t1 = min(t0 + ck.tiles, (vis.n + 1) / 2);
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int x = lane & 15, g = lane >> 4;
+  // this lane's query; the tile's rows' positions
+  const int qi = min(w.qt * 16 + x, qn - 1);
+  const int jq = ctx + qi / a.G;
+  const int j0 = ctx + w.qt * 16 / a.G, j1 = ctx + min(w.qt * 16 + 15, qn - 1) / a.G;
+  int head;
+  const int64_t row = out_row(a, R0, w.h, qi, head);
+  bf16x8 qf[KS];
+  {
+    const bf16* qr = (const bf16*)a.q + row * a.ldq + head * DH + 8 * g;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + 32 * s);
+  }
+  const int32_t* prow = a.kp.table + (int64_t)pl.order[w.p] * a.kp.max_pages;
+  const int lp = a.kp.log2_page;
+  const bf16* kh = (const bf16*)a.k + (int64_t)w.h * a.slots * DH;
+  const bf16* vh = (const bf16*)a.v + (int64_t)w.h * a.slots * DH;
+  bf16* Vs = reinterpret_cast<bf16*>(smem) + wave * 32 * DH;
+
+  // positions and slots of a tile's two 16-position runs (one page each, as a
+  // page holds a multiple of 16); runs past the last re-read it, unseen
+  auto run_pos = [&](int t, int e) { return 16 * vis.run(min(2 * t + e, vis.n - 1)); };
+  bf16x8 kf[2][2][KS], vf[2][VI];
+  int slot[2];
+  auto look_up = [&](int t) {
+    slot[0] = page_slot(prow, lp, run_pos(t, 0));
+    slot[1] = page_slot(prow, lp, run_pos(t, 1));
+  };
+  // keys of sub-tile e in rows x: 8 (x / 4) + x % 4 + 4 e, so that after the MFMA
+  // a lane holds the 8 consecutive keys 8 g .. 8 g + 7 over both sub-tiles
+  const int key0 = 8 * (x >> 2) + (x & 3);
+  auto load = [&](int b) {
+    const int64_t ks = (int64_t)(x < 8 ? slot[0] : slot[1]) + (key0 & 15);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        kf[b][e][s] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(kh + (ks + 4 * e) * DH + 8 * g + 32 * s));
+#pragma unroll
+    for (int i = 0; i < VI; ++i) {
+      const int64_t vs = (int64_t)slot[(RPI * i) >> 4] + ((RPI * i) & 15) + lane / LPR;
+      vf[b][i] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(vh + vs * DH + 8 * (lane % LPR)));
+    }
+  };
+
+  f32x4 o[ND];
+#pragma unroll
+  for (int i = 0; i < ND; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = NEG_BIG, l_run = 0.f;
+
+  const int vst_ch = lane % LPR, vst_row = lane / LPR;
+  const int vrow = 8 * g + (x >> 2);
+  const int vbase = vrow * DH * 2 + (few_vswz<DH>(vrow) << 5) + (x & 3) * 8;
+
+  auto compute = [&](int b, int t) {
+    const int p0 = run_pos(t, 0);
+    const int p1 = 2 * t + 1 < vis.n ? run_pos(t, 1) : INT32_MAX - 64;   // no second run: unseen
+    const bool full = p1 == p0 + 16 && seen_by_all(j0, j1, p0, p0 + 31, a.window, a.n_sink);
+    bool poison = false;
+    // V to LDS
+#pragma unroll
+    for (int i = 0; i < VI; ++i) {
+      const int r = RPI * i + vst_row;
+      bf16x8 v = vf[b][i];
+      if (!full) {
+        const int k = (((RPI * i) >> 4) ? p1 : p0) + (r & 15);
+        if (!seen_by_any(j0, j1, k, a.window, a.n_sink)) v = bf16x8{};
+        else if (j0 != j1 && !seen_by_all(j0, j1, k, k, a.window, a.n_sink)) v = drop_nonfinite(v, poison);
+      }
+      *reinterpret_cast<bf16x8*>(Vs + r * DH + ((((vst_ch >> 1) ^ few_vswz<DH>(r)) << 1) | (vst_ch & 1)) * 8) = v;
+    }
+    wave_lds_order();
+    // S^T
+    float s[8];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < KS; ++st) acc = mfma16(kf[b][e][st], qf[st], acc);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[4 * e + i] = acc[i];
+    }
+    if (!full) {
+      const int kb = (g < 2 ? p0 : p1) + 8 * (g & 1);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] = sees(jq, kb + i, a.window, a.n_sink) ? s[i] : -INFINITY;
+    }
+    float mb = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+    mb = max_x32(max_x16(mb)) * a.scale_log2;
+    if (__any(mb > m_run)) {                              // elsewhere the factor is 1
+      const float m_new = fmaxf(m_run, mb);
+      const float alpha = fast_exp2(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int i = 0; i < ND; ++i) o[i] *= alpha;
+    }
+    float e8[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      e8[i] = fast_exp2(fmaf(s[i], a.scale_log2, -m_run));
+      l_run += e8[i];
+    }
+    const bf16x8 pf = pack8(e8[0], e8[1], e8[2], e8[3], e8[4], e8[5], e8[6], e8[7]);
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      const char* vp = reinterpret_cast<const char*>(Vs) + (vbase ^ (d << 5));
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp + 4 * DH * 2));
+      bf16x8 f;
+      __builtin_memcpy(&f, &lo, 8);
+      __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
+      o[d] = mfma16(f, pf, o[d]);
+    }
+    wave_lds_order();
+    if (__any(poison)) {                                  // rare: re-read the tile's V rows from memory
+      for (int r = 0; r < 32; ++r) {
+        const int k = (r < 16 ? p0 : p1) + (r & 15);
+        if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
+        const bf16* vr = vh + (int64_t)page_slot(prow, lp, k) * DH + 4 * g;
+        const bool see = sees(jq, k, a.window, a.n_sink);
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float v = (float)vr[16 * d + i];
+            if (see && nonfinite(v)) o[d][i] += v;
+          }
+      }
+    }
+  };
+
+  // tiles t0 + wave, + 4, ...; a tile's loads are in flight while the one
+  // before is computed, its page lookups a tile before that
+  int t = t0 + wave;
+  if (t < t1) {
+    look_up(t);
+    load(0);
+    if (t + 4 < t1) look_up(t + 4);
+    for (;;) {
+      if (t + 4 < t1) { load(1); if (t + 8 < t1) look_up(t + 8); }
+      compute(0, t);
+      t += 4;
+      if (t >= t1) break;
+      if (t + 4 < t1) { load(0); if (t + 8 < t1) look_up(t + 8); }
+      compute(1, t);
+      t += 4;
+      if (t >= t1) break;
+    }
+  }
+  l_run = sum_x32(sum_x16(l_run));
+
+  // merge the four waves
+  __syncthreads();
+  float* so = reinterpret_cast<float*>(smem);             // [4][16][DH]
+  if (lane < 16) { sm[wave][x] = m_run; sl[wave][x] = l_run; }
+  // only queries that exist: their outputs lie at wave, query, dim
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+    *reinterpret_cast<f32x4*>(so + (wave * 16 + x) * DH + 16 * d + 4 * g) = o[d];
+  __syncthreads();
+  const int nq = min(16, qn - w.qt * 16);
+  for (int e = tid; e < nq * DH / 4; e += 256) {
+    const int q = e / (DH / 4), d = (e % (DH / 4)) * 4;
+    const float M = fmaxf(fmaxf(sm[0][q], sm[1][q]), fmaxf(sm[2][q], sm[3][q]));
+    float L = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float wt = fast_exp2(sm[i][q] - M);
+      L += sl[i][q] * wt;
+      // a wave without any visible key has weight 0 and zeros
+      acc += *reinterpret_cast<const f32x4*>(so + (i * 16 + q) * DH + d) * wt;
+    }
+    int hd;
+    const int64_t r = out_row(a, R0, w.h, w.qt * 16 + q, hd);
+    if (ck.n == 1) {
+      const float inv = 1.f / L;
+      bf16x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = (bf16)(acc[i] * inv);
+      *reinterpret_cast<bf16x4*>((bf16*)a.out + r * a.ldo + hd * DH + d) = v;
+    } else {
+      const int64_t rec = (r * a.H + hd) * a.nchunk + w.c;
+      *reinterpret_cast<f32x4*>(a.rec_o + rec * DH + d) = acc;
+      if (d == 0) a.rec_ml[rec] = make_float2(M, L);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows (prompts and chunks), bf16: one block per 128 packed queries of one
+// request and key head (and chunk of the keys where the request has few
+// blocks); 4 waves of 32 queries on v_mfma_f32_32x32x16_bf16, so a K or V
+// fragment read from LDS feeds 32 queries.  64-key tiles of K and V are staged
+// through registers into two LDS stages (one barrier per tile; the next
+// tile's loads are in flight during the current one's compute, their slots
+// looked up a tile earlier).
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ f32x16 mfma32(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// 16-byte chunk c of key row r: the 16 rows that one phase of a fragment read
+// touches lie in different banks
+template <int DH>
+__device__ __forceinline__ int rows_kswz(int r, int c) {
+  return DH == 128 ? (c ^ (r & 15)) : (c ^ ((r >> 1) & 7));
+}
+// 64-byte segment of V row r: the 4 rows that one half of a transposing read
+// touches lie in different banks
+template <int DH>
+__device__ __forceinline__ int rows_vswz(int r) {
+  return DH == 128 ? (r & 3) : ((r >> 1) & 1);
+}
+
+template <int DH>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attn_rows_bf16_kernel(Plan pl, PagedAttn a) {
+  constexpr int CH = DH / 8;             // 16-byte chunks per row
+  constexpr int KPT = 64 * CH / 256;     // K (and V) chunks per thread and tile
+  constexpr int KS = DH / 16;            // MFMA steps over the head dims
+  constexpr int ND = DH / 32;            // output tiles
+  __shared__ __attribute__((aligned(16))) bf16 Ks[2][64 * DH];
+  __shared__ __attribute__((aligned(16))) bf16 Vs[2][64 * DH];
+  __shared__ int s_poison[2];
+
+  const int rb = rows_per_block(a.G);
+  Work w;
+  int blk;
+  {
+    int id = blockIdx.x;
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % a.rows_chunks; id /= a.rows_chunks;
+    blk = id;
+  }
+  // request p's blocks start at cu[p] / rb + p: at least ceil(m / rb) before the next request's
+  {
+    int lo = 0, hi = pl.n_req - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (pl.cu_seqlens[mid] / rb + mid <= blk) lo = mid; else hi = mid - 1;
+    }
+    w.p = lo;
+  }
+  const int R0 = pl.cu_seqlens[w.p], m = pl.cu_seqlens[w.p + 1] - R0, ctx = pl.ctx[w.p];
+  // a request's last rows see the most keys: they come first
+  const int nb = (m + rb - 1) / rb;
+  const int bi = blk - (R0 / rb + w.p);
+  if (bi >= nb || few_rows(VFM_BF16, m, a.G)) return;     // block-uniform, as every exit below
+  const int r0 = (nb - 1 - bi) * rb, nr = min(rb, m - r0);
+  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink);
+  if (w.c >= ck.n) return;
+  const int j0 = ctx + r0, j1 = j0 + nr - 1, qn = nr * a.G;
+  const Vis vis = visible_runs<6>(j0, j1, a.window, a.n_sink);
+  const int tpc = (vis.n + ck.n - 1) / ck.n;
+  const int t0 = w.c * tpc, t1 = min(t0 + tpc, vis.n);    // may be empty: an empty record
+  const int lo_any = a.window > 0 ? max(0, j0 - a.window + 1) : 0;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int x = lane & 31, h2 = lane >> 5;
+  const int qi = min(wave * 32 + x, qn - 1);
+  const int jq = j0 + qi / a.G;
+  // the wave's rows
+  const int wj0 = j0 + min(wave * 32, qn - 1) / a.G, wj1 = j0 + min(wave * 32 + 31, qn - 1) / a.G;
+  int head;
+  const int64_t row = out_row(a, R0 + r0, w.h, qi, head);
+  bf16x8 qf[KS];
+  {
+    const bf16* qr = (const bf16*)a.q + row * a.ldq + head * DH + 8 * h2;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s);
+  }
+  const int32_t* prow = a.kp.table + (int64_t)pl.order[w.p] * a.kp.max_pages;
+  const int lp = a.kp.log2_page;
+  const bf16* kh = (const bf16*)a.k + (int64_t)w.h * a.slots * DH;
+  const bf16* vh = (const bf16*)a.v + (int64_t)w.h * a.slots * DH;
+  if (tid < 2) s_poison[tid] = -1;
+
+  f32x16 o[ND];
+#pragma unroll
+  for (int i = 0; i < ND; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+  float m_run = NEG_BIG, l_run = 0.f;
+
+  int slot[KPT];
+  bf16x8 kr[KPT], vr[KPT];
+  // positions that no row of the block sees read a seen one instead: their page may not exist
+  auto look_up = [&](int t) {
+    const int kb = 64 * vis.run(min(t, vis.n - 1));
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      int k = min(kb + (tid + 256 * i) / CH, j1);
+      if (k < lo_any && k >= a.n_sink) k = lo_any;
+      slot[i] = page_slot(prow, lp, k);
+    }
+  };
+  auto load = [&]() {
+#pragma unroll
+    for (int i = 0; i < KPT; ++i)
+      kr[i] = *reinterpret_cast<const bf16x8*>(kh + (int64_t)slot[i] * DH + 8 * ((tid + 256 * i) % CH));
+#pragma unroll
+    for (int i = 0; i < KPT; ++i)
+      vr[i] = *reinterpret_cast<const bf16x8*>(vh + (int64_t)slot[i] * DH + 8 * ((tid + 256 * i) % CH));
+  };
+  auto store = [&](int b, int t) {
+    const int kb = 64 * vis.run(t);
+    const bool full = seen_by_all(j0, j1, kb, kb + 63, a.window, a.n_sink);
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      const int c = tid + 256 * i, key = c / CH, ch = c % CH;
+      *reinterpret_cast<bf16x8*>(&Ks[b][key * DH + rows_kswz<DH>(key, ch) * 8]) = kr[i];
+      bf16x8 v = vr[i];
+      if (!full) {
+        const int k = kb + key;
+        bool found = false;
+        if (!seen_by_any(j0, j1, k, a.window, a.n_sink)) v = bf16x8{};
+        else if (!seen_by_all(j0, j1, k, k, a.window, a.n_sink)) v = drop_nonfinite(v, found);
+        if (found) s_poison[b] = t;
+      }
+      *reinterpret_cast<bf16x8*>(&Vs[b][key * DH + ((((ch >> 2) ^ rows_vswz<DH>(key)) << 2) | (ch & 3)) * 8]) = v;
+    }
+  };
+
+  // fragment addresses (bytes): K row x of a 32-key half, chunk 2 s + h2;
+  // V: the transposing read takes 4 keys x 16 dims per 16 lanes, lane (x & 15)
+  // bringing key (x & 15) / 4, dims 4 (x & 3)
+  const int kq = x & 15, gq = x >> 4;
+  int kaddr = x * DH * 2 + (rows_kswz<DH>(x, h2) << 4);
+  int vaddr = (4 * h2 + (kq >> 2)) * DH * 2 + (rows_vswz<DH>(kq >> 2) << 6) + gq * 32 + (kq & 3) * 8;
+  static_assert(DH == 128 || DH == 64, "");
+  // DH 64: the segment's swizzle takes bit 1 of the row, which 4 h2 and 8-row steps leave alone
+
+  auto compute = [&](int b, int t) {
+    const int kb = 64 * vis.run(t);
+    // the wave has no query, or none that sees the tile
+    if (wave * 32 >= qn || kb > wj1 || (a.window > 0 && wj0 - (kb + 63) >= a.window && kb >= a.n_sink)) return;
+    const bool full = seen_by_all(wj0, wj1, kb, kb + 63, a.window, a.n_sink);
+    f32x16 st[2];
+    const char* kp = reinterpret_cast<const char*>(Ks[b]);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      f32x16 acc;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) acc[j] = 0.f;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const bf16x8 f = *reinterpret_cast<const bf16x8*>(kp + kt * 32 * DH * 2 + (kaddr ^ (s << 5)));
+        acc = mfma32(f, qf[s], acc);
+      }
+      st[kt] = acc;
+    }
+    if (!full) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int k = kb + 32 * kt + 8 * (i >> 2) + 4 * h2 + (i & 3);
+          st[kt][i] = sees(jq, k, a.window, a.n_sink) ? st[kt][i] : -INFINITY;
+        }
+    }
+    float mb = st[0][0];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mb = fmaxf(mb, st[kt][i]);
+    mb = max_x32(mb) * a.scale_log2;
+    if (__any(mb > m_run)) {                              // elsewhere the factor is 1
+      const float m_new = fmaxf(m_run, mb);
+      const float alpha = fast_exp2(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int i = 0; i < ND; ++i) o[i] *= alpha;
+    }
+    const char* vp = reinterpret_cast<const char*>(Vs[b]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {                         // 16 keys: 8 of them in this lane
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        e[i] = fast_exp2(fmaf(st[u >> 1][8 * (u & 1) + i], a.scale_log2, -m_run));
+        l_run += e[i];
+      }
+      const bf16x8 pf = pack8(e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const char* q = vp + (vaddr ^ (d << 6)) + u * 16 * DH * 2;
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q + 8 * DH * 2));
+        bf16x8 f;
+        __builtin_memcpy(&f, &lo, 8);
+        __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
+        o[d] = mfma32(f, pf, o[d]);
+      }
+    }
+  };
+  // the infinities and NaN that the staging left out of tile t
+  auto add_nonfinite = [&](int t) {
+    const int kb = 64 * vis.run(t);
+    for (int r = 0; r < 64; ++r) {
+      const int k = kb + r;
+      if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
+      const bf16* vrow = vh + (int64_t)page_slot(prow, lp, k) * DH + 4 * h2;
+      const bool see = sees(jq, k, a.window, a.n_sink);
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float v = (float)vrow[32 * d + 8 * (i >> 2) + (i & 3)];
+          if (see && nonfinite(v)) o[d][i] += v;
+        }
+    }
+  };
+
+  if (t0 < t1) {
+    look_up(t0);
+    load();
+    look_up(t0 + 1);
+    __syncthreads();                                      // s_poison
+    store(0, t0);
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+      const int b = (t - t0) & 1;
+      const bool more = t + 1 < t1;
+      if (more) { load(); look_up(t + 2); }
+      compute(b, t);
+      if (s_poison[b] == t) add_nonfinite(t);
+      if (more) store(b ^ 1, t + 1);
+      __syncthreads();
+    }
+  }
+  l_run = sum_x32(l_run);
+  if (wave * 32 + x >= qn) return;
+  if (ck.n == 1) {
+    const float inv = 1.f / l_run;
+    bf16* orow = (bf16*)a.out + row * a.ldo + head * DH + 4 * h2;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bf16x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (bf16)(o[d][4 * j + i] * inv);
+        *reinterpret_cast<bf16x4*>(orow + 32 * d + 8 * j) = v;
+      }
+  } else {
+    const int64_t rec = (row * a.H + head) * a.nchunk + w.c;
+    float* ro = a.rec_o + rec * DH + 4 * h2;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(ro + 32 * d + 8 * j) =
+            f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+    if (h2 == 0) a.rec_ml[rec] = make_float2(m_run, l_run);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// fp32, any number of rows (v_mfma_f32_16x16x4_f32): 16 packed queries per
+// block, the chunk's 16-key runs dealt to the 4 waves, operands from memory
+// straight into registers.  A 16-byte load of K or Q holds 4 consecutive head
+// dims, MFMA e taking component e of both; P^T is the B operand of the PV
+// products as it lies (MFMA j takes keys 4 g + j), and a lane that loads dims
+// 4 x .. 4 x + 3 of its key's V row gives MFMA c row x of tile c = head dim
+// 4 x + c, which leaves a lane with 16 consecutive head dims of its query.
+// ---------------------------------------------------------------------------
+template <int DH>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attn_f32_kernel(Plan pl, PagedAttn a) {
+  constexpr int NC = DH / 16, NH = DH / 64;
+  __shared__ float sm[4][16], sl[4][16];
+  __shared__ __attribute__((aligned(16))) float so[4][16][DH];
+  auto mfma = [](float p, float q, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(p, q, c, 0, 0, 0); };
+  Work w;
+  {
+    int id = blockIdx.x;
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % a.few_chunks; id /= a.few_chunks;
+    // request p's query tiles start at cu[p] G / 16 + p
+    int lo = 0, hi = pl.n_req - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if ((int64_t)pl.cu_seqlens[mid] * a.G / 16 + mid <= id) lo = mid; else hi = mid - 1;
+    }
+    w.p = lo;
+    w.qt = id - (int)((int64_t)pl.cu_seqlens[lo] * a.G / 16 + lo);
+  }
+  const int R0 = pl.cu_seqlens[w.p], m = pl.cu_seqlens[w.p + 1] - R0, ctx = pl.ctx[w.p];
+  const int qn = m * a.G;
+  if (w.qt * 16 >= qn) return;                            // block-uniform, as every exit below
+  const Chunks ck = request_chunks(VFM_F32, m, ctx, a.G, a.KH, a.window, a.n_sink);
+  if (w.c >= ck.n) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int x = lane & 15, g = lane >> 4;
+  const int qi = min(w.qt * 16 + x, qn - 1);
+  const int jq = ctx + qi / a.G;
+  const int j0 = ctx + w.qt * 16 / a.G, j1 = ctx + min(w.qt * 16 + 15, qn - 1) / a.G;
+  // the tile's own runs, dealt over the request's chunks
+  const Vis vis = visible_runs<4>(j0, j1, a.window, a.n_sink);
+  const int rpc = (vis.n + ck.n - 1) / ck.n;
+  const int t0 = w.c * rpc, t1 = min(t0 + rpc, vis.n);
+  int head;
+  const int64_t row = out_row(a, R0, w.h, qi, head);
+  const int32_t* prow = a.kp.table + (int64_t)pl.order[w.p] * a.kp.max_pages;
+  const int lp = a.kp.log2_page;
+  const float* kh = (const float*)a.k + (int64_t)w.h * a.slots * DH;
+  const float* vh = (const float*)a.v + (int64_t)w.h * a.slots * DH;
+  f32x4 q[NC], o[NH][4];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    q[c] = *reinterpret_cast<const f32x4*>((const float*)a.q + row * a.ldq + head * DH + 16 * c + 4 * g);
+#pragma unroll
+  for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[hh][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = NEG_BIG, l_run = 0.f;
+  for (int t = t0 + wave; t < t1; t += 4) {
+    const int p0 = 16 * vis.run(t);
+    const int64_t slot = page_slot(prow, lp, p0);
+    const bool full = seen_by_all(j0, j1, p0, p0 + 15, a.window, a.n_sink);
+    f32x4 kf[NC], vf[4][NH];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      kf[c] = *reinterpret_cast<const f32x4*>(kh + (slot + x) * DH + 16 * c + 4 * g);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int hh = 0; hh < NH; ++hh)
+        vf[j][hh] = *reinterpret_cast<const f32x4*>(vh + (slot + 4 * g + j) * DH + 64 * hh + 4 * x);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = mfma(kf[c][e], q[c][e], s);
+    bool poison = false;
+    if (!full) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = p0 + 4 * g + j;
+        s[j] = sees(jq, k, a.window, a.n_sink) ? s[j] : -INFINITY;
+        const bool any = seen_by_any(j0, j1, k, a.window, a.n_sink);
+        const bool some = any && !seen_by_all(j0, j1, k, k, a.window, a.n_sink);
+#pragma unroll
+        for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const bool bad = some && nonfinite(vf[j][hh][c]);
+            poison = poison || bad;
+            vf[j][hh][c] = !any || bad ? 0.f : vf[j][hh][c];
+          }
+      }
+    }
+    float mb = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    mb = max_x32(max_x16(mb)) * a.scale_log2;
+    const float m_new = fmaxf(m_run, mb);
+    const float alpha = exp2f(m_run - m_new);
+    m_run = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[hh][c] *= alpha;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float e = exp2f(fmaf(s[j], a.scale_log2, -m_run));
+      l_run += e;
+#pragma unroll
+      for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[hh][c] = mfma(vf[j][hh][c], e, o[hh][c]);
+    }
+    if (__any(poison)) {                                  // rare: see add_nonfinite of the bf16 kernel
+      for (int r = 0; r < 16; ++r) {
+        const int k = p0 + r;
+        if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
+        const bool see = sees(jq, k, a.window, a.n_sink);
+#pragma unroll
+        for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float v = vh[(slot + r) * DH + 64 * hh + 16 * g + 4 * i + c];
+              if (see && nonfinite(v)) o[hh][c][i] += v;
+            }
+      }
+    }
+  }
+  l_run = sum_x32(sum_x16(l_run));
+  if (lane < 16) { sm[wave][x] = m_run; sl[wave][x] = l_run; }
+#pragma unroll
+  for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4*>(&so[wave][x][64 * hh + 16 * g + 4 * i]) =
+          f32x4{o[hh][0][i], o[hh][1][i], o[hh][2][i], o[hh][3][i]};
+  __syncthreads();
+  const int nq = min(16, qn - w.qt * 16);
+  for (int e = tid; e < nq * DH / 4; e += 256) {
+    const int qq = e / (DH / 4), d = (e % (DH / 4)) * 4;
+    const float M = fmaxf(fmaxf(sm[0][qq], sm[1][qq]), fmaxf(sm[2][qq], sm[3][qq]));
+    float L = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float wt = exp2f(sm[i][qq] - M);
+      L += sl[i][qq] * wt;
+      acc += *reinterpret_cast<const f32x4*>(&so[i][qq][d]) * wt;
+    }
+    int hd;
+    const int64_t r = out_row(a, R0, w.h, w.qt * 16 + qq, hd);
+    if (ck.n == 1) {
+      *reinterpret_cast<f32x4*>((float*)a.out + r * a.ldo + hd * DH + d) = acc / L;
+    } else {
+      const int64_t rec = (r * a.H + hd) * a.nchunk + w.c;
+      *reinterpret_cast<f32x4*>(a.rec_o + rec * DH + d) = acc;
+      if (d == 0) a.rec_ml[rec] = make_float2(M, L);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Joins the chunks' partial sums of rows whose keys were cut: a wave per row and
+// head, o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c, chunks in order.
+// ---------------------------------------------------------------------------
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void attn_join_kernel(Plan pl, PagedAttn a) {
+  constexpr int DT = std::is_same<T, bf16>::value ? VFM_BF16 : VFM_F32;
+  constexpr int E = DH / 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+  if (id >= (int64_t)pl.T * a.H) return;
+  const int r = (int)(id / a.H), head = (int)(id - (int64_t)r * a.H);
+  const int p = pl.row_req[r];
+  const int m = pl.cu_seqlens[p + 1] - pl.cu_seqlens[p];
+  const int n = request_chunks(DT, m, pl.ctx[p], a.G, a.KH, a.window, a.n_sink).n;
+  if (n <= 1) return;
+  const float2* ml = a.rec_ml + id * a.nchunk;
+  const float* ro = a.rec_o + id * a.nchunk * DH + E * lane;
+  float M = NEG_BIG;
+  for (int c = lane; c < n; c += 64) M = fmaxf(M, ml[c].x);
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) M = fmaxf(M, __shfl_xor(M, s, 64));
+  float L = 0.f, acc[E] = {};
+  for (int c0 = 0; c0 < n; c0 += 64) {
+    float wt = 0.f;
+    if (c0 + lane < n) {
+      const float2 v = ml[c0 + lane];
+      wt = exp2f(v.x - M);
+      L += wt * v.y;
+    }
+    const int cn = min(64, n - c0);
+    int c = 0;
+    for (; c + 4 <= cn; c += 4) {
+      float v[4][E];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[j][e] = ro[(int64_t)(c0 + c + j) * DH + e];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float wc = __shfl(wt, c + j, 64);
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = fmaf(wc, v[j][e], acc[e]);
+      }
+    }
+    for (; c < cn; ++c) {
+      const float wc = __shfl(wt, c, 64);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(wc, ro[(int64_t)(c0 + c) * DH + e], acc[e]);
+    }
+  }
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) L += __shfl_xor(L, s, 64);
+  T* dst = (T*)a.out + (int64_t)r * a.ldo + head * DH + E * lane;
+#pragma unroll
+  for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] / L);
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv,
+                            int64_t ld, void* q_out, void* k, void* v, int64_t slots, const KvPages& kp,
+                            hipStream_t s) {
+  const int rotate = theta > 0.f;
+  const double l2 = rotate ? log2((double)theta) : 0.0;
+#define APPEND(T_, D_)                                                                                     \
+  hipLaunchKernelGGL((kv_append_kernel<T_, D_>), dim3(pl.T), dim3(256), 0, s, pl, H, KH, rotate, l2, (const T_*)qkv, ld, \
+                     (T_*)q_out, (T_*)k, (T_*)v, slots, kp)
+  if (dtype == VFM_BF16) { if (head_dim == 64) APPEND(bf16, 64); else APPEND(bf16, 128); }
+  else { if (head_dim == 64) APPEND(float, 64); else APPEND(float, 128); }
+#undef APPEND
+  return hipGetLastError();
+}
+
+hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, bool need_few,
+                                  bool need_rows, bool split, hipStream_t s) {
+  int pi = prof_begin(VFM_PROF_ATTN, s);
+  const unsigned few = (unsigned)a.KH * a.few_chunks, rows = (unsigned)a.KH * a.rows_chunks;
+#define BY_DH(K_, G_) \
+  do { if (head_dim == 64) hipLaunchKernelGGL((K_<64>), G_, dim3(256), 0, s, pl, a); \
+       else hipLaunchKernelGGL((K_<128>), G_, dim3(256), 0, s, pl, a); } while (0)
+  if (dtype == VFM_BF16) {
+    if (need_few) BY_DH(attn_few_bf16_kernel, dim3(few * a.qtiles * pl.n_req));
+    if (need_rows) BY_DH(attn_rows_bf16_kernel, dim3(rows * (pl.T / rows_per_block(a.G) + pl.n_req)));
+  } else {
+    BY_DH(attn_f32_kernel, dim3(few * (unsigned)((int64_t)pl.T * a.G / 16 + pl.n_req)));
+  }
+#undef BY_DH
+  prof_end(pi, s);
+  if (split) {
+    pi = prof_begin(VFM_PROF_OTHER, s);
+    const dim3 grid((unsigned)(((int64_t)pl.T * a.H + 3) / 4));
+#define JOIN(T_) \
+  do { if (head_dim == 64) hipLaunchKernelGGL((attn_join_kernel<T_, 64>), grid, dim3(256), 0, s, pl, a); \
+       else hipLaunchKernelGGL((attn_join_kernel<T_, 128>), grid, dim3(256), 0, s, pl, a); } while (0)
+    if (dtype == VFM_BF16) JOIN(bf16); else JOIN(float);
+#undef JOIN
+    prof_end(pi, s);
+  }
+  return hipGetLastError();
+}
