@@ -16,36 +16,65 @@
 // over the range where weights are not 0; the bin in which a filter ends is the
 // only one that is put in order, and where all bins up to it hold few outputs
 // (top-k), nothing else is looked at again.  One block per request: the row is
-// read once where it fits the registers (up to 4096 outputs).
+// read once where it fits registers or LDS (up to 32768 outputs).
 #include "decode_internal.h"
 
 namespace {
 
 typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 
 struct SampleParams {
   const float* temperature; const int32_t* top_k; const float* top_p; const float* min_p;
 };
 
-// 2^t for t in [-46, 0], scaled by 2^sh and rounded to an integer.  Taylor series
-// of e^(f ln 2) on |f| <= 1/2: the first term left out, (f ln 2)^12 / 12!, is
-// below 7e-15.  Adding 2^52 leaves the integer in the low bits.
-__device__ __forceinline__ uint64_t fixed_exp2(double t, int sh) {
-  const double n = __builtin_rint(t), f = t - n;
-  double p = 4.4455382718708101e-10;                  // ln2^11 / 11!
-  p = fma(p, f, 7.0549116208011209e-09);               // ln2^10 / 10!
-  p = fma(p, f, 1.0178086009239696e-07);
-  p = fma(p, f, 1.3215486790144305e-06);
-  p = fma(p, f, 1.5252733804059838e-05);
-  p = fma(p, f, 1.5403530393381606e-04);
-  p = fma(p, f, 1.3333558146428441e-03);
-  p = fma(p, f, 9.6181291076284769e-03);
-  p = fma(p, f, 5.5504108664821576e-02);
-  p = fma(p, f, 2.4022650695910069e-01);
-  p = fma(p, f, 6.9314718055994529e-01);
-  p = fma(p, f, 1.0);
-  const double d = __builtin_ldexp(p, (int)n + sh) + 4503599627370496.0;
-  return (uint64_t)__double_as_longlong(d) & 0xFFFFFFFFFFFFFull;
+// 2^t, t <= 0, scaled by 2^sh and rounded to an integer.  t = n + f, |f| <= 1/2, and
+// 2^f by the polynomial of degree 10 through 1 at 0 that interpolates it at the
+// Chebyshev nodes (relative error 6e-16).  Adding 2^52 leaves the integer in the
+// low bits.  t below -100 (-inf) and NaN count as -100: 0.  No branch, so that a
+// thread's four chains run beside each other; the coefficients stay in scalar
+// registers (as literals each product would move one into a vector register).
+struct Exp2 {
+  double c[10];
+  __device__ __forceinline__ void init() {
+    constexpr double k[10] = {7.0709785640393195e-09, 1.0205905435457491e-07, 1.3215451629202315e-06,
+                              1.5252672924749049e-05, 1.5403530424784571e-04, 1.3333558200794733e-03,
+                              9.6181291076186601e-03, 5.5504108664651670e-02, 2.4022650695910075e-01,
+                              6.9314718055994617e-01};
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+      c[i] = k[i];
+      asm volatile("" : "+s"(c[i]));
+    }
+  }
+  __device__ __forceinline__ uint64_t operator()(double t, int sh) const {
+    t = fmax(t, -100.0);
+    const double n = __builtin_rint(t), f = t - n;
+    double p = c[0];
+#pragma unroll
+    for (int i = 1; i < 10; ++i) p = fma(p, f, c[i]);
+    p = fma(p, f, 1.0);
+    const double d = __builtin_ldexp(p, (int)n + sh) + 4503599627370496.0;
+    return (uint64_t)__double_as_longlong(d) & 0xFFFFFFFFFFFFFull;
+  }
+};
+
+// ln x, x >= 1: x = 2^e m, m in [2/3, 4/3), ln m = 2 atanh((m - 1) / (m + 1)) by its
+// series (|s| <= 1/5: the first term left out is below 1e-13).
+__device__ __forceinline__ double log_of(double x) {
+  int e = __builtin_amdgcn_frexp_exp(x);
+  double m = __builtin_amdgcn_frexp_mant(x);             // [1/2, 1)
+  if (m < 2.0 / 3.0) { m *= 2.0; --e; }
+  const double s = (m - 1.0) / (m + 1.0), z = s * s;
+  double p = 2.0 / 15;
+  p = fma(p, z, 2.0 / 13);
+  p = fma(p, z, 2.0 / 11);
+  p = fma(p, z, 2.0 / 9);
+  p = fma(p, z, 2.0 / 7);
+  p = fma(p, z, 2.0 / 5);
+  p = fma(p, z, 2.0 / 3);
+  p = fma(p, z, 2.0);
+  return fma((double)e, 0.6931471805599453, p * s);
 }
 
 // Integers in the order of the floats (no NaN); -0 and +0 are one.
@@ -54,471 +83,659 @@ __device__ __forceinline__ uint32_t float_key(float v) {
   return b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-__device__ __forceinline__ uint64_t shfl64(uint64_t v, int lane) { return __shfl((unsigned long long)v, lane, 64); }
-// inclusive sums over the lanes of a wave
-__device__ __forceinline__ uint64_t wave_scan(uint64_t v, int lane) {
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const uint64_t o = __shfl_up((unsigned long long)v, s, 64);
-    if (lane >= s) v += o;
-  }
+// Sums, maxima and scans over a wave with DPP moves (no LDS round trips); every
+// lane is active.  A 64-bit value moves as two halves.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp0(uint32_t v) {   // 0 where no lane is the source
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, true);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t dpp0(uint64_t v) {
+  return ((uint64_t)dpp0<CTRL, ROWS>((uint32_t)(v >> 32)) << 32) | dpp0<CTRL, ROWS>((uint32_t)v);
+}
+// inclusive sums over the lanes: within rows of 16 lanes, then lane 15 of rows
+// 0 and 2 into the row behind, then lane 31 into the upper half
+template <typename T>
+__device__ __forceinline__ T wave_scan(T v) {
+  v += dpp0<0x111, 0xF>(v);
+  v += dpp0<0x112, 0xF>(v);
+  v += dpp0<0x114, 0xF>(v);
+  v += dpp0<0x118, 0xF>(v);
+  v += dpp0<0x142, 0xA>(v);
+  v += dpp0<0x143, 0xC>(v);
   return v;
 }
-__device__ __forceinline__ uint32_t wave_scan(uint32_t v, int lane) {
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const uint32_t o = __shfl_up(v, s, 64);
-    if (lane >= s) v += o;
-  }
-  return v;
+__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ uint64_t last_lane(uint64_t v) {
+  return ((uint64_t)last_lane((uint32_t)(v >> 32)) << 32) | last_lane((uint32_t)v);
+}
+// every LDS access of the wave has finished (reads whose values a path does not use among them)
+__device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+template <typename T> __device__ __forceinline__ T wave_sum(T v) { return last_lane(wave_scan(v)); }
+
+// maximum over aligned groups of 2^(S + 1) lanes from that over groups of 2^S, in every lane
+template <int S>
+__device__ __forceinline__ uint32_t lane_pair(uint32_t v) {
+  static_assert(S >= 0 && S < 6, "64 lanes");
+  if constexpr (S == 0) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);
+  if constexpr (S == 1) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true);
+  if constexpr (S == 2) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true);   // 7 - lane of 8
+  if constexpr (S == 3) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true);   // 15 - lane of 16
+  // the two results of a lane swap are the lane's own value and its partner's, in one order or the other
+  if constexpr (S == 4) { const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false); return r[0] ^ r[1] ^ v; }
+  const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return r[0] ^ r[1] ^ v;
+}
+template <int S> __device__ __forceinline__ float lane_pair(float v) { return __uint_as_float(lane_pair<S>(__float_as_uint(v))); }
+template <int S = 0>
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, lane_pair<S>(v));
+  if constexpr (S < 5) return wave_max<S + 1>(v);
+  else return v;
+}
+template <int S = 0>
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max(v, lane_pair<S>(v));
+  if constexpr (S < 5) return wave_max<S + 1>(v);
+  else return v;
 }
 
-// NT threads; R > 0: the row's outputs in R x 4 registers per thread (n <= NT R 4),
-// R = 0: read again from memory (L2) by every pass.
-template <int NT, int R>
+// Where a row's outputs are between the passes over them.
+enum { IN_REGS = 0, IN_LDS = 1, IN_MEMORY = 2 };
+template <int NT, int WHERE> struct Shape;
+// up to 1024 outputs: 4 per thread in registers
+template <> struct Shape<256, IN_REGS> { static constexpr int RUNS = 1, PB = 256, SETS = 4; };
+// up to 32768: 128 KB of LDS, which leaves room for 4 sets of bins of weights
+template <> struct Shape<1024, IN_LDS> { static constexpr int RUNS = 8, PB = 512, SETS = 4; };
+// more: read again (from L2) by every pass; a set of bins per wave
+template <> struct Shape<1024, IN_MEMORY> { static constexpr int RUNS = 0, PB = 1024, SETS = 16; };
+
+template <int NT, int WHERE>
 __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __restrict__ out, SampleParams sp,
                                                     const float* __restrict__ us, int32_t* __restrict__ ids,
                                                     float* __restrict__ logprob) {
-  constexpr int NW = NT / 64, CAP = NT, NB = NT;
+  using Sh = Shape<NT, WHERE>;
+  constexpr int NW = NT / 64, NB = NT;
+  constexpr int CAP = NT / 2;          // outputs that are put in order at once, each against each
+  constexpr int NG = 256;              // at most this many groups of threads, whose largest outputs bound a top-k from below
+  constexpr int PB = Sh::PB, SETS = Sh::SETS, PER = NW / SETS;   // bins of weights; sets of them; waves per set
+  __shared__ __attribute__((aligned(16))) float s_row[WHERE == IN_LDS ? NT * 4 * Sh::RUNS : 4];
   __shared__ float red_f[2][NW];
-  __shared__ uint64_t red_u[NW];
-  __shared__ uint32_t red_c[NW];
-  __shared__ int red_i[NW];
-  __shared__ uint32_t h_cnt[NB];       // a bin's outputs, then the outputs up to and with it
-  __shared__ uint64_t h_mass[NB];
-  __shared__ uint64_t l_key[CAP];      // (float_key, ~index): descending order
-  __shared__ uint64_t l_sorted[CAP], l_mass[CAP], l_cum[CAP];
-  __shared__ uint32_t s_n, s_sel[3];   // list length; bin, outputs before it, outputs in it
-  __shared__ uint64_t s_before, s_last, s_total;
+  __shared__ uint64_t red_u[NW], set_u[SETS], run_u[64];
+  __shared__ uint32_t red_c[2][NW];
+  // bins: weights per set and bin (top-p), or of all outputs (a bin's weight, then up to and with it; its outputs)
+  constexpr size_t BINS = SETS * PB * 8 > NB * 12 ? SETS * PB * 8 : NB * 12;
+  __shared__ __attribute__((aligned(16))) char s_bins[BINS];
+  __shared__ __attribute__((aligned(16))) uint64_t l_key[CAP + 8];   // (float_key, ~index): descending order; then running sums
+  __shared__ uint64_t l_sorted[CAP], l_mass[CAP];
+  __shared__ uint32_t l_rank[CAP];
+  __shared__ uint32_t s_n, s_sel[3];   // kept outputs; bin, outputs before it, outputs in it
+  __shared__ uint64_t s_before;
+  __shared__ float s_bound;
+  auto h_mass = [&](int b) -> uint64_t& { return reinterpret_cast<uint64_t*>(s_bins)[b]; };
+  auto h_cnt = [&](int b) -> uint32_t& { return reinterpret_cast<uint32_t*>(s_bins + NB * 8)[b]; };
+  auto set_mass = [&](int set, int b) -> uint64_t& { return reinterpret_cast<uint64_t*>(s_bins)[set * PB + b]; };
+  uint64_t* const l_cum = l_key;
+  float* const g_max = reinterpret_cast<float*>(l_sorted);   // the groups' largest outputs and their ranks, before any list
+  static_assert(CAP * 8 >= NG * 4 && CAP >= NG / 2, "");
 
   const int row = blockIdx.x;
   const int o0 = pl.out_off[row], n = pl.out_off[row + 1] - o0;
   const float* src = out + o0;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int nr = (n + NT * 4 - 1) / (NT * 4);
-  const int first = wave * nr * 256 + lane * 4;        // the wave's outputs are one run
+  const int nr = (n + NT * 4 - 1) / (NT * 4);          // runs of 256 outputs per wave; a wave's runs are one piece
+  const int first = wave * nr * 256 + lane * 4;
+  // the row's parameters, requested with its first outputs
+  const float temp = sp.temperature ? sp.temperature[row] : 1.f;
+  const int tk = sp.top_k ? sp.top_k[row] : 0;
+  const float tp = sp.top_p ? sp.top_p[row] : 1.f, mp = sp.min_p ? sp.min_p[row] : 0.f;
+  const float u_row = us[row];
 
   const float nan = __uint_as_float(0x7FC00000u);
-  f4u reg[R > 0 ? R : 1];
-  auto fetch = [&](int r) -> f4u {
-    const int i = first + r * 256;
+  // An infinite largest output M0: those that equal it share the weight, the others have none.
+  // Once `remap` is set the row is taken as 0 there and as -inf elsewhere.
+  float M0 = -INFINITY;
+  bool remap = false;
+  auto mapped = [&](float v) { return v == M0 ? 0.f : v == v ? -INFINITY : v; };
+  auto fetch_at = [&](int i) -> f4u {
     f4u v = {nan, nan, nan, nan};
     if (i + 4 <= n) v = *reinterpret_cast<const f4u*>(src + i);
     else
 #pragma unroll
       for (int c = 0; c < 4; ++c) if (i + c < n) v[c] = src[i + c];
+    if (WHERE == IN_MEMORY && remap)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] = mapped((float)v[c]);
     return v;
   };
-  if constexpr (R > 0) {
+  f4u reg = {nan, nan, nan, nan};
+  if constexpr (WHERE == IN_REGS) reg = fetch_at(first);
+  // the four outputs from index i, which some thread of the block owns (registers: this one)
+  auto at = [&](int i) -> f4u {
+    if constexpr (WHERE == IN_REGS) return reg;
+    else if constexpr (WHERE == IN_LDS) { const f32x4 q = *reinterpret_cast<const f32x4*>(&s_row[i]); return f4u{q[0], q[1], q[2], q[3]}; }
+    else return fetch_at(i);
+  };
+  // f(four values, index of the first) for every run of the wave, in order
+  auto each4 = [&](auto&& f) {
+    if constexpr (WHERE == IN_MEMORY) {
+      for (int r0 = 0; r0 < nr; r0 += 4) {               // four runs' loads in flight
+        f4u q[4];
 #pragma unroll
-    for (int r = 0; r < R; ++r) reg[r] = r < nr ? fetch(r) : f4u{nan, nan, nan, nan};
-  }
-  // f(value, index) for every output of the thread
-  auto each = [&](auto&& f) {
-    if constexpr (R > 0) {
+        for (int j = 0; j < 4; ++j) q[j] = r0 + j < nr ? fetch_at(first + (r0 + j) * 256) : f4u{nan, nan, nan, nan};
 #pragma unroll
-      for (int r = 0; r < R; ++r)
-        if (r < nr) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) f((float)reg[r][c], first + r * 256 + c);
+        for (int j = 0; j < 4; ++j) {
+          if (r0 + j < nr) f(q[j], first + (r0 + j) * 256);
+          __builtin_amdgcn_sched_barrier(0);
         }
-    } else {
-      for (int r = 0; r < nr; ++r) {
-        const f4u v = fetch(r);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) f((float)v[c], first + r * 256 + c);
       }
+    } else {
+      for (int r = 0; r < nr; ++r) f(at(first + r * 256), first + r * 256);
     }
   };
-
-  // the largest output, and whether there is one
-  float mx = -INFINITY;
-  bool any = false;
-  each([&](float v, int) { mx = fmaxf(mx, v); any = any || v == v; });
+  auto each = [&](auto&& f) {                            // f(value, index) for every output of the thread
+    each4([&](const f4u& q, int i0) {
 #pragma unroll
-  for (int s = 1; s < 64; s <<= 1) mx = fmaxf(mx, __shfl_xor(mx, s, 64));
-  const bool any_w = __any(any);
-  if (lane == 0) { red_f[0][wave] = mx; red_i[wave] = any_w; }
+      for (int c = 0; c < 4; ++c) f((float)q[c], i0 + c);
+    });
+  };
+
+  // 0: off.  No weight reaches a min-p above 1: the first output alone stays
+  const int k = mp > 1.f && n > 1 ? 1 : tk > 0 && tk < n ? tk : 0;
+  const bool p_on = tp < 1.f;
+  const double p = (double)tp;
+  const bool small_k = k > 0 && k <= NG;                 // block-uniform, as every branch on the row's values below
+
+  // The largest and the smallest output, and for a small top-k the largest of each
+  // of 256 groups of threads
+  float mx = -INFINITY, mn = INFINITY;
+  if constexpr (WHERE == IN_LDS) {
+    f4u q[Sh::RUNS];
+#pragma unroll
+    for (int r = 0; r < Sh::RUNS; ++r) q[r] = r < nr ? fetch_at(first + r * 256) : f4u{nan, nan, nan, nan};
+#pragma unroll
+    for (int r = 0; r < Sh::RUNS; ++r)
+      if (r < nr) {
+        *reinterpret_cast<f32x4*>(&s_row[first + r * 256]) = f32x4{q[r][0], q[r][1], q[r][2], q[r][3]};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) { mx = fmaxf(mx, q[r][c]); mn = fminf(mn, q[r][c]); }
+      }
+  } else {
+    each([&](float v, int) { mx = fmaxf(mx, v); mn = fminf(mn, v); });
+  }
+  const bool any = mn <= mx;                             // some output is no NaN
+  // 64 groups up to k = 56 (then some 150 outputs lie above the 56th of them), else 256
+  const int lgg = k <= 56 ? 6 : 8, per_group = NT >> lgg;   // threads per group: 16 or 4 of 1024, 4 or 1 of 256
+  if (small_k) {
+    float gm = mx;
+    if (per_group >= 4) {
+      gm = fmaxf(gm, lane_pair<0>(gm));
+      gm = fmaxf(gm, lane_pair<1>(gm));
+    }
+    if (per_group >= 16) {
+      gm = fmaxf(gm, lane_pair<2>(gm));
+      gm = fmaxf(gm, lane_pair<3>(gm));
+    }
+    if ((tid & (per_group - 1)) == 0) g_max[tid / per_group] = gm;
+    if (tid < NG) l_rank[tid % CAP] = 0;
+  }
+  {
+    const float lo = -wave_max(-mn);
+    mx = wave_max(mx);
+    const bool anyw = __any(any);
+    if (lane == 0) { red_f[0][wave] = mx; red_f[1][wave] = lo; red_c[1][wave] = anyw; }
+  }
   __syncthreads();
   bool found = false;
-  float M = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < NW; ++i) { M = fmaxf(M, red_f[0][i]); found = found || red_i[i]; }
-  if (!found) {                                          // block-uniform, as every branch on the row's values below
+  for (int i = 0; i < NW; ++i) {
+    M0 = fmaxf(M0, red_f[0][i]);
+    mn = fminf(mn, red_f[1][i]);
+    found = found || red_c[1][i];
+  }
+  if (!found) {
     if (tid == 0) { ids[row] = -1; if (logprob) logprob[row] = nan; }
     return;
   }
-  const float temp = sp.temperature ? sp.temperature[row] : 1.f;
-  const int tk = sp.top_k ? sp.top_k[row] : 0;
-  const float tp = sp.top_p ? sp.top_p[row] : 1.f, mp = sp.min_p ? sp.min_p[row] : 0.f;
   if (!(temp > 0.f)) {                                   // greedy
-    int best = INT32_MAX;
-    each([&](float v, int i) { if (v == M) best = min(best, i); });
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) best = min(best, __shfl_xor(best, s, 64));
-    __syncthreads();                                     // red_i is read above
-    if (lane == 0) red_i[wave] = best;
+    uint32_t best = 0;                                   // ~index: the largest is the lowest index
+    each([&](float v, int i) { if (v == M0) best = max(best, ~(uint32_t)i); });
+    best = wave_max(best);
+    __syncthreads();                                     // red_c is read above
+    if (lane == 0) red_c[0][wave] = best;
     __syncthreads();
     if (tid == 0) {
-      for (int i = 1; i < NW; ++i) best = min(best, red_i[i]);
-      ids[row] = best;
+      for (int i = 1; i < NW; ++i) best = max(best, red_c[0][i]);
+      ids[row] = (int)~best;
       if (logprob) logprob[row] = 0.f;
     }
     return;
+  }
+  float M = M0;
+  if (!(fabsf(M0) < INFINITY)) {
+    remap = true;
+    M = 0.f;
+    mn = -INFINITY;
+    if constexpr (WHERE == IN_REGS) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) reg[c] = mapped((float)reg[c]);
+    } else if constexpr (WHERE == IN_LDS) {
+      for (int r = 0; r < nr; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s_row[first + r * 256 + c] = mapped(s_row[first + r * 256 + c]);
+      __syncthreads();
+    }
   }
   const double T = fmin(fmax((double)temp, 1e-30), 1e30);
   const double c2 = 1.4426950408889634 / T;
   const int sh = n < (1 << 19) ? 44 : 32;
   const uint64_t one = (uint64_t)1 << sh;
   const float cut = fminf((float)(31.2 * T), 3e38f);     // 45 ln 2: below M - cut every weight is 0
-  auto mass = [&](float v) -> uint64_t {
-    if (v == M) return one;
-    const double t = ((double)v - (double)M) * c2;
-    return t >= -45.0 ? fixed_exp2(t, sh) : 0;           // NaN: 0
+  Exp2 exp2_fixed;
+  exp2_fixed.init();
+  auto mass = [&](float v) -> uint64_t { return exp2_fixed(((double)v - (double)M) * c2, sh); };
+  auto value_of = [&](uint32_t key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu)); };
+  const double uu = u_row > 0.f ? (double)u_row : 0.0;   // NaN: 0
+  auto target_of = [&](uint64_t S) {
+    const uint64_t t = (uint64_t)fmin(uu * (double)S, 9.2e18);
+    return t < S - 1 ? t : S - 1;
   };
-  const double uu = us[row] > 0.f ? (double)us[row] : 0.0;   // NaN: 0
   auto finish = [&](float v, int i, uint64_t total) {    // one thread: the drawn output
     ids[row] = i;
-    if (logprob) {
-      const double lw = v == M ? 0.0 : ((double)v - (double)M) / T;
-      logprob[row] = (float)(lw - log((double)total) + (double)sh * 0.6931471805599453);
-    }
-  };
-  // 0: off.  No weight reaches a min-p above 1: the first output alone stays
-  const int k = mp > 1.f && n > 1 ? 1 : tk > 0 && tk < n ? tk : 0;
-  const bool p_on = tp < 1.f;
-  const double p = (double)tp;
-
-  // block-wide inclusive scan of the bins in place: h_cnt and, with `masses`, h_mass
-  auto scan_bins = [&](bool masses) {
-    const uint32_t cw = wave_scan(h_cnt[tid], lane);
-    uint64_t mw = 0;
-    if (masses) mw = wave_scan(h_mass[tid], lane);
-    if (lane == 63) { red_c[wave] = cw; red_u[wave] = mw; }
-    __syncthreads();
-    uint32_t cb = 0;
-    uint64_t mb = 0;
-    for (int i = 0; i < wave; ++i) { cb += red_c[i]; mb += red_u[i]; }
-    h_cnt[tid] = cw + cb;
-    if (masses) h_mass[tid] = mw + mb;
-    __syncthreads();
+    if (logprob) logprob[row] = (float)(((double)v - (double)M) / T - log_of((double)total) + (double)sh * 0.6931471805599453);
   };
 
-  float v_last = -INFINITY;                              // the last kept output: its value and index
-  int i_last = INT32_MAX;
-  if (k > 0 || p_on) {
-    // range of the bins: the outputs whose weights are not 0
-    float mn = M;
-    each([&](float v, int) { if (M - v <= cut) mn = fminf(mn, v); });
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) mn = fminf(mn, __shfl_xor(mn, s, 64));
-    if (lane == 0) red_f[1][wave] = mn;
-    h_cnt[tid] = 0;
-    h_mass[tid] = 0;
+  // The outputs that f(value, index) picks, if they are at most CAP: in descending order in
+  // l_sorted, their weights in l_mass and running sums in l_cum.  Returns their number.
+  auto list = [&](auto&& f) -> uint32_t {
+    uint32_t mine = 0;
+    each([&](float v, int i) { mine += f(v, i); });
+    const uint32_t inc = wave_scan(mine);
+    const bool some = last_lane(inc) > 0;
+    __syncthreads();                                     // red_c, the list
+    if (lane == 63) red_c[0][wave] = inc;
+    if (tid < CAP) l_rank[tid] = 0;
     __syncthreads();
+    uint32_t cnt = 0, pos = inc - mine;
 #pragma unroll
-    for (int i = 0; i < NW; ++i) mn = fminf(mn, red_f[1][i]);
-    const float cb = M - mn > 0.f ? (float)NB / (M - mn) : 0.f;
-    auto bin0 = [&](float v) -> int {                    // -1: weight 0 or NaN
-      if (v == M) return 0;
-      const float d = M - v;
-      return d <= cut ? (int)fminf(d * cb, (float)(NB - 1)) : -1;
-    };
-    // count outputs per bin, with their weights where a share of them is wanted.
-    // A small top-k first counts only: it needs the weights of few outputs
-    const bool small_k = k > 0 && k <= CAP / 2;
-    bool masses = p_on && !small_k;
-    auto fill = [&]() {
-      each([&](float v, int) {
-        const int b = bin0(v);
-        if (b >= 0) {
-          atomicAdd(&h_cnt[b], 1u);
-          if (masses) atomicAdd((unsigned long long*)&h_mass[b], (unsigned long long)mass(v));
-        }
-      });
-      __syncthreads();
-      scan_bins(masses);
-    };
-    fill();
-    // the bin in which the j-th output (j > 0) or the weight `target` lies; `c0`, `m0`: what lies before the bins
-    auto select = [&](uint32_t j, double target, uint32_t c0, uint64_t m0) {
-      const uint32_t ce = tid ? h_cnt[tid - 1] : 0, ci = h_cnt[tid];
-      bool hit;
-      if (j > 0) hit = c0 + ce < j && c0 + ci >= j;
-      else {
-        const uint64_t me = m0 + (tid ? h_mass[tid - 1] : 0), mi = m0 + h_mass[tid];
-        hit = ci > ce && (double)mi >= target && ((double)me < target || c0 + ce == 0);
+    for (int i = 0; i < NW; ++i) { pos += i < wave ? red_c[0][i] : 0; cnt += red_c[0][i]; }
+    if (cnt > CAP) return cnt;
+    if (some)
+      each([&](float v, int i) { if (f(v, i)) l_key[pos++] = ((uint64_t)float_key(v) << 32) | (uint32_t)~i; });
+    if (tid < 8) l_key[cnt + tid] = 0;                   // below every key
+    __syncthreads();
+    // every listed output against every other: 2^lg of them at a time, the others split among the rest of the block
+    const int lg = cnt <= 64 ? 6 : 32 - __builtin_clz(cnt - 1), parts = NT >> lg;
+    const uint32_t e = tid & ((1 << lg) - 1), len = (cnt / parts + 8) & ~7u;
+    const uint32_t j0 = (tid >> lg) * len, j1 = min(j0 + len, (cnt + 7) & ~7u);
+    if (parts > 0 && j0 < j1) {
+      const uint64_t me = l_key[min(e, cnt)];
+      uint32_t r = 0;
+      for (uint32_t j = j0; j < j1; j += 8) {
+        u64x2 q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const u64x2*>(&l_key[j + 2 * i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r += (uint32_t)(q[i][0] > me) + (uint32_t)(q[i][1] > me);
       }
-      if (hit) {
-        s_sel[0] = tid; s_sel[1] = c0 + ce; s_sel[2] = ci - ce;
-        s_before = m0 + (tid && masses ? h_mass[tid - 1] : 0);
-      }
-      __syncthreads();
-    };
-    // the outputs that f(value) picks (at most CAP), in descending order in l_sorted, their weights
-    // in l_mass and running sums (without what lies before) in l_cum
-    auto list = [&](uint32_t cnt, auto&& f) {
-      if (tid == 0) s_n = 0;
-      __syncthreads();
-      each([&](float v, int i) {
-        if (f(v)) {
-          const uint32_t at = atomicAdd(&s_n, 1u);
-          if (at < CAP) l_key[at] = ((uint64_t)float_key(v) << 32) | (uint32_t)~i;
-        }
-      });
-      __syncthreads();
-      const uint64_t mine = tid < cnt ? l_key[tid] : 0;
-      uint32_t rank = 0;
-      for (uint32_t j = 0; j < cnt; ++j) rank += l_key[j] > mine;
-      if (tid < cnt) l_sorted[rank] = mine;
-      __syncthreads();
-      uint64_t w = 0;
-      if (tid < cnt) {
-        const uint32_t key = (uint32_t)(l_sorted[tid] >> 32);
-        w = mass(__uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu)));
-      }
-      const uint64_t cw = wave_scan(w, lane);
-      if (lane == 63) red_u[wave] = cw;
-      __syncthreads();
-      uint64_t before = 0;
-      for (int i = 0; i < wave; ++i) before += red_u[i];
-      if (tid < CAP) { l_mass[tid] = w; l_cum[tid] = cw + before; }
-      __syncthreads();
-    };
-    auto value_of = [&](uint64_t e) {
-      const uint32_t key = (uint32_t)(e >> 32);
-      return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu));
-    };
+      if (e < cnt) atomicAdd(&l_rank[e], r);
+    }
+    __syncthreads();
+    if ((uint32_t)tid < cnt) l_sorted[l_rank[tid]] = l_key[tid];
+    __syncthreads();
+    uint64_t w = 0;
+    if ((uint32_t)tid < cnt) w = mass(value_of((uint32_t)(l_sorted[tid] >> 32)));
+    const uint64_t cw = wave_scan(w);
+    if (lane == 63) red_u[wave] = cw;
+    __syncthreads();
+    uint64_t before = 0;
+#pragma unroll
+    for (int i = 0; i < CAP / 64; ++i) before += i < wave ? red_u[i] : 0;
+    if (tid < CAP) { l_mass[tid] = w; l_cum[tid] = cw + before; }
+    __syncthreads();
+    return cnt;
+  };
 
-    uint32_t kk = k > 0 && (uint32_t)k < h_cnt[NB - 1] ? (uint32_t)k : 0;   // outputs of weight 0 do not count
-    if (kk == 0 && k > 0 && p_on && !masses) {
-      __syncthreads();
-      h_cnt[tid] = 0;
-      masses = true;
-      __syncthreads();
-      fill();
+  const uint64_t least = mp > 0.f ? (uint64_t)ceil(fmin((double)mp, 1.0) * (double)one) : 0;   // min-p's smallest weight
+
+  // ---- a small top-k: the k-th largest of the groups' largest outputs bounds it from below;
+  // what is not below that fits the list as a rule, and nothing else is needed ----
+  if (small_k) {
+    // each group against 2^lgg / per_group of the others per thread
+    const int groups = 1 << lgg, len = groups / per_group;
+    const int me = tid & (groups - 1), j0 = (tid >> lgg) * len;
+    const float g = g_max[me];
+    uint32_t r = 0;
+#pragma unroll 4
+    for (int j = j0; j < j0 + len; j += 4) {
+      const f32x4 q = *reinterpret_cast<const f32x4*>(&g_max[j]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) r += (uint32_t)((q[c] > g) | ((q[c] == g) & (j + c < me)));
     }
-    // where all outputs up to the filter's last bin fit the list, the list is all that is needed
-    bool listed = false;
-    uint64_t total = 0;                                  // weight that top_p takes its share of
-    if (kk > 0 || p_on) {
-      if (kk == 0) total = h_mass[NB - 1];
-      select(kk, p * (double)total, 0, 0);
-      const uint32_t bin = s_sel[0], upto = s_sel[1] + s_sel[2];
-      listed = upto <= CAP;
-      if (listed) {
-        list(upto, [&](float v) { const int b = bin0(v); return b >= 0 && (uint32_t)b <= bin; });
-        const uint32_t nk = kk > 0 ? kk : upto;
-        if (kk > 0) total = l_cum[kk - 1];
-        const double target = p_on ? p * (double)total : INFINITY, least = mp > 0.f ? (double)mp * (double)one : 0.0;
-        auto keep = [&](uint32_t r) {
-          return r == 0 || (r < nk && (double)l_cum[r - 1] < target && (double)l_mass[r] >= least);
-        };
-        const bool mine = (uint32_t)tid < nk && keep(tid);
-        if (mine && !((uint32_t)tid + 1 < nk && keep(tid + 1))) { s_n = tid + 1; s_total = l_cum[tid]; }
-        __syncthreads();
-        const uint32_t kept = s_n;
-        const uint64_t S = s_total;
-        const uint64_t tgt = min((uint64_t)fmin(uu * (double)S, 9.2e18), S - 1);
-        if (mine) {
-          const uint64_t me = l_sorted[tid];
-          uint64_t c = 0;                                // kept weight up to this output, by index
-          for (uint32_t j = 0; j < kept; ++j) c += (uint32_t)l_sorted[j] >= (uint32_t)me ? l_mass[j] : 0;
-          if (c > tgt && c - l_mass[tid] <= tgt) finish(value_of(me), (int)~(uint32_t)me, S);
-        }
-        return;
-      }
+    if (per_group > 1) {                                 // at most 256 of 1024 or 64 of 256 threads' groups: within l_rank
+      atomicAdd(&l_rank[me], r);
+      __syncthreads();
+      r = l_rank[me];
     }
-    // else: the last output of each filter, then a pass over everything kept
-    if (kk > 0 && p_on && !masses) {
+    if (tid < groups && r == (uint32_t)k - 1) s_bound = remap ? -INFINITY : g;
+    __syncthreads();
+    const float bound = s_bound;
+    const uint32_t cnt = list([&](float v, int) { return v >= bound; });
+    if (cnt <= CAP) {
+      const uint32_t nk = min((uint32_t)k, cnt);
+      const double target = p_on ? p * (double)l_cum[nk - 1] : INFINITY;
+      auto keep = [&](uint32_t q) {
+        return q == 0 || (q < nk && (double)l_cum[q - 1] < target && l_mass[q] >= least);
+      };
+      const bool mine = (uint32_t)tid < nk && keep(tid);
+      if (mine && !((uint32_t)tid + 1 < nk && keep(tid + 1))) s_n = tid + 1;
       __syncthreads();
-      h_cnt[tid] = 0;
-      masses = true;
-      __syncthreads();
-      fill();
-    }
-    auto resolve = [&](uint32_t j, double target) {      // -> v_last, i_last, s_last (weight up to and with it)
-      select(j, target, 0, 0);
-      const int bin = (int)s_sel[0];
-      uint32_t before = s_sel[1], cnt = s_sel[2];
-      uint64_t m0 = s_before;
-      // the bin's outputs as a range of keys, cut down while they are too many for the list
-      uint32_t lo = 0, hi = 0;
-      bool keys = false;
-      while (cnt > CAP) {
-        uint32_t a = 0xFFFFFFFFu, z = 0;
-        each([&](float v, int) {
-          if (!(v == v)) return;
-          const uint32_t q = float_key(v);
-          if (keys ? q >= lo && q <= hi : bin0(v) == bin) { a = min(a, q); z = max(z, q); }
-        });
-#pragma unroll
-        for (int s = 1; s < 64; s <<= 1) { a = min(a, (uint32_t)__shfl_xor(a, s, 64)); z = max(z, (uint32_t)__shfl_xor(z, s, 64)); }
-        __syncthreads();
-        if (lane == 0) { red_c[wave] = a; red_i[wave] = (int)z; }
-        __syncthreads();
-        for (int i = 0; i < NW; ++i) { a = min(a, red_c[i]); z = max(z, (uint32_t)red_i[i]); }
-        lo = a; hi = z; keys = true;
-        if (lo == hi) break;                             // all equal: by index alone
-        const int shift = max(0, 32 - __builtin_clz(hi - lo) - (NB == 1024 ? 10 : 8));
-        __syncthreads();
-        h_cnt[tid] = 0;
-        h_mass[tid] = 0;
-        __syncthreads();
-        each([&](float v, int) {
-          if (!(v == v)) return;
-          const uint32_t q = float_key(v);
-          if (q >= lo && q <= hi) {
-            const uint32_t b = (hi - q) >> shift;
-            atomicAdd(&h_cnt[b], 1u);
-            if (masses) atomicAdd((unsigned long long*)&h_mass[b], (unsigned long long)mass(v));
-          }
-        });
-        __syncthreads();
-        scan_bins(masses);
-        select(j, target, before, m0);
-        const uint32_t b = s_sel[0];
-        before = s_sel[1]; cnt = s_sel[2]; m0 = s_before;
-        const uint64_t top = (uint64_t)hi - ((uint64_t)b << shift);
-        hi = (uint32_t)top;
-        const uint64_t below = ((uint64_t)1 << shift) - 1;
-        lo = top - lo > below ? (uint32_t)(top - below) : lo;
+      const uint32_t kept = s_n;
+      const uint64_t S = l_cum[kept - 1];
+      const uint64_t tgt = target_of(S);
+      if (mine) {
+        const uint64_t it = l_sorted[tid];
+        uint64_t c = 0;                                  // kept weight up to this output, by index
+#pragma unroll 4
+        for (uint32_t j = 0; j < kept; ++j) c += (uint32_t)l_sorted[j] >= (uint32_t)it ? l_mass[j] : 0;
+        if (c > tgt && c - l_mass[tid] <= tgt) finish(value_of((uint32_t)(it >> 32)), (int)~(uint32_t)it, S);
       }
-      if (keys && lo == hi && cnt > CAP) {               // the x-th of equal outputs, by index
-        const float v = __uint_as_float(lo ^ ((lo >> 31) ? 0x80000000u : 0xFFFFFFFFu));
-        const uint64_t w = mass(v);
-        uint32_t want;
-        if (j > 0) want = j - before;
-        else {
-          const double need = (target - (double)m0) / (double)(w ? w : 1);
-          want = need <= 1.0 ? 1u : need >= (double)cnt ? cnt : (uint32_t)ceil(need);
-        }
-        uint32_t mine = 0;
-        each([&](float q, int) { mine += q == v; });
-        uint32_t ws = mine;
-#pragma unroll
-        for (int s = 1; s < 64; s <<= 1) ws += __shfl_xor(ws, s, 64);
-        __syncthreads();
-        if (lane == 0) red_c[wave] = ws;
-        __syncthreads();
-        uint32_t skip = 0;
-        int at = 0;
-        while (at < NW - 1 && skip + red_c[at] < want) skip += red_c[at++];
-        if (wave == at) {                                // runs of 256 outputs, 4 per lane, in index order
-          bool done = false;
-          auto step = [&](const f4u& q, int i0) {
-            uint32_t c4 = 0;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) c4 += q[c] == v;
-            const uint32_t inc = wave_scan(c4, lane), tot = __shfl(inc, 63, 64);
-            if (!done && skip + tot >= want) {
-              uint32_t s = skip + inc - c4;
-#pragma unroll
-              for (int c = 0; c < 4; ++c)
-                if (q[c] == v && ++s == want) s_sel[0] = (uint32_t)(i0 + c);
-              done = true;
-            }
-            skip += tot;
-          };
-          if constexpr (R > 0) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) if (r < nr) step(reg[r], first + r * 256);
-          } else {
-            for (int r = 0; r < nr; ++r) step(fetch(r), first + r * 256);
-          }
-        }
-        __syncthreads();
-        v_last = v;
-        i_last = (int)s_sel[0];
-        if (tid == 0) s_last = m0 + (uint64_t)want * w;
-        __syncthreads();
-        return;
-      }
-      list(cnt, [&](float v) {
-        if (!(v == v)) return false;
-        const uint32_t q = float_key(v);
-        return keys ? q >= lo && q <= hi : bin0(v) == bin;
-      });
-      if ((uint32_t)tid < cnt) {
-        const uint64_t me = m0 + l_cum[tid] - l_mass[tid], mi = m0 + l_cum[tid];
-        const bool hit = j > 0 ? before + tid + 1 == j
-                               : ((double)mi >= target || (uint32_t)tid + 1 == cnt) && ((double)me < target || before + tid == 0);
-        if (hit) { s_sel[0] = tid; s_last = mi; }
-      }
-      __syncthreads();
-      const uint64_t e = l_sorted[s_sel[0]];
-      v_last = value_of(e);
-      i_last = (int)~(uint32_t)e;
-      __syncthreads();
-    };
-    if (kk > 0) {
-      resolve(kk, 0.0);
-      total = s_last;
-    }
-    if (p_on) {
-      if (kk > 0) {                                      // the bins may have been cut down: fill them again
-        __syncthreads();
-        h_cnt[tid] = 0;
-        h_mass[tid] = 0;
-        __syncthreads();
-        fill();
-      }
-      const float vk = v_last;
-      const int ik = i_last;
-      resolve(0, p * (double)total);
-      if (kk > 0 && (v_last < vk || (v_last == vk && i_last > ik))) { v_last = vk; i_last = ik; }
+      return;
     }
   }
 
-  // a pass over the kept outputs: their sum, then the one at u times it
-  const double least = mp > 0.f ? fmin((double)mp, 1.0) * (double)one : 0.0;
+  float v_last = -INFINITY;                              // the last kept output: its value and index
+  int i_last = INT32_MAX;
+  auto above = [&](float v, int i) { return (v > v_last) | ((v == v_last) & (i <= i_last)); };   // NaN: no
+
+  // bins of equal width in l from M down to `low` (or where weights end): -1 past it, and for a NaN
+  auto bin_of = [&](float v, float range, float scale, int bins) -> int {
+    const float d = M - v;
+    const int b = (int)fminf(d * scale, (float)(bins - 1));
+    return d <= range ? b : -1;
+  };
+  auto range_to = [&](float low) { const float d = M - low; return d < cut ? d : cut; };
+  auto scale_of = [&](float range, int bins) { return range > 0.f ? fminf((float)bins / range, 3e38f) : 0.f; };
+
+  // block-wide inclusive scan of NB bins in place: h_cnt and h_mass
+  auto scan_bins = [&]() {
+    const uint32_t cw = wave_scan(h_cnt(tid));
+    const uint64_t mw = wave_scan(h_mass(tid));
+    if (lane == 63) { red_c[0][wave] = cw; red_u[wave] = mw; }
+    __syncthreads();
+    uint32_t cb = 0;
+    uint64_t mb = 0;
+    for (int i = 0; i < wave; ++i) { cb += red_c[0][i]; mb += red_u[i]; }
+    h_cnt(tid) = cw + cb;
+    h_mass(tid) = mw + mb;
+    __syncthreads();
+  };
+  // the bin in which the j-th output (j > 0) or the weight `target` lies; c0, m0: what lies before the bins
+  auto select = [&](uint32_t j, double target, uint32_t c0, uint64_t m0) {
+    const uint32_t ce = tid ? h_cnt(tid - 1) : 0, ci = h_cnt(tid);
+    const uint64_t me = m0 + (tid ? h_mass(tid - 1) : 0), mi = m0 + h_mass(tid);
+    const bool hit = j > 0 ? c0 + ce < j && c0 + ci >= j
+                           : ci > ce && (double)mi >= target && ((double)me < target || c0 + ce == 0);
+    if (hit) { s_sel[0] = tid; s_sel[1] = c0 + ce; s_sel[2] = ci - ce; s_before = me; }
+    __syncthreads();
+  };
+  // The last output of a prefix of the kept ones: the j-th (j > 0), or the one with which the
+  // weight reaches `target`; nothing changes where there are fewer with any weight (j).  The general
+  // way: bins of l, then bins of the floats' own order within one bin, until what is left fits the list.
+  auto resolve = [&](uint32_t j, double target, float low) {
+    const bool masses = j == 0;
+    const float range = range_to(low), scale = scale_of(range, NB);
+    auto clear = [&]() {
+      lds_done();
+      __syncthreads();
+      h_cnt(tid) = 0;
+      h_mass(tid) = 0;
+      __syncthreads();
+    };
+    auto add = [&](int b, float v) {
+      atomicAdd(&h_cnt(b), 1u);
+      if (masses) atomicAdd((unsigned long long*)&h_mass(b), (unsigned long long)mass(v));
+    };
+    clear();
+    each([&](float v, int i) {
+      const int b = bin_of(v, range, scale, NB);
+      if (b >= 0 && above(v, i)) add(b, v);
+    });
+    __syncthreads();
+    scan_bins();
+    if (j > h_cnt(NB - 1)) return;
+    select(j, target, 0, 0);
+    const int bin = (int)s_sel[0];
+    uint32_t before = s_sel[1], cnt = s_sel[2];
+    uint64_t m0 = s_before;
+    uint32_t lo = 0, hi = 0;                             // the bin's outputs as a range of keys
+    bool keys = false;
+    auto inside = [&](float v, int i) -> bool {
+      const uint32_t q = float_key(v);
+      return above(v, i) & (keys ? (q >= lo) & (q <= hi) : bin_of(v, range, scale, NB) == bin);
+    };
+    while (cnt > CAP) {
+      uint32_t a = 0, z = 0;                             // ~smallest, largest key
+      each([&](float v, int i) {
+        if (inside(v, i)) { const uint32_t q = float_key(v); a = max(a, ~q); z = max(z, q); }
+      });
+      a = wave_max(a);
+      z = wave_max(z);
+      __syncthreads();
+      if (lane == 0) { red_c[0][wave] = a; red_c[1][wave] = z; }
+      __syncthreads();
+      for (int i = 0; i < NW; ++i) { a = max(a, red_c[0][i]); z = max(z, red_c[1][i]); }
+      lo = ~a; hi = z; keys = true;
+      if (lo == hi) break;                               // all equal: by index alone
+      const int shift = max(0, 32 - __builtin_clz(hi - lo) - (31 - __builtin_clz(NB)));
+      clear();
+      each([&](float v, int i) { if (inside(v, i)) add((int)((hi - float_key(v)) >> shift), v); });
+      __syncthreads();
+      scan_bins();
+      select(j, target, before, m0);
+      const uint32_t b = s_sel[0];
+      before = s_sel[1]; cnt = s_sel[2]; m0 = s_before;
+      hi -= b << shift;
+      const uint32_t below = (1u << shift) - 1;
+      lo = hi - lo > below ? hi - below : lo;
+    }
+    if (cnt > CAP) {                                     // the x-th of equal outputs, by index
+      const float v = value_of(lo);
+      const uint64_t w = mass(v);
+      uint32_t want;
+      if (j > 0) want = j - before;
+      else {
+        const double need = (target - (double)m0) / (double)(w ? w : 1);
+        want = need <= 1.0 ? 1u : need >= (double)cnt ? cnt : (uint32_t)ceil(need);
+      }
+      uint32_t mine = 0;
+      each([&](float q, int i) { mine += (q == v) & above(q, i); });
+      mine = wave_sum(mine);
+      __syncthreads();
+      if (lane == 0) red_c[0][wave] = mine;
+      __syncthreads();
+      uint32_t skip = 0;
+      int wv = 0;
+      while (wv < NW - 1 && skip + red_c[0][wv] < want) skip += red_c[0][wv++];
+      if (wave == wv) {
+        each4([&](const f4u& q, int i0) {
+          uint32_t c4 = 0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) c4 += ((float)q[c] == v) & above((float)q[c], i0 + c);
+          const uint32_t inc = wave_scan(c4), tot = last_lane(inc);
+          uint32_t x = skip + inc - c4;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if ((float)q[c] == v && above((float)q[c], i0 + c) && ++x == want) s_sel[0] = (uint32_t)(i0 + c);
+          skip += tot;
+        });
+      }
+      __syncthreads();
+      v_last = v;
+      i_last = (int)s_sel[0];
+      __syncthreads();
+      return;
+    }
+    list(inside);
+    if ((uint32_t)tid < cnt) {
+      const uint64_t me = m0 + l_cum[tid] - l_mass[tid], mi = m0 + l_cum[tid];
+      const bool hit = j > 0 ? before + tid + 1 == j
+                             : ((double)mi >= target || (uint32_t)tid + 1 == cnt) && ((double)me < target || before + tid == 0);
+      if (hit) s_sel[0] = tid;
+    }
+    __syncthreads();
+    const uint64_t e = l_sorted[s_sel[0]];
+    __syncthreads();
+    v_last = value_of((uint32_t)(e >> 32));
+    i_last = (int)~(uint32_t)e;
+  };
+
+  // ---- a large top-k, then top-p.  Top-p: the kept weights in bins, in several sets by wave: the
+  // sums up to the last kept output are then each set's share of the kept weight ----
+  bool have = false;                                     // set_u holds the sets' kept weights
+#pragma unroll 1
+  for (int stage = 0; stage < 2; ++stage) {
+    if (stage == 0 ? k == 0 : !p_on) continue;
+    uint32_t j = (uint32_t)k;
+    double target = 0.0;
+    const float low = fmaxf(mn, v_last);
+    if (stage == 1) {
+      const float range = range_to(low), scale = scale_of(range, PB);
+      const int set = wave / PER;
+      lds_done();
+      __syncthreads();
+      for (int b = tid; b < SETS * PB; b += NT) set_mass(0, b) = 0;
+      __syncthreads();
+      each4([&](const f4u& q, int i0) {
+        uint64_t w[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[c] = mass((float)q[c]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int b = bin_of((float)q[c], range, scale, PB);
+          if ((b >= 0) & above((float)q[c], i0 + c)) atomicAdd((unsigned long long*)&set_mass(set, b), (unsigned long long)w[c]);
+        }
+      });
+      __syncthreads();
+      uint64_t sum = 0;
+      if (tid < PB)
+#pragma unroll
+        for (int i = 0; i < SETS; ++i) sum += set_mass(i, tid);
+      const uint64_t cw = wave_scan(sum);
+      if (lane == 63) red_u[wave] = cw;
+      __syncthreads();
+      uint64_t incl = cw, total = 0;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) { incl += i < wave ? red_u[i] : 0; total += red_u[i]; }
+      target = p * (double)total;
+      if (tid < PB) {
+        const uint64_t excl = incl - sum;
+        if (sum > 0 && (double)incl >= target && ((double)excl < target || excl == 0)) { s_sel[1] = tid; s_before = excl; }
+      }
+      __syncthreads();
+      const int bin = (int)s_sel[1];
+      const uint64_t m0 = s_before;
+      const uint32_t cnt = list([&](float v, int i) { return above(v, i) & (bin_of(v, range, scale, PB) == bin); });
+      if (cnt <= CAP) {
+        if ((uint32_t)tid < cnt) {
+          const uint64_t me = m0 + l_cum[tid] - l_mass[tid], mi = m0 + l_cum[tid];
+          if (((double)mi >= target || (uint32_t)tid + 1 == cnt) && ((double)me < target || (m0 == 0 && tid == 0))) s_sel[0] = tid;
+        }
+        uint64_t mine = 0;                               // one wave per set sums its bins before the last
+        if (wave < SETS)
+          for (int b = lane; b < bin; b += 64) mine += set_mass(wave, b);
+        mine = wave_sum(mine);
+        if (lane == 0 && wave < SETS) set_u[wave] = mine;
+        __syncthreads();
+        const uint32_t last = s_sel[0];
+        if ((uint32_t)tid <= last) {
+          const int i = (int)~(uint32_t)l_sorted[tid];
+          atomicAdd((unsigned long long*)&set_u[i / (nr * 256 * PER)], (unsigned long long)l_mass[tid]);
+        }
+        const uint64_t e = l_sorted[last];
+        v_last = value_of((uint32_t)(e >> 32));
+        i_last = (int)~(uint32_t)e;
+        have = !(mp > 0.f);
+        __syncthreads();
+        continue;
+      }
+      j = 0;
+    }
+    resolve(j, target, low);
+  }
+
+  // ---- the draw: the waves' (or sets') kept weights, then the run of outputs that holds u times their sum ----
   float v_least = v_last;
   if (mp > 0.f) v_least = fmaxf(v_least, (float)((double)M + T * log(fmin((double)mp, 1.0)) * 1.0001 - 1e-5 * fabs((double)M)));
-  auto kept_mass = [&](float v, int i) -> uint64_t {
-    if (!(v >= v_least) || (v == v_last && i > i_last)) return 0;
-    const uint64_t w = mass(v);
-    return (double)w >= least ? w : 0;
-  };
-  __syncthreads();                                       // red_u has been read
-  uint64_t sum = 0;
-  each([&](float v, int i) { sum += kept_mass(v, i); });
-  uint64_t ws = sum;
+  // the kept weights of four outputs (0 for the others); returns their sum
+  auto kept4 = [&](const f4u& q, int i0, uint64_t (&w)[4]) -> uint64_t {
+    float x[4];
+    bool any4 = false;
 #pragma unroll
-  for (int s = 1; s < 64; s <<= 1) ws += __shfl_xor((unsigned long long)ws, s, 64);
-  if (lane == 0) red_u[wave] = ws;
-  __syncthreads();
-  uint64_t S = 0;
-#pragma unroll
-  for (int i = 0; i < NW; ++i) S += red_u[i];
-  const uint64_t tgt = min((uint64_t)fmin(uu * (double)S, 9.2e18), S - 1);
-  uint64_t acc = 0;
-  int at = 0;
-  while (at < NW - 1 && acc + red_u[at] <= tgt) acc += red_u[at++];
-  if (wave != at) return;
-  // the wave whose run holds it: 256 outputs at a time
-  bool done = false;
-  auto step = [&](const f4u& q, int i0) {
-    if (done) return;
-    uint64_t w[4], l4 = 0;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) { w[c] = kept_mass((float)q[c], i0 + c); l4 += w[c]; }
-    const uint64_t inc = wave_scan(l4, lane), tot = shfl64(inc, 63);
-    if (acc + tot > tgt) {
-      uint64_t s = acc + inc - l4;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        if (s <= tgt && s + w[c] > tgt) finish((float)q[c], i0 + c, S);
-        s += w[c];
-      }
-      done = true;
+    for (int c = 0; c < 4; ++c) {
+      const float v = (float)q[c];
+      const bool in = (v >= v_least) & ((v != v_last) | (i0 + c <= i_last));            // NaN: no
+      x[c] = in ? v : -INFINITY;
+      any4 |= in;
+      w[c] = 0;
     }
-    acc += tot;
-  };
-  if constexpr (R > 0) {
+    if (any4) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) if (r < nr) step(reg[r], first + r * 256);
+      for (int c = 0; c < 4; ++c) w[c] = mass(x[c]);
+      if (mp > 0.f)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[c] = w[c] >= least ? w[c] : 0;
+    }
+    return w[0] + w[1] + w[2] + w[3];
+  };
+  uint64_t S = 0, acc = 0;
+  if (!have) {
+    __syncthreads();                                     // red_u has been read
+    uint64_t sum = 0;
+    each4([&](const f4u& q, int i0) { uint64_t w[4]; sum += kept4(q, i0, w); });
+    sum = wave_sum(sum);
+    if (lane == 0) red_u[wave] = sum;
+    __syncthreads();
+  }
+  // the piece (a wave's runs, or a set's) that holds the target
+  const int pieces = have ? SETS : NW, per = have ? PER * nr : nr;
+  auto share = [&](int i) { return have ? set_u[i] : red_u[i]; };
+  for (int i = 0; i < pieces; ++i) S += share(i);
+  const uint64_t tgt = target_of(S);
+  int piece = 0;
+  while (piece < pieces - 1 && acc + share(piece) <= tgt) acc += share(piece++);
+  int run = 0;                                           // the piece's run
+  if constexpr (WHERE == IN_REGS) {
+    if (wave != piece) return;                           // a piece is one run
   } else {
-    for (int r = 0; r < nr && !done; ++r) step(fetch(r), first + r * 256);
+    // its runs, 64 at a time, among all waves
+    for (;;) {
+      for (int i = wave; i < 64 && run + i < per; i += NW) {
+        const int i0 = (piece * per + run + i) * 256 + lane * 4;
+        uint64_t w[4];
+        const uint64_t t = wave_sum(kept4(at(i0), i0, w));
+        if (lane == 0) run_u[i] = t;
+      }
+      __syncthreads();
+      const int m = min(64, per - run);
+      const bool last = run + m >= per;
+      int i = 0;
+      while (i < (last ? m - 1 : m) && acc + run_u[i] <= tgt) acc += run_u[i++];
+      run += i;
+      if (i < m) break;
+      __syncthreads();
+    }
+    if (wave != 0) return;
+  }
+  const int i0 = (piece * per + run) * 256 + lane * 4;
+  uint64_t w[4];
+  const f4u q = at(i0);
+  const uint64_t l4 = kept4(q, i0, w);
+  uint64_t x = acc + wave_scan(l4) - l4;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    if (x <= tgt && x + w[c] > tgt) finish((float)q[c], i0 + c, S);
+    x += w[c];
   }
 }
 
@@ -528,11 +745,11 @@ hipError_t launch_sample(const Plan& pl, const float* out, const vfm_sampling& s
                          float* logprob, int max_out, hipStream_t s) {
   const SampleParams q = {sp.temperature, sp.top_k, sp.top_p, sp.min_p};
   const int pi = prof_begin(VFM_PROF_OTHER, s);
-#define SAMPLE(NT_, R_) \
-  hipLaunchKernelGGL((sample_kernel<NT_, R_>), dim3(pl.n_req), dim3(NT_), 0, s, pl, out, q, u, ids, logprob)
-  if (max_out <= 1024) SAMPLE(256, 1);
-  else if (max_out <= 4096) SAMPLE(256, 4);
-  else SAMPLE(1024, 0);
+#define SAMPLE(NT_, W_) \
+  hipLaunchKernelGGL((sample_kernel<NT_, W_>), dim3(pl.n_req), dim3(NT_), 0, s, pl, out, q, u, ids, logprob)
+  if (max_out <= 1024) SAMPLE(256, IN_REGS);
+  else if (max_out <= 32768) SAMPLE(1024, IN_LDS);
+  else SAMPLE(1024, IN_MEMORY);
 #undef SAMPLE
   prof_end(pi, s);
   return hipGetLastError();
