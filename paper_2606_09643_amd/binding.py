@@ -282,6 +282,10 @@ class PagedKV:
         self.c = vfm_kv_pages(k.data_ptr(), v.data_ptr(), k.shape[1] // page_size, int(page_size),
                               self.table.shape[1], self.table.ctypes.data_as(C.POINTER(C.c_int32)),
                               self.table_dev.data_ptr())
+        # what the bounded-cache calls compare with their attention and rows; None if the pools do not go together
+        same = k.shape == v.shape and k.dtype == v.dtype and k.device == v.device == self.table_dev.device
+        dense = k.dim() == 3 and k.is_contiguous() and v.is_contiguous() and k.shape[1] % int(page_size) == 0
+        self.layout = (k.dtype, k.shape[0], k.shape[2], k.device) if same and dense else None
 
 
 def vfm_layer_forward_paged(cfg, weights, lora, batch, x, kv, workspace, stream=None):
@@ -480,39 +484,35 @@ def vfm_greedy_tokens(batch, out, ids, stream=None):
 _TORCH_DTYPE = {VFM_F32: torch.float32, VFM_BF16: torch.bfloat16}
 
 
-def _operand(t, name, dtype, numel, device=None):
+def _operand(t, name, dtype, numel, device):
     """t as the library takes it: of that type, dense, at least numel elements, on `device`."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
-        raise ValueError(f"{name}: a {dtype} tensor is expected")
-    if not t.is_contiguous() or t.numel() < numel:
-        raise ValueError(f"{name}: a dense tensor of at least {numel} elements is expected")
-    if device is not None and t.device != device:
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < numel:
+        raise ValueError(f"{name}: a dense {dtype} tensor of at least {numel} elements is expected")
+    if t.device != device:
         raise ValueError(f"{name}: on {t.device}, the other operands on {device}")
     return t.data_ptr()
 
 
-def _rows(t, name, attn, batch, cols, device=None):
+def _rows(t, name, dtype, T, cols, device):
     """(pointer, row stride) of a [T, cols or more] tensor whose rows are dense."""
-    T = batch.plan_host[2]
-    if not isinstance(t, torch.Tensor) or t.dtype != _TORCH_DTYPE[attn.dtype] or t.dim() != 2:
-        raise ValueError(f"{name}: a 2-dimensional {_TORCH_DTYPE[attn.dtype]} tensor is expected")
-    if t.shape[0] < T or t.shape[1] < cols or t.stride(1) != 1 or (T > 1 and t.stride(0) < cols):
+    if t.dtype != dtype or t.dim() != 2:
+        raise ValueError(f"{name}: a 2-dimensional {dtype} tensor is expected")
+    n, width = t.shape
+    ld, step = t.stride()
+    if n < T or width < cols or step != 1 or (T > 1 and ld < cols):
         raise ValueError(f"{name}: {T} dense rows of at least {cols} columns are expected")
-    if device is not None and t.device != device:
+    if t.device != device:
         raise ValueError(f"{name}: on {t.device}, the other operands on {device}")
-    return t.data_ptr(), t.stride(0) if T > 1 else -(-cols // 8) * 8
+    return t.data_ptr(), ld if T > 1 else -(-cols // 8) * 8
 
 
-def _cache(kv, attn, device):
+def _cache(kv, attn, dtype, device):
     """The C struct of a PagedKV, its pools checked against the attention (a vfm_kv_pages is taken as it is)."""
     if not isinstance(kv, PagedKV):
         return kv
-    for t in (kv.k, kv.v):
-        if t.dtype != _TORCH_DTYPE[attn.dtype] or tuple(t.shape) != (attn.n_kv_heads, kv.c.n_pages * kv.c.page_size,
-                                                                     attn.head_dim) or not t.is_contiguous():
-            raise ValueError("the cache's pools are not [n_kv_heads, n_pages * page_size, head_dim] of the attention")
-        if t.device != device or kv.table_dev.device != device:
-            raise ValueError("the cache is on another device than the rows")
+    if kv.layout != (dtype, attn.n_kv_heads, attn.head_dim, device):
+        raise ValueError("the cache's pools and table are not dense [n_kv_heads, n_pages * page_size, head_dim] of the "
+                         "attention's type on the rows' device")
     return kv.c
 
 
@@ -522,11 +522,11 @@ def make_attn(dtype, n_heads, n_kv_heads, head_dim, window=0, n_sink=0, scale=0.
 
 def vfm_kv_append(attn, batch, qkv, q_out, kv, stream=None):
     """qkv: [T, (n_heads + 2 n_kv_heads) * head_dim or more]; q_out: dense [T, n_heads * head_dim]."""
-    hd = attn.head_dim
-    p, ld = _rows(qkv, "qkv", attn, batch, (attn.n_heads + 2 * attn.n_kv_heads) * hd)
-    q = _operand(q_out, "q_out", qkv.dtype, batch.plan_host[2] * attn.n_heads * hd, qkv.device)
-    st = _lib_handle().vfm_kv_append(C.byref(attn), C.byref(batch), p, ld, q,
-                                     C.byref(_cache(kv, attn, qkv.device)), _stream(stream))
+    hd, T, td, dev = attn.head_dim, batch.plan_host[2], _TORCH_DTYPE.get(attn.dtype), qkv.device
+    p, ld = _rows(qkv, "qkv", td, T, (attn.n_heads + 2 * attn.n_kv_heads) * hd, dev)
+    q = _operand(q_out, "q_out", td, T * attn.n_heads * hd, dev)
+    st = _lib_handle().vfm_kv_append(C.byref(attn), C.byref(batch), p, ld, q, C.byref(_cache(kv, attn, td, dev)),
+                                     _stream(stream))
     _check(st, "vfm_kv_append")
 
 
@@ -539,12 +539,12 @@ def vfm_attention_workspace(attn, batch) -> int:
 
 def vfm_attention_paged(attn, batch, q, kv, out, workspace=None, stream=None):
     """q, out: [T, n_heads * head_dim or more], rows dense; kv: a PagedKV or a vfm_kv_pages."""
-    cols = attn.n_heads * attn.head_dim
-    pq, ldq = _rows(q, "q", attn, batch, cols)
-    po, ldo = _rows(out, "out", attn, batch, cols, q.device)
+    cols, T, td, dev = attn.n_heads * attn.head_dim, batch.plan_host[2], _TORCH_DTYPE.get(attn.dtype), q.device
+    pq, ldq = _rows(q, "q", td, T, cols, dev)
+    po, ldo = _rows(out, "out", td, T, cols, dev)
     ws, nb = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
     st = _lib_handle().vfm_attention_paged(C.byref(attn), C.byref(batch), pq, ldq,
-                                           C.byref(_cache(kv, attn, q.device)), po, ldo, ws, nb, _stream(stream))
+                                           C.byref(_cache(kv, attn, td, dev)), po, ldo, ws, nb, _stream(stream))
     _check(st, "vfm_attention_paged")
 
 
@@ -574,24 +574,28 @@ class Sampling:
 
     def __init__(self, temperature=None, top_k=None, top_p=None, min_p=None):
         self.tensors = {"temperature": temperature, "top_k": top_k, "top_p": top_p, "min_p": min_p}
-        for n, t in self.tensors.items():
-            if t is not None and (t.dtype != (torch.int32 if n == "top_k" else torch.float32)
-                                  or not t.is_contiguous()):
-                raise ValueError(f"{n}: a dense {'int32' if n == 'top_k' else 'float32'} tensor is expected")
+        given = {n: t for n, t in self.tensors.items() if t is not None}
+        for n, t in given.items():
+            want = torch.int32 if n == "top_k" else torch.float32
+            if t.dtype != want or not t.is_contiguous():
+                raise ValueError(f"{n}: a dense {want} tensor is expected")
+        if len({t.device for t in given.values()}) > 1:
+            raise ValueError("the sampling parameters are on different devices")
+        self.n = min((t.numel() for t in given.values()), default=None)      # requests they are enough for
+        self.device = next((t.device for t in given.values()), None)
         self.c = vfm_sampling(*[_ptr(t) for t in self.tensors.values()])
 
 
 def vfm_sample_tokens(batch, out, sampling, u, ids, logprob=None, stream=None):
     """One token per request drawn from its head outputs; sampling: a Sampling."""
-    n = batch.plan_host[0]
-    po = _operand(out, "out", torch.float32, batch.plan_host[6])
-    for name, t in sampling.tensors.items():
-        if t is not None:
-            _operand(t, name, t.dtype, n, out.device)
-    st = _lib_handle().vfm_sample_tokens(C.byref(batch), po, C.byref(sampling.c),
-                                         _operand(u, "u", torch.float32, n, out.device),
-                                         _operand(ids, "ids", torch.int32, n, out.device),
-                                         _operand(logprob, "logprob", torch.float32, n, out.device)
+    n, dev = batch.plan_host[0], out.device
+    if sampling.n is not None and (sampling.n < n or sampling.device != dev):
+        raise ValueError(f"the sampling parameters are for {sampling.n} requests on {sampling.device}, the batch has "
+                         f"{n} on {dev}")
+    st = _lib_handle().vfm_sample_tokens(C.byref(batch), _operand(out, "out", torch.float32, batch.plan_host[6], dev),
+                                         C.byref(sampling.c), _operand(u, "u", torch.float32, n, dev),
+                                         _operand(ids, "ids", torch.int32, n, dev),
+                                         _operand(logprob, "logprob", torch.float32, n, dev)
                                          if logprob is not None else None, _stream(stream))
     _check(st, "vfm_sample_tokens")
 

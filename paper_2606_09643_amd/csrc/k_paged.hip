@@ -93,8 +93,18 @@ __device__ __forceinline__ bf16x8 drop_nonfinite(const bf16x8& v, bool& found) {
 }
 __device__ __forceinline__ bool nonfinite(float v) { return !(fabsf(v) < INFINITY); }
 
-// Slot of position k in a request's page row.
-__device__ __forceinline__ int page_slot(const int32_t* prow, int lp, int k) {
+// A value that every lane of the wave holds, as a scalar.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// A request's page row.  Nothing writes it during the kernel: positions that are
+// uniform over a wave are looked up with scalar loads, beside the vector loads
+// that are in flight.
+typedef const int32_t __attribute__((address_space(4)))* page_row;
+__device__ __forceinline__ page_row row_of(const KvPages& kp, int request) {
+  return (page_row)(uintptr_t)(kp.table + (int64_t)request * kp.max_pages);
+}
+// Slot of position k.
+__device__ __forceinline__ int page_slot(page_row prow, int lp, int k) {
   return (prow[k >> lp] << lp) + (k & ((1 << lp) - 1));
 }
 
@@ -192,7 +202,7 @@ __device__ __forceinline__ int few_vswz(int r) {
 }
 
 template <int DH>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attn_few_bf16_kernel(Plan pl, PagedAttn a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_few_bf16_kernel(Plan pl, PagedAttn a) {
   constexpr int LPR = DH / 8;          // lanes per K / V row (16 bytes each)
   constexpr int RPI = 64 / LPR;        // rows per wave-wide load
   constexpr int VI = 32 / RPI;         // V loads per lane and tile
@@ -209,7 +219,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
     w.qt = id % a.qtiles;
     w.p = id / a.qtiles;
   }
-  const int R0 = pl.cu_seqlens[w.p], m = pl.cu_seqlens[w.p + 1] - R0, ctx = pl.ctx[w.p];
+  const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
   if (!few_rows(VFM_BF16, m, a.G)) return;              // block-uniform, as every exit below
   const int qn = m * a.G;
   if (w.qt * 16 >= qn) return;
@@ -232,7 +242,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + 32 * s);
   }
-  const int32_t* prow = a.kp.table + (int64_t)pl.order[w.p] * a.kp.max_pages;
+  const page_row prow = row_of(a.kp, uniform(pl.order[w.p]));
   const int lp = a.kp.log2_page;
   const bf16* kh = (const bf16*)a.k + (int64_t)w.h * a.slots * DH;
   const bf16* vh = (const bf16*)a.v + (int64_t)w.h * a.slots * DH;
@@ -414,37 +424,56 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
 // Many rows (prompts and chunks), bf16: one block per 128 packed queries of one
 // request and key head (and chunk of the keys where the request has few
 // blocks); 4 waves of 32 queries on v_mfma_f32_32x32x16_bf16, so a K or V
-// fragment read from LDS feeds 32 queries.  64-key tiles of K and V are staged
-// through registers into two LDS stages (one barrier per tile; the next
-// tile's loads are in flight during the current one's compute, their slots
-// looked up a tile earlier).
+// fragment read from LDS feeds 32 queries.  64-key tiles of K and V go from
+// memory straight into a ring of LDS stages (global_load_lds, one barrier per
+// tile), two stages of 32 KB with head dim 128 and four of 16 KB with 64: two
+// blocks share a CU.  A wave-wide load takes whole rows of one 16-position run,
+// whose page it looks up as a scalar, a tile ahead of the load.
 // ---------------------------------------------------------------------------
+typedef const __attribute__((address_space(1))) void* gptr_t;
+typedef __attribute__((address_space(3))) void* lptr_t;
+
 __device__ __forceinline__ f32x16 mfma32(const bf16x8& a, const bf16x8& b, const f32x16& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-// 16-byte chunk c of key row r: the 16 rows that one phase of a fragment read
-// touches lie in different banks
+// The stages swizzle their rows: physical 16-byte chunk of logical chunk c of K
+// row r: the 16 rows that one phase of a fragment read touches lie in different
+// banks.  (An involution: it maps physical to logical chunks as well.)
 template <int DH>
 __device__ __forceinline__ int rows_kswz(int r, int c) {
   return DH == 128 ? (c ^ (r & 15)) : (c ^ ((r >> 1) & 7));
 }
-// 64-byte segment of V row r: the 4 rows that one half of a transposing read
-// touches lie in different banks
+// V by 64-byte segments: the 4 rows that one half of a transposing read touches
+// lie in different banks
 template <int DH>
-__device__ __forceinline__ int rows_vswz(int r) {
-  return DH == 128 ? (r & 3) : ((r >> 1) & 1);
+__device__ __forceinline__ int rows_vswz(int r, int c) {
+  return c ^ ((DH == 128 ? (r & 3) : ((r >> 1) & 1)) << 2);
 }
 
+// wait until at most n loads of the wave are outstanding and its LDS accesses have finished
+template <int N>
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14)); }
+
 template <int DH>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attn_rows_bf16_kernel(Plan pl, PagedAttn a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_rows_bf16_kernel(Plan pl, PagedAttn a) {
   constexpr int CH = DH / 8;             // 16-byte chunks per row
-  constexpr int KPT = 64 * CH / 256;     // K (and V) chunks per thread and tile
+  constexpr int RPI = 64 / CH;           // rows per wave-wide load
+  constexpr int NI = 64 / (4 * RPI);     // K (and V) loads per wave and tile
   constexpr int KS = DH / 16;            // MFMA steps over the head dims
   constexpr int ND = DH / 32;            // output tiles
-  __shared__ __attribute__((aligned(16))) bf16 Ks[2][64 * DH];
-  __shared__ __attribute__((aligned(16))) bf16 Vs[2][64 * DH];
-  __shared__ int s_poison[2];
+  constexpr int NST = DH == 128 ? 2 : 4; // LDS stages
+  // a variable per stage (K, then V), so that the compiler can tell the one that is read from the
+  // ones being filled and does not wait for their loads
+  constexpr int TE = 64 * DH, SE = 2 * TE;
+  __shared__ __attribute__((aligned(16))) bf16 stage0[SE], stage1[SE], stage2[NST > 2 ? SE : 8], stage3[NST > 3 ? SE : 8];
+  auto stage = [&](auto b) -> bf16* {
+    if constexpr (b == 0) return stage0;
+    else if constexpr (b == 1) return stage1;
+    else if constexpr (b == 2) return stage2;
+    else return stage3;
+  };
+  __shared__ int s_poison;
 
   const int rb = rows_per_block(a.G);
   Work w;
@@ -460,11 +489,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
     int lo = 0, hi = pl.n_req - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (pl.cu_seqlens[mid] / rb + mid <= blk) lo = mid; else hi = mid - 1;
+      if (uniform(pl.cu_seqlens[mid]) / rb + mid <= blk) lo = mid; else hi = mid - 1;
     }
     w.p = lo;
   }
-  const int R0 = pl.cu_seqlens[w.p], m = pl.cu_seqlens[w.p + 1] - R0, ctx = pl.ctx[w.p];
+  const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
   // a request's last rows see the most keys: they come first
   const int nb = (m + rb - 1) / rb;
   const int bi = blk - (R0 / rb + w.p);
@@ -492,11 +521,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s);
   }
-  const int32_t* prow = a.kp.table + (int64_t)pl.order[w.p] * a.kp.max_pages;
+  const int64_t trow = (int64_t)uniform(pl.order[w.p]) * a.kp.max_pages;   // the request's page row
   const int lp = a.kp.log2_page;
   const bf16* kh = (const bf16*)a.k + (int64_t)w.h * a.slots * DH;
   const bf16* vh = (const bf16*)a.v + (int64_t)w.h * a.slots * DH;
-  if (tid < 2) s_poison[tid] = -1;
+  if (tid == 0) s_poison = -1;
 
   f32x16 o[ND];
 #pragma unroll
@@ -505,61 +534,66 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   float m_run = NEG_BIG, l_run = 0.f;
 
-  int slot[KPT];
-  bf16x8 kr[KPT], vr[KPT];
-  // positions that no row of the block sees read a seen one instead: their page may not exist
+  // A lane's load i of a tile: row RPI (4 i + wave) + lane / CH, physical chunk lane % CH;
+  // within its 16-position run the row, and with it the swizzle, is the same for every i.
+  const int lrow = RPI * wave + lane / CH;                // mod 16: the row in its run
+  const int koff = (lrow & 15) * DH + rows_kswz<DH>(lrow, lane % CH) * 8;
+  const int voff = (lrow & 15) * DH + rows_vswz<DH>(lrow, lane % CH) * 8;
+  // The pages of a tile's four runs and where the runs start in them, in lanes 0..3 (of every four).
+  // A run that no row sees reads a seen one instead: its page may not exist.
+  int page = 0, in_page = 0;
   auto look_up = [&](int t) {
-    const int kb = 64 * vis.run(min(t, vis.n - 1));
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-      int k = min(kb + (tid + 256 * i) / CH, j1);
-      if (k < lo_any && k >= a.n_sink) k = lo_any;
-      slot[i] = page_slot(prow, lp, k);
-    }
+    int k = min(64 * vis.run(min(t, vis.n - 1)) + 16 * (lane & 3), j1 & ~15);
+    if (k + 15 < lo_any && k >= a.n_sink) k = lo_any & ~15;
+    page = a.kp.table[trow + (k >> lp)];
+    in_page = k & ((1 << lp) - 1);
   };
-  auto load = [&]() {
+  auto issue = [&](auto b, int next) {                    // the tile looked up last into stage b; looks `next` up
+    int64_t run[NI];
+    const int slots = (page << lp) + in_page;
 #pragma unroll
-    for (int i = 0; i < KPT; ++i)
-      kr[i] = *reinterpret_cast<const bf16x8*>(kh + (int64_t)slot[i] * DH + 8 * ((tid + 256 * i) % CH));
+    for (int i = 0; i < NI; ++i)
+      run[i] = (int64_t)__builtin_amdgcn_readlane(slots, RPI * (4 * i + wave) >> 4) * DH;
+    look_up(next);
 #pragma unroll
-    for (int i = 0; i < KPT; ++i)
-      vr[i] = *reinterpret_cast<const bf16x8*>(vh + (int64_t)slot[i] * DH + 8 * ((tid + 256 * i) % CH));
+    for (int i = 0; i < NI; ++i)
+      __builtin_amdgcn_global_load_lds((gptr_t)(kh + run[i] + koff), (lptr_t)(stage(b) + RPI * (4 * i + wave) * DH), 16, 0, 0);
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      __builtin_amdgcn_global_load_lds((gptr_t)(vh + run[i] + voff), (lptr_t)(stage(b) + TE + RPI * (4 * i + wave) * DH), 16, 0, 0);
   };
-  auto store = [&](int b, int t) {
+  // V rows of a tile that some row of the block does not see: zeros where none sees them, no
+  // infinities or NaN where some do
+  auto mend = [&](auto b, int t) {
     const int kb = 64 * vis.run(t);
-    const bool full = seen_by_all(j0, j1, kb, kb + 63, a.window, a.n_sink);
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-      const int c = tid + 256 * i, key = c / CH, ch = c % CH;
-      *reinterpret_cast<bf16x8*>(&Ks[b][key * DH + rows_kswz<DH>(key, ch) * 8]) = kr[i];
-      bf16x8 v = vr[i];
-      if (!full) {
-        const int k = kb + key;
+#pragma unroll 1
+    for (int i = 0; i < NI; ++i) {
+      const int r = RPI * 4 * i + lrow, k = kb + r;
+      bf16x8* at = reinterpret_cast<bf16x8*>(stage(b) + TE + r * DH + (lane % CH) * 8);
+      if (!seen_by_any(j0, j1, k, a.window, a.n_sink)) *at = bf16x8{};
+      else if (!seen_by_all(j0, j1, k, k, a.window, a.n_sink)) {
         bool found = false;
-        if (!seen_by_any(j0, j1, k, a.window, a.n_sink)) v = bf16x8{};
-        else if (!seen_by_all(j0, j1, k, k, a.window, a.n_sink)) v = drop_nonfinite(v, found);
-        if (found) s_poison[b] = t;
+        const bf16x8 v = drop_nonfinite(*at, found);
+        if (found) { *at = v; s_poison = t; }
       }
-      *reinterpret_cast<bf16x8*>(&Vs[b][key * DH + ((((ch >> 2) ^ rows_vswz<DH>(key)) << 2) | (ch & 3)) * 8]) = v;
     }
   };
 
   // fragment addresses (bytes): K row x of a 32-key half, chunk 2 s + h2;
   // V: the transposing read takes 4 keys x 16 dims per 16 lanes, lane (x & 15)
-  // bringing key (x & 15) / 4, dims 4 (x & 3)
+  // bringing key (x & 15) / 4, dims 4 (x & 3).  Its rows differ from the lane's
+  // first by multiples of 8, which leave the swizzle alone.
   const int kq = x & 15, gq = x >> 4;
-  int kaddr = x * DH * 2 + (rows_kswz<DH>(x, h2) << 4);
-  int vaddr = (4 * h2 + (kq >> 2)) * DH * 2 + (rows_vswz<DH>(kq >> 2) << 6) + gq * 32 + (kq & 3) * 8;
-  static_assert(DH == 128 || DH == 64, "");
-  // DH 64: the segment's swizzle takes bit 1 of the row, which 4 h2 and 8-row steps leave alone
+  const int kaddr = x * DH * 2 + (rows_kswz<DH>(x, h2) << 4);
+  const int vaddr = (4 * h2 + (kq >> 2)) * DH * 2 + (rows_vswz<DH>(kq >> 2, 0) << 4) + gq * 32 + (kq & 3) * 8;
 
-  auto compute = [&](int b, int t) {
+  auto compute = [&](auto b, int t) {
     const int kb = 64 * vis.run(t);
     // the wave has no query, or none that sees the tile
     if (wave * 32 >= qn || kb > wj1 || (a.window > 0 && wj0 - (kb + 63) >= a.window && kb >= a.n_sink)) return;
     const bool full = seen_by_all(wj0, wj1, kb, kb + 63, a.window, a.n_sink);
     f32x16 st[2];
-    const char* kp = reinterpret_cast<const char*>(Ks[b]);
+    const char* kp = reinterpret_cast<const char*>(stage(b));
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       f32x16 acc;
@@ -572,13 +606,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
       }
       st[kt] = acc;
     }
+    // fragments are read six ahead of their MFMA
+    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+    for (int s = 0; s < 2 * KS - 6; ++s) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
     if (!full) {
+      // made anew in each masked tile: held over the loop, the compares' lane masks would fill the scalar registers
+      int d0 = jq - kb - 4 * h2, n0 = a.n_sink - kb - 4 * h2;   // of the lane's key 0
+      asm volatile("" : "+v"(d0), "+v"(n0));
+      const int win = a.window > 0 ? a.window : INT32_MAX;
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int k = kb + 32 * kt + 8 * (i >> 2) + 4 * h2 + (i & 3);
-          st[kt][i] = sees(jq, k, a.window, a.n_sink) ? st[kt][i] : -INFINITY;
+          const int k = 32 * kt + 8 * (i >> 2) + (i & 3);
+          const bool see = (d0 >= k) & ((d0 - k < win) | (k < n0));
+          st[kt][i] = see ? st[kt][i] : -INFINITY;
         }
     }
     float mb = st[0][0];
@@ -595,7 +642,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
 #pragma unroll
       for (int i = 0; i < ND; ++i) o[i] *= alpha;
     }
-    const char* vp = reinterpret_cast<const char*>(Vs[b]);
+    const char* vp = reinterpret_cast<const char*>(stage(b) + TE);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {                         // 16 keys: 8 of them in this lane
       float e[8];
@@ -618,39 +665,58 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
       }
     }
   };
-  // the infinities and NaN that the staging left out of tile t
+  // the infinities and NaN that `mend` took out of tile t
   auto add_nonfinite = [&](int t) {
     const int kb = 64 * vis.run(t);
+#pragma unroll 1
     for (int r = 0; r < 64; ++r) {
       const int k = kb + r;
       if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
-      const bf16* vrow = vh + (int64_t)page_slot(prow, lp, k) * DH + 4 * h2;
-      const bool see = sees(jq, k, a.window, a.n_sink);
+      const bf16* vrow = vh + (int64_t)((a.kp.table[trow + (k >> lp)] << lp) + (k & ((1 << lp) - 1))) * DH + 4 * h2;
+      if (sees(jq, k, a.window, a.n_sink)) {
 #pragma unroll
-      for (int d = 0; d < ND; ++d)
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float v = (float)vrow[32 * d + 8 * (i >> 2) + (i & 3)];
-          if (see && nonfinite(v)) o[d][i] += v;
-        }
+          for (int i = 0; i < 16; ++i) {
+            const float v = (float)vrow[32 * d + 8 * (i >> 2) + (i & 3)];
+            o[d][i] += nonfinite(v) ? v : 0.f;
+          }
+      }
     }
   };
 
   if (t0 < t1) {
     look_up(t0);
-    load();
-    look_up(t0 + 1);
-    __syncthreads();                                      // s_poison
-    store(0, t0);
-    __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-      const int b = (t - t0) & 1;
-      const bool more = t + 1 < t1;
-      if (more) { load(); look_up(t + 2); }
-      compute(b, t);
-      if (s_poison[b] == t) add_nonfinite(t);
-      if (more) store(b ^ 1, t + 1);
-      __syncthreads();
+    auto fill = [&](auto j) {
+      if (t0 + j < t1) issue(j, t0 + j + 1);
+    };
+    fill(std::integral_constant<int, 0>{});
+    if constexpr (NST > 2) { fill(std::integral_constant<int, 1>{}); fill(std::integral_constant<int, 2>{}); }
+    // Tile t, in stage j, has landed once at most the NST - 2 later ones are outstanding; the
+    // barrier makes every wave's part of it visible, and frees the stage of t - 1.
+    auto step = [&](auto j, int t) {
+      if (NST > 3 && t + 2 < t1) wait_loads<2 * 2 * NI>();
+      else if (NST > 2 && t + 1 < t1) wait_loads<2 * NI>();
+      else wait_loads<0>();
+      __builtin_amdgcn_s_barrier();
+      if (t + NST - 1 < t1) issue(std::integral_constant<int, (j + NST - 1) % NST>{}, t + NST);
+      const int kb = 64 * vis.run(t);
+      if (!seen_by_all(j0, j1, kb, kb + 63, a.window, a.n_sink)) {
+        mend(j, t);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+      }
+      compute(j, t);
+      if (s_poison == t) add_nonfinite(t);
+      return t + 1 < t1;
+    };
+    for (int t = t0;; t += NST) {
+      if (!step(std::integral_constant<int, 0>{}, t)) break;
+      if (!step(std::integral_constant<int, 1>{}, t + 1)) break;
+      if constexpr (NST > 2) {
+        if (!step(std::integral_constant<int, 2>{}, t + 2)) break;
+        if (!step(std::integral_constant<int, 3>{}, t + 3)) break;
+      }
     }
   }
   l_run = sum_x32(l_run);
@@ -704,12 +770,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
     int lo = 0, hi = pl.n_req - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if ((int64_t)pl.cu_seqlens[mid] * a.G / 16 + mid <= id) lo = mid; else hi = mid - 1;
+      if ((int64_t)uniform(pl.cu_seqlens[mid]) * a.G / 16 + mid <= id) lo = mid; else hi = mid - 1;
     }
     w.p = lo;
-    w.qt = id - (int)((int64_t)pl.cu_seqlens[lo] * a.G / 16 + lo);
+    w.qt = id - (int)((int64_t)uniform(pl.cu_seqlens[lo]) * a.G / 16 + lo);
   }
-  const int R0 = pl.cu_seqlens[w.p], m = pl.cu_seqlens[w.p + 1] - R0, ctx = pl.ctx[w.p];
+  const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
   const int qn = m * a.G;
   if (w.qt * 16 >= qn) return;                            // block-uniform, as every exit below
   const Chunks ck = request_chunks(VFM_F32, m, ctx, a.G, a.KH, a.window, a.n_sink);
@@ -725,7 +791,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
   const int t0 = w.c * rpc, t1 = min(t0 + rpc, vis.n);
   int head;
   const int64_t row = out_row(a, R0, w.h, qi, head);
-  const int32_t* prow = a.kp.table + (int64_t)pl.order[w.p] * a.kp.max_pages;
+  const page_row prow = row_of(a.kp, uniform(pl.order[w.p]));
   const int lp = a.kp.log2_page;
   const float* kh = (const float*)a.k + (int64_t)w.h * a.slots * DH;
   const float* vh = (const float*)a.v + (int64_t)w.h * a.slots * DH;
