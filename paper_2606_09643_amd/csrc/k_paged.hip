@@ -421,9 +421,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 }
 
 // ---------------------------------------------------------------------------
-// Many rows (prompts and chunks), bf16: one block per 128 packed queries of one
-// request and key head (and chunk of the keys where the request has few
-// blocks); 4 waves of 32 queries on v_mfma_f32_32x32x16_bf16, so a K or V
+// Many rows (prompts and chunks), bf16: one block per 128 or 256 packed queries
+// of one request and key head (and chunk of the keys where the request has few
+// blocks); waves of 32 queries on v_mfma_f32_32x32x16_bf16, so a K or V
 // fragment read from LDS feeds 32 queries.  64-key tiles of K and V go from
 // memory straight into a ring of LDS stages (global_load_lds, one barrier per
 // tile), two stages of 32 KB with head dim 128 and four of 16 KB with 64: two
@@ -455,16 +455,18 @@ __device__ __forceinline__ int rows_vswz(int r, int c) {
 template <int N>
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14)); }
 
-template <int DH>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_rows_bf16_kernel(Plan pl, PagedAttn a) {
+// NW waves: 4 (two blocks share a CU) or 8 (one).
+template <int DH, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_rows_bf16_kernel(Plan pl, PagedAttn a) {
   constexpr int CH = DH / 8;             // 16-byte chunks per row
   constexpr int RPI = 64 / CH;           // rows per wave-wide load
-  constexpr int NI = 64 / (4 * RPI);     // K (and V) loads per wave and tile
+  constexpr int NI = 64 / (NW * RPI);    // K (and V) loads per wave and tile
   constexpr int KS = DH / 16;            // MFMA steps over the head dims
   constexpr int ND = DH / 32;            // output tiles
-  constexpr int NST = DH == 128 ? 2 : 4; // LDS stages
-  // a variable per stage (K, then V), so that the compiler can tell the one that is read from the
-  // ones being filled and does not wait for their loads
+  constexpr int NST = DH == 128 && NW == 4 ? 2 : 4;   // LDS stages
+  // Stage j: K of a tile t with t mod NST = j, then V of tile t - 1 (a step reads K a tile ahead of V).
+  // A variable per stage, so that the compiler can tell the one that is read from the one being
+  // filled and does not wait for its loads.
   constexpr int TE = 64 * DH, SE = 2 * TE;
   __shared__ __attribute__((aligned(16))) bf16 stage0[SE], stage1[SE], stage2[NST > 2 ? SE : 8], stage3[NST > 3 ? SE : 8];
   auto stage = [&](auto b) -> bf16* {
@@ -475,13 +477,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   };
   __shared__ int s_poison;
 
-  const int rb = rows_per_block(a.G);
+  const int rb = rows_per_block(NW, a.G);
   Work w;
   int blk;
   {
     int id = blockIdx.x;
     w.h = id % a.KH; id /= a.KH;
-    w.c = id % a.rows_chunks; id /= a.rows_chunks;
+    if constexpr (NW == 4) { w.c = id % a.rows_chunks; id /= a.rows_chunks; }
+    else w.c = 0;                         // a request of wide blocks has no need to cut its keys
     blk = id;
   }
   // request p's blocks start at cu[p] / rb + p: at least ceil(m / rb) before the next request's
@@ -497,7 +500,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   // a request's last rows see the most keys: they come first
   const int nb = (m + rb - 1) / rb;
   const int bi = blk - (R0 / rb + w.p);
-  if (bi >= nb || few_rows(VFM_BF16, m, a.G)) return;     // block-uniform, as every exit below
+  if (bi >= nb || few_rows(VFM_BF16, m, a.G) || row_waves(m, a.G, a.KH) != NW) return;   // block-uniform, as every exit below
   const int r0 = (nb - 1 - bi) * rb, nr = min(rb, m - r0);
   const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink);
   if (w.c >= ck.n) return;
@@ -521,7 +524,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s);
   }
-  const int64_t trow = (int64_t)uniform(pl.order[w.p]) * a.kp.max_pages;   // the request's page row
+  const page_row prow = row_of(a.kp, uniform(pl.order[w.p]));
   const int lp = a.kp.log2_page;
   const bf16* kh = (const bf16*)a.k + (int64_t)w.h * a.slots * DH;
   const bf16* vh = (const bf16*)a.v + (int64_t)w.h * a.slots * DH;
@@ -534,33 +537,45 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   float m_run = NEG_BIG, l_run = 0.f;
 
-  // A lane's load i of a tile: row RPI (4 i + wave) + lane / CH, physical chunk lane % CH;
+  // A lane's load i of a tile: row RPI (NW i + wave) + lane / CH, physical chunk lane % CH;
   // within its 16-position run the row, and with it the swizzle, is the same for every i.
   const int lrow = RPI * wave + lane / CH;                // mod 16: the row in its run
-  const int koff = (lrow & 15) * DH + rows_kswz<DH>(lrow, lane % CH) * 8;
-  const int voff = (lrow & 15) * DH + rows_vswz<DH>(lrow, lane % CH) * 8;
-  // The pages of a tile's four runs and where the runs start in them, in lanes 0..3 (of every four).
-  // A run that no row sees reads a seen one instead: its page may not exist.
-  int page = 0, in_page = 0;
+  // Byte offsets from the run's first row, which is a scalar.
+  const uint32_t koff = 2 * ((lrow & 15) * DH + rows_kswz<DH>(lrow, lane % CH) * 8);
+  const uint32_t voff = 2 * ((lrow & 15) * DH + rows_vswz<DH>(lrow, lane % CH) * 8);
+  // Pages of the wave's runs of a tile (scalar loads, a step ahead of their use) and where the runs
+  // start in them.  A run that no row sees reads a seen one instead: its page may not exist.
+  int page[NI], in_page[NI];
   auto look_up = [&](int t) {
-    int k = min(64 * vis.run(min(t, vis.n - 1)) + 16 * (lane & 3), j1 & ~15);
-    if (k + 15 < lo_any && k >= a.n_sink) k = lo_any & ~15;
-    page = a.kp.table[trow + (k >> lp)];
-    in_page = k & ((1 << lp) - 1);
-  };
-  auto issue = [&](auto b, int next) {                    // the tile looked up last into stage b; looks `next` up
-    int64_t run[NI];
-    const int slots = (page << lp) + in_page;
+    const int kb = 64 * vis.run(min(t, vis.n - 1));
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
-      run[i] = (int64_t)__builtin_amdgcn_readlane(slots, RPI * (4 * i + wave) >> 4) * DH;
+    for (int i = 0; i < NI; ++i) {
+      int k = min(kb + (RPI * (NW * i + wave) & ~15), j1 & ~15);
+      if (k + 15 < lo_any && k >= a.n_sink) k = lo_any & ~15;
+      page[i] = prow[k >> lp];
+      in_page[i] = k & ((1 << lp) - 1);
+    }
+  };
+  // K of the tile looked up last and V of the one looked up before it into stage b; looks `next` up.  Past the last tile that one is loaded again, into stages that nothing reads any
+  // more: the loop needs no branch, and the count of loads in flight is always the same.
+  int64_t vrun[NI] = {};
+  auto issue = [&](auto b, int next, auto with_v) {
+    int64_t krun[NI], prun[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      krun[i] = (int64_t)((page[i] << lp) + in_page[i]) * DH;
+      prun[i] = vrun[i];
+      vrun[i] = krun[i];
+    }
     look_up(next);
 #pragma unroll
     for (int i = 0; i < NI; ++i)
-      __builtin_amdgcn_global_load_lds((gptr_t)(kh + run[i] + koff), (lptr_t)(stage(b) + RPI * (4 * i + wave) * DH), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gptr_t)((const char*)(kh + krun[i]) + koff), (lptr_t)(stage(b) + RPI * (NW * i + wave) * DH), 16, 0, 0);
+    if constexpr (with_v)
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
-      __builtin_amdgcn_global_load_lds((gptr_t)(vh + run[i] + voff), (lptr_t)(stage(b) + TE + RPI * (4 * i + wave) * DH), 16, 0, 0);
+      for (int i = 0; i < NI; ++i)
+        __builtin_amdgcn_global_load_lds((gptr_t)((const char*)(vh + prun[i]) + voff),
+                                         (lptr_t)(stage(b) + TE + RPI * (NW * i + wave) * DH), 16, 0, 0);
   };
   // V rows of a tile that some row of the block does not see: zeros where none sees them, no
   // infinities or NaN where some do
@@ -568,7 +583,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int kb = 64 * vis.run(t);
 #pragma unroll 1
     for (int i = 0; i < NI; ++i) {
-      const int r = RPI * 4 * i + lrow, k = kb + r;
+      const int r = RPI * NW * i + lrow, k = kb + r;
       bf16x8* at = reinterpret_cast<bf16x8*>(stage(b) + TE + r * DH + (lane % CH) * 8);
       if (!seen_by_any(j0, j1, k, a.window, a.n_sink)) *at = bf16x8{};
       else if (!seen_by_all(j0, j1, k, k, a.window, a.n_sink)) {
@@ -587,12 +602,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const int kaddr = x * DH * 2 + (rows_kswz<DH>(x, h2) << 4);
   const int vaddr = (4 * h2 + (kq >> 2)) * DH * 2 + (rows_vswz<DH>(kq >> 2, 0) << 4) + gq * 32 + (kq & 3) * 8;
 
-  auto compute = [&](auto b, int t) {
-    const int kb = 64 * vis.run(t);
-    // the wave has no query, or none that sees the tile
-    if (wave * 32 >= qn || kb > wj1 || (a.window > 0 && wj0 - (kb + 63) >= a.window && kb >= a.n_sink)) return;
-    const bool full = seen_by_all(wj0, wj1, kb, kb + 63, a.window, a.n_sink);
-    f32x16 st[2];
+  // S^T of a tile: two 32-key halves; lane half h2, register i: key 8 (i / 4) + 4 h2 + i % 4
+  auto scores = [&](auto b, f32x16 (&st)[2]) {
     const char* kp = reinterpret_cast<const char*>(stage(b));
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
@@ -606,35 +617,37 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       }
       st[kt] = acc;
     }
-    // fragments are read six ahead of their MFMA
-    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+  };
+  auto mask = [&](int t, f32x16 (&st)[2]) {
+    const int kb = 64 * vis.run(t);
+    if (seen_by_all(wj0, wj1, kb, kb + 63, a.window, a.n_sink)) return;
+    // made anew in each masked tile: held over the loop, the compares' lane masks would fill the scalar registers
+    int d0 = jq - kb - 4 * h2, n0 = a.n_sink - kb - 4 * h2;     // of the lane's key 0
+    asm volatile("" : "+v"(d0), "+v"(n0));
+    const int win = a.window > 0 ? a.window : INT32_MAX;
 #pragma unroll
-    for (int s = 0; s < 2 * KS - 6; ++s) {
-      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
-    if (!full) {
-      // made anew in each masked tile: held over the loop, the compares' lane masks would fill the scalar registers
-      int d0 = jq - kb - 4 * h2, n0 = a.n_sink - kb - 4 * h2;   // of the lane's key 0
-      asm volatile("" : "+v"(d0), "+v"(n0));
-      const int win = a.window > 0 ? a.window : INT32_MAX;
+    for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int k = 32 * kt + 8 * (i >> 2) + (i & 3);
-          const bool see = (d0 >= k) & ((d0 - k < win) | (k < n0));
-          st[kt][i] = see ? st[kt][i] : -INFINITY;
-        }
-    }
+      for (int i = 0; i < 16; ++i) {
+        const int k = 32 * kt + 8 * (i >> 2) + (i & 3);
+        const bool see = (d0 >= k) & ((d0 - k < win) | (k < n0));
+        st[kt][i] = see ? st[kt][i] : -INFINITY;
+      }
+  };
+  // largest score (log2 units) of the lane's query
+  auto largest = [&](const f32x16 (&st)[2]) {
     float mb = st[0][0];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mb = fmaxf(mb, st[kt][i]);
-    mb = max_x32(mb) * a.scale_log2;
-    if (__any(mb > m_run)) {                              // elsewhere the factor is 1
+    return max_x32(mb) * a.scale_log2;
+  };
+  // The running maximum follows the scores only where one passes it by 8 (a factor of 256, which
+  // neither fp32 sums nor bf16 weights mind): with 32 queries a wave, some maximum grows in most
+  // tiles, and the products would be rescaled that often.
+  auto follow = [&](float mb) {
+    if (__any(mb > m_run + 8.f)) {
       const float m_new = fmaxf(m_run, mb);
       const float alpha = fast_exp2(m_run - m_new);
       m_run = m_new;
@@ -642,16 +655,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
       for (int i = 0; i < ND; ++i) o[i] *= alpha;
     }
+  };
+  // P^T of 16 keys u of a tile, 8 of them in this lane
+  auto weights = [&](const f32x16 (&st)[2], int u, bf16x8 (&pf)[4]) {
+    float e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = fast_exp2(fmaf(st[u >> 1][8 * (u & 1) + i], a.scale_log2, -m_run));
+    pf[u] = pack8(e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]);
+  };
+  // their sum, of the rounded weights that the products use, and the products
+  auto products = [&](auto b, const bf16x8 (&pf)[4]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        l_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[u][2 * i], pf[u][2 * i + 1]}, bf16x2{(bf16)1.f, (bf16)1.f}, l_run, false);
     const char* vp = reinterpret_cast<const char*>(stage(b) + TE);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {                         // 16 keys: 8 of them in this lane
-      float e[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        e[i] = fast_exp2(fmaf(st[u >> 1][8 * (u & 1) + i], a.scale_log2, -m_run));
-        l_run += e[i];
-      }
-      const bf16x8 pf = pack8(e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]);
+    for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
         const char* q = vp + (vaddr ^ (d << 6)) + u * 16 * DH * 2;
@@ -661,9 +682,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         bf16x8 f;
         __builtin_memcpy(&f, &lo, 8);
         __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
-        o[d] = mfma32(f, pf, o[d]);
+        o[d] = mfma32(f, pf[u], o[d]);
       }
-    }
   };
   // the infinities and NaN that `mend` took out of tile t
   auto add_nonfinite = [&](int t) {
@@ -672,7 +692,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     for (int r = 0; r < 64; ++r) {
       const int k = kb + r;
       if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
-      const bf16* vrow = vh + (int64_t)((a.kp.table[trow + (k >> lp)] << lp) + (k & ((1 << lp) - 1))) * DH + 4 * h2;
+      const bf16* vrow = vh + (int64_t)(page_slot(prow, lp, k)) * DH + 4 * h2;
       if (sees(jq, k, a.window, a.n_sink)) {
 #pragma unroll
         for (int d = 0; d < ND; ++d)
@@ -680,44 +700,88 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
           for (int i = 0; i < 16; ++i) {
             const float v = (float)vrow[32 * d + 8 * (i >> 2) + (i & 3)];
             o[d][i] += nonfinite(v) ? v : 0.f;
+            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // rare: no registers for loads in flight
           }
       }
     }
   };
 
+  // While the weights of tile t are computed (vector ALU), the matrix cores already take the scores
+  // of tile t + 1; while they take the products of t, its largest scores are found.  K of tile t + 1
+  // and V of tile t have landed once at most the loads of the NST - 2 later steps are outstanding;
+  // the barrier makes every wave's part visible, and frees K of tile t and V of tile t - 1.
   if (t0 < t1) {
+    f32x16 sa[2], sb[2];
     look_up(t0);
-    auto fill = [&](auto j) {
-      if (t0 + j < t1) issue(j, t0 + j + 1);
-    };
+    auto fill = [&](auto j) { issue(j, t0 + j + 1, std::bool_constant<(j > 0)>{}); };
     fill(std::integral_constant<int, 0>{});
-    if constexpr (NST > 2) { fill(std::integral_constant<int, 1>{}); fill(std::integral_constant<int, 2>{}); }
-    // Tile t, in stage j, has landed once at most the NST - 2 later ones are outstanding; the
-    // barrier makes every wave's part of it visible, and frees the stage of t - 1.
-    auto step = [&](auto j, int t) {
-      if (NST > 3 && t + 2 < t1) wait_loads<2 * 2 * NI>();
-      else if (NST > 2 && t + 1 < t1) wait_loads<2 * NI>();
-      else wait_loads<0>();
+    fill(std::integral_constant<int, 1>{});
+    if constexpr (NST > 2) { fill(std::integral_constant<int, 2>{}); fill(std::integral_constant<int, 3>{}); }
+    wait_loads<(NST - 1) * 2 * NI>();
+    __builtin_amdgcn_s_barrier();
+    scores(std::integral_constant<int, 0>{}, sa);
+    mask(t0, sa);
+    follow(largest(sa));
+    // tile t, t mod NST = j: its scores st, the next one's sn (behind the last tile: of what the stage
+    // holds, and not used)
+    auto step = [&](auto j, int t, f32x16 (&st)[2], f32x16 (&sn)[2]) {
+      constexpr auto jn = std::integral_constant<int, (j + 1) % NST>{};   // holds K of tile t + 1, V of tile t
+      wait_loads<(NST - 2) * 2 * NI>();
       __builtin_amdgcn_s_barrier();
-      if (t + NST - 1 < t1) issue(std::integral_constant<int, (j + NST - 1) % NST>{}, t + NST);
       const int kb = 64 * vis.run(t);
       if (!seen_by_all(j0, j1, kb, kb + 63, a.window, a.n_sink)) {
-        mend(j, t);
+        mend(jn, t);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
       }
-      compute(j, t);
+      bf16x8 pf[4];
+      __builtin_amdgcn_sched_barrier(0);
+      // Scores of t + 1 (2 KS MFMAs) beside the first half of t's weights and the next loads (32 KB
+      // take the CU 512 cycles to address); a fragment is read four ahead of its MFMA.
+      scores(jn, sn);
+      weights(st, 0, pf);
+      weights(st, 1, pf);
+      issue(j, t + NST + 1, std::true_type{});
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int s = 0; s < 2 * KS; ++s) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 64 / (2 * KS), 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        if (s % (2 * KS / (2 * NI)) == 1) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(pf[u]));   // not put off behind the mask
+      __builtin_amdgcn_sched_barrier(0);
+      if (t + 1 < t1) mask(t + 1, sn);
+      __builtin_amdgcn_sched_barrier(0);
+      // products of t (4 ND MFMAs) beside the second half of its weights and the largest scores of t + 1
+      weights(st, 2, pf);
+      weights(st, 3, pf);
+      products(jn, pf);
+      const float mb = largest(sn);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int s = 0; s < 4 * ND; ++s) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 96 / (4 * ND), 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
       if (s_poison == t) add_nonfinite(t);
-      return t + 1 < t1;
+      if (t + 1 >= t1) return false;
+      follow(mb);
+      return true;
     };
     for (int t = t0;; t += NST) {
-      if (!step(std::integral_constant<int, 0>{}, t)) break;
-      if (!step(std::integral_constant<int, 1>{}, t + 1)) break;
+      if (!step(std::integral_constant<int, 0>{}, t, sa, sb)) break;
+      if (!step(std::integral_constant<int, 1>{}, t + 1, sb, sa)) break;
       if constexpr (NST > 2) {
-        if (!step(std::integral_constant<int, 2>{}, t + 2)) break;
-        if (!step(std::integral_constant<int, 3>{}, t + 3)) break;
+        if (!step(std::integral_constant<int, 2>{}, t + 2, sa, sb)) break;
+        if (!step(std::integral_constant<int, 3>{}, t + 3, sb, sa)) break;
       }
     }
+    wait_loads<0>();                                      // nothing still writes to LDS when the block ends
   }
   l_run = sum_x32(l_run);
   if (wave * 32 + x >= qn) return;
@@ -983,16 +1047,22 @@ hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_d
   return hipGetLastError();
 }
 
-hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, bool need_few,
-                                  bool need_rows, bool split, hipStream_t s) {
+hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, bool few_, bool rows_,
+                                  bool wide, bool split, hipStream_t s) {
   int pi = prof_begin(VFM_PROF_ATTN, s);
   const unsigned few = (unsigned)a.KH * a.few_chunks, rows = (unsigned)a.KH * a.rows_chunks;
 #define BY_DH(K_, G_) \
   do { if (head_dim == 64) hipLaunchKernelGGL((K_<64>), G_, dim3(256), 0, s, pl, a); \
        else hipLaunchKernelGGL((K_<128>), G_, dim3(256), 0, s, pl, a); } while (0)
   if (dtype == VFM_BF16) {
-    if (need_few) BY_DH(attn_few_bf16_kernel, dim3(few * a.qtiles * pl.n_req));
-    if (need_rows) BY_DH(attn_rows_bf16_kernel, dim3(rows * (pl.T / rows_per_block(a.G) + pl.n_req)));
+    if (few_) BY_DH(attn_few_bf16_kernel, dim3(few * a.qtiles * pl.n_req));
+#define ROWS(D_, W_)                                                                                             \
+  hipLaunchKernelGGL((attn_rows_bf16_kernel<D_, W_>),                                                             \
+                     dim3((W_ == 8 ? (unsigned)a.KH : rows) * (pl.T / rows_per_block(W_, a.G) + pl.n_req)), dim3(64 * W_), \
+                     0, s, pl, a)
+    if (rows_) { if (head_dim == 64) ROWS(64, 4); else ROWS(128, 4); }
+    if (wide) { if (head_dim == 64) ROWS(64, 8); else ROWS(128, 8); }
+#undef ROWS
   } else {
     BY_DH(attn_f32_kernel, dim3(few * (unsigned)((int64_t)pl.T * a.G / 16 + pl.n_req)));
   }

@@ -183,6 +183,39 @@ def test_attention_keys_that_only_some_rows_see(dtype, H, KH, dh, lens, ctx, win
             assert np.isnan(got[see]).all()
 
 
+@pytest.mark.parametrize("H,KH,dh,page,window,sinks,lens,ctx", [
+    (32, 32, 64, 64, 0, 0, [2050], [0]), (64, 16, 128, 16, 90, 5, [1100, 1, 40], [333, 50, 0]),
+    (56, 8, 64, 32, 300, 0, [1300], [70])])
+def test_attention_prompts_of_wide_blocks(H, KH, dh, page, window, sinks, lens, ctx):
+    """Prompts whose blocks of 256 queries fill the chip: rows at the blocks' and
+    tiles' borders and a spread of others against the 64-bit form."""
+    assert KH * -(-lens[0] * (H // KH) // 256) >= 256
+    c = Cache(lens, ctx, KH, dh, page, window, sinks, "bf16", seed=21)
+    rng = np.random.default_rng(12)
+    q = [np64(torch.from_numpy(rng.standard_normal((m, H, dh), dtype=np.float32) * 1.5).to(torch.bfloat16)) for m in lens]
+    task = _tasks(len(lens), 4)
+    got = _attend(c, task, H, KH, dh, window, sinks, "bf16", q)
+    worst, m = 0.0, lens[0]
+    heads = [0, H // 2 + 1, H - 1]
+    for i in sorted({0, 1, 31, 32, 63, 64, 127, 128, 255, 256, 257, m // 2, m - 2, m - 1} | set(rng.integers(0, m, 20).tolist())):
+        see = D.visible(ctx[0] + i, np.arange(ctx[0] + m), window, sinks)
+        for h in heads:
+            k, v = c.k[0][see, h * KH // H], c.v[0][see, h * KH // H]
+            p = np.exp((sc := k @ q[0][i, h] * dh ** -0.5) - sc.max())
+            p /= p.sum()
+            a, ref = p @ np.abs(v), p @ v
+            dot = np.abs(q[0][i, h]).max() * np.abs(k).max() * dh ** 0.5
+            tol = 2.0 ** -8 * (a + np.abs(ref)) + (see.sum() + 16) * 2.0 ** -24 * (a + np.abs(ref)) \
+                + a * 2 * ((dh + 2) * 2.0 ** -24 * dot + 2.0 ** -22)
+            far = np.abs(got[0][i, h] - ref) / tol
+            worst = max(worst, float(far.max()))
+            assert far.max() <= 1, (i, h, far.max())
+    log(f"  {worst:.3f} of the tolerance")
+    if len(lens) > 1:
+        _check(c, {i: got[i] for i in range(1, len(lens))}, q, window, sinks, "bf16", dh ** -0.5)
+    assert np.array_equal(_attend(c, task, H, KH, dh, window, sinks, "bf16", q, only=[0], ws_fill=0)[0], got[0])
+
+
 def test_attention_large_logits_and_scale():
     """Scores of hundreds (one key takes the whole weight) and a given scale."""
     for dtype in ("bf16", "f32"):
