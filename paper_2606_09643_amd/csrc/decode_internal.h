@@ -47,7 +47,7 @@ __host__ __device__ inline Vis visible_runs(int first_pos, int last_pos, int win
 struct Chunks { int n, tiles; };   // chunks, tiles per chunk
 __host__ __device__ inline Chunks key_chunks(int tiles, int par, int min_tiles) {
   int want = 256 / par;
-  const int most = (tiles + min_tiles - 1) / min_tiles;
+  const int most = tiles / min_tiles;
   if (want > most) want = most;
   if (want < 1) want = 1;
   Chunks c;
@@ -57,8 +57,13 @@ __host__ __device__ inline Chunks key_chunks(int tiles, int par, int min_tiles) 
 }
 
 constexpr int FEW_QUERIES = 32;      // packed queries (rows x group) up to which a request takes the few-row kernel
-constexpr int FEW_MIN_TILES = 8;     // 32-key tiles
-constexpr int ROWS_MIN_TILES = 16;   // 64-key tiles
+// The fewest tiles of a chunk, so long as a request has them. A chunk costs its block's start and its share
+// of the join; uncut, a request alone uses few CUs. 32 heads of 128 on 32 of keys. Few-row kernel, 32-key
+// tiles: one row after 1500 keys takes 14.4 us with 8 tiles, 17.0 with 12, 26.5 with 24; one row of each of 256
+// requests with up to 2048 keys under a window of 1024 654, 597, 582. Many-row kernel, 64-key tiles: 100 rows
+// after 1500 keys take 26.3 us with 8 and 32.3 with 16; 512 rows after none 21.2 with 8 and 30.6 with 4.
+constexpr int FEW_MIN_TILES = 12;
+constexpr int ROWS_MIN_TILES = 8;
 
 // few-row kernel (bf16; fp32: every request): 16 packed queries per block
 __host__ __device__ inline bool few_rows(int dtype, int m, int G) { return dtype != VFM_BF16 || (int64_t)m * G <= FEW_QUERIES; }
