@@ -82,7 +82,8 @@ int vfm_attention_paged(const vfm_attn* attn, const vfm_batch* batch, const void
                         const vfm_kv_pages* kv, void* out, int64_t ldo, void* workspace,
                         size_t ws_bytes, void* stream);
 
-/* vfm_layer_forward_paged with that attention (n_kv_heads = cfg->n_heads):
+/* vfm_layer_forward_paged with that append and attention (n_kv_heads =
+ * cfg->n_heads; the rotation's angles in 64 bits):
  * one backbone layer of a causal, decode or mixed step whose rows see the
  * window and the sinks only.  Any request may be a prompt, a chunk after
  * cached tokens or a single row, in bf16 and fp32.  Pages are needed for the

@@ -484,6 +484,13 @@ def vfm_greedy_tokens(batch, out, ids, stream=None):
 _TORCH_DTYPE = {VFM_F32: torch.float32, VFM_BF16: torch.bfloat16}
 
 
+def _same_device(dev):
+    """The operands' device, which has to be the current one: its stream is what the call runs on."""
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+        raise ValueError(f"operands on {dev}: the current GPU is expected")
+    return dev
+
+
 def _operand(t, name, dtype, numel, device):
     """t as the library takes it: of that type, dense, at least numel elements, on `device`."""
     if t.dtype != dtype or not t.is_contiguous() or t.numel() < numel:
@@ -521,12 +528,13 @@ def make_attn(dtype, n_heads, n_kv_heads, head_dim, window=0, n_sink=0, scale=0.
 
 
 def vfm_kv_append(attn, batch, qkv, q_out, kv, stream=None):
-    """qkv: [T, (n_heads + 2 n_kv_heads) * head_dim or more]; q_out: dense [T, n_heads * head_dim]."""
+    """qkv: [T, (n_heads + 2 n_kv_heads) * head_dim or more]; q_out: dense [T, n_heads * head_dim].
+
+    Like the other calls below, on the current device and `stream` (default: torch's current one)."""
     hd, T, td, dev = attn.head_dim, batch.plan_host[2], _TORCH_DTYPE.get(attn.dtype), qkv.device
     p, ld = _rows(qkv, "qkv", td, T, (attn.n_heads + 2 * attn.n_kv_heads) * hd, dev)
-    q = _operand(q_out, "q_out", td, T * attn.n_heads * hd, dev)
-    st = _lib_handle().vfm_kv_append(C.byref(attn), C.byref(batch), p, ld, q, C.byref(_cache(kv, attn, td, dev)),
-                                     _stream(stream))
+    q, c = _operand(q_out, "q_out", td, T * attn.n_heads * hd, dev), _cache(kv, attn, td, _same_device(dev))
+    st = _lib_handle().vfm_kv_append(C.byref(attn), C.byref(batch), p, ld, q, C.byref(c), _stream(stream))
     _check(st, "vfm_kv_append")
 
 
@@ -542,9 +550,14 @@ def vfm_attention_paged(attn, batch, q, kv, out, workspace=None, stream=None):
     cols, T, td, dev = attn.n_heads * attn.head_dim, batch.plan_host[2], _TORCH_DTYPE.get(attn.dtype), q.device
     pq, ldq = _rows(q, "q", td, T, cols, dev)
     po, ldo = _rows(out, "out", td, T, cols, dev)
-    ws, nb = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
-    st = _lib_handle().vfm_attention_paged(C.byref(attn), C.byref(batch), pq, ldq,
-                                           C.byref(_cache(kv, attn, td, dev)), po, ldo, ws, nb, _stream(stream))
+    c = _cache(kv, attn, td, _same_device(dev))
+    ws, nb = None, 0
+    if workspace is not None:
+        if workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace: a dense tensor on {dev} is expected")
+        ws, nb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    st = _lib_handle().vfm_attention_paged(C.byref(attn), C.byref(batch), pq, ldq, C.byref(c), po, ldo, ws, nb,
+                                           _stream(stream))
     _check(st, "vfm_attention_paged")
 
 
@@ -592,7 +605,8 @@ def vfm_sample_tokens(batch, out, sampling, u, ids, logprob=None, stream=None):
     if sampling.n is not None and (sampling.n < n or sampling.device != dev):
         raise ValueError(f"the sampling parameters are for {sampling.n} requests on {sampling.device}, the batch has "
                          f"{n} on {dev}")
-    st = _lib_handle().vfm_sample_tokens(C.byref(batch), _operand(out, "out", torch.float32, batch.plan_host[6], dev),
+    st = _lib_handle().vfm_sample_tokens(C.byref(batch),
+                                         _operand(out, "out", torch.float32, batch.plan_host[6], _same_device(dev)),
                                          C.byref(sampling.c), _operand(u, "u", torch.float32, n, dev),
                                          _operand(ids, "ids", torch.int32, n, dev),
                                          _operand(logprob, "logprob", torch.float32, n, dev)

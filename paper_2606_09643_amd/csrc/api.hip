@@ -616,12 +616,13 @@ int layer_impl(const vfm_cfg& c, const vfm_layer_weights* w, const vfm_lora_tabl
   // (large bf16 batches): the QKV GEMM's store pass rotates q and k, and the
   // cache write is the attention launcher's plain copy
   const bool cache_write = k_cache != nullptr && c.attn != VFM_ATTN_BIDIR;
-  const bool rope_fusable = c.dtype == VFM_BF16 && c.rope_theta > 0.f &&
+  // (windowed: the append pass, whose angles hold at any position; see below)
+  const bool rope_fusable = !win && c.dtype == VFM_BF16 && c.rope_theta > 0.f &&
                             (c.head_dim == 64 || c.head_dim == 128) && d % 256 == 0;
   const bool rope_in_finalize = skinny && rope_fusable;
   const bool rope_in_gemm = !skinny && rope_fusable && T >= 1024 &&
                             (int64_t)T * d < ((int64_t)1 << 31) && (int64_t)3 * d * d < ((int64_t)1 << 31);
-  const bool rope_writes_kv = c.rope_theta > 0.f && cache_write && !rope_in_gemm;
+  const bool rope_writes_kv = !win && c.rope_theta > 0.f && cache_write && !rope_in_gemm;
   if (rope_in_gemm) {
     gemm_rope.on = 1; gemm_rope.d = d; gemm_rope.head_dim = c.head_dim;
     gemm_rope.log2_theta = log2f(c.rope_theta); gemm_rope.pos = pl.pos;
@@ -639,16 +640,18 @@ int layer_impl(const vfm_cfg& c, const vfm_layer_weights* w, const vfm_lora_tabl
   gemm_rope = GemmRope{};
   // a5: rotary embedding of q and k
   // (with a KV cache the same pass writes each row's rotated k and its v)
-  if (c.rope_theta > 0.f && !rope_in_finalize && !rope_in_gemm)
+  if (!win && c.rope_theta > 0.f && !rope_in_finalize && !rope_in_gemm)
     VFM_TIMED(VFM_PROF_OTHER, launch_rope(c.dtype, pl, qkv, d, c.n_heads, c.head_dim, c.rope_theta,
                                           rope_writes_kv ? k_cache : nullptr, rope_writes_kv ? v_cache : nullptr,
                                           kv_slots, kp, s));
   // a6: attention per request (and the KV-cache write)
   // (timed per kernel inside the launcher)
   if (win) {
-    if (!rope_writes_kv)
-      VFM_TIMED(VFM_PROF_OTHER, launch_kv_append(c.dtype, pl, c.n_heads, c.n_heads, c.head_dim, 0.f, qkv, 3 * (int64_t)d,
-                                                 nullptr, k_cache, v_cache, kv_slots, kp, s));
+    // Rotation in place and cache write in one pass: a sequence that keeps a window of its past goes on to
+    // positions at which an angle in fp32 is off (position 700: by up to 4e-5, position 10^6: by 0.06).
+    VFM_TIMED(VFM_PROF_OTHER, launch_kv_append(c.dtype, pl, c.n_heads, c.n_heads, c.head_dim, c.rope_theta, qkv,
+                                               3 * (int64_t)d, c.rope_theta > 0.f ? qkv : nullptr, 3 * (int64_t)d,
+                                               k_cache, v_cache, kv_slots, kp, s));
     VFM_HIP(run_attention(*win, pl, ap, qkv, 3 * (int64_t)d, k_cache, v_cache, kv_slots, kp, attn, d, base + ws.aws, s));
   }
   bool chunked = false;                      // a prompt chunk after cached tokens
@@ -791,7 +794,8 @@ extern "C" int vfm_kv_append(const vfm_attn* attn, const vfm_batch* batch, const
   VFM_TRY(check_stream(stream));
   hipStream_t s = (hipStream_t)stream;
   VFM_TIMED(VFM_PROF_OTHER, launch_kv_append(attn->dtype, pl, attn->n_heads, attn->n_kv_heads, attn->head_dim,
-                                             attn->rope_theta, qkv, ld, q_out, kv->k, kv->v,
+                                             attn->rope_theta, qkv, ld, q_out,
+                                             (int64_t)attn->n_heads * attn->head_dim, kv->k, kv->v,
                                              kv->n_pages * kv->page_size, pages_of(kv), s));
   return VFM_OK;
 }

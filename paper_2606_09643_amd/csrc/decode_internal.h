@@ -89,9 +89,9 @@ __host__ __device__ inline Chunks request_chunks(int dtype, int m, int ctx, int 
   return key_chunks(tiles, par > 256 ? 256 : (int)par, ROWS_MIN_TILES);
 }
 
-// q_out NULL: keys and values only.
+// q_out: rows ldq apart; qkv itself (ldq = ld) to rotate the queries in place, NULL for keys and values only.
 hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv,
-                            int64_t ld, void* q_out, void* k, void* v, int64_t slots, const KvPages& kp,
+                            int64_t ld, void* q_out, int64_t ldq, void* k, void* v, int64_t slots, const KvPages& kp,
                             hipStream_t s);
 
 // few, rows, wide: the batch has requests of the few-row kernel, of the many-row kernel's narrow and wide blocks (bf16).

@@ -111,7 +111,8 @@ __device__ __forceinline__ int page_slot(page_row prow, int lp, int k) {
 // ---------------------------------------------------------------------------
 // Append: rotate-half of the q and k heads, q to q_out, k and v to their slots.
 // One block per row; a thread takes 8 pairs (i, i + dh/2) of one head with
-// 16-byte accesses (32 for fp32).  Bound by its bytes: every element is read and
+// 16-byte accesses (32 for fp32) and writes them after it has read both halves,
+// so q_out may be the queries' own place.  Bound by its bytes: every element is read and
 // written once.  The row's dh/2 angles go through LDS: revolutions in fp64
 // (position times theta^(-2i/dh) / 2 pi loses nothing up to 2^30 positions),
 // their fraction in fp32.
@@ -126,7 +127,7 @@ __device__ __forceinline__ void put(Vec8<float>& x, int i, float f) { x.v[i >> 2
 
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void kv_append_kernel(Plan pl, int H, int KH, int rotate, double log2_theta,
-                                                        const T* __restrict__ qkv, int64_t ld, T* __restrict__ q_out,
+                                                        const T* qkv, int64_t ld, T* q_out, int64_t ldq,
                                                         T* __restrict__ kc, T* __restrict__ vc, int64_t slots,
                                                         KvPages kp) {
   constexpr int HALF = DH / 2, PER = HALF / 8;
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(Plan pl, int H, int KH, 
         put(b, j, x * s + y * c);
       }
     }
-    T* dst = hh < H ? q_out + ((int64_t)r * H + hh) * DH
+    T* dst = hh < H ? q_out + (int64_t)r * ldq + hh * DH
                     : (hh < H + KH ? kc + ((int64_t)(hh - H) * slots + slot) * DH
                                    : vc + ((int64_t)(hh - H - KH) * slots + slot) * DH);
     *reinterpret_cast<Vec8<T>*>(dst + i0) = a;
@@ -1034,13 +1035,13 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Plan pl, PagedAttn a) {
 }  // namespace
 
 hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv,
-                            int64_t ld, void* q_out, void* k, void* v, int64_t slots, const KvPages& kp,
+                            int64_t ld, void* q_out, int64_t ldq, void* k, void* v, int64_t slots, const KvPages& kp,
                             hipStream_t s) {
   const int rotate = theta > 0.f;
   const double l2 = rotate ? log2((double)theta) : 0.0;
 #define APPEND(T_, D_)                                                                                     \
   hipLaunchKernelGGL((kv_append_kernel<T_, D_>), dim3(pl.T), dim3(256), 0, s, pl, H, KH, rotate, l2, (const T_*)qkv, ld, \
-                     (T_*)q_out, (T_*)k, (T_*)v, slots, kp)
+                     (T_*)q_out, ldq, (T_*)k, (T_*)v, slots, kp)
   if (dtype == VFM_BF16) { if (head_dim == 64) APPEND(bf16, 64); else APPEND(bf16, 128); }
   else { if (head_dim == 64) APPEND(float, 64); else APPEND(float, 128); }
 #undef APPEND

@@ -195,10 +195,23 @@ class Forward:
         return self.out
 
 
-class _Seq:
-    __slots__ = ("rid", "task", "prompt", "max_new", "slot", "cached", "generated", "budget", "row")
+class SamplingParams:
+    """How a request's tokens are drawn (vfm_sample_tokens); the defaults
+    draw from the whole distribution.  The uniform numbers come from a
+    generator of the request's own, one per token, so its tokens do not
+    depend on what else is in the batch."""
 
-    def __init__(self, rid, task, prompt, max_new, page_size):
+    def __init__(self, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, seed=0):
+        self.temperature, self.top_k, self.top_p, self.min_p = float(temperature), int(top_k), float(top_p), float(min_p)
+        if self.top_k < 0 or self.top_k >= 2 ** 31 or not (self.temperature >= 0 and self.top_p >= 0 and self.min_p >= 0):
+            raise ValueError("temperature, top_k, top_p and min_p are not negative")
+        self.seed = seed
+
+
+class _Seq:
+    __slots__ = ("rid", "task", "prompt", "max_new", "slot", "cached", "generated", "budget", "row", "sampling", "rng")
+
+    def __init__(self, rid, task, prompt, max_new, page_size, sampling=None):
         self.rid, self.task = rid, int(task)
         self.prompt = np.asarray(prompt, np.int32)
         self.max_new = int(max_new)
@@ -208,6 +221,8 @@ class _Seq:
         self.row = -1                   # index in the latest step's batch
         # pages for every token that will ever be written (the last generated one never is)
         self.budget = -(-(len(self.prompt) + self.max_new - 1) // page_size)
+        self.sampling = sampling        # None: greedy
+        self.rng = np.random.default_rng(sampling.seed) if sampling is not None else None
 
 
 class ContinuousBatcher:
@@ -229,10 +244,19 @@ class ContinuousBatcher:
     token budget, and the pages it will ever need fit next to those the
     running sequences may still need, so a running sequence never waits for
     a page (no preemption).  The host decides only the schedule; every row
-    of the step is computed by the library's kernels."""
+    of the step is computed by the library's kernels.
+
+    With `window` a row sees the last `window` positions and the first
+    `n_sink` (vfm_layer_forward_windowed), and a sequence keeps a bounded
+    number of pages however long it gets: those of the sinks, and a ring of
+    as many as the window and one step's new rows can touch, used again in
+    turn.  A prompt then takes at most `max_chunk` rows of a step (default:
+    the window, but no less than a page), in fp32 too.  Requests submitted
+    with a SamplingParams have their tokens drawn by vfm_sample_tokens."""
 
     def __init__(self, model: Model, emb, page_size=64, n_pages=1024, max_seqs=256, max_step_tokens=8192,
-                 max_pages=None, bfq=None, token_time=1.0, chunk_prompts=None, record=False, device="cuda"):
+                 max_pages=None, bfq=None, token_time=1.0, chunk_prompts=None, record=False, device="cuda",
+                 window=None, n_sink=0, max_chunk=None):
         w = model.w
         self.m, self.emb, self.device = model, emb, device
         self.page_size, self.n_pages = int(page_size), int(n_pages)
@@ -245,8 +269,16 @@ class ContinuousBatcher:
         self.cfg = B.vfm_cfg.from_buffer_copy(model.cfg)
         self.cfg.attn = B.VFM_ATTN_MIXED
         self.bfq, self.record, self.token_time = bfq, record, float(token_time)
-        # prompt chunks after cached tokens run on the bf16 path only
-        self.chunk = (w.dtype == "bf16") if chunk_prompts is None else bool(chunk_prompts)
+        # prompt chunks after cached tokens run on the bf16 path only, under a window in fp32 too
+        self.chunk = (w.dtype == "bf16" or window is not None) if chunk_prompts is None else bool(chunk_prompts)
+        if window is not None and (window < 1 or n_sink < 0):
+            raise ValueError("window: at least 1 position, n_sink: at least 0")
+        self.window, self.n_sink = (int(window), int(n_sink)) if window is not None else (None, 0)
+        if max_chunk is None:
+            max_chunk = self.max_step_tokens if window is None else max(self.window, self.page_size)
+        if max_chunk < 1:
+            raise ValueError("max_chunk: at least 1 row")
+        self.max_chunk = min(int(max_chunk), self.max_step_tokens)
         self.waiting, self.running, self.done = [], [], {}
         self.requests = {}
         self.free_slots = list(range(self.max_seqs - 1, -1, -1))
@@ -257,14 +289,47 @@ class ContinuousBatcher:
         self._picks, self._prev_nxt, self._keep = [], None, None
         self._ready = []                # taken from BFQ, not yet admitted (in its order)
 
-    def submit(self, rid, task, prompt, max_new, now=0.0):
-        s = _Seq(rid, task, prompt, max_new, self.page_size)
+    def _ring(self, s):
+        """(pages of the sinks, pages of the ring behind them) of a windowed
+        sequence.  A step's n new rows and the window - 1 positions before
+        them are window - 1 + n positions in a row, which touch at most
+        ceil((window - 2 + n) / page_size) + 1 pages."""
+        n = min(len(s.prompt), self.max_chunk) if self.chunk else len(s.prompt)
+        return -(-self.n_sink // self.page_size), -(-(self.window - 2 + n) // self.page_size) + 1
+
+    def submit(self, rid, task, prompt, max_new, now=0.0, sampling=None):
+        s = _Seq(rid, task, prompt, max_new, self.page_size, sampling)
+        if self.window is not None:
+            s.budget = min(s.budget, sum(self._ring(s)))
         if s.budget > self.max_pages or len(s.prompt) < 1 or s.max_new < 1:
             raise ValueError(f"request {rid}: needs {s.budget} pages (max {self.max_pages}) or is empty")
         self.requests[rid] = s
         if self.bfq is not None:
             self.bfq.enqueue(s.task, rid, now)
         self.waiting.append(s)
+
+    def _rows(self, s, left):
+        """Rows of its prompt that s takes of a step with `left` rows left."""
+        n = len(s.prompt) - s.cached
+        return min(n, self.max_chunk, left) if self.chunk else n
+
+    def _tables(self, batch, n_tok):
+        """Page tables of the batch's sequences up to n_tok[i] tokens, logical
+        pages in order; pages that a windowed sequence has used again stand
+        where they stood, for positions that no row sees any more."""
+        slots = np.array([s.slot for s in batch], np.int32)
+        for s, n in zip(batch, n_tok):
+            self.alloc.reserve(s.slot, min(int(n), s.budget * self.page_size))
+        table = self.alloc.table(slots, max(int(self.alloc.count(int(x))[0]) for x in slots))
+        if self.window is None:
+            return table
+        page = np.arange(max(-(-int(n) // self.page_size) for n in n_tok))
+        out = np.empty((len(batch), len(page)), np.int32)
+        for i, s in enumerate(batch):
+            sinks, ring = self._ring(s)
+            held = np.where(page < sinks + ring, page, sinks + (page - sinks) % ring)
+            out[i] = table[i, np.minimum(held, table.shape[1] - 1)]
+        return out
 
     def _fits(self, s, tokens):
         first = 1 if self.chunk else len(s.prompt)   # tokens it needs in this step
@@ -282,7 +347,7 @@ class ContinuousBatcher:
         # the next chunk of every sequence still in its prompt
         tokens = 0
         for s in self.running:
-            tokens += 1 if s.cached >= len(s.prompt) else min(len(s.prompt) - s.cached,
+            tokens += 1 if s.cached >= len(s.prompt) else min(self._rows(s, self.max_step_tokens),
                                                               max(self.max_step_tokens - tokens, 0))
         new = []
         if self.bfq is None:
@@ -291,7 +356,7 @@ class ContinuousBatcher:
                     break
                 self._admit_one(s)
                 new.append(s)
-                tokens += min(len(s.prompt), self.max_step_tokens - tokens)
+                tokens += self._rows(s, self.max_step_tokens - tokens)
             return new
         # BFQ: batches come whole in tag order; their requests join as
         # they fit (slot, token budget, pages), the rest first in later steps
@@ -307,19 +372,35 @@ class ContinuousBatcher:
             self._ready.pop(0)
             self._admit_one(s)
             new.append(s)
-            tokens += min(len(s.prompt), self.max_step_tokens - tokens)
+            tokens += self._rows(s, self.max_step_tokens - tokens)
         return new
 
     def _h2d(self, arr):
         """Host array -> device without waiting for the stream (pinned staging)."""
         return torch.from_numpy(np.ascontiguousarray(arr)).pin_memory().to(self.device, non_blocking=True)
 
+    def _sample(self, pb, batch, emits, out, nxt):
+        """Draws the batch's tokens; requests without parameters stay greedy."""
+        par = np.zeros((5, len(batch)), np.float32)        # temperature, top-k (int32), top-p, min-p, uniform
+        par[2] = 1.0
+        top_k = par[1].view(np.int32)
+        for i, s in enumerate(batch):
+            if s.sampling is None:
+                continue
+            sp = s.sampling
+            par[0, i], top_k[i], par[2, i], par[3, i] = sp.temperature, sp.top_k, sp.top_p, sp.min_p
+            if emits[i]:
+                par[4, i] = s.rng.random(dtype=np.float32)
+        dev = self._h2d(par)
+        sp = B.Sampling(dev[0], dev[1].view(torch.int32), dev[2], dev[3])
+        B.vfm_sample_tokens(pb.c, out, sp, dev[4], nxt)
+
     def step(self, now=0.0):
         """One continuous-batching step; returns the ids of the requests that finished.
 
         Nothing here waits for the GPU (unless `record` is set): a decode
         row's input token is gathered on the device from the previous step's
-        greedy picks, the host copies go through pinned memory, and a
+        picks, the host copies go through pinned memory, and a
         sequence finishes by its token count, so the host plans step n + 1
         while the GPU still runs step n.  Token values are read back by
         `tokens()`."""
@@ -333,9 +414,7 @@ class ContinuousBatcher:
         budget = self.max_step_tokens - len(dec)
         chunks = []
         for s in [s for s in old if s.cached < len(s.prompt)] + new:
-            n = len(s.prompt) - s.cached
-            if self.chunk:
-                n = min(n, budget)
+            n = self._rows(s, budget)
             if n <= 0:
                 continue
             chunks.append((s, n))
@@ -347,14 +426,15 @@ class ContinuousBatcher:
         task = np.array([s.task for s in batch], np.int32)
         lens = np.array([1] * len(dec) + [n for _, n in chunks], np.int32)
         ctx = np.array([s.cached for s in batch], np.int32)
-        for s, c, n in zip(batch, ctx, lens):
-            self.alloc.reserve(s.slot, int(c) + int(n))
-        slots = np.array([s.slot for s in batch], np.int32)
-        table = self.alloc.table(slots, max(int(self.alloc.count(int(x))[0]) for x in slots))
+        table = self._tables(batch, ctx.astype(np.int64) + lens)
         table_dev = self._h2d(table)
         pb = B.Batch(task, lens, w.n_tasks, ctx_len=ctx, n_out=self.m.heads.n_out, device=self.device,
                      non_blocking=True)
-        need = max(B.vfm_workspace_size(self.cfg, pb.c, self.m.lora_c(i)) for i in range(self.m.n_layers))
+        if self.window is None:
+            need = max(B.vfm_workspace_size(self.cfg, pb.c, self.m.lora_c(i)) for i in range(self.m.n_layers))
+        else:
+            need = max(B.vfm_workspace_size_windowed(self.cfg, pb.c, self.m.lora_c(i), self.window, self.n_sink)
+                       for i in range(self.m.n_layers))
         if need > self.ws.numel():
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         x = torch.empty(pb.T, w.d, dtype=torch.float32, device=self.device)
@@ -372,12 +452,20 @@ class ContinuousBatcher:
         for li in range(self.m.n_layers):
             kv = B.vfm_kv_pages(self.k[li].data_ptr(), self.v[li].data_ptr(), self.n_pages, self.page_size,
                                 table.shape[1], tp, table_dev.data_ptr())
-            B.vfm_layer_forward_paged(self.cfg, self.m.c_layers[li], self.m.lora_c(li), pb.c, x, kv, self.ws)
+            if self.window is None:
+                B.vfm_layer_forward_paged(self.cfg, self.m.c_layers[li], self.m.lora_c(li), pb.c, x, kv, self.ws)
+            else:
+                B.vfm_layer_forward_windowed(self.cfg, self.m.c_layers[li], self.m.lora_c(li), pb.c, x, kv,
+                                             self.window, self.n_sink, self.ws)
         out = torch.empty(max(pb.total_outputs, 1), dtype=torch.float32, device=self.device)
         fn = self.m.final
         B.vfm_head_forward(self.cfg, fn["w"], fn.get("b"), self.m.head_tab.c, pb.c, x, out, self.ws)
         nxt = torch.empty(len(batch), dtype=torch.int32, device=self.device)
-        B.vfm_greedy_tokens(pb.c, out, nxt)
+        emits = [s.cached + int(n) >= len(s.prompt) for s, n in zip(batch, lens)]
+        if any(s.sampling is not None for s in batch):
+            self._sample(pb, batch, emits, out, nxt)
+        else:
+            B.vfm_greedy_tokens(pb.c, out, nxt)
         self._prev_nxt = nxt
         self._picks.append(nxt)
         self._keep = (pb, table, table_dev)            # host arrays the stream may still read
@@ -390,7 +478,7 @@ class ContinuousBatcher:
         rec, finished = [], []
         for i, s in enumerate(batch):
             s.cached += int(lens[i])
-            if s.cached < len(s.prompt):               # a chunk inside the prompt: no token yet
+            if not emits[i]:                           # a chunk inside the prompt: no token yet
                 continue
             s.generated.append((self.steps, i))
             s.row = i

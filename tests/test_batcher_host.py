@@ -87,3 +87,49 @@ def test_requests_that_can_never_fit_are_refused():
         cb.submit(0, 0, np.zeros(40, np.int32), 1)   # 40 tokens need 3 pages of 16
     with pytest.raises(ValueError):
         cb.submit(1, 0, np.zeros(0, np.int32), 1)    # empty prompt
+
+
+def test_windowed_sequences_hold_a_ring_of_pages():
+    """Pages of 16, window 40, 20 sinks: 2 pages for the sinks and, with at most 40 new rows a step, ring pages for
+    79 positions in a row, which touch at most 6."""
+    cb = _batcher(n_pages=32, max_pages=8, max_step_tokens=64, window=40, n_sink=20)
+    assert cb.chunk and cb.max_chunk == 40
+    cb.submit(0, 0, np.zeros(200, np.int32), 10000)      # far more positions than the pool has
+    cb.submit(1, 0, np.zeros(3, np.int32), 20)           # 22 positions: no ring needed
+    cb.submit(2, 0, np.zeros(1, np.int32), 10000)        # window - 1 + 1 positions: 4 pages
+    a, b, c = cb._admit(0.0)
+    assert [s.budget for s in (a, b, c)] == [8, 2, 6] and cb.committed == 16
+    rng = np.random.default_rng(0)
+    for s, most in ((a, 40), (c, 1)):
+        ctx, owner = 0, {}                               # physical page -> the logical page that was written last
+        while ctx < 3000:
+            n = min(int(rng.integers(1, most + 1)), len(s.prompt) - ctx) if ctx < len(s.prompt) else 1
+            t = cb._tables([s, b], [ctx + n, 5])
+            assert t.shape[1] == -(-(ctx + n) // 16)
+            for j in range(ctx // 16, t.shape[1]):
+                owner[int(t[0, j])] = j
+            first = max(0, ctx - 40 + 1) // 16
+            for j in list(range(first, t.shape[1])) + [j for j in (0, 1) if j < t.shape[1]]:
+                assert owner[int(t[0, j])] == j          # a page that some row sees still holds its positions
+            ctx += n
+        assert len(owner) <= s.budget == cb.alloc.count(s.slot)[0]
+    held = {int(p) for s in (a, b, c) for p in cb.alloc.table([s.slot])[0][:cb.alloc.count(s.slot)[0]]}
+    assert len(held) == sum(cb.alloc.count(s.slot)[0] for s in (a, b, c))      # no page belongs to two
+
+
+def test_windowed_prompts_take_bounded_chunks():
+    cb = _batcher(n_pages=32, max_pages=8, max_step_tokens=64, window=40)
+    cb.submit(0, 0, np.zeros(100, np.int32), 2)
+    cb.submit(1, 0, np.zeros(100, np.int32), 2)
+    a, b = cb._admit(0.0)
+    assert cb._rows(a, 64) == 40 and cb._rows(b, 24) == 24
+
+
+def test_windows_and_sampling_parameters_are_refused():
+    for kw in (dict(window=0), dict(window=16, n_sink=-1), dict(max_chunk=0)):
+        with pytest.raises(ValueError):
+            _batcher(**kw)
+    for kw in (dict(temperature=-0.5), dict(temperature=float("nan")), dict(top_k=-1), dict(top_k=2 ** 31),
+               dict(top_p=-0.1), dict(min_p=float("nan"))):
+        with pytest.raises(ValueError):
+            R.SamplingParams(**kw)

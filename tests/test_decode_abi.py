@@ -214,3 +214,19 @@ def test_binding_checks_operands():
         args.update(bad)
         with pytest.raises(ValueError):
             B.vfm_sample_tokens(b, args["out"], args["sampling"], args["u"], args["ids"], args["logprob"], stream=1)
+
+
+def test_binding_refuses_host_memory():
+    """Operands that would pass but for their device never reach the library."""
+    import torch
+    host, b = _batch(lens=(1, 2), ctx=(3, 0))
+    a = _attn()
+    kp = torch.zeros(KH, 10 * 16, DH, dtype=torch.bfloat16)
+    kv = B.PagedKV(kp, kp.clone(), 16, np.arange(2 * 4).reshape(2, 4), device="cpu")
+    q, qkv = torch.zeros(3, H * DH, dtype=torch.bfloat16), torch.zeros(3, (H + 2 * KH) * DH, dtype=torch.bfloat16)
+    for call in (lambda: B.vfm_attention_paged(a, b, q, kv, q.clone(), None, stream=1),
+                 lambda: B.vfm_kv_append(a, b, qkv, q, kv, stream=1),
+                 lambda: B.vfm_sample_tokens(b, torch.zeros(14), B.Sampling(), torch.zeros(2),
+                                             torch.zeros(2, dtype=torch.int32), stream=1)):
+        with pytest.raises(ValueError, match="current GPU"):
+            call()
