@@ -281,8 +281,9 @@ int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, At
   const int64_t most = ((int64_t)1 << 24) - 1;
   const int64_t few_tiles = a.dtype == VFM_BF16 ? (int64_t)ap.qtiles * pl.n_req : (int64_t)pl.T * G / 16 + pl.n_req;
   const int64_t rows_tiles = (int64_t)pl.T / rows_per_block(4, G) + pl.n_req;
-  if ((ap.few && few_tiles * a.n_kv_heads * ap.few_chunks > most) ||
-      ((ap.rows || ap.wide) && rows_tiles * a.n_kv_heads * ap.rows_chunks > most) ||
+  const int64_t few_blocks = ap.few ? few_tiles * a.n_kv_heads * ap.few_chunks : 0;
+  const int64_t rows_blocks = ap.rows || ap.wide ? rows_tiles * a.n_kv_heads * ap.rows_chunks : 0;
+  if (few_blocks > most || rows_blocks > most || few_blocks + rows_blocks > most ||
       (ap.nchunk() > 1 && (int64_t)pl.T * a.n_heads / 4 >= most))
     return VFM_ERR_UNSUPPORTED;
   if (ap.nchunk() > 1) {

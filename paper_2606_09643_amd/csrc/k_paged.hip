@@ -202,19 +202,18 @@ __device__ __forceinline__ int few_vswz(int r) {
   return DH == 128 ? ((r & 3) | (((r >> 3) & 1) << 2)) : (((r >> 1) & 1) | (((r >> 3) & 1) << 1));
 }
 
+// smem: 256 DH bytes, V tiles, then the waves' outputs
 template <int DH>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_few_bf16_kernel(Plan pl, PagedAttn a) {
+__device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, int id, char* smem) {
   constexpr int LPR = DH / 8;          // lanes per K / V row (16 bytes each)
   constexpr int RPI = 64 / LPR;        // rows per wave-wide load
   constexpr int VI = 32 / RPI;         // V loads per lane and tile
   constexpr int KS = DH / 32;          // MFMA steps over the head dims
   constexpr int ND = DH / 16;          // output tiles
-  __shared__ __attribute__((aligned(16))) char smem[4 * 32 * DH * 2];   // V tiles, then the waves' outputs
   __shared__ float sm[4][16], sl[4][16];
 
   Work w;
   {
-    int id = blockIdx.x;
     w.h = id % a.KH; id /= a.KH;
     w.c = id % a.few_chunks; id /= a.few_chunks;
     w.qt = id % a.qtiles;
@@ -353,12 +352,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         const bf16* vr = vh + (int64_t)page_slot(prow, lp, k) * DH + 4 * g;
         const bool see = sees(jq, k, a.window, a.n_sink);
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+        for (int d = 0; d < ND; ++d) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float v = (float)vr[16 * d + i];
             if (see && nonfinite(v)) o[d][i] += v;
           }
+          __builtin_amdgcn_sched_barrier(0);              // no registers for more loads in flight
+        }
       }
     }
   };
@@ -456,20 +457,23 @@ __device__ __forceinline__ int rows_vswz(int r, int c) {
 template <int N>
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14)); }
 
+// LDS stages of 256 DH bytes
+constexpr int rows_stages(int dh, int waves) { return dh == 128 && waves == 4 ? 2 : 4; }
+
 // NW waves: 4 (two blocks share a CU) or 8 (one).
 template <int DH, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_rows_bf16_kernel(Plan pl, PagedAttn a) {
+__device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, int id, bf16* stage0, bf16* stage1, bf16* stage2,
+                                           bf16* stage3) {
   constexpr int CH = DH / 8;             // 16-byte chunks per row
   constexpr int RPI = 64 / CH;           // rows per wave-wide load
   constexpr int NI = 64 / (NW * RPI);    // K (and V) loads per wave and tile
   constexpr int KS = DH / 16;            // MFMA steps over the head dims
   constexpr int ND = DH / 32;            // output tiles
-  constexpr int NST = DH == 128 && NW == 4 ? 2 : 4;   // LDS stages
+  constexpr int NST = rows_stages(DH, NW);
   // Stage j: K of a tile t with t mod NST = j, then V of tile t - 1 (a step reads K a tile ahead of V).
   // A variable per stage, so that the compiler can tell the one that is read from the one being
   // filled and does not wait for its loads.
-  constexpr int TE = 64 * DH, SE = 2 * TE;
-  __shared__ __attribute__((aligned(16))) bf16 stage0[SE], stage1[SE], stage2[NST > 2 ? SE : 8], stage3[NST > 3 ? SE : 8];
+  constexpr int TE = 64 * DH;
   auto stage = [&](auto b) -> bf16* {
     if constexpr (b == 0) return stage0;
     else if constexpr (b == 1) return stage1;
@@ -482,7 +486,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   Work w;
   int blk;
   {
-    int id = blockIdx.x;
     w.h = id % a.KH; id /= a.KH;
     if constexpr (NW == 4) { w.c = id % a.rows_chunks; id /= a.rows_chunks; }
     else w.c = 0;                         // a request of wide blocks has no need to cut its keys
@@ -811,6 +814,23 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 }
 
+// rows_blocks blocks of the many-row kind with NW waves (0: none), then, with FEW, those of the few-row
+// kind: a step's single rows run beside its prompts, on the CUs that these leave free.  24 requests of
+// 64 to 2000 positions, 5 of them with up to 250 rows, 16 heads of 64: 31.5 us, as two launches 45.7.
+template <int DH, int NW, bool FEW>
+__global__ __launch_bounds__(NW == 8 ? 512 : 256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_bf16_kernel(
+    Plan pl, PagedAttn a, int rows_blocks) {
+  static_assert(!(NW == 8 && FEW), "a few-row block has 4 waves");
+  constexpr int NST = NW > 0 ? rows_stages(DH, NW) : 1, SE = 128 * DH;
+  __shared__ __attribute__((aligned(16))) bf16 stage0[SE], stage1[NST > 1 ? SE : 8], stage2[NST > 2 ? SE : 8], stage3[NST > 3 ? SE : 8];
+  if constexpr (FEW)
+    if ((int)blockIdx.x >= rows_blocks) {
+      few_block<DH>(pl, a, (int)blockIdx.x - rows_blocks, reinterpret_cast<char*>(stage0));
+      return;
+    }
+  if constexpr (NW > 0) rows_block<DH, NW>(pl, a, blockIdx.x, stage0, stage1, stage2, stage3);
+}
+
 // ---------------------------------------------------------------------------
 // fp32, any number of rows (v_mfma_f32_16x16x4_f32): 16 packed queries per
 // block, the chunk's 16-key runs dealt to the 4 waves, operands from memory
@@ -1056,14 +1076,20 @@ hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const
   do { if (head_dim == 64) hipLaunchKernelGGL((K_<64>), G_, dim3(256), 0, s, pl, a); \
        else hipLaunchKernelGGL((K_<128>), G_, dim3(256), 0, s, pl, a); } while (0)
   if (dtype == VFM_BF16) {
-    if (few_) BY_DH(attn_few_bf16_kernel, dim3(few * a.qtiles * pl.n_req));
-#define ROWS(D_, W_)                                                                                             \
-  hipLaunchKernelGGL((attn_rows_bf16_kernel<D_, W_>),                                                             \
-                     dim3((W_ == 8 ? (unsigned)a.KH : rows) * (pl.T / rows_per_block(W_, a.G) + pl.n_req)), dim3(64 * W_), \
-                     0, s, pl, a)
-    if (rows_) { if (head_dim == 64) ROWS(64, 4); else ROWS(128, 4); }
-    if (wide) { if (head_dim == 64) ROWS(64, 8); else ROWS(128, 8); }
-#undef ROWS
+    const unsigned nf = few_ ? few * a.qtiles * pl.n_req : 0;
+    const unsigned nr = rows_ ? rows * (pl.T / rows_per_block(4, a.G) + pl.n_req) : 0;
+    const unsigned nw = wide ? (unsigned)a.KH * (pl.T / rows_per_block(8, a.G) + pl.n_req) : 0;
+#define BF16(W_, F_, N_, R_)                                                                                      \
+  do {                                                                                                            \
+    const dim3 grid(N_), block(W_ == 8 ? 512 : 256);                                                            \
+    if (head_dim == 64) hipLaunchKernelGGL((attn_bf16_kernel<64, W_, F_>), grid, block, 0, s, pl, a, (int)(R_));  \
+    else hipLaunchKernelGGL((attn_bf16_kernel<128, W_, F_>), grid, block, 0, s, pl, a, (int)(R_));                \
+  } while (0)
+    if (wide) BF16(8, false, nw, nw);
+    if (rows_ && few_) BF16(4, true, nr + nf, nr);
+    else if (rows_) BF16(4, false, nr, nr);
+    else if (few_) BF16(0, true, nf, 0);
+#undef BF16
   } else {
     BY_DH(attn_f32_kernel, dim3(few * (unsigned)((int64_t)pl.T * a.G / 16 + pl.n_req)));
   }
