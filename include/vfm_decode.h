@@ -127,7 +127,7 @@ typedef struct vfm_sampling {
  * Weights are computed in fp64 and summed as 44-bit fixed point (32-bit for
  * heads of 2^19 outputs and more), exactly and in any order: a weight below
  * 2^-45 of the largest counts as 0, and the result does not depend on how
- * the work is split. */
+ * the work is split.  VFM_ERR_SHAPE: a request of more than 2^30 outputs. */
 int vfm_sample_tokens(const vfm_batch* batch, const float* out, const vfm_sampling* sampling,
                       const float* u, int32_t* ids, float* logprob, void* stream);
 

@@ -208,8 +208,10 @@ int check_stream(void* stream) {
   if (stream == nullptr) return VFM_OK;
   int dev = -1;
   hipDevice_t sdev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || hipStreamGetDevice((hipStream_t)stream, &sdev) != hipSuccess)
+  if (hipGetDevice(&dev) != hipSuccess || hipStreamGetDevice((hipStream_t)stream, &sdev) != hipSuccess) {
+    (void)hipGetLastError();               // reported here, not by the next launch
     return VFM_ERR_HIP;
+  }
   return sdev == dev ? VFM_OK : VFM_ERR_ARG;
 }
 
@@ -842,6 +844,7 @@ extern "C" int vfm_sample_tokens(const vfm_batch* batch, const float* out, const
   const int32_t* off = host_arr(batch, po.out_off);
   int most = 0;
   for (int i = 0; i < pl.n_req; ++i) most = std::max(most, off[i + 1] - off[i]);
+  if (most > 1 << 30) return VFM_ERR_SHAPE;
   VFM_TRY(check_stream(stream));
   return hip_status(launch_sample(pl, out, *sampling, u, ids, logprob, most, (hipStream_t)stream));
 }

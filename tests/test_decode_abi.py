@@ -230,3 +230,10 @@ def test_binding_refuses_host_memory():
                                              torch.zeros(2, dtype=torch.int32), stream=1)):
         with pytest.raises(ValueError, match="current GPU"):
             call()
+
+
+def test_sample_refuses_huge_heads():
+    host = B.vfm_plan(np.array([0]), np.array([1]), 1, n_out=np.array([(1 << 30) + 1]))
+    b = B.vfm_batch(host.ctypes.data_as(C.POINTER(C.c_int32)), PTR, host.size)
+    s = B.vfm_sampling(None, None, None, None)
+    assert B.lib().vfm_sample_tokens(C.byref(b), PTR, C.byref(s), PTR, PTR, None, 1) == B.VFM_ERR_SHAPE
