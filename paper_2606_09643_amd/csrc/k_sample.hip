@@ -17,6 +17,8 @@
 // only one that is put in order, and where all bins up to it hold few outputs
 // (top-k), nothing else is looked at again.  One block per request: the row is
 // read once where it fits registers or LDS (up to 32768 outputs).
+#include <type_traits>
+
 #include "decode_internal.h"
 
 namespace {
@@ -30,13 +32,17 @@ struct SampleParams {
 
 // 2^t, t <= 0, scaled by 2^sh and rounded to an integer.  t = n + f, |f| <= 1/2, and
 // 2^f by the polynomial of degree 10 through 1 at 0 that interpolates it at the
-// Chebyshev nodes (relative error 6e-16).  Adding 2^52 leaves the integer in the
-// low bits.  t below -100 (-inf) and NaN count as -100: 0.  No branch, so that a
-// thread's four chains run beside each other; the coefficients stay in scalar
-// registers (as literals each product would move one into a vector register).
+// Chebyshev nodes (relative error 6e-16).  Adding 1.5 2^52 rounds t to n and leaves
+// n (plus what is added beside it: the exponent field of 2^(n + sh)) in the low
+// bits; adding 2^52 rounds the weight and leaves it there.  t below -100 (-inf) and
+// NaN count as -100: 0.  No branch, so that a thread's four chains run beside each
+// other.  The coefficients are made anew for every four outputs, in scalar registers:
+// as literals each product would move one into a vector register, and held over the
+// whole kernel they do not fit beside the rest.
 struct Exp2 {
-  double c[10];
-  __device__ __forceinline__ void init() {
+  double c[10], magic;
+  __device__ __forceinline__ explicit Exp2(int sh) {
+    magic = 6755399441055744.0 + (double)(1023 + sh);
     constexpr double k[10] = {7.0709785640393195e-09, 1.0205905435457491e-07, 1.3215451629202315e-06,
                               1.5252672924749049e-05, 1.5403530424784571e-04, 1.3333558200794733e-03,
                               9.6181291076186601e-03, 5.5504108664651670e-02, 2.4022650695910075e-01,
@@ -47,16 +53,20 @@ struct Exp2 {
       asm volatile("" : "+s"(c[i]));
     }
   }
-  __device__ __forceinline__ uint64_t operator()(double t, int sh) const {
+  // the weight beside the bits of 2^52, which a sum takes out at its end
+  static constexpr uint64_t BIAS = 0x4330000000000000ull;
+  __device__ __forceinline__ uint64_t biased(double t) const {
     t = fmax(t, -100.0);
-    const double n = __builtin_rint(t), f = t - n;
+    const double x = t + magic, f = t - (x - magic);
     double p = c[0];
 #pragma unroll
     for (int i = 1; i < 10; ++i) p = fma(p, f, c[i]);
     p = fma(p, f, 1.0);
-    const double d = __builtin_ldexp(p, (int)n + sh) + 4503599627370496.0;
-    return (uint64_t)__double_as_longlong(d) & 0xFFFFFFFFFFFFFull;
+    const uint32_t e = (uint32_t)__double_as_longlong(x) << 20;        // of 2^(n + sh): a normal number
+    const double d = fma(p, __longlong_as_double((long long)((uint64_t)e << 32)), 4503599627370496.0);
+    return (uint64_t)__double_as_longlong(d);
   }
+  __device__ __forceinline__ uint64_t operator()(double t) const { return biased(t) & 0xFFFFFFFFFFFFFull; }
 };
 
 // ln x, x >= 1: x = 2^e m, m in [2/3, 4/3), ln m = 2 atanh((m - 1) / (m + 1)) by its
@@ -156,7 +166,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
                                                     float* __restrict__ logprob) {
   using Sh = Shape<NT, WHERE>;
   constexpr int NW = NT / 64, NB = NT;
-  constexpr int CAP = NT / 2;          // outputs that are put in order at once, each against each
+  constexpr int CAP = NT == 256 ? 256 : 512;   // outputs that are put in order at once, each against each
   constexpr int NG = 256;              // at most this many groups of threads, whose largest outputs bound a top-k from below
   constexpr int PB = Sh::PB, SETS = Sh::SETS, PER = NW / SETS;   // bins of weights; sets of them; waves per set
   __shared__ __attribute__((aligned(16))) float s_row[WHERE == IN_LDS ? NT * 4 * Sh::RUNS : 4];
@@ -169,7 +179,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
   __shared__ __attribute__((aligned(16))) uint64_t l_key[CAP + 8];   // (float_key, ~index): descending order; then running sums
   __shared__ uint64_t l_sorted[CAP], l_mass[CAP];
   __shared__ uint32_t l_rank[CAP];
-  __shared__ uint32_t s_n, s_sel[3];   // kept outputs; bin, outputs before it, outputs in it
+  __shared__ uint32_t s_n, s_listed[2], s_sel[3];   // kept outputs; listed ones, by turns; bin, outputs before it, outputs in it
   __shared__ uint64_t s_before;
   __shared__ float s_bound;
   auto h_mass = [&](int b) -> uint64_t& { return reinterpret_cast<uint64_t*>(s_bins)[b]; };
@@ -244,7 +254,14 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
   const int k = mp > 1.f && n > 1 ? 1 : tk > 0 && tk < n ? tk : 0;
   const bool p_on = tp < 1.f;
   const double p = (double)tp;
-  const bool small_k = k > 0 && k <= NG;                 // block-uniform, as every branch on the row's values below
+  // (registers: up to 56, where bins take 7.7 us for 256 rows of 1000 and a list of twice as many as k 14 and more)
+  const bool small_k = k > 0 && k <= (WHERE == IN_REGS ? 56 : NG);   // block-uniform, as every branch on the row's values below
+  const double T = fmin(fmax((double)temp, 1e-30), 1e30);
+  const double c2 = 1.4426950408889634 / T;
+  if (tid < 2) s_listed[tid] = 0;
+  int turn = 0;
+  if (p_on && k == 0)                                    // while the row's loads are in flight
+    for (int b = tid; b < SETS * PB; b += NT) set_mass(0, b) = 0;
 
   // The largest and the smallest output, and for a small top-k the largest of each
   // of 256 groups of threads
@@ -286,13 +303,10 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
     if (lane == 0) { red_f[0][wave] = mx; red_f[1][wave] = lo; red_c[1][wave] = anyw; }
   }
   __syncthreads();
-  bool found = false;
-#pragma unroll
-  for (int i = 0; i < NW; ++i) {
-    M0 = fmaxf(M0, red_f[0][i]);
-    mn = fminf(mn, red_f[1][i]);
-    found = found || red_c[1][i];
-  }
+  const int wl = lane % NW;                              // (short code: each block runs it once, from a cold cache)
+  M0 = wave_max(red_f[0][wl]);
+  mn = -wave_max(-red_f[1][wl]);
+  const bool found = __any(red_c[1][wl]);
   if (!found) {
     if (tid == 0) { ids[row] = -1; if (logprob) logprob[row] = nan; }
     return;
@@ -326,14 +340,11 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
       __syncthreads();
     }
   }
-  const double T = fmin(fmax((double)temp, 1e-30), 1e30);
-  const double c2 = 1.4426950408889634 / T;
   const int sh = n < (1 << 19) ? 44 : 32;
   const uint64_t one = (uint64_t)1 << sh;
   const float cut = fminf((float)(31.2 * T), 3e38f);     // 45 ln 2: below M - cut every weight is 0
-  Exp2 exp2_fixed;
-  exp2_fixed.init();
-  auto mass = [&](float v) -> uint64_t { return exp2_fixed(((double)v - (double)M) * c2, sh); };
+  auto power = [&](float v) { return ((double)v - (double)M) * c2; };
+  auto mass = [&](float v) -> uint64_t { return Exp2(sh)(power(v)); };
   auto value_of = [&](uint32_t key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu)); };
   const double uu = u_row > 0.f ? (double)u_row : 0.0;   // NaN: 0
   auto target_of = [&](uint64_t S) {
@@ -347,21 +358,36 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
 
   // The outputs that f(value, index) picks, if they are at most CAP: in descending order in
   // l_sorted, their weights in l_mass and running sums in l_cum.  Returns their number.
-  auto list = [&](auto&& f) -> uint32_t {
-    uint32_t mine = 0;
-    each([&](float v, int i) { mine += f(v, i); });
-    const uint32_t inc = wave_scan(mine);
-    const bool some = last_lane(inc) > 0;
-    __syncthreads();                                     // red_c, the list
-    if (lane == 63) red_c[0][wave] = inc;
+  // One pass: a wave that finds some takes places behind those taken before; the order of the
+  // places does not matter, and a wave that finds no place left stops.
+  // by_index: each one's place in the order of the indices, at its place in l_sorted, in l_rank.
+  auto list = [&](auto by_index, auto&& f) -> uint32_t {
     if (tid < CAP) l_rank[tid] = 0;
-    __syncthreads();
-    uint32_t cnt = 0, pos = inc - mine;
+    __syncthreads();                                     // the list of before, and its number, have been read
+    turn ^= 1;
+    if (tid == 0) s_listed[turn ^ 1] = 0;
+    bool room = true;
+    each4([&](const f4u& q, int i0) {
+      bool hit[4];
+      uint64_t m[4];
 #pragma unroll
-    for (int i = 0; i < NW; ++i) { pos += i < wave ? red_c[0][i] : 0; cnt += red_c[0][i]; }
+      for (int c = 0; c < 4; ++c) { hit[c] = f((float)q[c], i0 + c); m[c] = __ballot(hit[c]); }
+      if (room && (m[0] | m[1] | m[2] | m[3])) {
+        uint32_t base = 0;
+        if (lane == 0) base = atomicAdd(&s_listed[turn], (uint32_t)(__popcll(m[0]) + __popcll(m[1]) + __popcll(m[2]) + __popcll(m[3])));
+        base = (uint32_t)__builtin_amdgcn_readfirstlane((int)base);
+        room = base < (uint32_t)CAP;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t pos = base + __builtin_amdgcn_mbcnt_hi((uint32_t)(m[c] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m[c], 0));
+          if (hit[c] && pos < (uint32_t)CAP) l_key[pos] = ((uint64_t)float_key((float)q[c]) << 32) | (uint32_t)~(i0 + c);
+          base += (uint32_t)__popcll(m[c]);
+        }
+      }
+    });
+    __syncthreads();
+    const uint32_t cnt = s_listed[turn];                 // more than CAP: some that were not counted
     if (cnt > CAP) return cnt;
-    if (some)
-      each([&](float v, int i) { if (f(v, i)) l_key[pos++] = ((uint64_t)float_key(v) << 32) | (uint32_t)~i; });
     if (tid < 8) l_key[cnt + tid] = 0;                   // below every key
     __syncthreads();
     // every listed output against every other: 2^lg of them at a time, the others split among the rest of the block
@@ -370,19 +396,26 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
     const uint32_t j0 = (tid >> lg) * len, j1 = min(j0 + len, (cnt + 7) & ~7u);
     if (parts > 0 && j0 < j1) {
       const uint64_t me = l_key[min(e, cnt)];
-      uint32_t r = 0;
+      uint32_t r = 0;                                    // larger keys; in the upper half, smaller indices
       for (uint32_t j = j0; j < j1; j += 8) {
         u64x2 q[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const u64x2*>(&l_key[j + 2 * i]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) r += (uint32_t)(q[i][0] > me) + (uint32_t)(q[i][1] > me);
+        if constexpr (by_index)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            r += ((uint32_t)q[i][0] > (uint32_t)me ? 1u << 16 : 0u) + ((uint32_t)q[i][1] > (uint32_t)me ? 1u << 16 : 0u);
       }
       if (e < cnt) atomicAdd(&l_rank[e], r);
     }
     __syncthreads();
-    if ((uint32_t)tid < cnt) l_sorted[l_rank[tid]] = l_key[tid];
+    const uint32_t ranks = tid < CAP ? l_rank[tid] : 0;
+    if ((uint32_t)tid < cnt) l_sorted[ranks & 0xFFFF] = l_key[tid];
     __syncthreads();
+    if constexpr (by_index)
+      if ((uint32_t)tid < cnt) l_rank[ranks & 0xFFFF] = ranks >> 16;
     uint64_t w = 0;
     if ((uint32_t)tid < cnt) w = mass(value_of((uint32_t)(l_sorted[tid] >> 32)));
     const uint64_t cw = wave_scan(w);
@@ -420,7 +453,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
     if (tid < groups && r == (uint32_t)k - 1) s_bound = remap ? -INFINITY : g;
     __syncthreads();
     const float bound = s_bound;
-    const uint32_t cnt = list([&](float v, int) { return v >= bound; });
+    const uint32_t cnt = list(std::true_type{}, [&](float v, int) { return v >= bound; });
     if (cnt <= CAP) {
       const uint32_t nk = min((uint32_t)k, cnt);
       const double target = p_on ? p * (double)l_cum[nk - 1] : INFINITY;
@@ -433,12 +466,21 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
       const uint32_t kept = s_n;
       const uint64_t S = l_cum[kept - 1];
       const uint64_t tgt = target_of(S);
-      if (mine) {
-        const uint64_t it = l_sorted[tid];
-        uint64_t c = 0;                                  // kept weight up to this output, by index
-#pragma unroll 4
-        for (uint32_t j = 0; j < kept; ++j) c += (uint32_t)l_sorted[j] >= (uint32_t)it ? l_mass[j] : 0;
-        if (c > tgt && c - l_mass[tid] <= tgt) finish(value_of((uint32_t)(it >> 32)), (int)~(uint32_t)it, S);
+      // the listed ones in the order of their indices: weight (0 unless kept) and place
+      uint64_t* const x_mass = reinterpret_cast<uint64_t*>(s_bins);
+      uint32_t* const x_at = reinterpret_cast<uint32_t*>(s_bins + CAP * 8);
+      static_assert(BINS >= CAP * 12, "");
+      if ((uint32_t)tid < cnt) { x_mass[l_rank[tid]] = (uint32_t)tid < kept ? l_mass[tid] : 0; x_at[l_rank[tid]] = tid; }
+      __syncthreads();
+      const uint64_t x = (uint32_t)tid < cnt ? x_mass[tid] : 0;
+      uint64_t c = wave_scan(x);
+      if (lane == 63) red_u[wave] = c;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < CAP / 64; ++i) c += i < wave ? red_u[i] : 0;
+      if (c > tgt && c - x <= tgt) {
+        const uint64_t it = l_sorted[x_at[tid]];
+        finish(value_of((uint32_t)(it >> 32)), (int)~(uint32_t)it, S);
       }
       return;
     }
@@ -576,7 +618,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
       __syncthreads();
       return;
     }
-    list(inside);
+    list(std::false_type{}, inside);
     if ((uint32_t)tid < cnt) {
       const uint64_t me = m0 + l_cum[tid] - l_mass[tid], mi = m0 + l_cum[tid];
       const bool hit = j > 0 ? before + tid + 1 == j
@@ -602,20 +644,29 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
     if (stage == 1) {
       const float range = range_to(low), scale = scale_of(range, PB);
       const int set = wave / PER;
-      lds_done();
-      __syncthreads();
-      for (int b = tid; b < SETS * PB; b += NT) set_mass(0, b) = 0;
-      __syncthreads();
-      each4([&](const f4u& q, int i0) {
-        uint64_t w[4];
+      if (k > 0) {                                       // cleared at the start, but the top-k has used them
+        lds_done();
+        __syncthreads();
+        for (int b = tid; b < SETS * PB; b += NT) set_mass(0, b) = 0;
+        __syncthreads();
+      }
+      // an output without a weight (a NaN, too) adds nothing anywhere
+      auto into_bins = [&](auto all) {
+        each4([&](const f4u& q, int i0) {
+          const Exp2 weight(sh);
+          uint64_t w[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) w[c] = mass((float)q[c]);
+          for (int c = 0; c < 4; ++c) w[c] = weight(power((float)q[c]));
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int b = bin_of((float)q[c], range, scale, PB);
-          if ((b >= 0) & above((float)q[c], i0 + c)) atomicAdd((unsigned long long*)&set_mass(set, b), (unsigned long long)w[c]);
-        }
-      });
+          for (int c = 0; c < 4; ++c) {
+            const int b = (int)fminf((M - (float)q[c]) * scale, (float)(PB - 1));
+            if ((w[c] != 0) & (all || above((float)q[c], i0 + c)))
+              atomicAdd((unsigned long long*)&set_mass(set, b), (unsigned long long)w[c]);
+          }
+        });
+      };
+      if (k == 0) into_bins(std::true_type{});
+      else into_bins(std::false_type{});
       __syncthreads();
       uint64_t sum = 0;
       if (tid < PB)
@@ -635,7 +686,12 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
       __syncthreads();
       const int bin = (int)s_sel[1];
       const uint64_t m0 = s_before;
-      const uint32_t cnt = list([&](float v, int i) { return above(v, i) & (bin_of(v, range, scale, PB) == bin); });
+      // in the bin, by its borders: what truncation takes to it
+      const float b0 = (float)bin, b1 = bin == PB - 1 ? INFINITY : (float)(bin + 1);
+      const uint32_t cnt = list(std::false_type{}, [&](float v, int i) {
+        const float d = M - v, x = d * scale;
+        return (x >= b0) & (x < b1) & (d <= range) & above(v, i);
+      });
       if (cnt <= CAP) {
         if ((uint32_t)tid < cnt) {
           const uint64_t me = m0 + l_cum[tid] - l_mass[tid], mi = m0 + l_cum[tid];
@@ -655,7 +711,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
         const uint64_t e = l_sorted[last];
         v_last = value_of((uint32_t)(e >> 32));
         i_last = (int)~(uint32_t)e;
-        have = !(mp > 0.f);
+        have = l_mass[last] >= least;                    // else min-p keeps fewer still
         __syncthreads();
         continue;
       }
@@ -666,7 +722,10 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
 
   // ---- the draw: the waves' (or sets') kept weights, then the run of outputs that holds u times their sum ----
   float v_least = v_last;
-  if (mp > 0.f) v_least = fmaxf(v_least, (float)((double)M + T * log(fmin((double)mp, 1.0)) * 1.0001 - 1e-5 * fabs((double)M)));
+  // below this, with room for every rounding, min-p keeps nothing (the weights themselves decide above it)
+  if (mp > 0.f)
+    v_least = fmaxf(v_least, (float)((double)M + T * ((double)__builtin_amdgcn_logf(fminf(mp, 1.f)) * 0.6932165 - 1e-5) -
+                                     1e-5 * fabs((double)M)));
   // the kept weights of four outputs (0 for the others); returns their sum
   auto kept4 = [&](const f4u& q, int i0, uint64_t (&w)[4]) -> uint64_t {
     float x[4];
@@ -680,8 +739,9 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
       w[c] = 0;
     }
     if (any4) {
+      const Exp2 weight(sh);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) w[c] = mass(x[c]);
+      for (int c = 0; c < 4; ++c) w[c] = weight(power(x[c]));
       if (mp > 0.f)
 #pragma unroll
         for (int c = 0; c < 4; ++c) w[c] = w[c] >= least ? w[c] : 0;
@@ -692,18 +752,37 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
   if (!have) {
     __syncthreads();                                     // red_u has been read
     uint64_t sum = 0;
-    each4([&](const f4u& q, int i0) { uint64_t w[4]; sum += kept4(q, i0, w); });
+    if (k == 0 && !p_on && !(mp > 0.f)) {                // no filter: every weight
+      each4([&](const f4u& q, int) {
+        const Exp2 weight(sh);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum += weight.biased(power((float)q[c]));
+      });
+      sum -= (uint64_t)(4 * nr) * Exp2::BIAS;
+    } else {
+      each4([&](const f4u& q, int i0) { uint64_t w[4]; sum += kept4(q, i0, w); });
+    }
     sum = wave_sum(sum);
     if (lane == 0) red_u[wave] = sum;
     __syncthreads();
   }
   // the piece (a wave's runs, or a set's) that holds the target
   const int pieces = have ? SETS : NW, per = have ? PER * nr : nr;
-  auto share = [&](int i) { return have ? set_u[i] : red_u[i]; };
-  for (int i = 0; i < pieces; ++i) S += share(i);
+  // the first of the wave's 64 values (the later ones 0) with which acc passes tgt, the last of m if none: its
+  // lane; acc is then what lies before it
+  auto find = [&](uint64_t v, uint64_t tgt, int m) -> int {
+    const uint64_t c = wave_scan(v) + acc;
+    const uint64_t over = __ballot(c > tgt);
+    const int i = over ? min((int)__builtin_ctzll(over), m - 1) : m - 1;
+    const uint64_t before = c - v;
+    acc = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(before >> 32), i) << 32) |
+          (uint32_t)__builtin_amdgcn_readlane((int)before, i);
+    return i;
+  };
+  const uint64_t part = lane < pieces ? (have ? set_u[lane] : red_u[lane]) : 0;
+  S = wave_sum(part);
   const uint64_t tgt = target_of(S);
-  int piece = 0;
-  while (piece < pieces - 1 && acc + share(piece) <= tgt) acc += share(piece++);
+  const int piece = find(part, tgt, pieces);
   int run = 0;                                           // the piece's run
   if constexpr (WHERE == IN_REGS) {
     if (wave != piece) return;                           // a piece is one run
@@ -718,11 +797,13 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
       }
       __syncthreads();
       const int m = min(64, per - run);
-      const bool last = run + m >= per;
-      int i = 0;
-      while (i < (last ? m - 1 : m) && acc + run_u[i] <= tgt) acc += run_u[i++];
-      run += i;
-      if (i < m) break;
+      const uint64_t v = lane < m ? run_u[lane] : 0, all = wave_sum(v);
+      if (run + m >= per || acc + all > tgt) {
+        run += find(v, tgt, m);
+        break;
+      }
+      acc += all;
+      run += m;
       __syncthreads();
     }
     if (wave != 0) return;
