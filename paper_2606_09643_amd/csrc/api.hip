@@ -256,13 +256,13 @@ int check_pages(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, const
 // Launch facts of the paged attention over a batch.
 struct AttnPlan {
   int few_chunks, rows_chunks, qtiles;
-  bool few, rows, wide;      // requests of the few-row kernel, of the many-row kernel's narrow and wide blocks
+  bool few, rows;            // the batch has requests of the few-row and of the many-row kind
   int64_t bytes;             // workspace
   int nchunk() const { return std::max(few_chunks, rows_chunks); }
 };
 
 int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, AttnPlan* out) {
-  AttnPlan ap = {1, 1, 1, false, false, false, 0};
+  AttnPlan ap = {1, 1, 1, false, false, 0};
   const int G = a.n_heads / a.n_kv_heads;
   const PlanOffsets po = plan_offsets(pl.n_req, pl.n_tasks, pl.T);
   const int32_t *ctx = host_arr(batch, po.ctx), *cu = host_arr(batch, po.cu_seqlens);
@@ -275,16 +275,16 @@ int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, At
       ap.few_chunks = std::max(ap.few_chunks, n);
       if (a.dtype == VFM_BF16) ap.qtiles = std::max(ap.qtiles, few_qtiles(m, G));
     } else {
-      (row_waves(m, G, a.n_kv_heads) == 8 ? ap.wide : ap.rows) = true;
+      ap.rows = true;
       ap.rows_chunks = std::max(ap.rows_chunks, n);
     }
   }
   // a launch holds at most 2^32 - 1 threads, 256 a block
   const int64_t most = ((int64_t)1 << 24) - 1;
   const int64_t few_tiles = a.dtype == VFM_BF16 ? (int64_t)ap.qtiles * pl.n_req : (int64_t)pl.T * G / 16 + pl.n_req;
-  const int64_t rows_tiles = (int64_t)pl.T / rows_per_block(4, G) + pl.n_req;
+  const int64_t rows_tiles = (int64_t)pl.T / rows_per_block(G) + pl.n_req;
   const int64_t few_blocks = ap.few ? few_tiles * a.n_kv_heads * ap.few_chunks : 0;
-  const int64_t rows_blocks = ap.rows || ap.wide ? rows_tiles * a.n_kv_heads * ap.rows_chunks : 0;
+  const int64_t rows_blocks = ap.rows ? rows_tiles * a.n_kv_heads * ap.rows_chunks : 0;
   if (few_blocks > most || rows_blocks > most || few_blocks + rows_blocks > most ||
       (ap.nchunk() > 1 && (int64_t)pl.T * a.n_heads / 4 >= most))
     return VFM_ERR_UNSUPPORTED;
@@ -309,7 +309,7 @@ hipError_t run_attention(const vfm_attn& a, const Plan& pl, const AttnPlan& ap, 
     p.rec_o = (float*)ws;
     p.rec_ml = (float2*)(ws + align_up((size_t)pl.T * p.H * p.nchunk * a.head_dim * 4));
   }
-  return launch_attention_paged(a.dtype, a.head_dim, pl, p, ap.few, ap.rows, ap.wide, p.nchunk > 1, s);
+  return launch_attention_paged(a.dtype, a.head_dim, pl, p, ap.few, ap.rows, p.nchunk > 1, s);
 }
 
 vfm_attn attn_of_layer(const vfm_cfg& c, int32_t window, int32_t n_sink) {

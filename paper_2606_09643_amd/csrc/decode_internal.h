@@ -68,13 +68,8 @@ constexpr int ROWS_MIN_TILES = 8;
 // few-row kernel (bf16; fp32: every request): 16 packed queries per block
 __host__ __device__ inline bool few_rows(int dtype, int m, int G) { return dtype != VFM_BF16 || (int64_t)m * G <= FEW_QUERIES; }
 __host__ __device__ inline int few_qtiles(int m, int G) { return (int)(((int64_t)m * G + 15) / 16); }
-// many-row kernel (bf16): blocks of 256 packed queries (8 waves) where the request then still has a
-// block per CU, else of 128 (4 waves)
-__host__ __device__ inline int rows_per_block(int waves, int G) { return 32 * waves / G; }
-__host__ __device__ inline int row_waves(int m, int G, int KH) {
-  const int rb = rows_per_block(8, G);
-  return (int64_t)KH * ((m + rb - 1) / rb) >= 256 ? 8 : 4;
-}
+// many-row kernel (bf16): blocks of 128 packed queries, 32 a wave
+__host__ __device__ inline int rows_per_block(int G) { return 128 / G; }
 
 // chunks of the request with m rows after ctx cached tokens
 __host__ __device__ inline Chunks request_chunks(int dtype, int m, int ctx, int G, int KH, int window, int n_sink) {
@@ -82,7 +77,7 @@ __host__ __device__ inline Chunks request_chunks(int dtype, int m, int ctx, int 
     const int tiles = (visible_runs<4>(ctx, ctx + m - 1, window, n_sink).n + 1) / 2;
     return key_chunks(tiles, KH * few_qtiles(m, G) > 256 ? 256 : KH * few_qtiles(m, G), FEW_MIN_TILES);
   }
-  const int rb = rows_per_block(row_waves(m, G, KH), G);
+  const int rb = rows_per_block(G);
   const int64_t par = (int64_t)KH * ((m + rb - 1) / rb);
   const int m1 = m < rb ? m : rb;     // a block sees at most this many tiles more or fewer than another
   const int tiles = visible_runs<6>(ctx + m - m1, ctx + m - 1, window, n_sink).n;
@@ -94,10 +89,10 @@ hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_d
                             int64_t ld, void* q_out, int64_t ldq, void* k, void* v, int64_t slots, const KvPages& kp,
                             hipStream_t s);
 
-// few, rows, wide: the batch has requests of the few-row kernel, of the many-row kernel's narrow and wide blocks (bf16).
-// split: some request has more than one chunk.
+// few, rows: the batch has requests of the few-row and of the many-row kind.  split: some request has more than
+// one chunk.
 hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, bool few, bool rows,
-                                  bool wide, bool split, hipStream_t s);
+                                  bool split, hipStream_t s);
 
 // max_out: the batch's longest row of head outputs.
 hipError_t launch_sample(const Plan& pl, const float* out, const vfm_sampling& sp, const float* u, int32_t* ids,

@@ -116,6 +116,9 @@ __device__ __forceinline__ int page_slot(page_row prow, int lp, int k) {
 // written once.  The row's dh/2 angles go through LDS: revolutions in fp64
 // (position times theta^(-2i/dh) / 2 pi loses nothing up to 2^30 positions),
 // their fraction in fp32.
+// 32 prompts of 128 to 1024 tokens, 32 heads of 128 on 32: 178 us, 5.2 TB/s (a
+// copy of 2 GiB runs at 4.95).  Blocks of 8 rows by 12 heads, which write longer
+// runs into a page, take the same.  One row: 4.3 us, all latency.
 // ---------------------------------------------------------------------------
 template <typename T> struct Vec8;
 template <> struct Vec8<bf16> { bf16x8 v; };
@@ -188,7 +191,12 @@ __device__ __forceinline__ int64_t out_row(const PagedAttn& a, int R0, int h, in
 // Memory bound: each visible K / V row is read once per query tile.  K fragments
 // go straight to registers (lane: one key's row, 16 bytes per MFMA step), V
 // through a wave-private LDS tile that the transposing LDS read turns into the
-// V^T operand; a tile's loads are issued while the tile before is computed.
+// V^T operand; a tile's loads are issued while the tile before is computed, which
+// takes half the registers: with one tile at a time and 3 waves per SIMD instead of
+// 2 the compiler spills, and a step takes twice as long.
+// 256 requests with up to 1028 visible keys, 32 heads of 128 on 32: 598 us, 6.3
+// TB/s; 8 requests of 32768 to 131072, 32 heads on 8: 390 us, 6.5 TB/s.  One row
+// after 300 keys: 9.4 us, the latency of a few dependent loads.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -423,14 +431,22 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
 }
 
 // ---------------------------------------------------------------------------
-// Many rows (prompts and chunks), bf16: one block per 128 or 256 packed queries
-// of one request and key head (and chunk of the keys where the request has few
-// blocks); waves of 32 queries on v_mfma_f32_32x32x16_bf16, so a K or V
-// fragment read from LDS feeds 32 queries.  64-key tiles of K and V go from
-// memory straight into a ring of LDS stages (global_load_lds, one barrier per
-// tile), two stages of 32 KB with head dim 128 and four of 16 KB with 64: two
-// blocks share a CU.  A wave-wide load takes whole rows of one 16-position run,
-// whose page it looks up as a scalar, a tile ahead of the load.
+// Many rows (prompts and chunks), bf16: one block per 128 packed queries of one
+// request and key head (and chunk of the keys where the request has few blocks);
+// waves of 32 queries on v_mfma_f32_32x32x16_bf16, so a K or V fragment read from
+// LDS feeds 32 queries.  64-key tiles of K and V go from memory straight into two
+// LDS stages by turns (global_load_lds, one barrier per tile).  A wave-wide load
+// takes whole rows of one 16-position run, whose page it looks up as a scalar, a
+// tile ahead of the load.
+// Bound by LDS reads: every wave reads the whole tile for its 32 queries, and with
+// head dim 128 the 8 waves of a CU read 256 KB per tile, 4096 of its 4500 cycles
+// at 64 bytes each; the matrix cores are busy for 40%.  Blocks of 8 waves, which
+// halve the fills but not the reads, gain nothing (587 us for the 585 below, 169
+// for 151 with head dim 64); 64 queries per wave, which would halve the reads, do
+// not fit the registers.  With head dim 64, four stages instead of two keep a third
+// block off the CU (250 us for 240: 8 prompts of 4096, window 1024, 16 heads on 4).
+// 4 chunks of 1900 to 2048 rows after 3000 to 9000, window 4096, 32 heads of 128 on
+// 8: 585 us, 900 TFLOP/s of visible products (a large matrix product: 1370).
 // ---------------------------------------------------------------------------
 typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
@@ -457,38 +473,30 @@ __device__ __forceinline__ int rows_vswz(int r, int c) {
 template <int N>
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14)); }
 
-// LDS stages of 256 DH bytes
-constexpr int rows_stages(int dh, int waves) { return dh == 128 && waves == 4 ? 2 : 4; }
-
-// NW waves: 4 (two blocks share a CU) or 8 (one).
-template <int DH, int NW>
-__device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, int id, bf16* stage0, bf16* stage1, bf16* stage2,
-                                           bf16* stage3) {
+template <int DH>
+__device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, int id, bf16* stage0, bf16* stage1) {
+  constexpr int NW = 4;                  // waves
   constexpr int CH = DH / 8;             // 16-byte chunks per row
   constexpr int RPI = 64 / CH;           // rows per wave-wide load
   constexpr int NI = 64 / (NW * RPI);    // K (and V) loads per wave and tile
   constexpr int KS = DH / 16;            // MFMA steps over the head dims
   constexpr int ND = DH / 32;            // output tiles
-  constexpr int NST = rows_stages(DH, NW);
-  // Stage j: K of a tile t with t mod NST = j, then V of tile t - 1 (a step reads K a tile ahead of V).
+  // Stage j: K of a tile t with t mod 2 = j, then V of tile t - 1 (a step reads K a tile ahead of V).
   // A variable per stage, so that the compiler can tell the one that is read from the one being
   // filled and does not wait for its loads.
   constexpr int TE = 64 * DH;
   auto stage = [&](auto b) -> bf16* {
     if constexpr (b == 0) return stage0;
-    else if constexpr (b == 1) return stage1;
-    else if constexpr (b == 2) return stage2;
-    else return stage3;
+    else return stage1;
   };
   __shared__ int s_poison;
 
-  const int rb = rows_per_block(NW, a.G);
+  const int rb = rows_per_block(a.G);
   Work w;
   int blk;
   {
     w.h = id % a.KH; id /= a.KH;
-    if constexpr (NW == 4) { w.c = id % a.rows_chunks; id /= a.rows_chunks; }
-    else w.c = 0;                         // a request of wide blocks has no need to cut its keys
+    w.c = id % a.rows_chunks; id /= a.rows_chunks;
     blk = id;
   }
   // request p's blocks start at cu[p] / rb + p: at least ceil(m / rb) before the next request's
@@ -504,7 +512,7 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
   // a request's last rows see the most keys: they come first
   const int nb = (m + rb - 1) / rb;
   const int bi = blk - (R0 / rb + w.p);
-  if (bi >= nb || few_rows(VFM_BF16, m, a.G) || row_waves(m, a.G, a.KH) != NW) return;   // block-uniform, as every exit below
+  if (bi >= nb || few_rows(VFM_BF16, m, a.G)) return;   // block-uniform, as every exit below
   const int r0 = (nb - 1 - bi) * rb, nr = min(rb, m - r0);
   const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink);
   if (w.c >= ck.n) return;
@@ -712,7 +720,7 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
 
   // While the weights of tile t are computed (vector ALU), the matrix cores already take the scores
   // of tile t + 1; while they take the products of t, its largest scores are found.  K of tile t + 1
-  // and V of tile t have landed once at most the loads of the NST - 2 later steps are outstanding;
+  // and V of tile t were asked for a step ago, and nothing later has been;
   // the barrier makes every wave's part visible, and frees K of tile t and V of tile t - 1.
   if (t0 < t1) {
     f32x16 sa[2], sb[2];
@@ -720,17 +728,16 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
     auto fill = [&](auto j) { issue(j, t0 + j + 1, std::bool_constant<(j > 0)>{}); };
     fill(std::integral_constant<int, 0>{});
     fill(std::integral_constant<int, 1>{});
-    if constexpr (NST > 2) { fill(std::integral_constant<int, 2>{}); fill(std::integral_constant<int, 3>{}); }
-    wait_loads<(NST - 1) * 2 * NI>();
+    wait_loads<2 * NI>();
     __builtin_amdgcn_s_barrier();
     scores(std::integral_constant<int, 0>{}, sa);
     mask(t0, sa);
     follow(largest(sa));
-    // tile t, t mod NST = j: its scores st, the next one's sn (behind the last tile: of what the stage
+    // tile t, t mod 2 = j: its scores st, the next one's sn (behind the last tile: of what the stage
     // holds, and not used)
     auto step = [&](auto j, int t, f32x16 (&st)[2], f32x16 (&sn)[2]) {
-      constexpr auto jn = std::integral_constant<int, (j + 1) % NST>{};   // holds K of tile t + 1, V of tile t
-      wait_loads<(NST - 2) * 2 * NI>();
+      constexpr auto jn = std::integral_constant<int, 1 - j>{};   // holds K of tile t + 1, V of tile t
+      wait_loads<0>();
       __builtin_amdgcn_s_barrier();
       const int kb = 64 * vis.run(t);
       if (!seen_by_all(j0, j1, kb, kb + 63, a.window, a.n_sink)) {
@@ -745,7 +752,7 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
       scores(jn, sn);
       weights(st, 0, pf);
       weights(st, 1, pf);
-      issue(j, t + NST + 1, std::true_type{});
+      issue(j, t + 3, std::true_type{});
       __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
       for (int s = 0; s < 2 * KS; ++s) {
@@ -777,13 +784,9 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
       follow(mb);
       return true;
     };
-    for (int t = t0;; t += NST) {
+    for (int t = t0;; t += 2) {
       if (!step(std::integral_constant<int, 0>{}, t, sa, sb)) break;
       if (!step(std::integral_constant<int, 1>{}, t + 1, sb, sa)) break;
-      if constexpr (NST > 2) {
-        if (!step(std::integral_constant<int, 2>{}, t + 2, sa, sb)) break;
-        if (!step(std::integral_constant<int, 3>{}, t + 3, sb, sa)) break;
-      }
     }
     wait_loads<0>();                                      // nothing still writes to LDS when the block ends
   }
@@ -814,21 +817,19 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
   }
 }
 
-// rows_blocks blocks of the many-row kind with NW waves (0: none), then, with FEW, those of the few-row
-// kind: a step's single rows run beside its prompts, on the CUs that these leave free.  24 requests of
-// 64 to 2000 positions, 5 of them with up to 250 rows, 16 heads of 64: 31.5 us, as two launches 45.7.
-template <int DH, int NW, bool FEW>
-__global__ __launch_bounds__(NW == 8 ? 512 : 256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_bf16_kernel(
-    Plan pl, PagedAttn a, int rows_blocks) {
-  static_assert(!(NW == 8 && FEW), "a few-row block has 4 waves");
-  constexpr int NST = NW > 0 ? rows_stages(DH, NW) : 1, SE = 128 * DH;
-  __shared__ __attribute__((aligned(16))) bf16 stage0[SE], stage1[NST > 1 ? SE : 8], stage2[NST > 2 ? SE : 8], stage3[NST > 3 ? SE : 8];
+// rows_blocks blocks of the many-row kind (ROWS), then, with FEW, those of the few-row kind: a step's
+// single rows run beside its prompts, on the CUs that these leave free.  24 requests of 64 to 2000
+// positions, 5 of them with up to 250 rows, 16 heads of 64: 31.5 us, as two launches 45.7.
+template <int DH, bool ROWS, bool FEW>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_bf16_kernel(Plan pl, PagedAttn a,
+                                                                                                   int rows_blocks) {
+  __shared__ __attribute__((aligned(16))) bf16 stage0[128 * DH], stage1[ROWS ? 128 * DH : 8];
   if constexpr (FEW)
     if ((int)blockIdx.x >= rows_blocks) {
       few_block<DH>(pl, a, (int)blockIdx.x - rows_blocks, reinterpret_cast<char*>(stage0));
       return;
     }
-  if constexpr (NW > 0) rows_block<DH, NW>(pl, a, blockIdx.x, stage0, stage1, stage2, stage3);
+  if constexpr (ROWS) rows_block<DH>(pl, a, blockIdx.x, stage0, stage1);
 }
 
 // ---------------------------------------------------------------------------
@@ -839,6 +840,10 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256) __attribute__((amdgpu_waves_pe
 // products as it lies (MFMA j takes keys 4 g + j), and a lane that loads dims
 // 4 x .. 4 x + 3 of its key's V row gives MFMA c row x of tile c = head dim
 // 4 x + c, which leaves a lane with 16 consecutive head dims of its query.
+// Every K and V element is read once per 16 queries, from L2 for the later ones.
+// 64 rows after 2000 keys, 16 heads of 64: 199 us, 5.3 TB/s.  8 chunks of 512 rows
+// after 1000: 269 us, 79 TFLOP/s (a large fp32 matrix product: 154): bound by the
+// operand loads, which no other block's queries share through LDS.
 // ---------------------------------------------------------------------------
 template <int DH>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attn_f32_kernel(Plan pl, PagedAttn a) {
@@ -997,6 +1002,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
 // ---------------------------------------------------------------------------
 // Joins the chunks' partial sums of rows whose keys were cut: a wave per row and
 // head, o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c, chunks in order.
+// Bound by its launch: 5 to 7 us for 256 rows of 32 heads in up to 8 chunks.
 // ---------------------------------------------------------------------------
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void attn_join_kernel(Plan pl, PagedAttn a) {
@@ -1069,7 +1075,7 @@ hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_d
 }
 
 hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, bool few_, bool rows_,
-                                  bool wide, bool split, hipStream_t s) {
+                                  bool split, hipStream_t s) {
   int pi = prof_begin(VFM_PROF_ATTN, s);
   const unsigned few = (unsigned)a.KH * a.few_chunks, rows = (unsigned)a.KH * a.rows_chunks;
 #define BY_DH(K_, G_) \
@@ -1077,18 +1083,15 @@ hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const
        else hipLaunchKernelGGL((K_<128>), G_, dim3(256), 0, s, pl, a); } while (0)
   if (dtype == VFM_BF16) {
     const unsigned nf = few_ ? few * a.qtiles * pl.n_req : 0;
-    const unsigned nr = rows_ ? rows * (pl.T / rows_per_block(4, a.G) + pl.n_req) : 0;
-    const unsigned nw = wide ? (unsigned)a.KH * (pl.T / rows_per_block(8, a.G) + pl.n_req) : 0;
-#define BF16(W_, F_, N_, R_)                                                                                      \
+    const unsigned nr = rows_ ? rows * (pl.T / rows_per_block(a.G) + pl.n_req) : 0;
+#define BF16(R_, F_)                                                                                              \
   do {                                                                                                            \
-    const dim3 grid(N_), block(W_ == 8 ? 512 : 256);                                                            \
-    if (head_dim == 64) hipLaunchKernelGGL((attn_bf16_kernel<64, W_, F_>), grid, block, 0, s, pl, a, (int)(R_));  \
-    else hipLaunchKernelGGL((attn_bf16_kernel<128, W_, F_>), grid, block, 0, s, pl, a, (int)(R_));                \
+    if (head_dim == 64) hipLaunchKernelGGL((attn_bf16_kernel<64, R_, F_>), dim3(nr + nf), dim3(256), 0, s, pl, a, (int)nr);  \
+    else hipLaunchKernelGGL((attn_bf16_kernel<128, R_, F_>), dim3(nr + nf), dim3(256), 0, s, pl, a, (int)nr);     \
   } while (0)
-    if (wide) BF16(8, false, nw, nw);
-    if (rows_ && few_) BF16(4, true, nr + nf, nr);
-    else if (rows_) BF16(4, false, nr, nr);
-    else if (few_) BF16(0, true, nf, 0);
+    if (rows_ && few_) BF16(true, true);
+    else if (rows_) BF16(true, false);
+    else BF16(false, true);
 #undef BF16
   } else {
     BY_DH(attn_f32_kernel, dim3(few * (unsigned)((int64_t)pl.T * a.G / 16 + pl.n_req)));

@@ -17,6 +17,13 @@
 // only one that is put in order, and where all bins up to it hold few outputs
 // (top-k), nothing else is looked at again.  One block per request: the row is
 // read once where it fits registers or LDS (up to 32768 outputs).
+//
+// Bound by the weights' fp64 work, 19 instructions each on the one CU that a row
+// has, and by the latency of the block's steps; bytes would allow 7 us for 256 rows
+// of 32000.  Measured, 256 rows of 32000: greedy 9.2 us, no filter 17.5, top-k 40
+// 14.5, top-k 199 26.6, top-k 1000 30.4, top-p 0.9 29, with min-p 35.  48 rows of
+// 100003 (48 of 256 CUs): no filter 31.5, top-p 0.9 58.5.  256 rows of 700: 2.8 to 8.
+// Several blocks per row would need a second launch and scratch memory from the caller.
 #include <type_traits>
 
 #include "decode_internal.h"
