@@ -229,7 +229,10 @@ def loop_bench(args):
     requests with prompts of U[64, 512] tokens and U[32, 128] new tokens each,
     at most 256 running sequences, pages of 64 slots, prompts admitted FIFO
     (or by BFQ with --admission bfq) up to 8192 tokens per step.  Timed from the first step to the last request
-    finishing, host scheduling and the per-step token read-back included."""
+    finishing, host scheduling and the per-step token read-back included.
+    --window W: every row sees the last W positions and the first --sinks (a
+    ring of pages per sequence); --draw: tokens drawn at temperature 0.8 from
+    the 40 largest outputs, of those from 0.95 of the weight."""
     import torch
     from paper_2606_09643_amd import binding as B
     from paper_2606_09643_amd import runner as R
@@ -253,9 +256,10 @@ def loop_bench(args):
             bfq = B.BFQ(np.ones(w.n_tasks), [0.0] + [1.0 + 0.25 * b for b in range(1, 17)], b_max=16)
         cb = R.ContinuousBatcher(model, emb, page_size=page, n_pages=n_pages, max_seqs=max_seqs,
                                  max_step_tokens=8192, max_pages=(512 + 128 + page - 1) // page, bfq=bfq,
-                                 token_time=1.0 / max_seqs)
+                                 token_time=1.0 / max_seqs, window=args.window or None, n_sink=args.sinks)
         for i in range(n):
-            cb.submit(i, int(tasks[i]), rng.integers(0, w.vocab, size=int(plen[i])), int(new[i]))
+            cb.submit(i, int(tasks[i]), rng.integers(0, w.vocab, size=int(plen[i])), int(new[i]),
+                      sampling=R.SamplingParams(0.8, top_k=40, top_p=0.95, seed=i) if args.draw else None)
         return cb
     warm = make()                                      # warm-up run (kernels, allocator caches)
     for _ in range(3):
@@ -276,6 +280,10 @@ def loop_bench(args):
                       "prompt_tokens": int(plen.sum()), "generated_tokens": gen, "max_running": max_seqs,
                       "page_size": page, "max_step_tokens": 8192, "admission": args.admission},
            "seconds": sec}
+    if args.window:
+        out["config"].update(window=args.window, sinks=args.sinks)
+    if args.draw:
+        out["config"]["draw"] = "temperature 0.8, top-k 40, top-p 0.95"
     print(json.dumps(out), flush=True)
 
 
@@ -348,6 +356,9 @@ def main():
                     help="run the continuous-batching loop over this many requests instead of one step")
     ap.add_argument("--admission", choices=("fifo", "bfq"), default="fifo",
                     help="--loop: admit prompts FIFO or by BFQ (16-request batches, decode tokens charged)")
+    ap.add_argument("--window", type=int, default=0, help="--loop: attend to this many last positions (0: all)")
+    ap.add_argument("--sinks", type=int, default=0, help="--loop --window: and to this many first ones")
+    ap.add_argument("--draw", action="store_true", help="--loop: draw the tokens instead of taking the largest output")
     ap.add_argument("--paged", type=int, default=0,
                     help="decode workloads: read the KV cache through pages of this many slots "
                          "(random page order) instead of the contiguous cache")

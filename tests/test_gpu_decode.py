@@ -187,8 +187,8 @@ def test_attention_keys_that_only_some_rows_see(dtype, H, KH, dh, lens, ctx, win
     (32, 32, 64, 64, 0, 0, [2050], [0]), (64, 16, 128, 16, 90, 5, [1100, 1, 40], [333, 50, 0]),
     (56, 8, 64, 32, 300, 0, [1300], [70])])
 def test_attention_prompts_of_wide_blocks(H, KH, dh, page, window, sinks, lens, ctx):
-    """Prompts whose blocks of 256 queries fill the chip: rows at the blocks' and
-    tiles' borders and a spread of others against the 64-bit form."""
+    """Prompts whose blocks fill the chip: rows at the blocks' and tiles' borders
+    and a spread of others against the 64-bit form."""
     assert KH * -(-lens[0] * (H // KH) // 256) >= 256
     c = Cache(lens, ctx, KH, dh, page, window, sinks, "bf16", seed=21)
     rng = np.random.default_rng(12)
