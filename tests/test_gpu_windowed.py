@@ -380,3 +380,86 @@ def test_append_attend_sample_in_one_step():
         torch.cuda.synchronize()
         for t, want in zip((out, ids, logp, kv.k, kv.v), first):
             assert torch.equal(t, want)
+
+
+def test_windowed_layer_replayed_from_a_graph():
+    """A captured layer replays to the eager bits, with eager work on the same stream between the replays."""
+    w = _decoder("bf16", 64)
+    lens, ctx, task = np.array([1, 30, 1], np.int32), np.array([80, 10, 300], np.int32), np.array([0, 2, 1], np.int32)
+    window, sinks, page = 40, 2, 16
+    model = R.Model(w, n_layers=1, b_std=0.1)
+    cache = _Cache(w, lens, ctx, page, window, sinks, seed=3)
+    cfg = R.cfg_for(w)
+    cfg.attn = B.VFM_ATTN_MIXED
+    pb = B.Batch(task, lens, w.n_tasks, ctx_len=ctx)
+    x0 = torch.from_numpy(np.random.default_rng(8).standard_normal((pb.T, w.d)).astype(np.float32)).cuda()
+    ws = torch.empty(B.vfm_workspace_size_windowed(cfg, pb.c, model.lora_c(0), window, sinks), dtype=torch.uint8, device="cuda")
+    kv = B.PagedKV(cache.k, cache.v, page, cache.table)
+    x = x0.clone()
+
+    def layer():
+        B.vfm_layer_forward_windowed(cfg, model.c_layers[0], model.lora_c(0), pb.c, x, kv, window, sinks, ws)
+    log("windowed layer in a graph")
+    layer()
+    torch.cuda.synchronize()
+    want, k1, v1 = x.clone(), cache.k.clone(), cache.v.clone()
+    assert torch.isfinite(want).all()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        layer()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer()
+    for _ in range(3):
+        x.copy_(x0)
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(x, want)
+        assert torch.equal(cache.k.view(torch.int16), k1.view(torch.int16))
+        assert torch.equal(cache.v.view(torch.int16), v1.view(torch.int16))
+        (x0 @ x0.T).sum().item()
+
+
+@pytest.mark.parametrize("dtype,lens", [("bf16", [1, 1]), ("bf16", [1, 70]), ("f32", [1, 9])])
+def test_pages_past_32_bit_offsets_and_shared_by_requests(dtype, lens):
+    """A pool whose later elements lie past 2^31 (bytes past 2^32): the step's pages are the pool's last ones, and both
+    requests' tables begin with the same pages (a prefix that they share)."""
+    code, td, eps = (B.VFM_BF16, torch.bfloat16, 2.0 ** -8) if dtype == "bf16" else (B.VFM_F32, torch.float32, 2.0 ** -24)
+    H, KH, dh, page = 4, 2, 128, 64
+    n_pages = (1 << 18) + 64                                   # 2^24 slots and more of 128 per head
+    lens, ctx, task = np.array(lens, np.int32), np.array([150, 200], np.int32), np.zeros(2, np.int32)
+    last = n_pages - 1
+    table = np.array([[last, last - 3, last - 1, 0, 0], [last, last - 3, last - 2, last - 5, last - 4]], np.int32)
+    kp, vp = [torch.empty(KH, n_pages * page, dh, dtype=td, device="cuda") for _ in range(2)]
+    rng = np.random.default_rng(17)
+    for t in (kp, vp):                                          # the last pages alone are written
+        t[:, -8 * page:] = torch.from_numpy(rng.standard_normal((KH, 8 * page, dh))).to(td).cuda()
+    attn = B.make_attn(code, H, KH, dh)
+    pb = B.Batch(task, lens, 1, ctx_len=ctx)
+    qkv = torch.from_numpy(rng.standard_normal((pb.T, (H + 2 * KH) * dh))).to(td).cuda()
+    kv = B.PagedKV(kp, vp, page, table)
+    q, out = [torch.empty(pb.T, H * dh, dtype=td, device="cuda") for _ in range(2)]
+    ws = torch.empty(max(1, B.vfm_attention_workspace(attn, pb.c)), dtype=torch.uint8, device="cuda")
+    log(f"far pages {dtype} {lens}")
+    B.vfm_kv_append(attn, pb.c, qkv, q, kv)
+    B.vfm_attention_paged(attn, pb.c, q, kv, out, ws)
+    torch.cuda.synchronize()
+    rows, o = np64(qkv), np64(out)
+    assert np.array_equal(np64(q), rows[:, :H * dh])            # no rotation: as they were
+    at = 0
+    for i, (m, c) in enumerate(zip(lens, ctx)):
+        pos = np.arange(int(c + m))
+        slots = torch.from_numpy(table[i, pos // page].astype(np.int64) * page + pos % page).cuda()
+        k, v = np64(kp[:, slots]).transpose(1, 0, 2), np64(vp[:, slots]).transpose(1, 0, 2)
+        r = rows[at:at + m].reshape(m, H + 2 * KH, dh)
+        assert np.array_equal(k[c:], r[:, H:H + KH]) and np.array_equal(v[c:], r[:, H + KH:])
+        ref, a, n = D.attention(r[:, :H], k, v, int(c), 0, 0, dh ** -0.5)
+        dot = float(np.abs(r[:, :H]).max() * np.abs(k).max()) * dh * dh ** -0.5
+        lim = ((eps if dtype == "bf16" else 0.0) + (n[:, None, None] + 16) * 2.0 ** -24) * (a + np.abs(ref)) \
+            + a * 2 * ((dh + 2) * 2.0 ** -24 * dot + 2.0 ** -22)
+        assert np.all(np.abs(o[at:at + m].reshape(m, H, dh) - ref) <= lim)
+        at += m
