@@ -388,6 +388,19 @@ def test_sample_filters(spread, size):
     _check_draw(rows, *[list(x) for x in zip(*par)])
 
 
+@pytest.mark.parametrize("spread", [0.3, 2.5])
+def test_sample_middle_k(spread):
+    """A top-k around the sizes of the lists that are put in order, with the other filters tighter or looser."""
+    rng = np.random.default_rng(int(spread * 10))
+    rows, par = [], []
+    for s in (60, 300, 1000, 5000, 40000):
+        for k in (55, 56, 57, 64, 100, 199, 256, 257, 513):
+            for p, m in ((1.0, 0.0), (0.9, 0.0), (0.999, 0.02), (0.4, 0.02), (1.0, 0.3)):
+                rows.append((rng.standard_normal(s) * spread).astype(np.float32))
+                par.append((1.0, k, p, m, rng.random()))
+    _check_draw(rows, *[list(x) for x in zip(*par)])
+
+
 def test_sample_ties():
     """Equal outputs, few or thousands: the lowest indexes are kept first."""
     rng = np.random.default_rng(0)
