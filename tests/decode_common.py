@@ -29,6 +29,13 @@ def attention(q, k, v, ctx, window, n_sink, scale):
     return o, a, n
 
 
+def score_sizes(q, k, scale):
+    """[m, H]: the largest sum |q k| scale over the keys, the size of the terms of a row's scores."""
+    G = q.shape[1] // k.shape[1]
+    s = np.matmul(np.abs(q).transpose(1, 0, 2), np.abs(np.repeat(k, G, 1)).transpose(1, 2, 0))
+    return s.max(-1).T * scale
+
+
 def rotate(x, pos, theta):
     """Rotate-half of x [m, heads, dh] by positions pos, base theta (0: as it is)."""
     if theta == 0:

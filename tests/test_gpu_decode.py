@@ -89,7 +89,7 @@ def _check(c, got, q, window, sinks, dtype, scale):
     for i, o in got.items():
         ref, a, n = D.attention(q[i], c.k[i], c.v[i], int(c.ctx[i]), window, sinks, scale)
         dh = ref.shape[-1]
-        dot = float(np.abs(q[i]).max() * np.abs(c.k[i]).max()) * dh * scale    # more than any sum |q k|
+        dot = D.score_sizes(q[i], c.k[i], scale)[:, :, None]
         nn = n[:, None, None]
         tol = (u if dtype == "bf16" else 0.0) * (a + np.abs(ref)) + (nn + 16) * 2.0 ** -24 * (a + np.abs(ref)) \
             + a * 2 * ((dh + 2) * 2.0 ** -24 * dot + 2.0 ** -22)

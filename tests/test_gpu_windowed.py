@@ -350,7 +350,7 @@ def test_append_attend_sample_in_one_step():
             ka = np.concatenate([at(kp, old), at(kv.k.cpu(), pos)])
             va = np.concatenate([at(vp, old), r[:, H + KH:]])
             ref, a, n = D.attention(q_got, ka, va, c, window, sinks, dh ** -0.5)
-            dot = float(np.abs(q_got).max() * np.abs(ka).max()) * dh * dh ** -0.5
+            dot = D.score_sizes(q_got, ka, dh ** -0.5)[:, :, None]
             lim = (eps + (n[:, None, None] + 16) * 2.0 ** -24) * (a + np.abs(ref)) \
                 + a * 2 * ((dh + 2) * 2.0 ** -24 * dot + 2.0 ** -22)
             assert np.all(np.abs(o[cu[i]:cu[i + 1]].reshape(m, H, dh) - ref) <= lim)
@@ -458,7 +458,7 @@ def test_pages_past_32_bit_offsets_and_shared_by_requests(dtype, lens):
         r = rows[at:at + m].reshape(m, H + 2 * KH, dh)
         assert np.array_equal(k[c:], r[:, H:H + KH]) and np.array_equal(v[c:], r[:, H + KH:])
         ref, a, n = D.attention(r[:, :H], k, v, int(c), 0, 0, dh ** -0.5)
-        dot = float(np.abs(r[:, :H]).max() * np.abs(k).max()) * dh * dh ** -0.5
+        dot = D.score_sizes(r[:, :H], k, dh ** -0.5)[:, :, None]
         lim = ((eps if dtype == "bf16" else 0.0) + (n[:, None, None] + 16) * 2.0 ** -24) * (a + np.abs(ref)) \
             + a * 2 * ((dh + 2) * 2.0 ** -24 * dot + 2.0 ** -22)
         assert np.all(np.abs(o[at:at + m].reshape(m, H, dh) - ref) <= lim)
