@@ -204,10 +204,10 @@ def _ptr(t) -> int | None:
     return int(t)
 
 
-def _stream(stream) -> int:
+def _stream(stream, device=None) -> int:
     if stream is None:
         # the handle alone: building torch.cuda.current_stream()'s object takes 2.6 us, as long as a launch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device.index)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -535,7 +535,8 @@ def vfm_kv_append(attn, batch, qkv, q_out, kv, stream=None):
     hd, T, td, dev = attn.head_dim, batch.plan_host[2], _TORCH_DTYPE.get(attn.dtype), qkv.device
     p, ld = _rows(qkv, "qkv", td, T, (attn.n_heads + 2 * attn.n_kv_heads) * hd, dev)
     q, c = _operand(q_out, "q_out", td, T * attn.n_heads * hd, dev), _cache(kv, attn, td, _same_device(dev))
-    st = _lib_handle().vfm_kv_append(C.byref(attn), C.byref(batch), p, ld, q, C.byref(c), _stream(stream))
+    st = _lib_handle().vfm_kv_append(C.byref(attn), C.byref(batch), p, ld, q, C.byref(c),
+                                     _stream(stream, dev))
     _check(st, "vfm_kv_append")
 
 
@@ -558,7 +559,7 @@ def vfm_attention_paged(attn, batch, q, kv, out, workspace=None, stream=None):
             raise ValueError(f"workspace: a dense tensor on {dev} is expected")
         ws, nb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     st = _lib_handle().vfm_attention_paged(C.byref(attn), C.byref(batch), pq, ldq, C.byref(c), po, ldo, ws, nb,
-                                           _stream(stream))
+                                           _stream(stream, dev))
     _check(st, "vfm_attention_paged")
 
 
@@ -611,7 +612,7 @@ def vfm_sample_tokens(batch, out, sampling, u, ids, logprob=None, stream=None):
                                          C.byref(sampling.c), _operand(u, "u", torch.float32, n, dev),
                                          _operand(ids, "ids", torch.int32, n, dev),
                                          _operand(logprob, "logprob", torch.float32, n, dev)
-                                         if logprob is not None else None, _stream(stream))
+                                         if logprob is not None else None, _stream(stream, dev))
     _check(st, "vfm_sample_tokens")
 
 

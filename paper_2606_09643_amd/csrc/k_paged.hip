@@ -58,6 +58,24 @@ __device__ __forceinline__ float sum_x16(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// v combined over the 16 lanes of a row (rotations within it), in every lane
+template <int CTRL>
+__device__ __forceinline__ float rotated(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float max_row(float v) {
+  v = fmaxf(v, rotated<0x128>(v));
+  v = fmaxf(v, rotated<0x124>(v));
+  v = fmaxf(v, rotated<0x122>(v));
+  return fmaxf(v, rotated<0x121>(v));
+}
+__device__ __forceinline__ float sum_row(float v) {
+  v += rotated<0x128>(v);
+  v += rotated<0x124>(v);
+  v += rotated<0x122>(v);
+  return v + rotated<0x121>(v);
+}
+
 // A wave's own LDS accesses complete in order; only the compiler must keep them.
 __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -228,6 +246,7 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
     w.p = id / a.qtiles;
   }
   const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
+  const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide
   if (!few_rows(VFM_BF16, m, a.G)) return;              // block-uniform, as every exit below
   const int qn = m * a.G;
   if (w.qt * 16 >= qn) return;
@@ -250,7 +269,7 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + 32 * s);
   }
-  const page_row prow = row_of(a.kp, uniform(pl.order[w.p]));
+  const page_row prow = row_of(a.kp, request);
   const int lp = a.kp.log2_page;
   const bf16* kh = (const bf16*)a.k + (int64_t)w.h * a.slots * DH;
   const bf16* vh = (const bf16*)a.v + (int64_t)w.h * a.slots * DH;
@@ -509,6 +528,7 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
     w.p = lo;
   }
   const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
+  const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide
   // a request's last rows see the most keys: they come first
   const int nb = (m + rb - 1) / rb;
   const int bi = blk - (R0 / rb + w.p);
@@ -536,7 +556,7 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s);
   }
-  const page_row prow = row_of(a.kp, uniform(pl.order[w.p]));
+  const page_row prow = row_of(a.kp, request);
   const int lp = a.kp.log2_page;
   const bf16* kh = (const bf16*)a.k + (int64_t)w.h * a.slots * DH;
   const bf16* vh = (const bf16*)a.v + (int64_t)w.h * a.slots * DH;
@@ -866,6 +886,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
     w.qt = id - (int)((int64_t)uniform(pl.cu_seqlens[lo]) * a.G / 16 + lo);
   }
   const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
+  const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide
   const int qn = m * a.G;
   if (w.qt * 16 >= qn) return;                            // block-uniform, as every exit below
   const Chunks ck = request_chunks(VFM_F32, m, ctx, a.G, a.KH, a.window, a.n_sink);
@@ -881,7 +902,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
   const int t0 = w.c * rpc, t1 = min(t0 + rpc, vis.n);
   int head;
   const int64_t row = out_row(a, R0, w.h, qi, head);
-  const page_row prow = row_of(a.kp, uniform(pl.order[w.p]));
+  const page_row prow = row_of(a.kp, request);
   const int lp = a.kp.log2_page;
   const float* kh = (const float*)a.k + (int64_t)w.h * a.slots * DH;
   const float* vh = (const float*)a.v + (int64_t)w.h * a.slots * DH;
@@ -1009,19 +1030,18 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Plan pl, PagedAttn a) {
   constexpr int DT = std::is_same<T, bf16>::value ? VFM_BF16 : VFM_F32;
   constexpr int E = DH / 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
-  if (id >= (int64_t)pl.T * a.H) return;
-  const int r = (int)(id / a.H), head = (int)(id - (int64_t)r * a.H);
-  const int p = pl.row_req[r];
-  const int m = pl.cu_seqlens[p + 1] - pl.cu_seqlens[p];
-  const int n = request_chunks(DT, m, pl.ctx[p], a.G, a.KH, a.window, a.n_sink).n;
+  const int id = (int)blockIdx.x * 4 + wave;              // the launch has fewer than 2^26
+  if (id >= pl.T * a.H) return;
+  const int r = id / a.H, head = id - r * a.H;
+  const int p = uniform(pl.row_req[r]);
+  const int m = uniform(pl.cu_seqlens[p + 1]) - uniform(pl.cu_seqlens[p]), ctx = uniform(pl.ctx[p]);
+  const int n = request_chunks(DT, m, ctx, a.G, a.KH, a.window, a.n_sink).n;
   if (n <= 1) return;
-  const float2* ml = a.rec_ml + id * a.nchunk;
-  const float* ro = a.rec_o + id * a.nchunk * DH + E * lane;
+  const float2* ml = a.rec_ml + (int64_t)id * a.nchunk;
+  const float* ro = a.rec_o + (int64_t)id * a.nchunk * DH + E * lane;
   float M = NEG_BIG;
   for (int c = lane; c < n; c += 64) M = fmaxf(M, ml[c].x);
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) M = fmaxf(M, __shfl_xor(M, s, 64));
+  M = max_x32(max_x16(max_row(M)));
   float L = 0.f, acc[E] = {};
   for (int c0 = 0; c0 < n; c0 += 64) {
     float wt = 0.f;
@@ -1040,19 +1060,18 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Plan pl, PagedAttn a) {
         for (int e = 0; e < E; ++e) v[j][e] = ro[(int64_t)(c0 + c + j) * DH + e];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float wc = __shfl(wt, c + j, 64);
+        const float wc = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wt), c + j));
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = fmaf(wc, v[j][e], acc[e]);
       }
     }
     for (; c < cn; ++c) {
-      const float wc = __shfl(wt, c, 64);
+      const float wc = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wt), c));
 #pragma unroll
       for (int e = 0; e < E; ++e) acc[e] = fmaf(wc, ro[(int64_t)(c0 + c) * DH + e], acc[e]);
     }
   }
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) L += __shfl_xor(L, s, 64);
+  L = sum_x32(sum_x16(sum_row(L)));
   T* dst = (T*)a.out + (int64_t)r * a.ldo + head * DH + E * lane;
 #pragma unroll
   for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] / L);
