@@ -257,21 +257,24 @@ int check_pages(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, const
 struct AttnPlan {
   int few_chunks, rows_chunks, qtiles;
   bool few, rows;            // the batch has requests of the few-row and of the many-row kind
+  bool one;                  // no few-row request has more than 4 tiles of keys
   int64_t bytes;             // workspace
   int nchunk() const { return std::max(few_chunks, rows_chunks); }
 };
 
 int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, AttnPlan* out) {
-  AttnPlan ap = {1, 1, 1, false, false, 0};
+  AttnPlan ap = {1, 1, 1, false, false, true, 0};
   const int G = a.n_heads / a.n_kv_heads;
   const PlanOffsets po = plan_offsets(pl.n_req, pl.n_tasks, pl.T);
   const int32_t *ctx = host_arr(batch, po.ctx), *cu = host_arr(batch, po.cu_seqlens);
   for (int p = 0; p < pl.n_req; ++p) {
     const int m = cu[p + 1] - cu[p];
     if (ctx[p] < 0 || (int64_t)ctx[p] + m > kMaxPos) return VFM_ERR_SHAPE;
-    const int n = request_chunks(a.dtype, m, ctx[p], G, a.n_kv_heads, a.window, a.n_sink).n;
+    const Chunks ck = request_chunks(a.dtype, m, ctx[p], G, a.n_kv_heads, a.window, a.n_sink);
+    const int n = ck.n;
     if (few_rows(a.dtype, m, G)) {
       ap.few = true;
+      ap.one = ap.one && n * ck.tiles <= 4;
       ap.few_chunks = std::max(ap.few_chunks, n);
       if (a.dtype == VFM_BF16) ap.qtiles = std::max(ap.qtiles, few_qtiles(m, G));
     } else {
@@ -309,7 +312,7 @@ hipError_t run_attention(const vfm_attn& a, const Plan& pl, const AttnPlan& ap, 
     p.rec_o = (float*)ws;
     p.rec_ml = (float2*)(ws + align_up((size_t)pl.T * p.H * p.nchunk * a.head_dim * 4));
   }
-  return launch_attention_paged(a.dtype, a.head_dim, pl, p, ap.few, ap.rows, p.nchunk > 1, s);
+  return launch_attention_paged(a.dtype, a.head_dim, pl, p, ap.few, ap.rows, ap.one, p.nchunk > 1, s);
 }
 
 vfm_attn attn_of_layer(const vfm_cfg& c, int32_t window, int32_t n_sink) {

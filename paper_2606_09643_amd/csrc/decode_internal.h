@@ -89,10 +89,10 @@ hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_d
                             int64_t ld, void* q_out, int64_t ldq, void* k, void* v, int64_t slots, const KvPages& kp,
                             hipStream_t s);
 
-// few, rows: the batch has requests of the few-row and of the many-row kind.  split: some request has more than
-// one chunk.
+// few, rows: the batch has requests of the few-row and of the many-row kind; one: no few-row request has more than a
+// tile per wave.  split: some request has more than one chunk.
 hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, bool few, bool rows,
-                                  bool split, hipStream_t s);
+                                  bool one, bool split, hipStream_t s);
 
 // max_out: the batch's longest row of head outputs.
 hipError_t launch_sample(const Plan& pl, const float* out, const vfm_sampling& sp, const float* u, int32_t* ids,

@@ -228,8 +228,8 @@ __device__ __forceinline__ int few_vswz(int r) {
   return DH == 128 ? ((r & 3) | (((r >> 3) & 1) << 2)) : (((r >> 1) & 1) | (((r >> 3) & 1) << 1));
 }
 
-// smem: 256 DH bytes, V tiles, then the waves' outputs
-template <int DH>
+// smem: 256 DH bytes, V tiles, then the waves' outputs.  ONE: no request has more than a tile per wave.
+template <int DH, bool ONE>
 __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, int id, char* smem) {
   constexpr int LPR = DH / 8;          // lanes per K / V row (16 bytes each)
   constexpr int RPI = 64 / LPR;        // rows per wave-wide load
@@ -397,8 +397,9 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
   if (t < t1) {
     look_up(t);
     load(0);
-    if (t + 4 < t1) look_up(t + 4);
-    for (;;) {
+    if constexpr (ONE) compute(0, t);
+    else if (t + 4 < t1) look_up(t + 4);
+    for (; !ONE;) {
       if (t + 4 < t1) { load(1); if (t + 8 < t1) look_up(t + 8); }
       compute(0, t);
       t += 4;
@@ -840,13 +841,16 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
 // rows_blocks blocks of the many-row kind (ROWS), then, with FEW, those of the few-row kind: a step's
 // single rows run beside its prompts, on the CUs that these leave free.  24 requests of 64 to 2000
 // positions, 5 of them with up to 250 rows, 16 heads of 64: 31.5 us, as two launches 45.7.
-template <int DH, bool ROWS, bool FEW>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_bf16_kernel(Plan pl, PagedAttn a,
-                                                                                                   int rows_blocks) {
+// ONE (no rows, at most 128 keys per few-row request): with one tile per wave the blocks' start is what
+// counts, and without registers for a second tile 4 blocks share a CU instead of 2.  256 rows of 70 to 120
+// keys, 32 heads of 128: 76 us, else 108; of 30 to 60 keys: 60 and 80; one row of 100 keys: 7.5 and 7.4.
+template <int DH, bool ROWS, bool FEW, bool ONE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ONE ? 4 : 2, ONE ? 4 : 2))) void attn_bf16_kernel(
+    Plan pl, PagedAttn a, int rows_blocks) {
   __shared__ __attribute__((aligned(16))) bf16 stage0[128 * DH], stage1[ROWS ? 128 * DH : 8];
   if constexpr (FEW)
     if ((int)blockIdx.x >= rows_blocks) {
-      few_block<DH>(pl, a, (int)blockIdx.x - rows_blocks, reinterpret_cast<char*>(stage0));
+      few_block<DH, ONE>(pl, a, (int)blockIdx.x - rows_blocks, reinterpret_cast<char*>(stage0));
       return;
     }
   if constexpr (ROWS) rows_block<DH>(pl, a, blockIdx.x, stage0, stage1);
@@ -1094,7 +1098,7 @@ hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_d
 }
 
 hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, bool few_, bool rows_,
-                                  bool split, hipStream_t s) {
+                                  bool one, bool split, hipStream_t s) {
   int pi = prof_begin(VFM_PROF_ATTN, s);
   const unsigned few = (unsigned)a.KH * a.few_chunks, rows = (unsigned)a.KH * a.rows_chunks;
 #define BY_DH(K_, G_) \
@@ -1103,14 +1107,15 @@ hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const
   if (dtype == VFM_BF16) {
     const unsigned nf = few_ ? few * a.qtiles * pl.n_req : 0;
     const unsigned nr = rows_ ? rows * (pl.T / rows_per_block(a.G) + pl.n_req) : 0;
-#define BF16(R_, F_)                                                                                              \
+#define BF16(R_, F_, O_)                                                                                              \
   do {                                                                                                            \
-    if (head_dim == 64) hipLaunchKernelGGL((attn_bf16_kernel<64, R_, F_>), dim3(nr + nf), dim3(256), 0, s, pl, a, (int)nr);  \
-    else hipLaunchKernelGGL((attn_bf16_kernel<128, R_, F_>), dim3(nr + nf), dim3(256), 0, s, pl, a, (int)nr);     \
+    if (head_dim == 64) hipLaunchKernelGGL((attn_bf16_kernel<64, R_, F_, O_>), dim3(nr + nf), dim3(256), 0, s, pl, a, (int)nr);  \
+    else hipLaunchKernelGGL((attn_bf16_kernel<128, R_, F_, O_>), dim3(nr + nf), dim3(256), 0, s, pl, a, (int)nr);     \
   } while (0)
-    if (rows_ && few_) BF16(true, true);
-    else if (rows_) BF16(true, false);
-    else BF16(false, true);
+    if (rows_ && few_) BF16(true, true, false);
+    else if (rows_) BF16(true, false, false);
+    else if (one) BF16(false, true, true);
+    else BF16(false, true, false);
 #undef BF16
   } else {
     BY_DH(attn_f32_kernel, dim3(few * (unsigned)((int64_t)pl.T * a.G / 16 + pl.n_req)));
