@@ -210,8 +210,7 @@ __device__ __forceinline__ int64_t out_row(const PagedAttn& a, int R0, int h, in
 // go straight to registers (lane: one key's row, 16 bytes per MFMA step), V
 // through a wave-private LDS tile that the transposing LDS read turns into the
 // V^T operand; a tile's loads are issued while the tile before is computed, which
-// takes half the registers: with one tile at a time and 3 waves per SIMD instead of
-// 2 the compiler spills, and a step takes twice as long.
+// takes half the registers (see SINGLE below for where it does not pay).
 // 256 requests with up to 1028 visible keys, 32 heads of 128 on 32: 598 us, 6.3
 // TB/s; 8 requests of 32768 to 131072, 32 heads on 8: 390 us, 6.5 TB/s.  One row
 // after 300 keys: 9.4 us, the latency of a few dependent loads.
@@ -228,8 +227,9 @@ __device__ __forceinline__ int few_vswz(int r) {
   return DH == 128 ? ((r & 3) | (((r >> 3) & 1) << 2)) : (((r >> 1) & 1) | (((r >> 3) & 1) << 1));
 }
 
-// smem: 256 DH bytes, V tiles, then the waves' outputs.  ONE: no request has more than a tile per wave.
-template <int DH, bool ONE>
+// smem: 256 DH bytes, V tiles, then the waves' outputs.  SINGLE: one tile at a time in registers, with head dim
+// 128 the wave's only one.
+template <int DH, bool SINGLE>
 __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, int id, char* smem) {
   constexpr int LPR = DH / 8;          // lanes per K / V row (16 bytes each)
   constexpr int RPI = 64 / LPR;        // rows per wave-wide load
@@ -391,23 +391,33 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
     }
   };
 
-  // tiles t0 + wave, + 4, ...; a tile's loads are in flight while the one
-  // before is computed, its page lookups a tile before that
+  // tiles t0 + wave, + 4, ...: one at a time, its page lookups a tile ahead, or (not SINGLE) a tile's loads
+  // in flight while the one before is computed, its page lookups a tile before that
   int t = t0 + wave;
   if (t < t1) {
     look_up(t);
-    load(0);
-    if constexpr (ONE) compute(0, t);
-    else if (t + 4 < t1) look_up(t + 4);
-    for (; !ONE;) {
-      if (t + 4 < t1) { load(1); if (t + 8 < t1) look_up(t + 8); }
+    if constexpr (SINGLE && DH == 128) {                  // the caller has seen that there is no other
+      load(0);
       compute(0, t);
-      t += 4;
-      if (t >= t1) break;
-      if (t + 4 < t1) { load(0); if (t + 8 < t1) look_up(t + 8); }
-      compute(1, t);
-      t += 4;
-      if (t >= t1) break;
+    } else if constexpr (SINGLE) {
+      for (; t < t1; t += 4) {
+        load(0);
+        if (t + 4 < t1) look_up(t + 4);
+        compute(0, t);
+      }
+    } else {
+      load(0);
+      if (t + 4 < t1) look_up(t + 4);
+      for (;;) {
+        if (t + 4 < t1) { load(1); if (t + 8 < t1) look_up(t + 8); }
+        compute(0, t);
+        t += 4;
+        if (t >= t1) break;
+        if (t + 4 < t1) { load(0); if (t + 8 < t1) look_up(t + 8); }
+        compute(1, t);
+        t += 4;
+        if (t >= t1) break;
+      }
     }
   }
   l_run = sum_x32(sum_x16(l_run));
@@ -841,16 +851,20 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
 // rows_blocks blocks of the many-row kind (ROWS), then, with FEW, those of the few-row kind: a step's
 // single rows run beside its prompts, on the CUs that these leave free.  24 requests of 64 to 2000
 // positions, 5 of them with up to 250 rows, 16 heads of 64: 31.5 us, as two launches 45.7.
-// ONE (no rows, at most 128 keys per few-row request): with one tile per wave the blocks' start is what
-// counts, and without registers for a second tile 4 blocks share a CU instead of 2.  256 rows of 70 to 120
-// keys, 32 heads of 128: 76 us, else 108; of 30 to 60 keys: 60 and 80; one row of 100 keys: 7.5 and 7.4.
-template <int DH, bool ROWS, bool FEW, bool ONE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ONE ? 4 : 2, ONE ? 4 : 2))) void attn_bf16_kernel(
+// SINGLE (no rows): without registers for a second tile 4 blocks share a CU instead of 2, and other blocks'
+// work hides a block's start and its loads.  It is taken where no few-row request has more than 128 keys
+// (a tile per wave): 256 rows of 70 to 120 keys, 32 heads of 128: 76 us, else 108; of 30 to 60 keys: 60 and
+// 80; one row of 100 keys: 7.5 and 7.4.  With head dim 64 also where there are more blocks than 2 per CU:
+// 256 rows of 200 to 2000 keys, 16 heads: 209 us and 232; one row of 3000 keys, with its few blocks, would
+// take 13.3 instead of 12.5.  With head dim 128 a loop of single tiles spills at 4 blocks (954 us for 598)
+// and gains nothing at 3.  The order of a row's sums is the same in both.
+template <int DH, bool ROWS, bool FEW, bool SINGLE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SINGLE ? 4 : 2, SINGLE ? 4 : 2))) void attn_bf16_kernel(
     Plan pl, PagedAttn a, int rows_blocks) {
   __shared__ __attribute__((aligned(16))) bf16 stage0[128 * DH], stage1[ROWS ? 128 * DH : 8];
   if constexpr (FEW)
     if ((int)blockIdx.x >= rows_blocks) {
-      few_block<DH, ONE>(pl, a, (int)blockIdx.x - rows_blocks, reinterpret_cast<char*>(stage0));
+      few_block<DH, SINGLE>(pl, a, (int)blockIdx.x - rows_blocks, reinterpret_cast<char*>(stage0));
       return;
     }
   if constexpr (ROWS) rows_block<DH>(pl, a, blockIdx.x, stage0, stage1);
@@ -1114,7 +1128,7 @@ hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const
   } while (0)
     if (rows_ && few_) BF16(true, true, false);
     else if (rows_) BF16(true, false, false);
-    else if (one) BF16(false, true, true);
+    else if (one || (head_dim == 64 && nf > 512)) BF16(false, true, true);
     else BF16(false, true, false);
 #undef BF16
   } else {
