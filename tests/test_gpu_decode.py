@@ -216,6 +216,20 @@ def test_attention_prompts_of_wide_blocks(H, KH, dh, page, window, sinks, lens, 
     assert np.array_equal(_attend(c, task, H, KH, dh, window, sinks, "bf16", q, only=[0], ws_fill=0)[0], got[0])
 
 
+@pytest.mark.parametrize("dh,lo,hi", [(64, 100, 700), (64, 1, 100), (128, 100, 700), (128, 1, 100)])
+def test_attention_rows_alone_and_among_many(dh, lo, hi):
+    """A step of more blocks than the chip holds at once, and rows of it alone: the 64-bit form's, and the same bits."""
+    rng = np.random.default_rng(dh + hi)
+    ctx = rng.integers(lo, hi, 40).tolist()
+    c = Cache([1] * 40, ctx, 16, dh, 16, 0, 0, "bf16", seed=31)
+    q = [np64(torch.from_numpy(rng.standard_normal((1, 16, dh), dtype=np.float32)).to(torch.bfloat16)) for _ in ctx]
+    task = _tasks(40, 6)
+    got = _attend(c, task, 16, 16, dh, 0, 0, "bf16", q)
+    _check(c, got, q, 0, 0, "bf16", dh ** -0.5)
+    for i in (0, 17, int(np.argmax(ctx)), int(np.argmin(ctx))):
+        assert np.array_equal(_attend(c, task, 16, 16, dh, 0, 0, "bf16", q, only=[i], ws_fill=0)[i], got[i])
+
+
 def test_attention_large_logits_and_scale():
     """Scores of hundreds (one key takes the whole weight) and a given scale."""
     for dtype in ("bf16", "f32"):
