@@ -127,7 +127,8 @@ int vfm_plan_size(int32_t n_req, int32_t n_tasks, int64_t total_rows, size_t* n_
  * ctx_len, kv_start: host [n_req] or NULL (decode: cached tokens and the
  * first cache slot of each request; the new token's K/V go to slot
  * kv_start + ctx_len).  n_out: host [n_tasks] head widths or NULL.
- * Returns VFM_ERR_TASK for an id outside [0, n_tasks). */
+ * Returns VFM_ERR_TASK for an id outside [0, n_tasks), VFM_ERR_SHAPE for 2^31
+ * rows or head outputs and more in the batch. */
 int vfm_plan(const int32_t* task_id, const int32_t* seq_len, const int32_t* ctx_len,
              const int32_t* kv_start, const int32_t* n_out, int32_t n_req, int32_t n_tasks,
              int32_t* plan, size_t n_ints);

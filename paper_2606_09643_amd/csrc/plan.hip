@@ -23,7 +23,7 @@ extern "C" int vfm_plan(const int32_t* task_id, const int32_t* seq_len, const in
                         int32_t n_tasks, int32_t* plan, size_t n_ints) {
   if (!task_id || !seq_len || !plan) return VFM_ERR_ARG;
   if (n_req < 1 || n_tasks < 1) return VFM_ERR_SHAPE;
-  int64_t T = 0;
+  int64_t T = 0, outputs = 0;
   int32_t max_len = 0;
   for (int32_t i = 0; i < n_req; ++i) {
     if (task_id[i] < 0 || task_id[i] >= n_tasks) return VFM_ERR_TASK;
@@ -31,10 +31,11 @@ extern "C" int vfm_plan(const int32_t* task_id, const int32_t* seq_len, const in
     if (ctx_len && ctx_len[i] < 0) return VFM_ERR_SHAPE;
     if (kv_start && kv_start[i] < 0) return VFM_ERR_SHAPE;
     if (n_out && (n_out[task_id[i]] < 0)) return VFM_ERR_SHAPE;
+    if (n_out) outputs += n_out[task_id[i]];
     T += seq_len[i];
     if (seq_len[i] > max_len) max_len = seq_len[i];
   }
-  if (T > INT32_MAX) return VFM_ERR_SHAPE;
+  if (T > INT32_MAX || outputs > INT32_MAX) return VFM_ERR_SHAPE;   // row numbers and out_off are 32-bit
   const PlanOffsets o = plan_offsets(n_req, n_tasks, T);
   if (n_ints < (size_t)o.total) return VFM_ERR_SHAPE;
 

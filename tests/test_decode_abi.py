@@ -237,3 +237,16 @@ def test_sample_refuses_huge_heads():
     b = B.vfm_batch(host.ctypes.data_as(C.POINTER(C.c_int32)), PTR, host.size)
     s = B.vfm_sampling(None, None, None, None)
     assert B.lib().vfm_sample_tokens(C.byref(b), PTR, C.byref(s), PTR, PTR, None, 1) == B.VFM_ERR_SHAPE
+
+
+def test_head_offsets_past_int32_are_refused():
+    """Offsets of head outputs are 32-bit: a batch whose requests have 2^31 and more of them together would
+    have offsets before the buffer, so it has no plan (and no call on heads or draws ever sees one)."""
+    def plan(n_out, tasks):
+        return B.vfm_plan(np.array(tasks), np.ones(len(tasks)), len(n_out), n_out=np.array(n_out))
+    for n_out, tasks in (([1 << 30], [0, 0, 0]), ([1 << 30], [0, 0]), ([(1 << 31) - 1, 1], [0, 1]),
+                         ([600000], [0] * 3580)):
+        with pytest.raises(RuntimeError, match="vfm_plan"):
+            plan(n_out, tasks)
+    host = plan([(1 << 30), (1 << 30) - 1], [0, 1])          # 2^31 - 1 outputs: the last offset still fits
+    assert host[6] == (1 << 31) - 1
