@@ -14,7 +14,7 @@ struct PagedAttn {
   KvPages kp;
   void* out; int64_t ldo;
   float* rec_o;                // [T][H][nchunk][head_dim] partial outputs
-  float2* rec_ml;              // [T][H][nchunk] running maximum (log2 units), sum
+  float2* rec_ml;              // [T][H][nchunk] largest score, sum
   int few_chunks, rows_chunks; // the largest chunk count of a few-row and of a many-row request (1 if none)
   int nchunk;                  // the larger of the two (the records' stride)
   int qtiles;                  // the largest query-tile count of a few-row request

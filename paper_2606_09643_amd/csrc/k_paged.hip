@@ -10,6 +10,11 @@
 // in-lane plus one or two lane swaps, and exp(S^T) already lies as the B operand
 // of O^T = V^T P^T.
 //
+// A weight is 2^((s - m) scale), m the running maximum of the scores s as they are: with s scale
+// rounded for m alone, a score of 2^33 would leave a rest of hundreds in the exponent.  The difference is
+// 0 for the largest score whatever its size, so every finite score has its weight.  m starts at the
+// lowest number; sums of nothing (and their weight in a merge) are 0 beside any m.
+//
 // Unseen keys.  Scores of unseen keys become -inf by a select, so what K holds
 // there does not matter.  V rows that no query of the tile sees are staged as
 // zeros.  Where some queries of a tile see a key and others do not, a zero
@@ -22,8 +27,7 @@
 
 namespace {
 
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float NEG_BIG = -1e30f;
+constexpr float LOWEST = -3.40282347e38f;   // below or at every finite score
 
 typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -304,7 +308,7 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
   f32x4 o[ND];
 #pragma unroll
   for (int i = 0; i < ND; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_run = NEG_BIG, l_run = 0.f;
+  float m_run = LOWEST, l_run = 0.f;
 
   const int vst_ch = lane % LPR, vst_row = lane / LPR;
   const int vrow = 8 * g + (x >> 2);
@@ -344,10 +348,10 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
       for (int i = 0; i < 8; ++i) s[i] = sees(jq, kb + i, a.window, a.n_sink) ? s[i] : -INFINITY;
     }
     float mb = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-    mb = max_x32(max_x16(mb)) * a.scale_log2;
+    mb = max_x32(max_x16(mb));
     if (__any(mb > m_run)) {                              // elsewhere the factor is 1
       const float m_new = fmaxf(m_run, mb);
-      const float alpha = fast_exp2(m_run - m_new);
+      const float alpha = fast_exp2((m_run - m_new) * a.scale_log2);
       m_run = m_new;
       l_run *= alpha;
 #pragma unroll
@@ -356,7 +360,7 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
     float e8[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      e8[i] = fast_exp2(fmaf(s[i], a.scale_log2, -m_run));
+      e8[i] = fast_exp2((s[i] - m_run) * a.scale_log2);
       l_run += e8[i];
     }
     const bf16x8 pf = pack8(e8[0], e8[1], e8[2], e8[3], e8[4], e8[5], e8[6], e8[7]);
@@ -439,7 +443,7 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float wt = fast_exp2(sm[i][q] - M);
+      const float wt = fast_exp2((sm[i][q] - M) * a.scale_log2);
       L += sl[i][q] * wt;
       // a wave without any visible key has weight 0 and zeros
       acc += *reinterpret_cast<const f32x4*>(so + (i * 16 + q) * DH + d) * wt;
@@ -578,7 +582,7 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
   for (int i = 0; i < ND; ++i)
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
-  float m_run = NEG_BIG, l_run = 0.f;
+  float m_run = LOWEST, l_run = 0.f;
 
   // A lane's load i of a tile: row RPI (NW i + wave) + lane / CH, physical chunk lane % CH;
   // within its 16-position run the row, and with it the swizzle, is the same for every i.
@@ -677,33 +681,47 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
         st[kt][i] = see ? st[kt][i] : -INFINITY;
       }
   };
-  // largest score (log2 units) of the lane's query
+  // largest score of the lane's query
   auto largest = [&](const f32x16 (&st)[2]) {
     float mb = st[0][0];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mb = fmaxf(mb, st[kt][i]);
-    return max_x32(mb) * a.scale_log2;
+    return max_x32(mb);
   };
   // The running maximum follows the scores only where one passes it by 8 (a factor of 256, which
   // neither fp32 sums nor bf16 weights mind): with 32 queries a wave, some maximum grows in most
   // tiles, and the products would be rescaled that often.
   auto follow = [&](float mb) {
-    if (__any(mb > m_run + 8.f)) {
+    if (__any((mb - m_run) * a.scale_log2 > 8.f)) {
       const float m_new = fmaxf(m_run, mb);
-      const float alpha = fast_exp2(m_run - m_new);
+      const float alpha = fast_exp2((m_run - m_new) * a.scale_log2);
       m_run = m_new;
       l_run *= alpha;
 #pragma unroll
       for (int i = 0; i < ND; ++i) o[i] *= alpha;
     }
   };
+  // A weight is one fma here, 2^(s scale - m scale): the rest that m scale's rounding leaves is a factor common
+  // to all of a query's weights, below 2^(1/16) while |m scale| < 2^20.  Beyond (m at its start, too) the
+  // tile's scores are made differences from m first.  (Differences throughout: 579 us for the 564 of 4 chunks.)
+  float neg_m = 0.f;
+  auto settle = [&](f32x16 (&st)[2]) {
+    neg_m = -m_run * a.scale_log2;
+    if (__any(!(fabsf(neg_m) < 1048576.f))) {
+      neg_m = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[kt][i] -= m_run;
+    }
+  };
   // P^T of 16 keys u of a tile, 8 of them in this lane
   auto weights = [&](const f32x16 (&st)[2], int u, bf16x8 (&pf)[4]) {
     float e[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] = fast_exp2(fmaf(st[u >> 1][8 * (u & 1) + i], a.scale_log2, -m_run));
+    for (int i = 0; i < 8; ++i) e[i] = fast_exp2(fmaf(st[u >> 1][8 * (u & 1) + i], a.scale_log2, neg_m));
     pf[u] = pack8(e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]);
   };
   // their sum, of the rounded weights that the products use, and the products
@@ -764,6 +782,7 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
     scores(std::integral_constant<int, 0>{}, sa);
     mask(t0, sa);
     follow(largest(sa));
+    settle(sa);
     // tile t, t mod 2 = j: its scores st, the next one's sn (behind the last tile: of what the stage
     // holds, and not used)
     auto step = [&](auto j, int t, f32x16 (&st)[2], f32x16 (&sn)[2]) {
@@ -813,6 +832,7 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
       if (s_poison == t) add_nonfinite(t);
       if (t + 1 >= t1) return false;
       follow(mb);
+      settle(sn);
       return true;
     };
     for (int t = t0;; t += 2) {
@@ -932,7 +952,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
   for (int hh = 0; hh < NH; ++hh)
 #pragma unroll
     for (int c = 0; c < 4; ++c) o[hh][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_run = NEG_BIG, l_run = 0.f;
+  float m_run = LOWEST, l_run = 0.f;
   for (int t = t0 + wave; t < t1; t += 4) {
     const int p0 = 16 * vis.run(t);
     const int64_t slot = page_slot(prow, lp, p0);
@@ -970,9 +990,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
       }
     }
     float mb = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-    mb = max_x32(max_x16(mb)) * a.scale_log2;
+    mb = max_x32(max_x16(mb));
     const float m_new = fmaxf(m_run, mb);
-    const float alpha = exp2f(m_run - m_new);
+    const float alpha = exp2f((m_run - m_new) * a.scale_log2);
     m_run = m_new;
     l_run *= alpha;
 #pragma unroll
@@ -981,7 +1001,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
       for (int c = 0; c < 4; ++c) o[hh][c] *= alpha;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float e = exp2f(fmaf(s[j], a.scale_log2, -m_run));
+      const float e = exp2f((s[j] - m_run) * a.scale_log2);
       l_run += e;
 #pragma unroll
       for (int hh = 0; hh < NH; ++hh)
@@ -1022,7 +1042,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float wt = exp2f(sm[i][qq] - M);
+      const float wt = exp2f((sm[i][qq] - M) * a.scale_log2);
       L += sl[i][qq] * wt;
       acc += *reinterpret_cast<const f32x4*>(&so[i][qq][d]) * wt;
     }
@@ -1040,7 +1060,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
 
 // ---------------------------------------------------------------------------
 // Joins the chunks' partial sums of rows whose keys were cut: a wave per row and
-// head, o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c, chunks in order.
+// head, o = sum_c w_c o_c / sum_c w_c l_c with w_c = 2^((m_c - M) scale), chunks in order.
 // Bound by its launch: 5 to 7 us for 256 rows of 32 heads in up to 8 chunks.
 // ---------------------------------------------------------------------------
 template <typename T, int DH>
@@ -1057,7 +1077,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Plan pl, PagedAttn a) {
   if (n <= 1) return;
   const float2* ml = a.rec_ml + (int64_t)id * a.nchunk;
   const float* ro = a.rec_o + (int64_t)id * a.nchunk * DH + E * lane;
-  float M = NEG_BIG;
+  float M = LOWEST;
   for (int c = lane; c < n; c += 64) M = fmaxf(M, ml[c].x);
   M = max_x32(max_x16(max_row(M)));
   float L = 0.f, acc[E] = {};
@@ -1065,7 +1085,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Plan pl, PagedAttn a) {
     float wt = 0.f;
     if (c0 + lane < n) {
       const float2 v = ml[c0 + lane];
-      wt = exp2f(v.x - M);
+      wt = exp2f((v.x - M) * a.scale_log2);
       L += wt * v.y;
     }
     const int cn = min(64, n - c0);

@@ -515,3 +515,40 @@ def test_sample_replayed_graph():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(ids, eager)
+
+
+@pytest.mark.parametrize("dtype,H,KH,dh", [("bf16", 4, 2, 128), ("bf16", 2, 1, 64), ("f32", 4, 2, 64), ("f32", 2, 1, 128)])
+@pytest.mark.parametrize("sign,power", [(-1, 101), (1, 101), (-1, 33), (1, 33), (-1, 110), (1, 120)])
+@pytest.mark.parametrize("window", [0, 1, 40])
+def test_attention_scores_of_any_size(dtype, H, KH, dh, sign, power, window):
+    """Scores of 2^33 to 2^122, all of one sign.  Queries and keys have one dim that is not 0, so a score is one
+    product of two short numbers, exact in fp32; two scores are equal or differ by 2^(power - 8) and more, of which
+    2^23 times the scale still puts every weight but the largest ones' below 2^-1000.  An output is then the mean of
+    the V rows with the largest score: one V row, bit for bit, or the mean of n, whose weights 1 are exact, off by
+    the n additions, the division and the type's rounding."""
+    _, td, u = DT[dtype]
+    lens, ctx = [1, 1, 90, 3, 1], [60, 0, 200, 5000, 7000]
+    c = Cache(lens, ctx, KH, dh, 16, window, 0, dtype, seed=4)
+    rng = np.random.default_rng(power)
+    steps = [rng.integers(128, 256, (n, KH)) for n in c.lens + c.ctx]     # 8 bits each
+    for i, st in enumerate(steps):
+        pos = np.arange(len(st))
+        k = torch.zeros(KH, len(st), dh, dtype=td)
+        k[:, :, 3] = torch.from_numpy((sign * st * 2.0 ** (power // 2 - 8)).T).to(td)
+        there = c.table[i, pos // 16] >= 0
+        c.kp[:, torch.from_numpy(c.slots(i, pos)[there]).cuda()] = k[:, torch.from_numpy(there)].cuda()
+    q = [np.zeros((m, H, dh)) for m in lens]
+    for x in q:
+        x[:, :, 3] = 2.0 ** (power - power // 2)
+    got = _attend(c, np.zeros(5, np.int32), H, KH, dh, window, 0, dtype, q)
+    for i, m in enumerate(lens):
+        for r in range(m):
+            see = D.visible(ctx[i] + r, np.arange(ctx[i] + m), window, 0)
+            for h in range(H):
+                s = sign * steps[i][:, h * KH // H]
+                best = see & (s == s[see].max())
+                v, n = c.v[i][best, h * KH // H], int(best.sum())
+                ref = v.mean(0)
+                tol = 0.0 if n == 1 else (u if dtype == "bf16" else 0.0) * np.abs(ref) \
+                    + 2 * (n + 2) * 2.0 ** -24 * np.abs(v).sum(0) / n
+                assert np.all(np.abs(got[i][r, h] - ref) <= tol), (i, r, h, n, np.abs(got[i][r, h] - ref).max())
