@@ -355,7 +355,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
   auto value_of = [&](uint32_t key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu)); };
   const double uu = u_row > 0.f ? (double)u_row : 0.0;   // NaN: 0
   auto target_of = [&](uint64_t S) {
-    const uint64_t t = (uint64_t)fmin(uu * (double)S, 9.2e18);
+    const uint64_t t = (uint64_t)fmin(uu * (double)S, 1.8e19);   // above any S (2^63), below 2^64
     return t < S - 1 ? t : S - 1;
   };
   auto finish = [&](float v, int i, uint64_t total) {    // one thread: the drawn output

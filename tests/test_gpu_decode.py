@@ -552,3 +552,52 @@ def test_attention_scores_of_any_size(dtype, H, KH, dh, sign, power, window):
                 tol = 0.0 if n == 1 else (u if dtype == "bf16" else 0.0) * np.abs(ref) \
                     + 2 * (n + 2) * 2.0 ** -24 * np.abs(v).sum(0) / n
                 assert np.all(np.abs(got[i][r, h] - ref) <= tol), (i, r, h, n, np.abs(got[i][r, h] - ref).max())
+
+
+def _width(n):
+    """Fixed-point bits of a weight in a row of n outputs: as many as 64-bit sums of n of them hold, at most 44."""
+    return min(44, 63 - max(0, int(n - 1).bit_length()))
+
+
+LARGE = [262143, 262144, 262145, 300000, 2 ** 19 - 1, 2 ** 19, 2 ** 19 + 1, 1000003, 2 ** 20 + 5]
+
+
+@pytest.mark.parametrize("n", LARGE)
+@pytest.mark.parametrize("gap", [0.0])
+def test_sample_large_flat_tails(n, gap):
+    """One output at 0 and all others `gap` below it: each of them is next to nothing, together they are up to 5e-4
+    of the sum, or with gap 0 all of it, 2^63 units.  The drawn output's stretch of the exact running sum holds u S up
+    to the rounding of the weights, all of them by the same e <= 2^-(s + 1): n e at most.  logprob is off by fp32's
+    rounding and by n e / S.  A top-p border in the tail moves by as much and by one weight."""
+    s, T = _width(n), 1.0
+    x = np.full(n, -gap, np.float32)
+    x[n // 3] = 0.0
+    tail = float(np.exp(np.float64(x[0])))
+    room = n * 2.0 ** -(s + 1)
+    w = np.full(n, tail)
+    w[n // 3] = 1.0
+    c = np.cumsum(w)
+    S = float(c[-1])
+    us = [1e-6, 2e-5, 0.3, 1 - 2e-5, 1 - 1e-6, float(np.float32(1) - np.float32(2) ** -24)]
+    ids, lp = _draw([x] * len(us), [T] * len(us), u=us)
+    for i, u in enumerate(us):
+        t = float(np.float32(u)) * S
+        a = int(ids[i])
+        assert c[a] - w[a] - 2 * room <= t <= c[a] + 2 * room, (u, a, c[a] - w[a], t, room)
+        ref = np.log(w[a] / S)
+        assert abs(lp[i] - ref) <= 2.0 ** -23 * abs(ref) + room / S + 2.0 ** -40, (u, lp[i], ref)
+    # top-p: half of the tail stays, by index
+    if gap:
+        p = float(np.float32(1 - 0.5 * (S - 1) / S))
+        keep = np.zeros(n, bool)
+        keep[n // 3] = True
+        m = int(np.ceil((p * S - 1) / tail))
+        keep[np.delete(np.arange(n), n // 3)[:m]] = True
+        wk = np.where(keep, w, 0.0)
+        ck = np.cumsum(wk)
+        ids, lp = _draw([x] * len(us), [T] * len(us), top_p=[p] * len(us), u=us)
+        for i, u in enumerate(us):
+            a, t = int(ids[i]), float(np.float32(u)) * ck[-1]
+            assert ck[a] - w[a] - 4 * room - tail <= t <= ck[a] + 4 * room + tail, (u, a, ck[a], t, room)
+            ref = np.log(w[a] / ck[-1])
+            assert abs(lp[i] - ref) <= 2.0 ** -23 * abs(ref) + 3 * room + tail, (u, lp[i], ref)
