@@ -124,10 +124,11 @@ typedef struct vfm_sampling {
  * running sum of kept weights exceeds u times their sum S, and logprob
  * log(w_j / S).  Greedy (temperature <= 0): the largest output, ties to the
  * lowest index, logprob 0.  A request with no non-NaN output: -1, logprob NaN.
- * Weights are computed in fp64 and summed as 44-bit fixed point (32-bit for
- * heads of 2^19 outputs and more), exactly and in any order: a weight below
- * 2^-45 of the largest counts as 0, and the result does not depend on how
- * the work is split.  VFM_ERR_SHAPE: a request of more than 2^30 outputs. */
+ * Weights are computed in fp64, rounded to s-bit fixed point (s = 44 up to
+ * 2^19 outputs, then 63 - ceil(log2 n): 43 up to 2^20, 33 at 2^30, as many as
+ * a 64-bit sum holds) and summed exactly, in any order: a weight below
+ * 2^-(s + 1) of the largest counts as 0, and the result does not depend on
+ * how the work is split.  VFM_ERR_SHAPE: a request of more than 2^30 outputs. */
 int vfm_sample_tokens(const vfm_batch* batch, const float* out, const vfm_sampling* sampling,
                       const float* u, int32_t* ids, float* logprob, void* stream);
 

@@ -4,8 +4,8 @@
 //
 // Weights.  w_j = 2^t_j, t_j = (l_j - M) log2(e) / T <= 0, in fp64 (at full rate
 // here: 12 fused multiply-adds of a Taylor series after the split of t into
-// its nearest integer and a rest of at most 1/2), rounded to 2^-44: the sums are
-// then integers, exact in any order, so the order of atomics, the split over
+// its nearest integer and a rest of at most 1/2), rounded to 2^-44 (rows of more than
+// 2^19 outputs: to what a 64-bit sum of them holds): the sums are then integers, exact in any order, so the order of atomics, the split over
 // threads and the block's shape cannot change a result.  fp32 would shift the
 // borders of the running sum by 1e-7 of it, and a vocabulary has so many of
 // them that the token drawn would now and then be another.
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
       __syncthreads();
     }
   }
-  const int sh = n < (1 << 19) ? 44 : 32;
+  const int sh = min(44, 31 + __builtin_clz((n - 1) | 1));   // 63 - ceil(log2 n): n weights of 2^sh sum to 2^63 at most
   const uint64_t one = (uint64_t)1 << sh;
   const float cut = fminf((float)(31.2 * T), 3e38f);     // 45 ln 2: below M - cut every weight is 0
   auto power = [&](float v) { return ((double)v - (double)M) * c2; };

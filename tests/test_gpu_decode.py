@@ -563,7 +563,27 @@ LARGE = [262143, 262144, 262145, 300000, 2 ** 19 - 1, 2 ** 19, 2 ** 19 + 1, 1000
 
 
 @pytest.mark.parametrize("n", LARGE)
-@pytest.mark.parametrize("gap", [0.0])
+def test_sample_large_heads(n):
+    """Rows whose pieces have more than 64 runs, around the sizes at which weights get fewer bits, every kind of
+    filter, numbers u that land early and late.  A weight rounded by 2^-(s + 1) of the largest moves a border of the
+    running sum S >= 1, and u S, by n 2^-(s + 1) each at most: a target farther than n 2^-s S from every border
+    gives the 64-bit form's output."""
+    rng = np.random.default_rng(n)
+    x = (rng.standard_normal(n) * 2).astype(np.float32)
+    par = [(1.0, 0, 1.0, 0.0, 0.9995), (0.8, 0, 1.0, 0.0, 0.013), (1.0, 0, 0.9, 0.0, 0.51), (1.3, 0, 1.0, 0.01, 0.98),
+           (1.0, 150000, 1.0, 0.0, 0.77), (1.0, 150000, 0.8, 0.0, 0.999), (1.0, 3000, 0.95, 0.002, 0.3),
+           (1.0, 40, 1.0, 0.0, 0.6), (0.0, 0, 1.0, 0.0, 0.5), (1.0, 0, 0.4, 0.0, float(np.float32(1) - np.float32(2) ** -24))]
+    ids, lp = _draw([x] * len(par), *[list(c) for c in zip(*par)])
+    room = n * 2.0 ** -_width(n)
+    for i, (T, k, p, m, u) in enumerate(par):
+        a, l, near = D.sample(x, np.float32(T), k, np.float32(p), np.float32(m), np.float32(u))
+        assert ids[i] == a or near <= room, (i, ids[i], a, near)
+        if ids[i] == a:
+            assert abs(lp[i] - l) <= 2.0 ** -23 * abs(l) + room + 2.0 ** -40, (i, lp[i], l)
+
+
+@pytest.mark.parametrize("n", LARGE)
+@pytest.mark.parametrize("gap", [21.5, 22.9, 0.0])
 def test_sample_large_flat_tails(n, gap):
     """One output at 0 and all others `gap` below it: each of them is next to nothing, together they are up to 5e-4
     of the sum, or with gap 0 all of it, 2^63 units.  The drawn output's stretch of the exact running sum holds u S up
