@@ -76,7 +76,12 @@ int vfm_kv_append(const vfm_attn* attn, const vfm_batch* batch, const void* qkv,
  * (NaN and infinities too) does not reach any output.
  * A row's result does not depend on the batch around its request.  The
  * softmax is taken in fp32; bf16 rounds its weights to bf16 for the product
- * with V.  Errors as vfm_kv_append, plus VFM_ERR_WORKSPACE. */
+ * with V.  The workspace holds partial results of the requests whose keys go
+ * to many blocks (long contexts of few rows), of each as much as alone, up to
+ * twice that or 16 MB where this is simpler; 0 bytes where there is none.
+ * Errors as vfm_kv_append, plus VFM_ERR_WORKSPACE and VFM_ERR_UNSUPPORTED for
+ * steps of 2^24 blocks and more: key heads times, in bf16, 16 packed queries
+ * (rows x group) of requests with up to 32, 128 of others, in fp32 16. */
 int vfm_attention_workspace(const vfm_attn* attn, const vfm_batch* batch, size_t* bytes);
 int vfm_attention_paged(const vfm_attn* attn, const vfm_batch* batch, const void* q, int64_t ldq,
                         const vfm_kv_pages* kv, void* out, int64_t ldo, void* workspace,

@@ -253,48 +253,75 @@ int check_pages(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, const
   return VFM_OK;
 }
 
+// One request with a long context makes most blocks of a rectangle empty, and most of its records unused.  A table
+// of where each request's own begin costs a launch before the attention's and a search per block: it pays from some
+// 2500 empty blocks on where they are two in three.  Rows of 32 heads of 128 beside one of 30000 keys: 128 short
+// ones on 32 key heads 216 us, with the table 187 (33024 blocks, 4352 of them with work), on 8 130 and 59
+// (33024, 1280), on 1 of 8 heads 38 and 26 (9417, 201); 8 short ones and 8 of 8000 keys on 8 56.5 and 58.4 (2560, 1344),
+// and 256 rows of 200 to 2000 keys, 16 heads of 64, 194 and 198 (20480, 10608).
+// Records are kept to their own from 16 MB of unused ones on whatever the time (22.5 us and 24.7 for 300 rows beside
+// one after 8000 keys and two shorter: 101 MB and 0.4).
+constexpr int64_t TABLE_MIN_EMPTY = 2500;
+constexpr int64_t TABLE_MIN_BYTES = 16 << 20;
+
 // Launch facts of the paged attention over a batch.
 struct AttnPlan {
   int few_chunks, rows_chunks, qtiles;
-  bool few, rows;            // the batch has requests of the few-row and of the many-row kind
   bool one;                  // no few-row request has more than 4 tiles of keys
+  bool table;                // blocks and records where each request's own begin, not in rectangles
+  int64_t few_blocks, rows_blocks, recs, joins;
   int64_t bytes;             // workspace
   int nchunk() const { return std::max(few_chunks, rows_chunks); }
+  size_t table_bytes(const Plan& pl) const { return table ? align_up((size_t)4 * (pl.n_req + 1) * sizeof(int32_t)) : 0; }
 };
 
 int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, AttnPlan* out) {
-  AttnPlan ap = {1, 1, 1, false, false, true, 0};
+  AttnPlan ap = {};
+  ap.few_chunks = ap.rows_chunks = ap.qtiles = 1;
+  ap.one = true;
   const int G = a.n_heads / a.n_kv_heads;
   const PlanOffsets po = plan_offsets(pl.n_req, pl.n_tasks, pl.T);
   const int32_t *ctx = host_arr(batch, po.ctx), *cu = host_arr(batch, po.cu_seqlens);
+  int64_t own[4] = {};       // the requests' own blocks, records and joins
   for (int p = 0; p < pl.n_req; ++p) {
     const int m = cu[p + 1] - cu[p];
     if (ctx[p] < 0 || (int64_t)ctx[p] + m > kMaxPos) return VFM_ERR_SHAPE;
     const Chunks ck = request_chunks(a.dtype, m, ctx[p], G, a.n_kv_heads, a.window, a.n_sink);
     const int n = ck.n;
+    const AttnCounts c = request_counts(a.dtype, m, a.n_heads, a.n_kv_heads, n);
+    for (int i = 0; i < 4; ++i) own[i] += c.v[i];
     if (few_rows(a.dtype, m, G)) {
-      ap.few = true;
       ap.one = ap.one && n * ck.tiles <= 4;
       ap.few_chunks = std::max(ap.few_chunks, n);
       if (a.dtype == VFM_BF16) ap.qtiles = std::max(ap.qtiles, few_qtiles(m, G));
     } else {
-      ap.rows = true;
       ap.rows_chunks = std::max(ap.rows_chunks, n);
     }
   }
-  // a launch holds at most 2^32 - 1 threads, 256 a block
-  const int64_t most = ((int64_t)1 << 24) - 1;
   const int64_t few_tiles = a.dtype == VFM_BF16 ? (int64_t)ap.qtiles * pl.n_req : (int64_t)pl.T * G / 16 + pl.n_req;
   const int64_t rows_tiles = (int64_t)pl.T / rows_per_block(G) + pl.n_req;
-  const int64_t few_blocks = ap.few ? few_tiles * a.n_kv_heads * ap.few_chunks : 0;
-  const int64_t rows_blocks = ap.rows ? rows_tiles * a.n_kv_heads * ap.rows_chunks : 0;
-  if (few_blocks > most || rows_blocks > most || few_blocks + rows_blocks > most ||
-      (ap.nchunk() > 1 && (int64_t)pl.T * a.n_heads / 4 >= most))
-    return VFM_ERR_UNSUPPORTED;
-  if (ap.nchunk() > 1) {
-    const int64_t recs = (int64_t)pl.T * a.n_heads * ap.nchunk();
-    ap.bytes = (int64_t)align_up((size_t)recs * a.head_dim * 4) + (int64_t)align_up((size_t)recs * 8);
+  ap.few_blocks = own[TAB_FEW] > 0 ? few_tiles * a.n_kv_heads * ap.few_chunks : 0;
+  ap.rows_blocks = own[TAB_ROWS] > 0 ? rows_tiles * a.n_kv_heads * ap.rows_chunks : 0;
+  const bool cut = own[TAB_RECS] > 0;
+  ap.joins = cut ? (int64_t)pl.T * a.n_heads : 0;
+  ap.recs = ap.joins * ap.nchunk();
+  // A launch holds at most 2^32 - 1 threads, 256 a block.
+  const int64_t most = ((int64_t)1 << 24) - 1;
+  const int64_t rec_bytes = a.head_dim * 4 + 8;
+  const int64_t blocks = ap.few_blocks + ap.rows_blocks, with_work = own[TAB_FEW] + own[TAB_ROWS];
+  ap.table = blocks > most || (cut && ((blocks > 3 * with_work && blocks - with_work > TABLE_MIN_EMPTY) ||
+                                       (ap.recs - 2 * own[TAB_RECS]) * rec_bytes > TABLE_MIN_BYTES ||
+                                       ap.joins / 4 >= most));
+  if (ap.table) {
+    ap.few_blocks = own[TAB_FEW];
+    ap.rows_blocks = own[TAB_ROWS];
+    ap.recs = own[TAB_RECS];
+    ap.joins = own[TAB_JOIN];
   }
+  if (ap.few_blocks + ap.rows_blocks > most || ap.joins / 4 >= most || (ap.table && ap.recs > INT32_MAX)) return VFM_ERR_UNSUPPORTED;
+  if (cut || ap.table)
+    ap.bytes = (int64_t)ap.table_bytes(pl) + (int64_t)align_up((size_t)ap.recs * a.head_dim * 4) +
+               (int64_t)align_up((size_t)ap.recs * 8);
   *out = ap;
   return VFM_OK;
 }
@@ -307,12 +334,17 @@ hipError_t run_attention(const vfm_attn& a, const Plan& pl, const AttnPlan& ap, 
   p.window = a.window; p.n_sink = a.window > 0 ? a.n_sink : 0;
   p.scale_log2 = (a.scale > 0.f ? a.scale : 1.f / sqrtf((float)a.head_dim)) * 1.4426950408889634f;
   p.q = q; p.ldq = ldq; p.k = k; p.v = v; p.slots = slots; p.kp = kp; p.out = out; p.ldo = ldo;
-  p.few_chunks = ap.few_chunks; p.rows_chunks = ap.rows_chunks; p.nchunk = ap.nchunk(); p.qtiles = ap.qtiles;
-  if (p.nchunk > 1) {
-    p.rec_o = (float*)ws;
-    p.rec_ml = (float2*)(ws + align_up((size_t)pl.T * p.H * p.nchunk * a.head_dim * 4));
+  if (ap.table) {
+    p.table = (const int32_t*)ws;
+  } else {
+    p.few_chunks = ap.few_chunks; p.rows_chunks = ap.rows_chunks; p.nchunk = ap.nchunk(); p.qtiles = ap.qtiles;
   }
-  return launch_attention_paged(a.dtype, a.head_dim, pl, p, ap.few, ap.rows, ap.one, p.nchunk > 1, s);
+  if (ap.joins > 0) {
+    p.rec_o = (float*)(ws + ap.table_bytes(pl));
+    p.rec_ml = (float2*)((char*)p.rec_o + align_up((size_t)ap.recs * a.head_dim * 4));
+  }
+  return launch_attention_paged(a.dtype, a.head_dim, pl, p, ap.few_blocks, ap.rows_blocks, ap.joins, ap.one,
+                                ap.table, s);
 }
 
 vfm_attn attn_of_layer(const vfm_cfg& c, int32_t window, int32_t n_sink) {

@@ -13,12 +13,25 @@ struct PagedAttn {
   const void* k; const void* v; int64_t slots;   // slots per head
   KvPages kp;
   void* out; int64_t ldo;
-  float* rec_o;                // [T][H][nchunk][head_dim] partial outputs
-  float2* rec_ml;              // [T][H][nchunk] largest score, sum
-  int few_chunks, rows_chunks; // the largest chunk count of a few-row and of a many-row request (1 if none)
-  int nchunk;                  // the larger of the two (the records' stride)
-  int qtiles;                  // the largest query-tile count of a few-row request
+  // partial results of rows whose keys are cut, a record per row, head and chunk
+  float* rec_o;                // [records][head_dim] outputs
+  float2* rec_ml;              // [records] largest score, sum
+  union {                      // (a longer argument list costs a call of one row 0.2 us of 8.9)
+    struct {                   // blocks and records in rectangles over the largest counts:
+      int few_chunks, rows_chunks;   // chunks of a few-row and of a many-row request (1 if none)
+      int nchunk;              // the larger of the two (the records' stride)
+      int qtiles;              // query tiles of a few-row request
+    };
+    const int32_t* table;      // or where each request's own begin
+  };
 };
+
+// The table: four prefix sums over the batch's requests in plan order, [4][n_req + 1]: blocks of the many-row kind, of the
+// few-row kind, records, and rows times heads that are joined.  A request's blocks are in the order of tile, chunk
+// and head, its records in that of row, head and chunk, its joins in that of row and head.  A kernel before the
+// attention writes the table where rectangles would be mostly empty (plan_attention has the rule).
+enum { TAB_ROWS = 0, TAB_FEW = 1, TAB_RECS = 2, TAB_JOIN = 3 };
+struct AttnCounts { int64_t v[4]; };
 
 // What one request's rows see, in runs of 2^SH positions: ns runs from position
 // 0 (the sinks), then the runs from run `base` up to the last row's own.
@@ -84,15 +97,28 @@ __host__ __device__ inline Chunks request_chunks(int dtype, int m, int ctx, int 
   return key_chunks(tiles, par > 256 ? 256 : (int)par, ROWS_MIN_TILES);
 }
 
+// what a request of m rows and n chunks adds to the table
+__host__ __device__ inline AttnCounts request_counts(int dtype, int m, int H, int KH, int n) {
+  const int G = H / KH;
+  const bool few = few_rows(dtype, m, G);
+  const int rb = rows_per_block(G);
+  AttnCounts c;
+  c.v[TAB_ROWS] = few ? 0 : (int64_t)KH * n * (((int64_t)m + rb - 1) / rb);
+  c.v[TAB_FEW] = few ? (int64_t)KH * n * few_qtiles(m, G) : 0;
+  c.v[TAB_RECS] = n > 1 ? (int64_t)m * H * n : 0;
+  c.v[TAB_JOIN] = n > 1 ? (int64_t)m * H : 0;
+  return c;
+}
+
 // q_out: rows ldq apart; qkv itself (ldq = ld) to rotate the queries in place, NULL for keys and values only.
 hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv,
                             int64_t ld, void* q_out, int64_t ldq, void* k, void* v, int64_t slots, const KvPages& kp,
                             hipStream_t s);
 
-// few, rows: the batch has requests of the few-row and of the many-row kind; one: no few-row request has more than a
-// tile per wave.  split: some request has more than one chunk.
-hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, bool few, bool rows,
-                                  bool one, bool split, hipStream_t s);
+// few_blocks, rows_blocks, joins: the grids (few rows, many rows) and the rows times heads to join; one: no few-row
+// request has more than a tile per wave.  table: a.table is there, and is written first.
+hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, int64_t few_blocks,
+                                  int64_t rows_blocks, int64_t joins, bool one, bool table, hipStream_t s);
 
 // max_out: the batch's longest row of head outputs.
 hipError_t launch_sample(const Plan& pl, const float* out, const vfm_sampling& sp, const float* u, int32_t* ids,

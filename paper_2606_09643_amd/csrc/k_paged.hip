@@ -198,6 +198,30 @@ struct Work {
   int h, c, qt, p;    // key head, chunk, query tile, plan position
 };
 
+// The table's sum `which` (it is written by a kernel before this one).
+typedef const int32_t __attribute__((address_space(4)))* table_t;
+__device__ __forceinline__ table_t table_of(const Plan& pl, const PagedAttn& a, int which) {
+  return (table_t)(uintptr_t)(a.table + (int64_t)which * (pl.n_req + 1));
+}
+// The request that place id of a sum falls to, the last one whose part begins at or before it; id becomes the place
+// in its part.
+__device__ __forceinline__ int request_at(table_t t, int n_req, int& id) {
+  int lo = 0, hi = n_req - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (t[mid] <= id) lo = mid; else hi = mid - 1;
+  }
+  id -= t[lo];
+  return lo;
+}
+// The first record of a row and head, in a request p whose rows begin at R0 and whose keys are cut in n.
+template <bool TABLE>
+__device__ __forceinline__ int64_t record_of(const Plan& pl, const PagedAttn& a, int p, int R0, int n, int64_t row,
+                                             int head) {
+  if constexpr (TABLE) return table_of(pl, a, TAB_RECS)[p] + ((row - R0) * a.H + head) * n;
+  else return (row * a.H + head) * a.nchunk;
+}
+
 // Output of packed query `qi` (of the request's first row R0): the row's head.
 __device__ __forceinline__ int64_t out_row(const PagedAttn& a, int R0, int h, int qi, int& head) {
   const int i = qi / a.G;
@@ -233,7 +257,7 @@ __device__ __forceinline__ int few_vswz(int r) {
 
 // smem: 256 DH bytes, V tiles, then the waves' outputs.  SINGLE: one tile at a time in registers, with head dim
 // 128 the wave's only one.
-template <int DH, bool SINGLE>
+template <int DH, bool SINGLE, bool TABLE>
 __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, int id, char* smem) {
   constexpr int LPR = DH / 8;          // lanes per K / V row (16 bytes each)
   constexpr int RPI = 64 / LPR;        // rows per wave-wide load
@@ -243,7 +267,9 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
   __shared__ float sm[4][16], sl[4][16];
 
   Work w;
-  {
+  if constexpr (TABLE) {
+    w.p = request_at(table_of(pl, a, TAB_FEW), pl.n_req, id);
+  } else {
     w.h = id % a.KH; id /= a.KH;
     w.c = id % a.few_chunks; id /= a.few_chunks;
     w.qt = id % a.qtiles;
@@ -253,9 +279,15 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
   const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide
   if (!few_rows(VFM_BF16, m, a.G)) return;              // block-uniform, as every exit below
   const int qn = m * a.G;
-  if (w.qt * 16 >= qn) return;
+  if (!TABLE && w.qt * 16 >= qn) return;
   const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink);
-  if (w.c >= ck.n) return;
+  if constexpr (TABLE) {
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % ck.n;
+    w.qt = id / ck.n;
+  } else if (w.c >= ck.n) {
+    return;
+  }
   const Vis vis = visible_runs<4>(ctx, ctx + m - 1, a.window, a.n_sink);
   const int t0 = w.c * ck.tiles, t1 = min(t0 + ck.tiles, (vis.n + 1) / 2);
 
@@ -457,7 +489,7 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
       for (int i = 0; i < 4; ++i) v[i] = (bf16)(acc[i] * inv);
       *reinterpret_cast<bf16x4*>((bf16*)a.out + r * a.ldo + hd * DH + d) = v;
     } else {
-      const int64_t rec = (r * a.H + hd) * a.nchunk + w.c;
+      const int64_t rec = record_of<TABLE>(pl, a, w.p, R0, ck.n, r, hd) + w.c;
       *reinterpret_cast<f32x4*>(a.rec_o + rec * DH + d) = acc;
       if (d == 0) a.rec_ml[rec] = make_float2(M, L);
     }
@@ -507,7 +539,7 @@ __device__ __forceinline__ int rows_vswz(int r, int c) {
 template <int N>
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14)); }
 
-template <int DH>
+template <int DH, bool TABLE>
 __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, int id, bf16* stage0, bf16* stage1) {
   constexpr int NW = 4;                  // waves
   constexpr int CH = DH / 8;             // 16-byte chunks per row
@@ -527,18 +559,16 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
 
   const int rb = rows_per_block(a.G);
   Work w;
-  int blk;
-  {
+  if constexpr (TABLE) {
+    w.p = request_at(table_of(pl, a, TAB_ROWS), pl.n_req, id);
+  } else {
     w.h = id % a.KH; id /= a.KH;
     w.c = id % a.rows_chunks; id /= a.rows_chunks;
-    blk = id;
-  }
-  // request p's blocks start at cu[p] / rb + p: at least ceil(m / rb) before the next request's
-  {
+    // request p's blocks start at cu[p] / rb + p: at least ceil(m / rb) before the next request's
     int lo = 0, hi = pl.n_req - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (uniform(pl.cu_seqlens[mid]) / rb + mid <= blk) lo = mid; else hi = mid - 1;
+      if (uniform(pl.cu_seqlens[mid]) / rb + mid <= id) lo = mid; else hi = mid - 1;
     }
     w.p = lo;
   }
@@ -546,11 +576,17 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
   const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide
   // a request's last rows see the most keys: they come first
   const int nb = (m + rb - 1) / rb;
-  const int bi = blk - (R0 / rb + w.p);
-  if (bi >= nb || few_rows(VFM_BF16, m, a.G)) return;   // block-uniform, as every exit below
-  const int r0 = (nb - 1 - bi) * rb, nr = min(rb, m - r0);
+  int bi = id - (R0 / rb + w.p);
+  if (few_rows(VFM_BF16, m, a.G) || (!TABLE && bi >= nb)) return;   // block-uniform, as every exit below
   const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink);
-  if (w.c >= ck.n) return;
+  if constexpr (TABLE) {
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % ck.n;
+    bi = id / ck.n;
+  } else if (w.c >= ck.n) {
+    return;
+  }
+  const int r0 = (nb - 1 - bi) * rb, nr = min(rb, m - r0);
   const int j0 = ctx + r0, j1 = j0 + nr - 1, qn = nr * a.G;
   const Vis vis = visible_runs<6>(j0, j1, a.window, a.n_sink);
   const int tpc = (vis.n + ck.n - 1) / ck.n;
@@ -856,7 +892,7 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
         *reinterpret_cast<bf16x4*>(orow + 32 * d + 8 * j) = v;
       }
   } else {
-    const int64_t rec = (row * a.H + head) * a.nchunk + w.c;
+    const int64_t rec = record_of<TABLE>(pl, a, w.p, R0, ck.n, row, head) + w.c;
     float* ro = a.rec_o + rec * DH + 4 * h2;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -878,16 +914,16 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
 // 256 rows of 200 to 2000 keys, 16 heads: 209 us and 232; one row of 3000 keys, with its few blocks, would
 // take 13.3 instead of 12.5.  With head dim 128 a loop of single tiles spills at 4 blocks (954 us for 598)
 // and gains nothing at 3.  The order of a row's sums is the same in both.
-template <int DH, bool ROWS, bool FEW, bool SINGLE>
+template <int DH, bool ROWS, bool FEW, bool SINGLE, bool TABLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SINGLE ? 4 : 2, SINGLE ? 4 : 2))) void attn_bf16_kernel(
     Plan pl, PagedAttn a, int rows_blocks) {
   __shared__ __attribute__((aligned(16))) bf16 stage0[128 * DH], stage1[ROWS ? 128 * DH : 8];
   if constexpr (FEW)
     if ((int)blockIdx.x >= rows_blocks) {
-      few_block<DH, SINGLE>(pl, a, (int)blockIdx.x - rows_blocks, reinterpret_cast<char*>(stage0));
+      few_block<DH, SINGLE, TABLE>(pl, a, (int)blockIdx.x - rows_blocks, reinterpret_cast<char*>(stage0));
       return;
     }
-  if constexpr (ROWS) rows_block<DH>(pl, a, blockIdx.x, stage0, stage1);
+  if constexpr (ROWS) rows_block<DH, TABLE>(pl, a, blockIdx.x, stage0, stage1);
 }
 
 // ---------------------------------------------------------------------------
@@ -903,15 +939,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SINGLE ? 4 
 // after 1000: 269 us, 79 TFLOP/s (a large fp32 matrix product: 154): bound by the
 // operand loads, which no other block's queries share through LDS.
 // ---------------------------------------------------------------------------
-template <int DH>
+template <int DH, bool TABLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attn_f32_kernel(Plan pl, PagedAttn a) {
   constexpr int NC = DH / 16, NH = DH / 64;
   __shared__ float sm[4][16], sl[4][16];
   __shared__ __attribute__((aligned(16))) float so[4][16][DH];
   auto mfma = [](float p, float q, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(p, q, c, 0, 0, 0); };
   Work w;
-  {
-    int id = blockIdx.x;
+  int id = blockIdx.x;
+  if constexpr (TABLE) {
+    w.p = request_at(table_of(pl, a, TAB_FEW), pl.n_req, id);
+  } else {
     w.h = id % a.KH; id /= a.KH;
     w.c = id % a.few_chunks; id /= a.few_chunks;
     // request p's query tiles start at cu[p] G / 16 + p
@@ -926,9 +964,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
   const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
   const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide
   const int qn = m * a.G;
-  if (w.qt * 16 >= qn) return;                            // block-uniform, as every exit below
+  if (!TABLE && w.qt * 16 >= qn) return;      // block-uniform, as every exit below
   const Chunks ck = request_chunks(VFM_F32, m, ctx, a.G, a.KH, a.window, a.n_sink);
-  if (w.c >= ck.n) return;
+  if constexpr (TABLE) {
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % ck.n;
+    w.qt = id / ck.n;
+  } else if (w.c >= ck.n) {
+    return;
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = lane & 15, g = lane >> 4;
   const int qi = min(w.qt * 16 + x, qn - 1);
@@ -1051,7 +1095,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
     if (ck.n == 1) {
       *reinterpret_cast<f32x4*>((float*)a.out + r * a.ldo + hd * DH + d) = acc / L;
     } else {
-      const int64_t rec = (r * a.H + hd) * a.nchunk + w.c;
+      const int64_t rec = record_of<TABLE>(pl, a, w.p, R0, ck.n, r, hd) + w.c;
       *reinterpret_cast<f32x4*>(a.rec_o + rec * DH + d) = acc;
       if (d == 0) a.rec_ml[rec] = make_float2(M, L);
     }
@@ -1063,20 +1107,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
 // head, o = sum_c w_c o_c / sum_c w_c l_c with w_c = 2^((m_c - M) scale), chunks in order.
 // Bound by its launch: 5 to 7 us for 256 rows of 32 heads in up to 8 chunks.
 // ---------------------------------------------------------------------------
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void attn_join_kernel(Plan pl, PagedAttn a) {
+template <typename T, int DH, bool TABLE>
+__global__ __launch_bounds__(256) void attn_join_kernel(Plan pl, PagedAttn a, int joins) {
   constexpr int DT = std::is_same<T, bf16>::value ? VFM_BF16 : VFM_F32;
   constexpr int E = DH / 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int id = (int)blockIdx.x * 4 + wave;              // the launch has fewer than 2^26
-  if (id >= pl.T * a.H) return;
-  const int r = id / a.H, head = id - r * a.H;
-  const int p = uniform(pl.row_req[r]);
-  const int m = uniform(pl.cu_seqlens[p + 1]) - uniform(pl.cu_seqlens[p]), ctx = uniform(pl.ctx[p]);
+  int id = (int)blockIdx.x * 4 + wave;                    // the launch has fewer than 2^26
+  if (id >= joins) return;
+  int r, p;
+  if constexpr (TABLE) {
+    p = request_at(table_of(pl, a, TAB_JOIN), pl.n_req, id);
+    r = uniform(pl.cu_seqlens[p]) + id / a.H;
+  } else {
+    r = id / a.H;
+    p = uniform(pl.row_req[r]);
+  }
+  const int head = id % a.H;
+  const int R0 = uniform(pl.cu_seqlens[p]), m = uniform(pl.cu_seqlens[p + 1]) - R0, ctx = uniform(pl.ctx[p]);
   const int n = request_chunks(DT, m, ctx, a.G, a.KH, a.window, a.n_sink).n;
   if (n <= 1) return;
-  const float2* ml = a.rec_ml + (int64_t)id * a.nchunk;
-  const float* ro = a.rec_o + (int64_t)id * a.nchunk * DH + E * lane;
+  const int64_t rec = record_of<TABLE>(pl, a, p, R0, n, r, head);
+  const float2* ml = a.rec_ml + rec;
+  const float* ro = a.rec_o + rec * DH + E * lane;
   float M = LOWEST;
   for (int c = lane; c < n; c += 64) M = fmaxf(M, ml[c].x);
   M = max_x32(max_x16(max_row(M)));
@@ -1115,6 +1167,45 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Plan pl, PagedAttn a) {
   for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] / L);
 }
 
+// ---------------------------------------------------------------------------
+// The prefix sums of a.table: one block, 256 requests at a time.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void attn_table_kernel(Plan pl, PagedAttn a, int dtype, int32_t* table) {
+  __shared__ int64_t part[4][4];                          // sums of a wave's requests
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int64_t base[4] = {};
+  for (int p0 = 0; p0 < pl.n_req; p0 += 256) {
+    const int p = p0 + tid;
+    AttnCounts c = {};
+    if (p < pl.n_req) {
+      const int m = pl.cu_seqlens[p + 1] - pl.cu_seqlens[p];
+      c = request_counts(dtype, m, a.H, a.KH, request_chunks(dtype, m, pl.ctx[p], a.G, a.KH, a.window, a.n_sink).n);
+    }
+    int64_t sum[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sum[i] = c.v[i];
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int64_t o = __shfl_up(sum[i], d, 64);
+        sum[i] += lane >= d ? o : 0;
+      }
+      if (lane == 63) part[i][wave] = sum[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      for (int w = 0; w < 4; ++w) {
+        if (w < wave) sum[i] += part[i][w];
+      }
+      if (p < pl.n_req) table[(int64_t)i * (pl.n_req + 1) + p + 1] = (int32_t)(base[i] + sum[i]);
+      for (int w = 0; w < 4; ++w) base[i] += part[i][w];
+    }
+    __syncthreads();
+  }
+  if (tid < 4) table[(int64_t)tid * (pl.n_req + 1)] = 0;
+}
+
 }  // namespace
 
 hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv,
@@ -1131,40 +1222,51 @@ hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_d
   return hipGetLastError();
 }
 
-hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, bool few_, bool rows_,
-                                  bool one, bool split, hipStream_t s) {
-  int pi = prof_begin(VFM_PROF_ATTN, s);
-  const unsigned few = (unsigned)a.KH * a.few_chunks, rows = (unsigned)a.KH * a.rows_chunks;
-#define BY_DH(K_, G_) \
-  do { if (head_dim == 64) hipLaunchKernelGGL((K_<64>), G_, dim3(256), 0, s, pl, a); \
-       else hipLaunchKernelGGL((K_<128>), G_, dim3(256), 0, s, pl, a); } while (0)
-  if (dtype == VFM_BF16) {
-    const unsigned nf = few_ ? few * a.qtiles * pl.n_req : 0;
-    const unsigned nr = rows_ ? rows * (pl.T / rows_per_block(a.G) + pl.n_req) : 0;
-#define BF16(R_, F_, O_)                                                                                              \
-  do {                                                                                                            \
-    if (head_dim == 64) hipLaunchKernelGGL((attn_bf16_kernel<64, R_, F_, O_>), dim3(nr + nf), dim3(256), 0, s, pl, a, (int)nr);  \
-    else hipLaunchKernelGGL((attn_bf16_kernel<128, R_, F_, O_>), dim3(nr + nf), dim3(256), 0, s, pl, a, (int)nr);     \
-  } while (0)
-    if (rows_ && few_) BF16(true, true, false);
-    else if (rows_) BF16(true, false, false);
-    else if (one || (head_dim == 64 && nf > 512)) BF16(false, true, true);
-    else BF16(false, true, false);
+namespace {
+
+template <int DH, bool TABLE>
+void launch_attention_blocks(int dtype, const Plan& pl, const PagedAttn& a, unsigned nf, unsigned nr, bool one,
+                             hipStream_t s) {
+  const dim3 block(256), grid(nf + nr);
+  if (dtype != VFM_BF16) hipLaunchKernelGGL((attn_f32_kernel<DH, TABLE>), grid, block, 0, s, pl, a);
+#define BF16(R_, F_, O_) hipLaunchKernelGGL((attn_bf16_kernel<DH, R_, F_, O_, TABLE>), grid, block, 0, s, pl, a, (int)nr)
+  else if (nr && nf) BF16(true, true, false);
+  else if (nr) BF16(true, false, false);
+  else if (one || (DH == 64 && nf > 512)) BF16(false, true, true);
+  else BF16(false, true, false);
 #undef BF16
-  } else {
-    BY_DH(attn_f32_kernel, dim3(few * (unsigned)((int64_t)pl.T * a.G / 16 + pl.n_req)));
-  }
-#undef BY_DH
-  prof_end(pi, s);
-  if (split) {
-    pi = prof_begin(VFM_PROF_OTHER, s);
-    const dim3 grid((unsigned)(((int64_t)pl.T * a.H + 3) / 4));
-#define JOIN(T_) \
-  do { if (head_dim == 64) hipLaunchKernelGGL((attn_join_kernel<T_, 64>), grid, dim3(256), 0, s, pl, a); \
-       else hipLaunchKernelGGL((attn_join_kernel<T_, 128>), grid, dim3(256), 0, s, pl, a); } while (0)
-    if (dtype == VFM_BF16) JOIN(bf16); else JOIN(float);
-#undef JOIN
+}
+
+template <int DH, bool TABLE>
+void launch_attention_join(int dtype, const Plan& pl, const PagedAttn& a, int joins, hipStream_t s) {
+  const dim3 block(256), grid((unsigned)((joins + 3) / 4));
+  if (dtype == VFM_BF16) hipLaunchKernelGGL((attn_join_kernel<bf16, DH, TABLE>), grid, block, 0, s, pl, a, joins);
+  else hipLaunchKernelGGL((attn_join_kernel<float, DH, TABLE>), grid, block, 0, s, pl, a, joins);
+}
+
+}  // namespace
+
+hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, int64_t few_blocks,
+                                  int64_t rows_blocks, int64_t joins, bool one, bool table, hipStream_t s) {
+#define BY(F_, ...)                                                                       \
+  do {                                                                                    \
+    if (table) { if (head_dim == 64) F_<64, true>(__VA_ARGS__); else F_<128, true>(__VA_ARGS__); } \
+    else if (head_dim == 64) F_<64, false>(__VA_ARGS__);                                  \
+    else F_<128, false>(__VA_ARGS__);                                                     \
+  } while (0)
+  if (table) {
+    const int pi = prof_begin(VFM_PROF_OTHER, s);
+    hipLaunchKernelGGL(attn_table_kernel, dim3(1), dim3(256), 0, s, pl, a, dtype, const_cast<int32_t*>(a.table));
     prof_end(pi, s);
   }
+  int pi = prof_begin(VFM_PROF_ATTN, s);
+  BY(launch_attention_blocks, dtype, pl, a, (unsigned)few_blocks, (unsigned)rows_blocks, one, s);
+  prof_end(pi, s);
+  if (joins) {
+    pi = prof_begin(VFM_PROF_OTHER, s);
+    BY(launch_attention_join, dtype, pl, a, (int)joins, s);
+    prof_end(pi, s);
+  }
+#undef BY
   return hipGetLastError();
 }

@@ -250,3 +250,45 @@ def test_head_offsets_past_int32_are_refused():
             plan(n_out, tasks)
     host = plan([(1 << 30), (1 << 30) - 1], [0, 1])          # 2^31 - 1 outputs: the last offset still fits
     assert host[6] == (1 << 31) - 1
+
+
+def _ws(a, lens, ctx):
+    host, b = _batch(lens=lens, ctx=ctx, tasks=[0] * len(lens))          # b points into host
+    return B.vfm_attention_workspace(a, b)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dh,dtype,lens,ctx", [
+    (32, 8, 128, B.VFM_BF16, [2048, 1], [0, 20000]), (32, 8, 128, B.VFM_BF16, [8192, 1], [0, 20000]),
+    (32, 8, 128, B.VFM_BF16, [16384, 32], [0, 20000]), (32, 1, 128, B.VFM_BF16, [8192, 1], [0, 100000]),
+    (32, 8, 128, B.VFM_BF16, [8192, 1], [0, 131072]), (8, 1, 128, B.VFM_BF16, [1] * 256, [100] * 255 + [60000]),
+    (32, 32, 128, B.VFM_BF16, [1] * 200 + [4000], [50] * 199 + [4000, 0]), (8, 4, 64, B.VFM_F32, [4096, 1], [0, 20000]),
+    (4, 2, 64, B.VFM_F32, [1000, 70, 1], [0, 9000, 30000])])
+def test_workspace_is_that_of_the_requests(heads, kv_heads, dh, dtype, lens, ctx):
+    """Only requests whose keys are cut need room, each as much as alone: a long context beside prompts or short rows
+    costs its own records (up to twice as much, or 16 MB, where one stride for all is simpler), not a share for
+    every row of the step."""
+    a = _attn(n_heads=heads, n_kv_heads=kv_heads, head_dim=dh, dtype=dtype)
+    alone = sum(_ws(a, [m], [c]) for m, c in set(zip(lens, ctx)) for _ in range(list(zip(lens, ctx)).count((m, c))))
+    both = _ws(a, lens, ctx)
+    assert 0 < both <= 2 * alone + (16 << 20) + 1024 + 64 * (len(lens) + 1)
+    rows = sum(lens) * heads * dh * (2 if dtype == B.VFM_BF16 else 4)
+    assert both <= rows + 2 * alone + (16 << 20)
+
+
+def test_windowed_layer_workspace_beside_a_long_context():
+    """A prompt of 8191 rows and one row at 4000 in the layer: no more than the layer over the whole cache takes."""
+    from paper_2606_09643_amd import runner as R
+    from paper_2606_09643_amd import workloads as wl
+    cfg = R.cfg_for(wl.WORKLOADS[5])
+    cfg.attn = B.VFM_ATTN_MIXED
+    host, b = _batch(lens=[8191, 1], ctx=[0, 4000], tasks=[0, 0])
+    assert B.vfm_workspace_size_windowed(cfg, b, None, 0, 0) <= B.vfm_workspace_size(cfg, b) + (16 << 20)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dtype,lens,ctx", [
+    (64, 1, B.VFM_F32, [70000, 1], [0, 100000]), (64, 1, B.VFM_BF16, [140000, 1], [0, 200000]),
+    (16, 1, B.VFM_BF16, [1] * 70000, [20] * 69999 + [400000]), (32, 32, B.VFM_BF16, [1] * 300000 + [64], [20] * 300001)])
+def test_valid_steps_are_not_refused_for_empty_blocks(heads, kv_heads, dtype, lens, ctx):
+    """A launch holds 2^24 blocks; blocks that a long context's chunks or a prompt would add to the others do not count."""
+    a = _attn(n_heads=heads, n_kv_heads=kv_heads, head_dim=64, dtype=dtype)
+    assert _ws(a, lens, ctx) > 0

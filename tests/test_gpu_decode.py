@@ -621,3 +621,53 @@ def test_sample_large_flat_tails(n, gap):
             assert ck[a] - w[a] - 4 * room - tail <= t <= ck[a] + 4 * room + tail, (u, a, ck[a], t, room)
             ref = np.log(w[a] / ck[-1])
             assert abs(lp[i] - ref) <= 2.0 ** -23 * abs(ref) + 3 * room + tail, (u, lp[i], ref)
+
+
+@pytest.mark.parametrize("dtype,H,KH,dh,window,lens,ctx", [
+    ("bf16", 8, 1, 128, 0, [1] * 130, [20, 30000] + [40] * 127 + [9000]),
+    ("bf16", 32, 8, 64, 0, [700, 1, 2, 40], [0, 20000, 100, 9000]),
+    ("bf16", 32, 8, 128, 0, [5, 600, 1, 1], [30000, 10, 700, 12000]),
+    ("bf16", 16, 16, 64, 6000, [1] * 600 + [33], [90] * 599 + [20000, 9000]),
+    ("f32", 4, 2, 64, 0, [900, 1, 30], [0, 15000, 6000]), ("f32", 16, 2, 128, 0, [300, 2], [10, 12000])])
+def test_attention_long_contexts_beside_others(dtype, H, KH, dh, window, lens, ctx):
+    """Steps whose blocks and records, as rectangles over the longest request's chunks, would be mostly empty: every
+    request has the bits that it has alone, the long ones the 64-bit form's values, and the workspace is that of
+    the requests; replayed from a graph the same."""
+    log(f"long beside others {dtype} H {H} KH {KH} dh {dh} {len(lens)} requests")
+    c = Cache(lens, ctx, KH, dh, 64, window, 2 if window else 0, dtype, seed=13)
+    rng = np.random.default_rng(14)
+    code, td, _ = DT[dtype]
+    sinks = 2 if window else 0
+    q = [np64(torch.from_numpy(rng.standard_normal((m, H, dh), dtype=np.float32)).to(td)) for m in lens]
+    n = len(lens)
+    task = _tasks(n, 5)
+    attn = B.make_attn(code, H, KH, dh, window=window, n_sink=sinks)
+    pb = B.Batch(task, c.lens, 5, ctx_len=c.ctx)
+    size = B.vfm_attention_workspace(attn, pb.c)
+    got = _attend(c, task, H, KH, dh, window, sinks, dtype, q)
+    order = np.argsort(ctx)
+    some = sorted({0, 1, min(2, n - 1), n - 2, n - 1, int(order[-1]), int(order[-2]), int(np.argmax(lens))})
+    alone = 0
+    for i in some:
+        pi = B.Batch(task[i:i + 1], c.lens[i:i + 1], 5, ctx_len=c.ctx[i:i + 1])
+        alone += B.vfm_attention_workspace(attn, pi.c)
+        assert np.array_equal(_attend(c, task, H, KH, dh, window, sinks, dtype, q, only=[i], ws_fill=0)[i], got[i]), i
+    assert 0 < size <= 2 * alone + (16 << 20) + 1024 + 64 * (n + 1)
+    few = {i: got[i] for i in some if lens[i] <= 5 or ctx[i] > 1000}
+    log(f"  {_check(c, few, q, window, sinks, dtype, dh ** -0.5):.3f} of the tolerance")
+    by = np.argsort(task, kind="stable")
+    qd = torch.from_numpy(np.concatenate([q[o].reshape(-1, H * dh) for o in by])).to(td).cuda()
+    eager, out = torch.empty_like(qd), torch.zeros_like(qd)
+    ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    B.vfm_attention_paged(attn, pb.c, qd, c.kv, eager, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.vfm_attention_paged(attn, pb.c, qd, c.kv, out, ws)
+    for i in range(3):
+        out.fill_(float(i))
+        ws.fill_(170 + i)
+        (qd.float() @ qd[:1].float().T).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager), i
