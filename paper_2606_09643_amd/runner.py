@@ -199,9 +199,10 @@ class SamplingParams:
     """How a request's tokens are drawn (vfm_sample_tokens); the defaults
     draw from the whole distribution.  The uniform numbers come from a
     generator of the request's own, one per token, so its tokens do not
-    depend on what else is in the batch."""
+    depend on what else is in the batch.  It starts from `seed`, or without
+    one from the system's entropy, anew for every request."""
 
-    def __init__(self, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, seed=0):
+    def __init__(self, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, seed=None):
         self.temperature, self.top_k, self.top_p, self.min_p = float(temperature), int(top_k), float(top_p), float(min_p)
         if self.top_k < 0 or self.top_k >= 2 ** 31 or not (self.temperature >= 0 and self.top_p >= 0 and self.min_p >= 0):
             raise ValueError("temperature, top_k, top_p and min_p are not negative")

@@ -133,3 +133,19 @@ def test_windows_and_sampling_parameters_are_refused():
                dict(top_p=-0.1), dict(min_p=float("nan"))):
         with pytest.raises(ValueError):
             R.SamplingParams(**kw)
+
+
+def test_requests_without_a_seed_draw_their_own_numbers():
+    """Two requests with the default parameters do not share a run of uniform numbers; a given seed repeats its own."""
+    def numbers(seq):
+        return [float(seq.rng.random(dtype=np.float32)) for _ in range(20)]
+    cb = _batcher(n_pages=32, max_pages=8)
+    same = R.SamplingParams(1.0)
+    for rid, sp in enumerate([R.SamplingParams(), R.SamplingParams(), same, same, R.SamplingParams(seed=3),
+                              R.SamplingParams(seed=3)]):
+        cb.submit(rid, 0, np.zeros(3, np.int32), 2, sampling=sp)
+    runs = [numbers(cb.requests[rid]) for rid in range(6)]
+    for i in range(4):
+        for j in range(i):
+            assert runs[i] != runs[j], (i, j)
+    assert runs[4] == runs[5] == [float(x) for x in np.random.default_rng(3).random(20, dtype=np.float32)]
