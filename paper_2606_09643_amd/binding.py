@@ -524,8 +524,17 @@ def _cache(kv, attn, dtype, device):
     return kv.c
 
 
+def _i32(v, name) -> int:
+    """v as a C int32, which would keep the low bits of anything larger."""
+    n = int(v)
+    if n != v or not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name}: {v} is not a 32-bit integer")
+    return n
+
+
 def make_attn(dtype, n_heads, n_kv_heads, head_dim, window=0, n_sink=0, scale=0.0, rope_theta=0.0) -> vfm_attn:
-    return vfm_attn(dtype, n_heads, n_kv_heads, head_dim, window, n_sink, scale, rope_theta)
+    return vfm_attn(dtype, _i32(n_heads, "n_heads"), _i32(n_kv_heads, "n_kv_heads"), _i32(head_dim, "head_dim"),
+                    _i32(window, "window"), _i32(n_sink, "n_sink"), scale, rope_theta)
 
 
 def vfm_kv_append(attn, batch, qkv, q_out, kv, stream=None):
@@ -566,18 +575,18 @@ def vfm_attention_paged(attn, batch, q, kv, out, workspace=None, stream=None):
 def vfm_workspace_size_windowed(cfg, batch, lora=None, window=0, n_sink=0) -> int:
     n = C.c_size_t()
     st = _lib_handle().vfm_workspace_size_windowed(C.byref(cfg), C.byref(batch),
-                                                   C.byref(lora) if lora is not None else None, int(window),
-                                                   int(n_sink), C.byref(n))
+                                                   C.byref(lora) if lora is not None else None,
+                                                   _i32(window, "window"), _i32(n_sink, "n_sink"), C.byref(n))
     _check(st, "vfm_workspace_size_windowed")
     return n.value
 
 
 def vfm_layer_forward_windowed(cfg, weights, lora, batch, x, kv, window, n_sink, workspace, stream=None):
     """kv: a PagedKV, or a vfm_kv_pages struct built by the caller."""
-    kvc = kv.c if isinstance(kv, PagedKV) else kv
+    kvc, window, n_sink = kv.c if isinstance(kv, PagedKV) else kv, _i32(window, "window"), _i32(n_sink, "n_sink")
     st = _lib_handle().vfm_layer_forward_windowed(C.byref(cfg), C.byref(weights),
                                                   C.byref(lora) if lora is not None else None, C.byref(batch),
-                                                  _ptr(x), C.byref(kvc), int(window), int(n_sink),
+                                                  _ptr(x), C.byref(kvc), window, n_sink,
                                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                                   _stream(stream))
     _check(st, "vfm_layer_forward_windowed")

@@ -149,3 +149,10 @@ def test_requests_without_a_seed_draw_their_own_numbers():
         for j in range(i):
             assert runs[i] != runs[j], (i, j)
     assert runs[4] == runs[5] == [float(x) for x in np.random.default_rng(3).random(20, dtype=np.float32)]
+
+
+def test_windows_that_the_library_refuses_are_refused_up_front():
+    for kw in (dict(window=(1 << 30) + 1), dict(window=1 << 33), dict(window=16, n_sink=(1 << 30) + 1), dict(window=2.5)):
+        with pytest.raises(ValueError):
+            _batcher(**kw)
+    assert _batcher(window=1 << 30, max_step_tokens=64).max_chunk == 64

@@ -292,3 +292,22 @@ def test_valid_steps_are_not_refused_for_empty_blocks(heads, kv_heads, dtype, le
     """A launch holds 2^24 blocks; blocks that a long context's chunks or a prompt would add to the others do not count."""
     a = _attn(n_heads=heads, n_kv_heads=kv_heads, head_dim=64, dtype=dtype)
     assert _ws(a, lens, ctx) > 0
+
+
+@pytest.mark.parametrize("bad", [(1 << 32) + 5, 1 << 31, 1 << 33, -(1 << 32) + 7, 5.5])
+def test_numbers_past_32_bits_are_refused(bad):
+    """A ctypes int32 keeps the low bits of what it is given: 2^32 + 5 would be a window of 5."""
+    for name in ("n_heads", "n_kv_heads", "head_dim", "window", "n_sink"):
+        with pytest.raises((ValueError, TypeError)):
+            _attn(**{name: bad})
+    from paper_2606_09643_amd import runner as R
+    from paper_2606_09643_amd import workloads as wl
+    cfg = R.cfg_for(wl.WORKLOADS[5])
+    cfg.attn = B.VFM_ATTN_MIXED
+    host, b = _batch()
+    for window, n_sink in ((bad, 4), (16, bad)):
+        with pytest.raises((ValueError, TypeError)):
+            B.vfm_workspace_size_windowed(cfg, b, None, window, n_sink)
+        with pytest.raises((ValueError, TypeError)):
+            B.vfm_layer_forward_windowed(cfg, None, None, b, None, None, window, n_sink, None, stream=1)
+    assert B.make_attn(B.VFM_BF16, np.int64(H), KH, DH, window=np.int32(7)).window == 7
