@@ -56,7 +56,8 @@ typedef struct vfm_attn {
  * page table sends to one slot leave either of them there.
  * Errors: VFM_ERR_ARG, VFM_ERR_SHAPE (head layout, ld, a request's pages
  * outside the table or [0, n_pages), ctx + len above 2^30, n_pages *
- * page_size of 2^31 or more), VFM_ERR_UNSUPPORTED (head_dim, group). */
+ * page_size of 2^31 or more), VFM_ERR_UNSUPPORTED (head_dim, group, a step of
+ * 2^24 rows and more). */
 int vfm_kv_append(const vfm_attn* attn, const vfm_batch* batch, const void* qkv, int64_t ld,
                   void* q_out, const vfm_kv_pages* kv, void* stream);
 
@@ -133,7 +134,9 @@ typedef struct vfm_sampling {
  * 2^19 outputs, then 63 - ceil(log2 n): 43 up to 2^20, 33 at 2^30, as many as
  * a 64-bit sum holds) and summed exactly, in any order: a weight below
  * 2^-(s + 1) of the largest counts as 0, and the result does not depend on
- * how the work is split.  VFM_ERR_SHAPE: a request of more than 2^30 outputs. */
+ * how the work is split.
+ * VFM_ERR_SHAPE: a request of more than 2^30 outputs.  VFM_ERR_UNSUPPORTED:
+ * 2^24 requests and more, 2^22 where one has more than 1024 outputs. */
 int vfm_sample_tokens(const vfm_batch* batch, const float* out, const vfm_sampling* sampling,
                       const float* u, int32_t* ids, float* logprob, void* stream);
 

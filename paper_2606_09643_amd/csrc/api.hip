@@ -200,6 +200,7 @@ KvPages pages_of(const vfm_kv_pages* kv) {
 
 // ---- decoding over a bounded cache (vfm_decode.h) ----------------------------
 constexpr int kMaxPos = 1 << 30;
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;   // of a launch
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
@@ -305,8 +306,7 @@ int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, At
   const bool cut = own[TAB_RECS] > 0;
   ap.joins = cut ? (int64_t)pl.T * a.n_heads : 0;
   ap.recs = ap.joins * ap.nchunk();
-  // A launch holds at most 2^32 - 1 threads, 256 a block.
-  const int64_t most = ((int64_t)1 << 24) - 1;
+  const int64_t most = kMaxThreads / 256;                 // blocks
   const int64_t rec_bytes = a.head_dim * 4 + 8;
   const int64_t blocks = ap.few_blocks + ap.rows_blocks, with_work = own[TAB_FEW] + own[TAB_ROWS];
   ap.table = blocks > most || (cut && ((blocks > 3 * with_work && blocks - with_work > TABLE_MIN_EMPTY) ||
@@ -814,6 +814,7 @@ extern "C" int vfm_layer_forward_windowed(const vfm_cfg* cfg, const vfm_layer_we
   if (cfg->attn == VFM_ATTN_BIDIR) return VFM_ERR_UNSUPPORTED;
   const vfm_attn a = attn_of_layer(*cfg, window, n_sink);
   VFM_TRY(check_attn(&a));
+  if ((int64_t)pl.T * APPEND_THREADS > kMaxThreads) return VFM_ERR_UNSUPPORTED;
   VFM_TRY(check_pages(a, batch, pl, kv, true));
   VFM_TRY(check_stream(stream));
   return layer_impl(*cfg, w, lora, batch, pl, x, kv->k, kv->v, kv->n_pages * kv->page_size, pages_of(kv), workspace,
@@ -828,6 +829,7 @@ extern "C" int vfm_kv_append(const vfm_attn* attn, const vfm_batch* batch, const
   VFM_TRY(check_batch(batch, &pl));
   if (!qkv || !q_out || !aligned16(qkv) || !aligned16(q_out)) return VFM_ERR_ARG;
   if (ld % 8 || ld < (int64_t)(attn->n_heads + 2 * attn->n_kv_heads) * attn->head_dim) return VFM_ERR_SHAPE;
+  if ((int64_t)pl.T * APPEND_THREADS > kMaxThreads) return VFM_ERR_UNSUPPORTED;
   VFM_TRY(check_pages(*attn, batch, pl, kv, false));
   VFM_TRY(check_stream(stream));
   hipStream_t s = (hipStream_t)stream;
@@ -880,6 +882,7 @@ extern "C" int vfm_sample_tokens(const vfm_batch* batch, const float* out, const
   int most = 0;
   for (int i = 0; i < pl.n_req; ++i) most = std::max(most, off[i + 1] - off[i]);
   if (most > 1 << 30) return VFM_ERR_SHAPE;
+  if ((int64_t)pl.n_req * sample_threads(most) > kMaxThreads) return VFM_ERR_UNSUPPORTED;
   VFM_TRY(check_stream(stream));
   return hip_status(launch_sample(pl, out, *sampling, u, ids, logprob, most, (hipStream_t)stream));
 }

@@ -110,6 +110,8 @@ __host__ __device__ inline AttnCounts request_counts(int dtype, int m, int H, in
   return c;
 }
 
+constexpr int APPEND_THREADS = 256;  // a block per row
+
 // q_out: rows ldq apart; qkv itself (ldq = ld) to rotate the queries in place, NULL for keys and values only.
 hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv,
                             int64_t ld, void* q_out, int64_t ldq, void* k, void* v, int64_t slots, const KvPages& kp,
@@ -120,6 +122,7 @@ hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_d
 hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, int64_t few_blocks,
                                   int64_t rows_blocks, int64_t joins, bool one, bool table, hipStream_t s);
 
-// max_out: the batch's longest row of head outputs.
+// max_out: the batch's longest row of head outputs; a block of that many threads per request
+inline int sample_threads(int max_out) { return max_out <= 1024 ? 256 : 1024; }
 hipError_t launch_sample(const Plan& pl, const float* out, const vfm_sampling& sp, const float* u, int32_t* ids,
                          float* logprob, int max_out, hipStream_t s);

@@ -151,7 +151,7 @@ __device__ __forceinline__ void put(Vec8<bf16>& x, int i, float f) { x.v[i] = (b
 __device__ __forceinline__ void put(Vec8<float>& x, int i, float f) { x.v[i >> 2][i & 3] = f; }
 
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void kv_append_kernel(Plan pl, int H, int KH, int rotate, double log2_theta,
+__global__ __launch_bounds__(APPEND_THREADS) void kv_append_kernel(Plan pl, int H, int KH, int rotate, double log2_theta,
                                                         const T* qkv, int64_t ld, T* q_out, int64_t ldq,
                                                         T* __restrict__ kc, T* __restrict__ vc, int64_t slots,
                                                         KvPages kp) {
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(Plan pl, int H, int KH, 
   __syncthreads();
   const T* row = qkv + (int64_t)r * ld;
   const int first = q_out != nullptr ? 0 : H * PER;
-  for (int w = first + threadIdx.x; w < (H + 2 * KH) * PER; w += 256) {
+  for (int w = first + threadIdx.x; w < (H + 2 * KH) * PER; w += APPEND_THREADS) {
     const int hh = w / PER, i0 = (w % PER) * 8;
     Vec8<T> a = *reinterpret_cast<const Vec8<T>*>(row + hh * DH + i0);
     Vec8<T> b = *reinterpret_cast<const Vec8<T>*>(row + hh * DH + HALF + i0);
@@ -1214,7 +1214,7 @@ hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_d
   const int rotate = theta > 0.f;
   const double l2 = rotate ? log2((double)theta) : 0.0;
 #define APPEND(T_, D_)                                                                                     \
-  hipLaunchKernelGGL((kv_append_kernel<T_, D_>), dim3(pl.T), dim3(256), 0, s, pl, H, KH, rotate, l2, (const T_*)qkv, ld, \
+  hipLaunchKernelGGL((kv_append_kernel<T_, D_>), dim3(pl.T), dim3(APPEND_THREADS), 0, s, pl, H, KH, rotate, l2, (const T_*)qkv, ld, \
                      (T_*)q_out, ldq, (T_*)k, (T_*)v, slots, kp)
   if (dtype == VFM_BF16) { if (head_dim == 64) APPEND(bf16, 64); else APPEND(bf16, 128); }
   else { if (head_dim == 64) APPEND(float, 64); else APPEND(float, 128); }

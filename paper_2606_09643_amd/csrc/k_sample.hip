@@ -835,7 +835,7 @@ hipError_t launch_sample(const Plan& pl, const float* out, const vfm_sampling& s
   const int pi = prof_begin(VFM_PROF_OTHER, s);
 #define SAMPLE(NT_, W_) \
   hipLaunchKernelGGL((sample_kernel<NT_, W_>), dim3(pl.n_req), dim3(NT_), 0, s, pl, out, q, u, ids, logprob)
-  if (max_out <= 1024) SAMPLE(256, IN_REGS);
+  if (sample_threads(max_out) == 256) SAMPLE(256, IN_REGS);
   else if (max_out <= 32768) SAMPLE(1024, IN_LDS);
   else SAMPLE(1024, IN_MEMORY);
 #undef SAMPLE

@@ -311,3 +311,28 @@ def test_numbers_past_32_bits_are_refused(bad):
         with pytest.raises((ValueError, TypeError)):
             B.vfm_layer_forward_windowed(cfg, None, None, b, None, None, window, n_sink, None, stream=1)
     assert B.make_attn(B.VFM_BF16, np.int64(H), KH, DH, window=np.int32(7)).window == 7
+
+
+def test_batches_larger_than_a_launch_are_refused():
+    """A launch holds 2^32 - 1 threads: steps of 2^24 rows and more (the append's block of 256 threads each) and
+    draws of 2^22 requests from heads of more than 1024 outputs (1024 threads each) are refused before anything runs."""
+    n = 1 << 24
+    host = B.vfm_plan(np.zeros(1, np.int32), np.array([n]), 1, ctx_len=np.array([0]))
+    b = B.vfm_batch(host.ctypes.data_as(C.POINTER(C.c_int32)), PTR, host.size)
+    kv = _kv(np.zeros((1, n // 1024)), page=1024, n_pages=1)
+    assert _append(batch=(host, b), kv=kv) == B.VFM_ERR_UNSUPPORTED
+    from paper_2606_09643_amd import runner as R
+    from paper_2606_09643_amd import workloads as wl
+    cfg = R.cfg_for(wl.WORKLOADS[5])
+    cfg.attn = B.VFM_ATTN_CAUSAL
+    W = B.vfm_layer_weights(*[PTR] * len(B.vfm_layer_weights._fields_))
+    assert B.lib().vfm_layer_forward_windowed(C.byref(cfg), C.byref(W), None, C.byref(b), PTR, C.byref(kv[1]), 16, 0, None,
+                                              0, 1) == B.VFM_ERR_UNSUPPORTED
+    del host, b
+    n = 1 << 22
+    tasks = np.zeros(n, np.int32)
+    tasks[-1] = 1
+    host = B.vfm_plan(tasks, np.ones(n, np.int32), 2, n_out=np.array([2, 1025]))
+    b = B.vfm_batch(host.ctypes.data_as(C.POINTER(C.c_int32)), PTR, host.size)
+    s = B.vfm_sampling(None, None, None, None)
+    assert B.lib().vfm_sample_tokens(C.byref(b), PTR, C.byref(s), PTR, PTR, None, 1) == B.VFM_ERR_UNSUPPORTED
