@@ -336,3 +336,28 @@ def test_batches_larger_than_a_launch_are_refused():
     b = B.vfm_batch(host.ctypes.data_as(C.POINTER(C.c_int32)), PTR, host.size)
     s = B.vfm_sampling(None, None, None, None)
     assert B.lib().vfm_sample_tokens(C.byref(b), PTR, C.byref(s), PTR, PTR, None, 1) == B.VFM_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("window,n_sink,seen", [(20, 0, (5, 6)), (1, 0, (6,)), (16, 0, (5, 6)), (17, 1, (0, 5, 6)),
+                                                (5, 17, (0, 1, 6)), (5, 100, range(7)), (0, 0, range(7))])
+def test_pages_that_no_row_sees_are_not_looked_at(window, n_sink, seen):
+    """One row at position 100 (pages of 16: 0 .. 6) of a windowed layer without a workspace, so that no call gets to a
+    launch: a bad id in a seen page is refused as such, one in any other page is not what the call is refused for."""
+    from paper_2606_09643_amd import runner as R
+    from paper_2606_09643_amd import workloads as wl
+    cfg = R.cfg_for(wl.WORKLOADS[5])
+    cfg.attn = B.VFM_ATTN_MIXED
+    W = B.vfm_layer_weights(*[PTR] * len(B.vfm_layer_weights._fields_))
+    host, b = _batch(lens=(1,), ctx=(100,), tasks=(0,))
+
+    def status(t):
+        t, k = _kv(t)
+        return B.lib().vfm_layer_forward_windowed(C.byref(cfg), C.byref(W), None, C.byref(b), PTR, C.byref(k), window, n_sink,
+                                                  None, 0, None)
+    good = status(np.arange(8).reshape(1, 8))
+    assert good in (B.VFM_ERR_WORKSPACE, B.VFM_ERR_HIP)
+    for j in range(8):
+        for bad in (-1, 50):
+            t = np.arange(8).reshape(1, 8).copy()
+            t[0, j] = bad
+            assert status(t) == (B.VFM_ERR_SHAPE if j in seen else good), (j, bad)
