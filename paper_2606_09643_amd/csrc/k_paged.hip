@@ -462,7 +462,7 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
   __syncthreads();
   float* so = reinterpret_cast<float*>(smem);             // [4][16][DH]
   if (lane < 16) { sm[wave][x] = m_run; sl[wave][x] = l_run; }
-  // only queries that exist: their outputs lie at wave, query, dim
+  // all 16 queries, those past the last (copies of it) among them: their outputs lie at wave, query, dim
 #pragma unroll
   for (int d = 0; d < ND; ++d)
     *reinterpret_cast<f32x4*>(so + (wave * 16 + x) * DH + 16 * d + 4 * g) = o[d];

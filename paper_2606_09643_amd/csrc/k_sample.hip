@@ -289,13 +289,11 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
   }
   const bool any = mn <= mx;                             // some output is no NaN
   // 64 groups up to k = 56 (then some 150 outputs lie above the 56th of them), else 256
-  const int lgg = k <= 56 ? 6 : 8, per_group = NT >> lgg;   // threads per group: 16 or 4 of 1024, 4 or 1 of 256
+  const int lgg = k <= 56 ? 6 : 8, per_group = NT >> lgg;   // threads per group: 16 or 4 of 1024, 4 of 256
   if (small_k) {
     float gm = mx;
-    if (per_group >= 4) {
-      gm = fmaxf(gm, lane_pair<0>(gm));
-      gm = fmaxf(gm, lane_pair<1>(gm));
-    }
+    gm = fmaxf(gm, lane_pair<0>(gm));
+    gm = fmaxf(gm, lane_pair<1>(gm));
     if (per_group >= 16) {
       gm = fmaxf(gm, lane_pair<2>(gm));
       gm = fmaxf(gm, lane_pair<3>(gm));
@@ -452,11 +450,9 @@ __global__ __launch_bounds__(NT) void sample_kernel(Plan pl, const float* __rest
 #pragma unroll
       for (int c = 0; c < 4; ++c) r += (uint32_t)((q[c] > g) | ((q[c] == g) & (j + c < me)));
     }
-    if (per_group > 1) {                                 // at most 256 of 1024 or 64 of 256 threads' groups: within l_rank
-      atomicAdd(&l_rank[me], r);
-      __syncthreads();
-      r = l_rank[me];
-    }
+    atomicAdd(&l_rank[me], r);                           // at most 256 of 1024 or 64 of 256 threads' groups: within l_rank
+    __syncthreads();
+    r = l_rank[me];
     if (tid < groups && r == (uint32_t)k - 1) s_bound = remap ? -INFINITY : g;
     __syncthreads();
     const float bound = s_bound;
