@@ -294,7 +294,7 @@ int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, At
     if (few_rows(a.dtype, m, G)) {
       ap.one = ap.one && n * ck.tiles <= 4;
       ap.few_chunks = std::max(ap.few_chunks, n);
-      if (a.dtype == VFM_BF16) ap.qtiles = std::max(ap.qtiles, few_qtiles(m, G));
+      if (a.dtype == VFM_BF16) ap.qtiles = std::max(ap.qtiles, (int)few_qtiles(m, G));
     } else {
       ap.rows_chunks = std::max(ap.rows_chunks, n);
     }

@@ -80,7 +80,7 @@ constexpr int ROWS_MIN_TILES = 8;
 
 // few-row kernel (bf16; fp32: every request): 16 packed queries per block
 __host__ __device__ inline bool few_rows(int dtype, int m, int G) { return dtype != VFM_BF16 || (int64_t)m * G <= FEW_QUERIES; }
-__host__ __device__ inline int few_qtiles(int m, int G) { return (int)(((int64_t)m * G + 15) / 16); }
+__host__ __device__ inline int64_t few_qtiles(int m, int G) { return ((int64_t)m * G + 15) / 16; }
 // many-row kernel (bf16): blocks of 128 packed queries, 32 a wave
 __host__ __device__ inline int rows_per_block(int G) { return 128 / G; }
 
@@ -88,7 +88,8 @@ __host__ __device__ inline int rows_per_block(int G) { return 128 / G; }
 __host__ __device__ inline Chunks request_chunks(int dtype, int m, int ctx, int G, int KH, int window, int n_sink) {
   if (few_rows(dtype, m, G)) {
     const int tiles = (visible_runs<4>(ctx, ctx + m - 1, window, n_sink).n + 1) / 2;
-    return key_chunks(tiles, KH * few_qtiles(m, G) > 256 ? 256 : KH * few_qtiles(m, G), FEW_MIN_TILES);
+    const int64_t par = KH * few_qtiles(m, G);
+    return key_chunks(tiles, par > 256 ? 256 : (int)par, FEW_MIN_TILES);
   }
   const int rb = rows_per_block(G);
   const int64_t par = (int64_t)KH * ((m + rb - 1) / rb);
@@ -104,7 +105,7 @@ __host__ __device__ inline AttnCounts request_counts(int dtype, int m, int H, in
   const int rb = rows_per_block(G);
   AttnCounts c;
   c.v[TAB_ROWS] = few ? 0 : (int64_t)KH * n * (((int64_t)m + rb - 1) / rb);
-  c.v[TAB_FEW] = few ? (int64_t)KH * n * few_qtiles(m, G) : 0;
+  c.v[TAB_FEW] = few ? KH * n * few_qtiles(m, G) : 0;
   c.v[TAB_RECS] = n > 1 ? (int64_t)m * H * n : 0;
   c.v[TAB_JOIN] = n > 1 ? (int64_t)m * H : 0;
   return c;

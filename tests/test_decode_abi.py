@@ -338,6 +338,21 @@ def test_batches_larger_than_a_launch_are_refused():
     assert B.lib().vfm_sample_tokens(C.byref(b), PTR, C.byref(s), PTR, PTR, None, 1) == B.VFM_ERR_UNSUPPORTED
 
 
+@pytest.mark.parametrize("m,G,KH", [(1 << 30, 64, 1), (1 << 30, 64, 16), (1 << 30, 1, 64), (1 << 26, 64, 16),
+                                    ((1 << 30) - 1, 7, 100)])
+@pytest.mark.parametrize("dtype", [B.VFM_F32, B.VFM_BF16])
+def test_requests_of_any_length_have_a_plan(m, G, KH, dtype):
+    """Rows times heads past 2^32 are refused, or need no workspace, without a fault of the host.  (Of the plan only the
+    header and the arrays per request are read, so the arrays per row need not exist.)"""
+    host = np.zeros(64, np.int32)
+    host[:3] = 1, 1, m
+    host[B.VFM_PLAN_HEADER + 3] = m                              # cu_seqlens[1], behind order[1] and task[1]
+    b = B.vfm_batch(host.ctypes.data_as(C.POINTER(C.c_int32)), PTR, 1 << 34)
+    n = C.c_size_t()
+    st = B.lib().vfm_attention_workspace(C.byref(_attn(dtype=dtype, n_heads=G * KH, n_kv_heads=KH)), C.byref(b), C.byref(n))
+    assert (st, n.value) in ((B.VFM_OK, 0), (B.VFM_ERR_UNSUPPORTED, 0))
+
+
 @pytest.mark.parametrize("window,n_sink,seen", [(20, 0, (5, 6)), (1, 0, (6,)), (16, 0, (5, 6)), (17, 1, (0, 5, 6)),
                                                 (5, 17, (0, 1, 6)), (5, 100, range(7)), (0, 0, range(7))])
 def test_pages_that_no_row_sees_are_not_looked_at(window, n_sink, seen):
