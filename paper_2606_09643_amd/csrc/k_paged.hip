@@ -140,7 +140,7 @@ __device__ __forceinline__ int page_slot(page_row prow, int lp, int k) {
 // their fraction in fp32.
 // 32 prompts of 128 to 1024 tokens, 32 heads of 128 on 32: 178 us, 5.2 TB/s (a
 // copy of 2 GiB runs at 4.95).  Blocks of 8 rows by 12 heads, which write longer
-// runs into a page, take the same.  One row: 4.3 us, all latency.
+// runs into a page, take the same.  One row: 2.8 us by kernel trace, all latency.
 // ---------------------------------------------------------------------------
 template <typename T> struct Vec8;
 template <> struct Vec8<bf16> { bf16x8 v; };
@@ -239,9 +239,11 @@ __device__ __forceinline__ int64_t out_row(const PagedAttn& a, int R0, int h, in
 // through a wave-private LDS tile that the transposing LDS read turns into the
 // V^T operand; a tile's loads are issued while the tile before is computed, which
 // takes half the registers (see SINGLE below for where it does not pay).
+// A weight is rounded to bf16, by at most 2^-8 of itself, for the product alone; the
+// sum that divides is of the weights as they are, which costs nothing here.
 // 256 requests with up to 1028 visible keys, 32 heads of 128 on 32: 598 us, 6.3
-// TB/s; 8 requests of 32768 to 131072, 32 heads on 8: 390 us, 6.5 TB/s.  One row
-// after 300 keys: 9.4 us, the latency of a few dependent loads.
+// TB/s; 8 requests of 32768 to 131072, 32 heads on 8: 388 us, 6.5 TB/s.  One row
+// after 300 keys: 8.9 us, the latency of a few dependent loads.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -504,15 +506,17 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
 // LDS stages by turns (global_load_lds, one barrier per tile).  A wave-wide load
 // takes whole rows of one 16-position run, whose page it looks up as a scalar, a
 // tile ahead of the load.
-// Bound by LDS reads: every wave reads the whole tile for its 32 queries, and with
-// head dim 128 the 8 waves of a CU read 256 KB per tile, 4096 of its 4500 cycles
-// at 64 bytes each; the matrix cores are busy for 40%.  Blocks of 8 waves, which
-// halve the fills but not the reads, gain nothing (587 us for the 585 below, 169
-// for 151 with head dim 64); 64 queries per wave, which would halve the reads, do
-// not fit the registers.  With head dim 64, four stages instead of two keep a third
-// block off the CU (250 us for 240: 8 prompts of 4096, window 1024, 16 heads on 4).
+// No unit is at its limit: by counters (head dim 128) the matrix cores are busy for 45% of
+// the cycles, the vector ALU for 38 and LDS for 23 (no bank conflicts), and 28% of the
+// waves' time is waiting.  Two waves per SIMD, all that the registers of head dim 128
+// allow, take the two pipes by turns more than side by side.  Blocks of 8 waves, which
+// halve the fills, gain nothing (587 us for 585, 169 for 151 with head dim 64); 64
+// queries per wave, which would halve the LDS reads, do not fit the registers.  With head
+// dim 64 four stages take longer than two (250 us for 240); its 160 registers would
+// let a third wave onto a SIMD, which the kernel's attribute does not.
 // 4 chunks of 1900 to 2048 rows after 3000 to 9000, window 4096, 32 heads of 128 on
-// 8: 585 us, 900 TFLOP/s of visible products (a large matrix product: 1370).
+// 8: 575 us, 920 TFLOP/s of visible products (a large matrix product: 1370).  8 prompts
+// of 4096, window 1024, 16 heads of 64 on 4: 200 us, 600 TFLOP/s.
 // ---------------------------------------------------------------------------
 typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
@@ -760,7 +764,8 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
     for (int i = 0; i < 8; ++i) e[i] = fast_exp2(fmaf(st[u >> 1][8 * (u & 1) + i], a.scale_log2, neg_m));
     pf[u] = pack8(e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]);
   };
-  // their sum, of the rounded weights that the products use, and the products
+  // Their sum, of the weights rounded to bf16 that the products use (two to an instruction; and what rounding
+  // adds to all weights of a row divides out), and the products
   auto products = [&](auto b, const bf16x8 (&pf)[4]) {
 #pragma unroll
     for (int u = 0; u < 4; ++u)
@@ -906,13 +911,15 @@ __device__ __forceinline__ void rows_block(const Plan& pl, const PagedAttn& a, i
 
 // rows_blocks blocks of the many-row kind (ROWS), then, with FEW, those of the few-row kind: a step's
 // single rows run beside its prompts, on the CUs that these leave free.  24 requests of 64 to 2000
-// positions, 5 of them with up to 250 rows, 16 heads of 64: 31.5 us, as two launches 45.7.
+// positions, 5 of them with up to 250 rows, 16 heads of 64: 28.5 us (31.5 when two launches took 45.7).
 // SINGLE (no rows): without registers for a second tile 4 blocks share a CU instead of 2, and other blocks'
 // work hides a block's start and its loads.  It is taken where no few-row request has more than 128 keys
-// (a tile per wave): 256 rows of 70 to 120 keys, 32 heads of 128: 76 us, else 108; of 30 to 60 keys: 60 and
-// 80; one row of 100 keys: 7.5 and 7.4.  With head dim 64 also where there are more blocks than 2 per CU:
-// 256 rows of 200 to 2000 keys, 16 heads: 209 us and 232; one row of 3000 keys, with its few blocks, would
-// take 13.3 instead of 12.5.  With head dim 128 a loop of single tiles spills at 4 blocks (954 us for 598)
+// (a tile per wave): 256 rows of 70 to 120 keys, 32 heads of 128: 72 us, else 108; of 30 to 60 keys: 60 and
+// 80; one row of 100 keys: 7.5 and 7.4.  With head dim 64 also where the launch has more blocks than 2 per CU,
+// those that find no work among them, as they take places, too: 16 heads, 256 rows of 200 to 2000 keys
+// 177 us and 206, 64 of 8000 331 and 333, 3 of 80 to 200 beside one of 60000 47 and 67; 16 of 60000, the worst
+// found, 597 and 585.  With few blocks the loads in flight count: 16 rows of 130 to 400 keys (256 blocks) would
+// take 8.8 instead of 8.0.  With head dim 128 a loop of single tiles spills at 4 blocks (954 us for 598)
 // and gains nothing at 3.  The order of a row's sums is the same in both.
 template <int DH, bool ROWS, bool FEW, bool SINGLE, bool TABLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SINGLE ? 4 : 2, SINGLE ? 4 : 2))) void attn_bf16_kernel(
@@ -935,9 +942,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SINGLE ? 4 
 // 4 x .. 4 x + 3 of its key's V row gives MFMA c row x of tile c = head dim
 // 4 x + c, which leaves a lane with 16 consecutive head dims of its query.
 // Every K and V element is read once per 16 queries, from L2 for the later ones.
-// 64 rows after 2000 keys, 16 heads of 64: 199 us, 5.3 TB/s.  8 chunks of 512 rows
-// after 1000: 269 us, 79 TFLOP/s (a large fp32 matrix product: 154): bound by the
-// operand loads, which no other block's queries share through LDS.
+// 64 rows after 2000 keys, 16 heads of 64: 188 us, 5.6 TB/s.  8 chunks of 512 rows
+// after 1000: 225 us, 94 TFLOP/s (a large fp32 matrix product: 154): each 16 queries
+// load all of their K and V from L2, which no other block's queries share through LDS.
 // ---------------------------------------------------------------------------
 template <int DH, bool TABLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attn_f32_kernel(Plan pl, PagedAttn a) {

@@ -3,12 +3,12 @@
 // served with long-lived decode iterations; the outputs are a task's LM head's).
 //
 // Weights.  w_j = 2^t_j, t_j = (l_j - M) log2(e) / T <= 0, in fp64 (at full rate
-// here: 12 fused multiply-adds of a Taylor series after the split of t into
-// its nearest integer and a rest of at most 1/2), rounded to 2^-44 (rows of more than
-// 2^19 outputs: to what a 64-bit sum of them holds): the sums are then integers, exact in any order, so the order of atomics, the split over
-// threads and the block's shape cannot change a result.  fp32 would shift the
-// borders of the running sum by 1e-7 of it, and a vocabulary has so many of
-// them that the token drawn would now and then be another.
+// here: 11 fused multiply-adds of a polynomial after the split of t into its nearest
+// integer and a rest of at most 1/2), rounded to 2^-44 (rows of more than 2^19 outputs:
+// to what a 64-bit sum of them holds): the sums are then integers, exact in any
+// order, so the order of atomics, the split over threads and the block's shape cannot
+// change a result.  fp32 would shift the borders of the running sum by 1e-7 of it, and a
+// vocabulary has so many of them that the token drawn would now and then be another.
 //
 // The three filters each keep a prefix of the outputs in descending order (ties
 // by index), so only the last kept output has to be found, never a full order:
@@ -20,9 +20,10 @@
 //
 // Bound by the weights' fp64 work, 19 instructions each on the one CU that a row
 // has, and by the latency of the block's steps; bytes would allow 7 us for 256 rows
-// of 32000.  Measured, 256 rows of 32000: greedy 9.2 us, no filter 17.5, top-k 40
-// 14.5, top-k 199 26.6, top-k 1000 30.4, top-p 0.9 29, with min-p 35.  48 rows of
-// 100003 (48 of 256 CUs): no filter 31.5, top-p 0.9 58.5.  256 rows of 700: 2.8 to 8.
+// of 32000.  Measured, 256 rows of 32000: greedy 7.1 us, no filter 15.2, top-k 40
+// 12.2, top-k 199 24.1, top-k 1000 27.8, top-p 0.9 26, with min-p 31.  One such row: 5.8
+// to 26.  48 rows of 100003 (48 of 256 CUs): no filter 30.3, top-p 0.9 54.3.  256 rows of
+// 700: 6 (a call) to 11.2.
 // Several blocks per row would need a second launch and scratch memory from the caller.
 #include <type_traits>
 
