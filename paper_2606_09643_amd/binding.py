@@ -204,10 +204,14 @@ def _ptr(t) -> int | None:
     return int(t)
 
 
+# the current stream's handle alone: building torch.cuda.current_stream()'s object takes 2.6 us, as long as a launch
+_RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # not part of torch's public interface
+
+
 def _stream(stream, device=None) -> int:
     if stream is None:
-        # the handle alone: building torch.cuda.current_stream()'s object takes 2.6 us, as long as a launch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device.index)
+        index = torch.cuda.current_device() if device is None else device.index
+        return torch.cuda.current_stream(index).cuda_stream if _RAW_STREAM is None else _RAW_STREAM(index)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
