@@ -216,14 +216,7 @@ __device__ __forceinline__ int pair_key(int ks, int x) {  // key of row x of sub
 // hides the per-step staging and barriers of the others.
 // ---------------------------------------------------------------------------
 // V tile row-major in LDS ([64 keys][DH] bf16) with 32-byte segments
-// swizzled per row: segment s of key row r sits at s ^ vswz(r).  vswz makes
-// the transposing reads below bank-conflict free (each 32-lane half of a read
-// touches 8 rows, one 32-byte segment each, spread over all 64 banks) and is
-// a permutation within the row, so the row stores stay conflict-free too.
-template <int DH>
-__device__ __forceinline__ int vswz(int r) {
-  return DH == 128 ? ((r & 3) | (((r >> 3) & 1) << 2)) : (((r >> 1) & 1) | (((r >> 3) & 1) << 1));
-}
+// swizzled per row: segment s of key row r sits at s ^ vswz(r).
 // physical 16-byte chunk of logical chunk ch (head dims 8 ch .. 8 ch + 7) of row r
 template <int DH>
 __device__ __forceinline__ int vswz_chunk(int r, int ch) {

@@ -249,13 +249,7 @@ __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const 
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// V rows of a few-row tile in LDS, [32][DH]: the 32-byte segments of row r
-// swizzled so that the transposing reads (each 32-lane half: 8 rows, one segment
-// each) spread over all banks; a row's stores stay one contiguous run.
-template <int DH>
-__device__ __forceinline__ int few_vswz(int r) {
-  return DH == 128 ? ((r & 3) | (((r >> 3) & 1) << 2)) : (((r >> 1) & 1) | (((r >> 3) & 1) << 1));
-}
+// V rows of a few-row tile lie in LDS as [32][DH], their segments swizzled by vswz.
 
 // smem: 256 DH bytes, V tiles, then the waves' outputs.  SINGLE: one tile at a time in registers, with head dim
 // 128 the wave's only one.
@@ -346,7 +340,7 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
 
   const int vst_ch = lane % LPR, vst_row = lane / LPR;
   const int vrow = 8 * g + (x >> 2);
-  const int vbase = vrow * DH * 2 + (few_vswz<DH>(vrow) << 5) + (x & 3) * 8;
+  const int vbase = vrow * DH * 2 + (vswz<DH>(vrow) << 5) + (x & 3) * 8;
 
   auto compute = [&](int b, int t) {
     const int p0 = run_pos(t, 0);
@@ -363,7 +357,7 @@ __device__ __forceinline__ void few_block(const Plan& pl, const PagedAttn& a, in
         if (!seen_by_any(j0, j1, k, a.window, a.n_sink)) v = bf16x8{};
         else if (j0 != j1 && !seen_by_all(j0, j1, k, k, a.window, a.n_sink)) v = drop_nonfinite(v, poison);
       }
-      *reinterpret_cast<bf16x8*>(Vs + r * DH + ((((vst_ch >> 1) ^ few_vswz<DH>(r)) << 1) | (vst_ch & 1)) * 8) = v;
+      *reinterpret_cast<bf16x8*>(Vs + r * DH + ((((vst_ch >> 1) ^ vswz<DH>(r)) << 1) | (vst_ch & 1)) * 8) = v;
     }
     wave_lds_order();
     // S^T

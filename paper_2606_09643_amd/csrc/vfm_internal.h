@@ -320,6 +320,15 @@ hipError_t launch_gemm_skinny(const SkinnyArgs& a, hipStream_t s);
 inline bool skinny_takes_shrink(int M) { return M <= 64; }
 int skinny_splits(int N, int K);
 
+// Swizzle of the 32-byte segments of a V row in LDS ([keys][DH] bf16), for the
+// transposing reads: each 32-lane half of one touches 8 rows, one segment each,
+// which come to lie in different banks; a permutation within the row, so the
+// row's stores stay one conflict-free run.
+template <int DH>
+__device__ __forceinline__ int vswz(int r) {
+  return DH == 128 ? ((r & 3) | (((r >> 3) & 1) << 2)) : (((r >> 1) & 1) | (((r >> 3) & 1) << 1));
+}
+
 // Where the K / V of token k of plan position p live in a head-major cache:
 // slot kv_start[p] + k, or with a page table (original request order,
 // max_pages columns) slot table[order[p]][k >> log2_page] pages in.
