@@ -88,8 +88,9 @@ __host__ __device__ inline int rows_per_block(int G) { return 128 / G; }
 __host__ __device__ inline Chunks request_chunks(int dtype, int m, int ctx, int G, int KH, int window, int n_sink) {
   if (few_rows(dtype, m, G)) {
     const int tiles = (visible_runs<4>(ctx, ctx + m - 1, window, n_sink).n + 1) / 2;
-    const int64_t par = KH * few_qtiles(m, G);
-    return key_chunks(tiles, par > 256 ? 256 : (int)par, FEW_MIN_TILES);
+    const int64_t qt = few_qtiles(m, G);
+    const int par = KH * (qt > 256 ? 256 : (int)qt);
+    return key_chunks(tiles, par > 256 ? 256 : par, FEW_MIN_TILES);
   }
   const int rb = rows_per_block(G);
   const int64_t par = (int64_t)KH * ((m + rb - 1) / rb);
