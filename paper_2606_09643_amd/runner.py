@@ -272,7 +272,8 @@ class ContinuousBatcher:
         self.bfq, self.record, self.token_time = bfq, record, float(token_time)
         # prompt chunks after cached tokens run on the bf16 path only, under a window in fp32 too
         self.chunk = (w.dtype == "bf16" or window is not None) if chunk_prompts is None else bool(chunk_prompts)
-        if window is not None and (window != int(window) or not 1 <= window <= 2 ** 30 or not 0 <= n_sink <= 2 ** 30):
+        if window is not None and not (1 <= window <= 2 ** 30 and 0 <= n_sink <= 2 ** 30
+                                       and window == int(window) and n_sink == int(n_sink)):
             raise ValueError("window: 1 .. 2^30 positions, n_sink: 0 .. 2^30")
         self.window, self.n_sink = (int(window), int(n_sink)) if window is not None else (None, 0)
         if max_chunk is None:

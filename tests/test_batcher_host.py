@@ -152,7 +152,8 @@ def test_requests_without_a_seed_draw_their_own_numbers():
 
 
 def test_windows_that_the_library_refuses_are_refused_up_front():
-    for kw in (dict(window=(1 << 30) + 1), dict(window=1 << 33), dict(window=16, n_sink=(1 << 30) + 1), dict(window=2.5)):
+    for kw in (dict(window=(1 << 30) + 1), dict(window=1 << 33), dict(window=16, n_sink=(1 << 30) + 1), dict(window=2.5),
+               dict(window=float("inf")), dict(window=float("nan")), dict(window=16, n_sink=0.5)):
         with pytest.raises(ValueError):
             _batcher(**kw)
     assert _batcher(window=1 << 30, max_step_tokens=64).max_chunk == 64
