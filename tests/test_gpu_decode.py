@@ -671,3 +671,36 @@ def test_attention_long_contexts_beside_others(dtype, H, KH, dh, window, lens, c
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager), i
+
+
+def test_attention_of_a_step_that_fills_a_launch():
+    """300000 single rows beside a prompt, 32 heads of 64: 9.6 million blocks, which as rectangles with the prompt's
+    would be more than a launch holds.  All requests read the same page, so every row has the bits of one alone."""
+    H = KH = 32
+    dh, page, n = 64, 16, 300000
+    rng = np.random.default_rng(3)
+    kp, vp = [torch.from_numpy(rng.standard_normal((KH, 5 * page, dh), dtype=np.float32)).to(torch.bfloat16).cuda() for _ in range(2)]
+    attn = B.make_attn(B.VFM_BF16, H, KH, dh)
+    row = torch.from_numpy(rng.standard_normal((65, H * dh), dtype=np.float32)).to(torch.bfloat16).cuda()
+
+    def run(lens, ctx, q):
+        lens, ctx = np.asarray(lens, np.int32), np.asarray(ctx, np.int32)
+        pb = B.Batch(np.zeros(len(lens), np.int32), lens, 1, ctx_len=ctx)
+        table = np.zeros((len(lens), 5), np.int32)
+        table[-1] = np.arange(5)
+        ws = torch.empty(max(1, B.vfm_attention_workspace(attn, pb.c)), dtype=torch.uint8, device="cuda")
+        out = torch.full_like(q, 9.0)
+        B.vfm_attention_paged(attn, pb.c, q, B.PagedKV(kp, vp, page, table), out, ws)
+        torch.cuda.synchronize()
+        return out, ws.numel()
+    log("a step that fills a launch")
+    one, _ = run([1, 64], [15, 0], row)
+    many, size = run([1] * n + [64], [15] * n + [0], torch.cat([row[:1].expand(n, -1), row[1:]]))
+    assert size >= 16 * (n + 2)
+    assert torch.equal(many[:n], one[:1].expand(n, -1)) and torch.equal(many[n:], one[1:])
+    k, v = [np64(t[:, :page]).transpose(1, 0, 2) for t in (kp, vp)]
+    q = np64(row[:1]).reshape(1, H, dh)
+    ref, a, _ = D.attention(q, k, v, page - 1, 0, 0, dh ** -0.5)
+    dot = D.score_sizes(q, k, dh ** -0.5)[:, :, None]
+    tol = 2.0 ** -8 * (a + np.abs(ref)) + (page + 16) * 2.0 ** -24 * (a + np.abs(ref)) + a * 2 * ((dh + 2) * 2.0 ** -24 * dot + 2.0 ** -22)
+    assert np.all(np.abs(np64(one[:1]).reshape(1, H, dh) - ref) <= tol)

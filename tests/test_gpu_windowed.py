@@ -463,3 +463,19 @@ def test_pages_past_32_bit_offsets_and_shared_by_requests(dtype, lens):
             + a * 2 * ((dh + 2) * 2.0 ** -24 * dot + 2.0 ** -22)
         assert np.all(np.abs(o[at:at + m].reshape(m, H, dh) - ref) <= lim)
         at += m
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_windowed_layer_long_context_beside_a_prompt(dtype):
+    """One row at 12000 with everything visible beside a prompt of 600 rows and a chunk: the step's workspace holds the
+    long row's partial results, not the same number for every row."""
+    w = _decoder(dtype, 64, d=1024)
+    lens, ctx, task = [600, 1, 20], [0, 12000, 50], [1, 0, 2]
+    cfg = R.cfg_for(w)
+    cfg.attn = B.VFM_ATTN_MIXED
+
+    def size(at):
+        pb = B.Batch(np.array(task, np.int32), np.array(lens, np.int32), w.n_tasks, ctx_len=np.array([0, at, 50], np.int32))
+        return B.vfm_workspace_size_windowed(cfg, pb.c, None, 0, 0)
+    assert size(12000) <= size(100) + (16 << 20)
+    _run_layer(w, lens, ctx, task, 64, 0, 0, rows=6)
