@@ -1,0 +1,614 @@
+"""The operators of decoding over a KV cache held in 8 bits and of constrained draws, as a user calls them,
+and their plain forms: the rotary append of new keys and values to the 8-bit cache, attention of new tokens over it,
+and penalties, biases and masks on the head outputs.
+
+A case is a dict of plain values.  ``op`` is what is run:
+
+  append8  q and k of new rows rotated, k and v rounded to e4m3 codes under a power-of-two scale per 16 positions and head
+  attend8  new rows (one or many per request) over their requests' pages of that cache
+  adjust   head outputs under repetition, presence and frequency penalties, biases and masks of allowed outputs
+
+Requests' lengths, contexts, tasks and head sizes follow from the case alone (``comp`` seeds them); activations,
+caches, page orders, histories and masks from the seed.  Rows are in plan order (requests sorted by task, ties in
+arrival order), page tables and per-request values in arrival order.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+DEV = "cuda"
+RUN = 16                       # positions that share a scale
+TOP = 1.875 * 2.0 ** 127       # magnitudes above are taken as this
+
+
+# ---------------------------------------------------------------------------
+# cases
+# ---------------------------------------------------------------------------
+def _append(name, n_req, lo, hi, clo, chi, heads, kv_heads, dh, page, dtype="bf16", theta=10000.0, comp=1):
+    return {"name": name, "op": "append8", "n_req": n_req, "lo": lo, "hi": hi, "clo": clo, "chi": chi,
+            "heads": heads, "kv_heads": kv_heads, "dh": dh, "page": page, "dtype": dtype, "theta": theta,
+            "comp": comp}
+
+
+def _attend(name, n_req, lo, hi, clo, chi, heads, kv_heads, dh, page, window, sinks, dtype="bf16", chunks=-1,
+            comp=1):
+    """chunks: how many requests bring lo..hi rows, the others one (-1: all)."""
+    return {"name": name, "op": "attend8", "n_req": n_req, "lo": lo, "hi": hi, "clo": clo, "chi": chi,
+            "heads": heads, "kv_heads": kv_heads, "dh": dh, "page": page, "window": window, "sinks": sinks,
+            "dtype": dtype, "chunks": chunks, "comp": comp}
+
+
+def _adjust(name, n_req, lo, hi, hlo, hhi, biases, masked, in_place, comp=1):
+    """lo..hi outputs and hlo..hhi earlier tokens a request, up to `biases` biases each; masked: the share of the
+    requests with a mask of allowed outputs; in_place: the outputs themselves are changed."""
+    return {"name": name, "op": "adjust", "n_req": n_req, "lo": lo, "hi": hi, "hlo": hlo, "hhi": hhi,
+            "biases": biases, "masked": masked, "in_place": in_place, "comp": comp}
+
+
+def listed():
+    return [
+        # one user's decode step of the 7B decoder: the smallest append, all latency
+        _append("append8-1", 1, 1, 1, 1500, 1500, 32, 32, 128, 64),
+        # the 7B decoder's prompt batch goes to the cache: the largest append
+        _append("append8-prompts-32", 32, 128, 1024, 0, 0, 32, 32, 128, 64),
+        # one user's decode step early in a conversation: the smallest attention
+        _attend("attend8-decode-1", 1, 1, 1, 300, 300, 32, 32, 128, 64, 0, 0),
+        # the full decode step of the 7B decoder, a window of 1024 and 4 sinks
+        _attend("attend8-decode-256", 256, 1, 1, 256, 2048, 32, 32, 128, 64, 1024, 4),
+        # a few users deep in long documents, four query heads to a key head, everything visible
+        _attend("attend8-decode-long-8", 8, 1, 1, 32768, 131072, 32, 8, 128, 256, 0, 0),
+        # a continuous-batching step of 64-wide heads: decode rows beside prompt chunks
+        _attend("attend8-mixed-24", 24, 40, 250, 64, 2000, 16, 16, 64, 16, 512, 4, chunks=5),
+        # long prompts fed in chunks behind a window: the largest work of all
+        _attend("attend8-chunk-4x2048", 4, 1900, 2048, 3000, 9000, 32, 8, 128, 64, 4096, 4),
+        # the fp32 encoder's head shape, ragged chunks and single rows
+        _attend("attend8-f32-9", 9, 3, 120, 0, 700, 4, 2, 64, 32, 200, 1, dtype="f32", chunks=6),
+        # one user's penalties in the middle of a conversation, the outputs changed where they are: the smallest
+        _adjust("adjust-1x32000", 1, 32000, 32000, 700, 700, 4, 0.0, True),
+        # the decode batch over the vocabulary, a few of its requests held to a grammar, changed in place
+        _adjust("adjust-256x32000", 256, 32000, 32000, 200, 4000, 16, 0.25, True),
+        # per-task heads of all sizes in one batch, the outputs as they were kept beside
+        _adjust("adjust-tasks-256", 256, 2, 1000, 0, 300, 3, 0.5, False),
+        # a large vocabulary of odd size behind long documents, every request held to a grammar, outputs kept
+        _adjust("adjust-48x100003", 48, 100003, 100003, 5000, 60000, 300, 1.0, False),
+    ]
+
+
+def _log(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.49)))))))
+
+
+def draw(rng):
+    op = rng.choice(("append8", "attend8", "attend8", "adjust"))
+    comp = rng.randrange(1, 1 << 30)
+    if op == "adjust":
+        n = _log(rng, 1, 256)
+        hi = _log(rng, 2, 100003)
+        while n * hi > 256 * 32000:
+            n = max(1, n // 2)
+        hhi = rng.choice((0, _log(rng, 1, 60000), _log(rng, 1, 60000)))
+        while n * hhi > 3000000:
+            hhi = hhi * 2 // 3
+        c = _adjust("", n, rng.choice((hi, _log(rng, 1, hi))), hi, rng.randint(0, hhi), hhi,
+                    rng.choice((0, 1, _log(rng, 1, 300))), rng.choice((0.0, 0.3, 1.0)), rng.random() < 0.5, comp)
+        return {k: v for k, v in c.items() if k != "name"}
+    dh = rng.choice((64, 128))
+    kv_heads = rng.choice((1, 2, 4, 8, 16, 32))
+    group = rng.choice([g for g in (1, 1, 2, 4, 7, 8) if g * kv_heads * dh <= 8192])
+    heads = group * kv_heads
+    page = rng.choice((16, 32, 64, 128, 1024))
+    dtype = rng.choice(("bf16", "bf16", "bf16", "f32"))
+    if op == "append8":
+        n = _log(rng, 1, 200)
+        lo = 1 if rng.random() < 0.5 else _log(rng, 1, 600)
+        hi = lo if lo == 1 else rng.randint(lo, 600)
+        es = 2 if dtype == "bf16" else 4
+        while n > 1 and n * (lo + hi) // 2 * (heads + 2 * kv_heads) * dh * es > 450e6:
+            n = n // 2
+        c = _append("", n, lo, hi, 0, rng.choice((0, 500, 5000)), heads, kv_heads, dh, page, dtype,
+                    rng.choice((0.0, 10000.0, 500000.0)), comp)
+    else:
+        window = rng.choice((0, _log(rng, 1, 4096), _log(rng, 16, 4096)))
+        sinks = rng.choice((0, 1, 4, _log(rng, 1, 100))) if window else 0
+        kind = rng.choice(("decode", "decode", "chunk", "mixed"))
+        if kind == "decode":
+            n = _log(rng, 1, 256)
+            clo = _log(rng, 1, 60000)
+            chi = rng.randint(clo, max(clo, min(131072, 3 * clo)))
+            c = _attend("", n, 1, 1, clo, chi, heads, kv_heads, dh, page, window, sinks, dtype, -1, comp)
+        else:
+            n = _log(rng, 1, 8 if kind == "chunk" else 32)
+            hi = _log(rng, 2, 2048 if kind == "chunk" else 256)
+            chi = rng.choice((0, _log(rng, 1, 12000)))
+            c = _attend("", n, rng.randint(1, hi), hi, 0, chi, heads, kv_heads, dh, page, window, sinks, dtype,
+                        -1 if kind == "chunk" else max(1, n // 4), comp)
+        while True:
+            big = work(c)
+            flops = 4e11 if dtype == "bf16" else 4e10
+            lens, ctx = _lengths(c)
+            span = int((_span(c, lens, ctx)[2]).max())
+            pad = c["n_req"] * span * (kv_heads * dh + heads * int(lens.max()))    # the plain form's padded values
+            if big["bytes"] <= 1e9 and big["flops"] <= flops and pad <= 2e9 and int((ctx + lens).sum()) <= 1200000:
+                break
+            if c["n_req"] > 1:
+                c["n_req"] = c["n_req"] * 2 // 3
+                c["chunks"] = min(c["chunks"], c["n_req"])
+            else:
+                c["lo"], c["hi"] = max(1, c["lo"] * 2 // 3), max(1, c["hi"] * 2 // 3)
+                c["clo"], c["chi"] = c["clo"] * 2 // 3, c["chi"] * 2 // 3
+    return {k: v for k, v in c.items() if k != "name"}
+
+
+def _rng(case, what):
+    return np.random.default_rng([case["comp"], what])
+
+
+def _lengths(case):
+    """(new rows, cached tokens) of each request, arrival order."""
+    r, n = _rng(case, 1), case["n_req"]
+    lens = r.integers(case["lo"], case["hi"] + 1, n)
+    chunks = case.get("chunks", -1)
+    if chunks >= 0:
+        one = r.permutation(n)[chunks:]
+        lens[one] = 1
+    ctx = r.integers(case["clo"], case["chi"] + 1, n)
+    return lens.astype(np.int64), ctx.astype(np.int64)
+
+
+def _tasks(case):
+    return _rng(case, 2).integers(0, _n_tasks(case), case["n_req"]).astype(np.int32)
+
+
+def _n_tasks(case):
+    return max(1, min(128, case["n_req"] // 2))
+
+
+def _sizes(case):
+    """Head outputs of each request (one task per request), arrival order."""
+    return _rng(case, 3).integers(case["lo"], case["hi"] + 1, case["n_req"]).astype(np.int64)
+
+
+def _histories(case):
+    """(earlier tokens, biases, has a mask) of each request, arrival order."""
+    r, n = _rng(case, 4), case["n_req"]
+    hist = r.integers(case["hlo"], case["hhi"] + 1, n).astype(np.int64)
+    biases = r.integers(0, case["biases"] + 1, n).astype(np.int64)
+    if n == 1:
+        biases[:] = case["biases"]
+    return hist, biases, r.random(n) < case["masked"]
+
+
+def _span(case, lens, ctx):
+    """(sinks kept apart, first key behind them, keys) of each request's visible span."""
+    n = ctx + lens
+    if case["window"] == 0:
+        z = np.zeros_like(n)
+        return z, z, n
+    s = np.minimum(case["sinks"], n)
+    first = np.maximum(s, ctx - case["window"] + 1)
+    return s, first, s + np.maximum(n - first, 0)
+
+
+def _pairs(case, lens, ctx):
+    """Visible (row, key) pairs of one query head over all requests."""
+    total = 0
+    for m, c in zip(lens.tolist(), ctx.tolist()):
+        j = np.arange(c, c + m, dtype=np.int64)
+        if case["window"] == 0:
+            total += int((j + 1).sum())
+        else:
+            lo = np.maximum(0, j - case["window"] + 1)
+            total += int((j + 1 - lo + np.minimum(lo, case["sinks"])).sum())
+    return total
+
+
+def work(case):
+    if case["op"] == "adjust":
+        sizes, (hist, biases, masked) = _sizes(case), _histories(case)
+        # earlier tokens, biases, masks, and the outputs: all of them read and written, or those that change (the
+        # distinct ones of a history drawn as in prepare() read and written, the forbidden ones written)
+        read = 4 * int(hist.sum()) + 8 * int(biases.sum()) + int(((sizes + 31) // 32 * 4)[masked].sum())
+        if not case["in_place"]:
+            return {"bytes": read + 8 * int(sizes.sum()), "flops": 4 * int(sizes.sum())}
+        changed = 0
+        for v in np.unique(sizes):
+            i = sizes == v
+            edge = (np.arange(v + 1) / v) ** (1 / 3)
+            p = np.diff(edge)
+            changed += sum(int((-np.expm1(h * np.log1p(-np.minimum(p, 1 - 1e-12)))).sum()) + int(b)
+                           for h, b in zip(hist[i].tolist(), biases[i].tolist()))
+        return {"bytes": read + 8 * changed + 2 * int(sizes[masked].sum()), "flops": 4 * changed}
+    es = 2 if case["dtype"] == "bf16" else 4
+    lens, ctx = _lengths(case)
+    T, dh, H, KH = int(lens.sum()), case["dh"], case["heads"], case["kv_heads"]
+    if case["op"] == "append8":
+        return {"bytes": T * dh * (es * (2 * H + 2 * KH) + 2 * KH) + T * KH // 8, "flops": 3 * T * (H + KH) * dh}
+    keys = int(_span(case, lens, ctx)[2].sum())
+    return {"bytes": 2 * es * dh * T * H + 2 * keys * KH * dh + keys * KH // 8,
+            "flops": 4 * dh * H * _pairs(case, lens, ctx)}
+
+
+# ---------------------------------------------------------------------------
+# inputs
+# ---------------------------------------------------------------------------
+def _dtype(case):
+    return torch.bfloat16 if case["dtype"] == "bf16" else torch.float32
+
+
+def _randn(gen, shape, dtype, std=1.0):
+    t = torch.empty(shape, dtype=dtype, device=DEV)
+    t.normal_(0.0, std, generator=gen)
+    return t
+
+
+def _dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+def _pool(gen, KH, slots, dh):
+    """A pool's codes (of values as a scale's block holds them: the largest of 16 x dh near 448) and its exponents."""
+    codes = torch.empty(KH, slots, dh, dtype=torch.float8_e4m3fn, device=DEV)
+    for h in range(KH):
+        codes[h] = _randn(gen, (slots, dh), torch.float16, 90.0).clamp_(-448, 448).to(codes.dtype)
+    exps = torch.randint(119, 122, (KH, slots // RUN), generator=gen, device=DEV, dtype=torch.uint8)
+    return codes, exps
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    if case["op"] == "adjust":
+        return _prepare_adjust(case, seed, gen)
+    lens, ctx = _lengths(case)
+    n, page, dh, H, KH = case["n_req"], case["page"], case["dh"], case["heads"], case["kv_heads"]
+    T, dt = int(lens.sum()), _dtype(case)
+    tasks = _tasks(case)
+    order = np.argsort(tasks, kind="stable")
+    # pages in random order, some of the pool unused
+    need = -(-(ctx + lens) // page)
+    total = int(need.sum()) + 3
+    perm = np.random.default_rng(seed).permutation(total).astype(np.int32)
+    table = np.zeros((n, int(need.max())), np.int32)
+    at = 0
+    for i in range(n):
+        table[i, :need[i]] = perm[at:at + need[i]]
+        at += int(need[i])
+    s = {"case": case, "lens": lens, "ctx": ctx, "order": order}
+    s["k"], s["k_exp"] = _pool(gen, KH, total * page, dh)
+    s["v"], s["v_exp"] = _pool(gen, KH, total * page, dh)
+    if case["op"] == "append8":
+        # rows of different sizes, so that a block's scale has to grow under some of them
+        s["qkv"] = _randn(gen, (T, (H + 2 * KH) * dh), dt)
+        s["qkv"] *= torch.exp2(torch.randint(-2, 3, (T, 1), generator=gen, device=DEV).float()).to(dt)
+    else:
+        # queries that look somewhere: logits of a spread of about 1.5
+        s["q"] = _randn(gen, (T, H * dh), dt, 1.5)
+    # per plan-order row: the request and its position; the table in plan order
+    req = np.repeat(np.arange(n), lens[order])
+    first = np.concatenate([[0], np.cumsum(lens[order])])[:-1]
+    pos = np.arange(T) - first[req] + ctx[order][req]
+    s["pos"], s["req"], s["row"] = _dev(pos), _dev(req), _dev(np.arange(T) - first[req])
+    s["table"] = _dev(table[order].astype(np.int64))
+    s["plan_lens"], s["plan_ctx"] = _dev(lens[order]), _dev(ctx[order])
+    if case["op"] == "append8":
+        # the scales' blocks with new rows: each row's, each block's request and first position
+        _, start, block = np.unique(req * (1 << 32) + pos // RUN, return_index=True, return_inverse=True)
+        s["block"], s["block_req"], s["block_pos"] = _dev(block), _dev(req[start]), _dev(pos[start] // RUN * RUN)
+    if own:
+        from paper_2606_09643_amd import binding as B
+        s["B"] = B
+        s["attn"] = B.make_attn(B.VFM_BF16 if case["dtype"] == "bf16" else B.VFM_F32, H, KH, dh,
+                                window=case.get("window", 0), n_sink=case.get("sinks", 0),
+                                rope_theta=case.get("theta", 0.0))
+        s["batch"] = B.Batch(tasks, lens, _n_tasks(case), ctx_len=ctx)
+        s["kv"] = B.PagedKVQ8(s["k"], s["v"], s["k_exp"], s["v_exp"], page, table)
+        s["out"] = torch.empty(T, H * dh, dtype=dt, device=DEV)
+        if case["op"] == "attend8":
+            s["ws"] = torch.empty(max(1, B.vfm_attention_workspace_q8(s["attn"], s["batch"].c)), dtype=torch.uint8,
+                                  device=DEV)
+    return s
+
+
+def _prepare_adjust(case, seed, gen):
+    n = case["n_req"]
+    sizes, (hist, biases, masked) = _sizes(case), _histories(case)
+    r = np.random.default_rng(seed)
+    off = np.concatenate([[0], np.cumsum(sizes)])
+    hoff, boff = (np.concatenate([[0], np.cumsum(x)]) for x in (hist, biases))
+    some = lambda p: r.random(n) < p  # noqa: E731
+    # text repeats itself: low ids are frequent
+    of = np.repeat(np.arange(n), hist)
+    tokens = (sizes[of] * r.random(len(of)) ** 3).astype(np.int32)
+    bof = np.repeat(np.arange(n), biases)
+    bias_id = (sizes[bof] * r.random(len(bof))).astype(np.int32)
+    bias = np.where(r.random(len(bof)) < 0.2, -np.inf, r.normal(0, 4, len(bof))).astype(np.float32)
+    # masks: a grammar's step allows a few outputs, most of them, or (an error of the caller's) none
+    rows = np.full(n, -1, np.int32)
+    rows[masked] = r.permutation(int(masked.sum())).astype(np.int32)
+    words = -(-case["hi"] // 32)
+    share = np.where(r.random(max(1, int(masked.sum()))) < 0.7, 0.002, 0.95)
+    share[r.random(len(share)) < 0.03] = 0.0
+    allow = torch.rand(len(share), words, 32, generator=gen, device=DEV) < _dev(share)[:, None, None]
+    bits = (allow.long() << torch.arange(32, device=DEV)).sum(-1)
+    s = {"case": case, "sizes": sizes, "off": _dev(off), "out": _randn(gen, (int(off[-1]),), torch.float32, 3.0),
+         "repetition": _dev(np.where(some(0.6), r.uniform(0.8, 1.4, n), 1.0).astype(np.float32)),
+         "presence": _dev(np.where(some(0.5), r.uniform(-0.5, 1.5, n), 0.0).astype(np.float32)),
+         "frequency": _dev(np.where(some(0.5), r.uniform(0.0, 0.7, n), 0.0).astype(np.float32)),
+         "hist": _dev(np.append(tokens, np.int32(0))), "hist_begin": _dev(hoff[:-1]),
+         "hist_len": _dev(hist.astype(np.int32)),
+         "n_prompt": _dev((hist * r.random(n)).astype(np.int32)),
+         "bias_id": _dev(np.append(bias_id, np.int32(0))), "bias": _dev(np.append(bias, np.float32(0))),
+         "bias_begin": _dev(boff[:-1]), "bias_len": _dev(biases.astype(np.int32)),
+         "mask": torch.where(bits >= 1 << 31, bits - (1 << 32), bits).to(torch.int32), "mask_row": _dev(rows),
+         "hist_of": _dev(of), "bias_of": _dev(bof)}
+    s["adjusted"] = s["out"] if case["in_place"] else torch.empty_like(s["out"])
+    if own:
+        from paper_2606_09643_amd import binding as B
+        s["B"] = B
+        s["batch"] = B.Batch(np.arange(n, dtype=np.int32), np.ones(n, np.int32), n, n_out=sizes)
+        s["adjust"] = B.OutputAdjust(**{k: s[k] for k in (
+            "repetition", "presence", "frequency", "hist", "hist_begin", "hist_len", "n_prompt", "bias_id", "bias",
+            "bias_begin", "bias_len", "mask", "mask_row")})
+    return s
+
+
+# ---------------------------------------------------------------------------
+# one pass
+# ---------------------------------------------------------------------------
+def run(s):
+    op = s["case"]["op"]
+    if own:
+        B = s["B"]
+        if op == "append8":
+            B.vfm_kv_append_q8(s["attn"], s["batch"].c, s["qkv"], s["out"], s["kv"])
+            return {"q": s["out"], "k": s["k"], "v": s["v"], "k_exp": s["k_exp"], "v_exp": s["v_exp"]}
+        if op == "attend8":
+            B.vfm_attention_paged_q8(s["attn"], s["batch"].c, s["q"], s["kv"], s["out"], s["ws"])
+            return s["out"]
+        B.vfm_adjust_outputs(s["batch"].c, s["out"], s["adjust"], s["adjusted"])
+        return s["adjusted"]
+    if op == "append8":
+        return _plain_append(s)
+    return _plain_attend(s) if op == "attend8" else _plain_adjust(s)
+
+
+def _slots(s, req, pos):
+    """Slot of position pos of plan-order request req in every head."""
+    page = s["case"]["page"]
+    return s["table"][req, pos // page] * page + pos % page
+
+
+def _codes(y):
+    """e4m3 codes nearest to y (64 bits, magnitudes up to 448, ties to the even one)."""
+    _, e = torch.frexp(y)
+    step = torch.exp2((e.clamp(min=-5) - 4).double())
+    return (torch.round(y / step) * step).to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+def _plain_append(s):
+    c = s["case"]
+    H, KH, dh, T = c["heads"], c["kv_heads"], c["dh"], s["qkv"].shape[0]
+    x = s["qkv"].view(T, H + 2 * KH, dh)
+    qk = x[:, :H + KH].double()
+    if c["theta"] > 0:
+        half = dh // 2
+        inv = c["theta"] ** (-torch.arange(half, device=DEV, dtype=torch.float64) * 2 / dh)
+        ang = s["pos"].double()[:, None] * inv
+        cos, sin = ang.cos()[:, None], ang.sin()[:, None]
+        a, b = qk[..., :half], qk[..., half:]
+        qk = torch.cat([a * cos - b * sin, a * sin + b * cos], -1)
+    new = _slots(s, s["req"], s["pos"])
+    first = _slots(s, s["block_req"], s["block_pos"])
+    lane = torch.arange(RUN, device=DEV)
+    older = s["block_pos"][:, None] + lane < s["plan_ctx"][s["block_req"]][:, None]        # [blocks, RUN]
+    for name, y in (("k", qk[:, H:]), ("v", x[:, H + KH:].double())):
+        codes, exps = s[name].view(torch.uint8), s[name + "_exp"]
+        y = torch.where(y.isfinite(), y.clamp(-TOP, TOP), math.nan)
+        big = torch.zeros(len(first), KH, dtype=torch.float64, device=DEV)
+        big.scatter_reduce_(0, s["block"][:, None].expand(T, KH), y.abs().nan_to_num(0.0).amax(-1), "amax")
+        m, e = torch.frexp(big)                                                            # big = m 2^e, m in [1/2, 1)
+        e = torch.where(big > 0, e - 9 + (m > 0.875).int() + 127, 1).clamp(min=1)
+        was = exps[:, first // RUN].t().int()
+        e = torch.where(older.any(1, keepdim=True), torch.maximum(e, was), e)              # [blocks, KH]
+        # older rows of blocks whose scale grows
+        b, l = torch.nonzero(older, as_tuple=True)
+        old = codes[:, first[b] + l].view(torch.float8_e4m3fn).double()                    # [KH, older rows, dh]
+        codes[:, first[b] + l] = _codes(old * torch.exp2((was - e)[b].t().double())[..., None])
+        codes[:, new] = _codes(y * torch.exp2((127 - e)[s["block"]].double())[..., None]).transpose(0, 1)
+        exps[:, first // RUN] = e.t().to(torch.uint8)
+    return {"q": qk[:, :H].reshape(T, H * dh).to(x.dtype), "k": s["k"], "v": s["v"], "k_exp": s["k_exp"],
+            "v_exp": s["v_exp"]}
+
+
+def _values(codes, exps, slots):
+    """What a pool's slots stand for, 32 bits: [KH, *slots.shape, dh]."""
+    return codes[:, slots].float() * torch.exp2(exps[:, slots // RUN].float() - 127.0)[..., None]
+
+
+def _plain_attend(s):
+    c = s["case"]
+    H, KH, dh, W, S = c["heads"], c["kv_heads"], c["dh"], c["window"], c["sinks"]
+    G, n = H // KH, c["n_req"]
+    lens, ctx = s["plan_lens"], s["plan_ctx"]
+    L = int(s["lens"].max())
+    end = ctx + lens
+    # the keys that any row of a request sees: its sinks, then a run up to its end
+    if W:
+        sk = end.clamp(max=S)
+        first = torch.maximum(sk, ctx - W + 1)
+    else:
+        sk = first = torch.zeros_like(end)
+    J = int(_span(c, s["lens"], s["ctx"])[2].max())
+    j = torch.arange(J, device=DEV)
+    kpos = torch.where(j < sk[:, None], j, first[:, None] + j - sk[:, None])            # [n, J]
+    there = kpos < end[:, None]
+    rows = torch.arange(n, device=DEV)[:, None].expand(n, J)
+    slots = _slots(s, rows, torch.where(there, kpos, 0))
+    keys = _values(s["k"], s["k_exp"], slots)                                           # [KH, n, J, dh]
+    vals = torch.where(there[None, :, :, None], _values(s["v"], s["v_exp"], slots), 0.0)
+    q = torch.zeros(n, L, H, dh, device=DEV)
+    q[s["req"], s["row"]] = s["q"].float().view(-1, H, dh)
+    q = q.view(n, L, KH, G, dh).permute(2, 0, 3, 1, 4).reshape(KH, n, G * L, dh)
+    sc = torch.matmul(q, keys.transpose(2, 3).contiguous()) * (1.0 / math.sqrt(dh))
+    del keys
+    qpos = ctx[:, None] + torch.arange(L, device=DEV)
+    d = qpos[:, :, None] - kpos[:, None, :]
+    see = (d >= 0) & there[:, None, :]
+    if W:
+        see &= (d < W) | (kpos[:, None, :] < S)
+    sc = sc.view(KH, n, G, L, J).masked_fill(~see[None, :, None], -math.inf)
+    e = torch.exp(sc - sc.amax(-1, keepdim=True).clamp(min=-3e38))
+    del sc
+    o = torch.matmul(e.view(KH, n, G * L, J), vals) / e.sum(-1).view(KH, n, G * L, 1)
+    o = o.view(KH, n, G, L, dh).permute(1, 3, 0, 2, 4).reshape(n, L, H * dh)
+    return o[s["req"], s["row"]].to(s["q"].dtype)
+
+
+def _plain_adjust(s):
+    n, off, out = s["case"]["n_req"], s["off"], s["out"]
+    total = out.numel()
+    size = off[1:] - off[:-1]
+    req = torch.repeat_interleave(torch.arange(n, device=DEV), size, output_size=total)
+    col = torch.arange(total, device=DEV) - off[req]
+    # how often each output's token was generated, and whether it was seen at all
+    hist = s["hist"][:-1].long()
+    at = off[s["hist_of"]] + hist
+    place = torch.arange(len(hist), device=DEV) - s["hist_begin"][s["hist_of"]]
+    count = torch.zeros(total, dtype=torch.float64, device=DEV)
+    count.index_add_(0, at, (place >= s["n_prompt"][s["hist_of"]]).double())
+    seen = torch.zeros(total, dtype=torch.bool, device=DEV)
+    seen[at] = True
+    # an output's last bias counts
+    last = torch.full((total,), -1, dtype=torch.int64, device=DEV)
+    at = off[s["bias_of"]] + s["bias_id"][:-1].long()
+    last.scatter_reduce_(0, at, torch.arange(len(at), device=DEV), "amax")
+    l = out.double()
+    r = s["repetition"].double()[req]
+    l = torch.where(seen, torch.where(l > 0, l / r, l * r), l)
+    l = l - torch.where(count > 0, count * s["frequency"].double()[req] + s["presence"].double()[req], 0.0)
+    l = l + torch.where(last >= 0, s["bias"].double()[last], 0.0)
+    row = s["mask_row"].long()[req]
+    allowed = (s["mask"][row.clamp(min=0), col // 32] >> (col % 32).int() & 1).bool() | (row < 0)
+    left = torch.zeros(n, dtype=torch.int64, device=DEV).index_add_(0, req, allowed.long())
+    l = torch.where(left[req] > 0, torch.where(allowed, l, -math.inf), math.nan)
+    s["adjusted"].copy_(l)
+    return s["adjusted"]
+
+
+# ---------------------------------------------------------------------------
+# the definitions in 64 bits, request by request
+# ---------------------------------------------------------------------------
+def _e4m3():
+    """Value of each code."""
+    b = np.arange(256)
+    m, e = b & 7, b >> 3 & 15
+    v = np.where(e == 0, m * 2.0 ** -9, (8 + m) * 2.0 ** (e - 10.0))
+    v[(b & 127) == 127] = np.nan
+    return np.where(b > 127, -v, v)
+
+
+def exact(case, seed):
+    if case["op"] != "adjust" and case["n_req"] * case["heads"] > 100000:
+        return None
+    s = prepare(case, seed)
+    if case["op"] == "adjust":
+        return _exact_adjust(case, s)
+    table = s["table"].cpu().numpy()
+    lens, ctx = s["lens"][s["order"]], s["ctx"][s["order"]]
+    page, dh, H, KH = case["page"], case["dh"], case["heads"], case["kv_heads"]
+    at = np.concatenate([[0], np.cumsum(lens)])
+    value = _dev(_e4m3())
+
+    def slots_of(i, pos):
+        return _dev(table[i, pos // page] * page + pos % page)
+
+    if case["op"] == "append8":
+        return _exact_append(case, s, lens, ctx, at, value, slots_of)
+    out = torch.empty(int(at[-1]), H * dh, dtype=torch.float64, device=DEV)
+    G = H // KH
+    for i in range(len(lens)):
+        m, c = int(lens[i]), int(ctx[i])
+        first = max(0, c - case["window"] + 1) if case["window"] else 0
+        pos = np.arange(c + m)
+        pos = pos[(pos >= first) | (pos < case["sinks"])]
+        sl, kp = slots_of(i, pos), _dev(pos)
+        jp = torch.arange(c, c + m, device=DEV)[:, None]
+        see = kp[None] <= jp
+        if case["window"]:
+            see &= (jp - kp[None] < case["window"]) | (kp[None] < case["sinks"])
+        for h in range(KH):
+            k, v = (value[s[x][h, sl].view(torch.uint8).int()] * 2.0 ** (s[x + "_exp"][h, sl // RUN].double() - 127)[:, None]
+                    for x in "kv")
+            for g in range(h * G, h * G + G):
+                q = s["q"][at[i]:at[i + 1], g * dh:(g + 1) * dh].double()
+                a = torch.softmax(torch.where(see, q @ k.T.contiguous() / math.sqrt(dh), -math.inf), -1)
+                out[at[i]:at[i + 1], g * dh:(g + 1) * dh] = a @ v
+    return out
+
+
+def _exact_append(case, s, lens, ctx, at, value, slots_of):
+    dh, H, KH = case["dh"], case["heads"], case["kv_heads"]
+    x = s["qkv"].double().view(-1, H + 2 * KH, dh)
+    q = x[:, :H].clone()
+    res = {n: value[s[n].view(torch.uint8).int()] for n in "kv"}
+    exps = {n: s[n + "_exp"].int() for n in "kv"}
+    limit = _dev(448 * 2.0 ** np.arange(-126, 121))          # the largest value under exponent 1, 2, ...
+    border = (value[:127] + value[1:127 + 1].nan_to_num(512.0))[:126] / 2        # between code i and code i + 1
+
+    def nearest(y):
+        a = y.abs()
+        i = torch.searchsorted(border, a.contiguous())                    # a tie goes to the lower code, unless that is odd
+        i = i + ((a == border[i.clamp(max=125)]) & (i % 2 == 1)).long()
+        return torch.where(y.isnan(), math.nan, torch.copysign(value[i.clamp(max=126)], y))
+
+    for i in range(len(lens)):
+        c, m = int(ctx[i]), int(lens[i])
+        y = x[at[i]:at[i + 1]].clone()
+        if case["theta"] > 0:
+            z = torch.complex(y[:, :H + KH, :dh // 2], y[:, :H + KH, dh // 2:])
+            f = np.exp(-np.log(case["theta"]) * np.arange(dh // 2) * 2.0 / dh)
+            z = z * _dev(np.exp(1j * np.outer(np.arange(c, c + m, dtype=np.float64), f)))[:, None]
+            y[:, :H + KH] = torch.cat([z.real, z.imag], -1)
+        q[at[i]:at[i + 1]] = y[:, :H]
+        for n, new in (("k", y[:, H:H + KH]), ("v", y[:, H + KH:])):
+            for b in range(c // RUN, (c + m - 1) // RUN + 1):
+                lo, hi = max(c, b * RUN), min(c + m, (b + 1) * RUN)
+                rows = new[lo - c:hi - c].permute(1, 0, 2)                       # [KH, rows, dh]
+                rows = torch.where(rows.isfinite(), rows.clamp(-TOP, TOP), math.nan)
+                e = torch.searchsorted(limit, rows.abs().nan_to_num(0.0).amax((1, 2))).double() + 1
+                block = slots_of(i, np.array([b * RUN]))[0] // RUN
+                if c > b * RUN:
+                    old = slots_of(i, np.arange(b * RUN, c))
+                    was = exps[n][:, block].double()
+                    e = torch.maximum(e, was)
+                    res[n][:, old] = nearest(res[n][:, old] * torch.exp2(was - e)[:, None, None])
+                exps[n][:, block] = e.int()
+                res[n][:, slots_of(i, np.arange(lo, hi))] = nearest(rows * torch.exp2(127 - e)[:, None, None])
+    return {"q": q.reshape(-1, H * dh), "k": res["k"], "v": res["v"], "k_exp": exps["k"].to(torch.uint8),
+            "v_exp": exps["v"].to(torch.uint8)}
+
+
+def _exact_adjust(case, s):
+    a = {k: v.cpu().numpy() for k, v in s.items() if isinstance(v, torch.Tensor)}
+    out = a["out"].astype(np.float64)
+    bits = a["mask"].astype(np.int64) & 0xFFFFFFFF
+    for i in range(case["n_req"]):
+        l = out[a["off"][i]:a["off"][i + 1]]                 # a view
+        h = a["hist"][a["hist_begin"][i]:][:a["hist_len"][i]]
+        r = np.float64(a["repetition"][i])
+        seen = np.unique(h)
+        l[seen] = np.where(l[seen] > 0, l[seen] / r, l[seen] * r)
+        ids, times = np.unique(h[a["n_prompt"][i]:], return_counts=True)
+        l[ids] -= times * np.float64(a["frequency"][i]) + np.float64(a["presence"][i])
+        b = slice(a["bias_begin"][i], a["bias_begin"][i] + a["bias_len"][i])
+        for j, v in dict(zip(a["bias_id"][b].tolist(), a["bias"][b].tolist())).items():
+            l[j] += v
+        if a["mask_row"][i] >= 0:
+            w = bits[a["mask_row"][i]]
+            ok = (w[:, None] >> np.arange(32) & 1).reshape(-1)[:len(l)].astype(bool)
+            l[~ok] = -np.inf if ok.any() else np.nan
+    return _dev(out)
