@@ -250,12 +250,11 @@ def _dev(a):
 
 
 def _pool(gen, KH, slots, dh):
-    """A pool's codes (of values as a scale's block holds them: the largest of 16 x dh near 448) and its exponents."""
+    """A pool's codes, of values as a scale's block holds them: the largest of 16 x dh near 448."""
     codes = torch.empty(KH, slots, dh, dtype=torch.float8_e4m3fn, device=DEV)
     for h in range(KH):
         codes[h] = _randn(gen, (slots, dh), torch.float16, 90.0).clamp_(-448, 448).to(codes.dtype)
-    exps = torch.randint(119, 122, (KH, slots // RUN), generator=gen, device=DEV, dtype=torch.uint8)
-    return codes, exps
+    return codes
 
 
 def prepare(case, seed):
@@ -278,8 +277,9 @@ def prepare(case, seed):
         table[i, :need[i]] = perm[at:at + need[i]]
         at += int(need[i])
     s = {"case": case, "lens": lens, "ctx": ctx, "order": order}
-    s["k"], s["k_exp"] = _pool(gen, KH, total * page, dh)
-    s["v"], s["v_exp"] = _pool(gen, KH, total * page, dh)
+    s["k"], s["v"] = _pool(gen, KH, total * page, dh), _pool(gen, KH, total * page, dh)
+    # the exponents of the scales, K's and V's of a head beside each other
+    s["exps"] = torch.randint(119, 122, (total * page // RUN, KH, 2), generator=gen, device=DEV, dtype=torch.uint8)
     if case["op"] == "append8":
         # rows of different sizes, so that a block's scale has to grow under some of them
         s["qkv"] = _randn(gen, (T, (H + 2 * KH) * dh), dt)
@@ -305,7 +305,7 @@ def prepare(case, seed):
                                 window=case.get("window", 0), n_sink=case.get("sinks", 0),
                                 rope_theta=case.get("theta", 0.0))
         s["batch"] = B.Batch(tasks, lens, _n_tasks(case), ctx_len=ctx)
-        s["kv"] = B.PagedKVQ8(s["k"], s["v"], s["k_exp"], s["v_exp"], page, table)
+        s["kv"] = B.PagedKVQ8(s["k"], s["v"], s["exps"], page, table)
         s["out"] = torch.empty(T, H * dh, dtype=dt, device=DEV)
         if case["op"] == "attend8":
             s["ws"] = torch.empty(max(1, B.vfm_attention_workspace_q8(s["attn"], s["batch"].c)), dtype=torch.uint8,
@@ -365,7 +365,7 @@ def run(s):
         B = s["B"]
         if op == "append8":
             B.vfm_kv_append_q8(s["attn"], s["batch"].c, s["qkv"], s["out"], s["kv"])
-            return {"q": s["out"], "k": s["k"], "v": s["v"], "k_exp": s["k_exp"], "v_exp": s["v_exp"]}
+            return {"q": s["out"], "k": s["k"], "v": s["v"], "exps": s["exps"]}
         if op == "attend8":
             B.vfm_attention_paged_q8(s["attn"], s["batch"].c, s["q"], s["kv"], s["out"], s["ws"])
             return s["out"]
@@ -405,28 +405,28 @@ def _plain_append(s):
     first = _slots(s, s["block_req"], s["block_pos"])
     lane = torch.arange(RUN, device=DEV)
     older = s["block_pos"][:, None] + lane < s["plan_ctx"][s["block_req"]][:, None]        # [blocks, RUN]
-    for name, y in (("k", qk[:, H:]), ("v", x[:, H + KH:].double())):
-        codes, exps = s[name].view(torch.uint8), s[name + "_exp"]
+    for name, y, exps in (("k", qk[:, H:], s["exps"][..., 0]), ("v", x[:, H + KH:].double(), s["exps"][..., 1])):
+        codes = s[name].view(torch.uint8)
         y = torch.where(y.isfinite(), y.clamp(-TOP, TOP), math.nan)
         big = torch.zeros(len(first), KH, dtype=torch.float64, device=DEV)
         big.scatter_reduce_(0, s["block"][:, None].expand(T, KH), y.abs().nan_to_num(0.0).amax(-1), "amax")
         m, e = torch.frexp(big)                                                            # big = m 2^e, m in [1/2, 1)
         e = torch.where(big > 0, e - 9 + (m > 0.875).int() + 127, 1).clamp(min=1)
-        was = exps[:, first // RUN].t().int()
+        was = exps[first // RUN].int()
         e = torch.where(older.any(1, keepdim=True), torch.maximum(e, was), e)              # [blocks, KH]
         # older rows of blocks whose scale grows
         b, l = torch.nonzero(older, as_tuple=True)
         old = codes[:, first[b] + l].view(torch.float8_e4m3fn).double()                    # [KH, older rows, dh]
         codes[:, first[b] + l] = _codes(old * torch.exp2((was - e)[b].t().double())[..., None])
         codes[:, new] = _codes(y * torch.exp2((127 - e)[s["block"]].double())[..., None]).transpose(0, 1)
-        exps[:, first // RUN] = e.t().to(torch.uint8)
-    return {"q": qk[:, :H].reshape(T, H * dh).to(x.dtype), "k": s["k"], "v": s["v"], "k_exp": s["k_exp"],
-            "v_exp": s["v_exp"]}
+        exps[first // RUN] = e.to(torch.uint8)
+    return {"q": qk[:, :H].reshape(T, H * dh).to(x.dtype), "k": s["k"], "v": s["v"], "exps": s["exps"]}
 
 
-def _values(codes, exps, slots):
+def _values(s, name, slots):
     """What a pool's slots stand for, 32 bits: [KH, *slots.shape, dh]."""
-    return codes[:, slots].float() * torch.exp2(exps[:, slots // RUN].float() - 127.0)[..., None]
+    exps = s["exps"][..., "kv".index(name)].t()[:, slots // RUN]
+    return s[name][:, slots].float() * torch.exp2(exps.float() - 127.0)[..., None]
 
 
 def _plain_attend(s):
@@ -448,8 +448,8 @@ def _plain_attend(s):
     there = kpos < end[:, None]
     rows = torch.arange(n, device=DEV)[:, None].expand(n, J)
     slots = _slots(s, rows, torch.where(there, kpos, 0))
-    keys = _values(s["k"], s["k_exp"], slots)                                           # [KH, n, J, dh]
-    vals = torch.where(there[None, :, :, None], _values(s["v"], s["v_exp"], slots), 0.0)
+    keys = _values(s, "k", slots)                                           # [KH, n, J, dh]
+    vals = torch.where(there[None, :, :, None], _values(s, "v", slots), 0.0)
     q = torch.zeros(n, L, H, dh, device=DEV)
     q[s["req"], s["row"]] = s["q"].float().view(-1, H, dh)
     q = q.view(n, L, KH, G, dh).permute(2, 0, 3, 1, 4).reshape(KH, n, G * L, dh)
@@ -541,8 +541,8 @@ def exact(case, seed):
         if case["window"]:
             see &= (jp - kp[None] < case["window"]) | (kp[None] < case["sinks"])
         for h in range(KH):
-            k, v = (value[s[x][h, sl].view(torch.uint8).int()] * 2.0 ** (s[x + "_exp"][h, sl // RUN].double() - 127)[:, None]
-                    for x in "kv")
+            k, v = (value[s[x][h, sl].view(torch.uint8).int()]
+                    * 2.0 ** (s["exps"][sl // RUN, h, "kv".index(x)].double() - 127)[:, None] for x in "kv")
             for g in range(h * G, h * G + G):
                 q = s["q"][at[i]:at[i + 1], g * dh:(g + 1) * dh].double()
                 a = torch.softmax(torch.where(see, q @ k.T.contiguous() / math.sqrt(dh), -math.inf), -1)
@@ -555,7 +555,8 @@ def _exact_append(case, s, lens, ctx, at, value, slots_of):
     x = s["qkv"].double().view(-1, H + 2 * KH, dh)
     q = x[:, :H].clone()
     res = {n: value[s[n].view(torch.uint8).int()] for n in "kv"}
-    exps = {n: s[n + "_exp"].int() for n in "kv"}
+    exps = s["exps"].int()
+    of = {"k": exps[..., 0].t(), "v": exps[..., 1].t()}
     limit = _dev(448 * 2.0 ** np.arange(-126, 121))          # the largest value under exponent 1, 2, ...
     border = (value[:127] + value[1:127 + 1].nan_to_num(512.0))[:126] / 2        # between code i and code i + 1
 
@@ -583,13 +584,12 @@ def _exact_append(case, s, lens, ctx, at, value, slots_of):
                 block = slots_of(i, np.array([b * RUN]))[0] // RUN
                 if c > b * RUN:
                     old = slots_of(i, np.arange(b * RUN, c))
-                    was = exps[n][:, block].double()
+                    was = of[n][:, block].double()
                     e = torch.maximum(e, was)
                     res[n][:, old] = nearest(res[n][:, old] * torch.exp2(was - e)[:, None, None])
-                exps[n][:, block] = e.int()
+                of[n][:, block] = e.int()
                 res[n][:, slots_of(i, np.arange(lo, hi))] = nearest(rows * torch.exp2(127 - e)[:, None, None])
-    return {"q": q.reshape(-1, H * dh), "k": res["k"], "v": res["v"], "k_exp": exps["k"].to(torch.uint8),
-            "v_exp": exps["v"].to(torch.uint8)}
+    return {"q": q.reshape(-1, H * dh), "k": res["k"], "v": res["v"], "exps": exps.to(torch.uint8)}
 
 
 def _exact_adjust(case, s):
