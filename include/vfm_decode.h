@@ -1,7 +1,8 @@
 /* Decoding over a bounded KV cache (libvfm.so): appending rotated keys and
  * values to a paged cache, attention of new tokens over that cache with a
  * sliding window and first tokens that stay visible, one backbone layer with
- * that attention, and drawing the next tokens from the head outputs.
+ * that attention, penalties, biases and masks on the head outputs, and drawing
+ * the next tokens from them.
  *
  * Token-based FMs are served with continuous batching and long-lived decode
  * iterations (paper Section 4.2; Section 6: a vLLM-style runtime, whose KV
@@ -103,6 +104,57 @@ int vfm_workspace_size_windowed(const vfm_cfg* cfg, const vfm_batch* batch, cons
 int vfm_layer_forward_windowed(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_table* lora,
                                const vfm_batch* batch, float* x, const vfm_kv_pages* kv, int32_t window,
                                int32_t n_sink, void* workspace, size_t ws_bytes, void* stream);
+
+/* What is done to a batch's head outputs before tokens are picked or drawn
+ * from them.  Every array is a device array; per-request ones are [n_req] in
+ * ORIGINAL order.  They are read by the kernel, so values out of range are
+ * given a meaning instead of an error; what lies outside a list's stated size
+ * is not read.
+ *   Penalties.  Request i's earlier tokens are hist[hist_begin[i] + 0 ..
+ *     hist_len[i]), the first n_prompt[i] of them its prompt's (NULL: none),
+ *     the others generated.  hist NULL: no penalties.
+ *   Biases.  Request i's pairs are bias_id / bias [bias_begin[i] + 0 ..
+ *     bias_len[i]); of several for one output the last one counts.
+ *   Masks.  Row mask_row[i] of mask [n_masks][mask_words] has a bit per output
+ *     (output j is bit j % 32 of word j / 32): 1 allows it.  Outputs past the
+ *     row's words are not allowed.  mask_row[i] outside [0, n_masks): no mask.
+ * Ids and tokens outside the request's outputs are passed over. */
+typedef struct vfm_adjust {
+  const float* repetition;    /* > 0: r; NULL, <= 0 or NaN: 1, off */
+  const float* presence;      /* p; NULL or NaN: 0 */
+  const float* frequency;     /* f; NULL or NaN: 0 */
+  const int32_t* hist;
+  int64_t n_hist;
+  const int64_t* hist_begin;
+  const int32_t* hist_len;
+  const int32_t* n_prompt;
+  const float* bias;
+  const int32_t* bias_id;
+  int64_t n_bias;
+  const int64_t* bias_begin;
+  const int32_t* bias_len;
+  const uint32_t* mask;
+  int32_t n_masks;
+  int32_t mask_words;
+  const int32_t* mask_row;
+} vfm_adjust;
+
+/* adjusted: device float32, as out (vfm_head_forward's layout), or out itself:
+ * then only the outputs that change are written.  For output j = l of request
+ * i, in 64 bits with one rounding at the end:
+ *   l > 0 ? l / r : l * r   if j is among the earlier tokens;
+ *   l - (f * n + p)         if n > 0 of the generated ones are j;
+ *   l + bias                if j has one;
+ *   -infinity               if a mask does not allow j.
+ * A request whose mask allows none of its outputs gets NaN throughout, so that
+ * vfm_sample_tokens and vfm_greedy_tokens answer -1 and not a token that is
+ * not allowed.
+ * Errors: VFM_ERR_ARG for null pointers, out or adjusted not 16-byte aligned,
+ * a list without its other arrays; VFM_ERR_SHAPE for negative sizes, a mask
+ * without words; VFM_ERR_UNSUPPORTED for a batch of more blocks than a launch
+ * holds (2^23 requests, or the longest row's outputs times requests 2^35). */
+int vfm_adjust_outputs(const vfm_batch* batch, const float* out, const vfm_adjust* adjust,
+                       float* adjusted, void* stream);
 
 /* Per-request sampling parameters: device arrays [n_req] in ORIGINAL order,
  * each may be NULL (its filter off, temperature 1).  They are read by the

@@ -42,7 +42,9 @@ EXPORTS = ("vfm_status_string", "vfm_plan_size", "vfm_plan", "vfm_workspace_size
            "vfm_pages_state_size", "vfm_pages_init", "vfm_pages_reserve", "vfm_pages_release",
            "vfm_pages_table", "vfm_pages_count", "vfm_bfq_charge",
            "vfm_layer_forward_noalloc", "vfm_kv_append", "vfm_attention_workspace", "vfm_attention_paged",
-           "vfm_workspace_size_windowed", "vfm_layer_forward_windowed", "vfm_sample_tokens")
+           "vfm_workspace_size_windowed", "vfm_layer_forward_windowed", "vfm_sample_tokens", "vfm_adjust_outputs",
+           "vfm_kv_append_q8", "vfm_attention_workspace_q8", "vfm_attention_paged_q8", "vfm_workspace_size_q8",
+           "vfm_layer_forward_q8")
 PROF_CLASSES = ("gemm_qkv", "gemm_o", "gemm_up", "gemm_down", "attn", "norm", "shrink", "other")
 
 
@@ -86,6 +88,10 @@ class vfm_kv_pages(C.Structure):
                 ("max_pages", C.c_int32), ("table_host", C.POINTER(C.c_int32)), ("table_dev", C.c_void_p)]
 
 
+class vfm_kv_pages_q8(C.Structure):
+    _fields_ = [("pages", vfm_kv_pages), ("exps", C.c_void_p)]
+
+
 class vfm_attn(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("window", C.c_int32), ("n_sink", C.c_int32), ("scale", C.c_float), ("rope_theta", C.c_float)]
@@ -93,6 +99,14 @@ class vfm_attn(C.Structure):
 
 class vfm_sampling(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
+
+
+class vfm_adjust(C.Structure):
+    _fields_ = [("repetition", C.c_void_p), ("presence", C.c_void_p), ("frequency", C.c_void_p),
+                ("hist", C.c_void_p), ("n_hist", C.c_int64), ("hist_begin", C.c_void_p), ("hist_len", C.c_void_p),
+                ("n_prompt", C.c_void_p), ("bias", C.c_void_p), ("bias_id", C.c_void_p), ("n_bias", C.c_int64),
+                ("bias_begin", C.c_void_p), ("bias_len", C.c_void_p), ("mask", C.c_void_p), ("n_masks", C.c_int32),
+                ("mask_words", C.c_int32), ("mask_row", C.c_void_p)]
 
 
 class vfm_pages_config(C.Structure):
@@ -178,6 +192,19 @@ def _lib_handle():
                                                    C.c_size_t, C.c_void_p]
         lib.vfm_sample_tokens.argtypes = [C.POINTER(vfm_batch), C.c_void_p, C.POINTER(vfm_sampling), C.c_void_p,
                                           C.c_void_p, C.c_void_p, C.c_void_p]
+        lib.vfm_adjust_outputs.argtypes = [C.POINTER(vfm_batch), C.c_void_p, C.POINTER(vfm_adjust), C.c_void_p,
+                                           C.c_void_p]
+        lib.vfm_kv_append_q8.argtypes = [C.POINTER(vfm_attn), C.POINTER(vfm_batch), C.c_void_p, C.c_int64, C.c_void_p,
+                                         C.POINTER(vfm_kv_pages_q8), C.c_void_p]
+        lib.vfm_attention_workspace_q8.argtypes = lib.vfm_attention_workspace.argtypes
+        lib.vfm_attention_paged_q8.argtypes = [C.POINTER(vfm_attn), C.POINTER(vfm_batch), C.c_void_p, C.c_int64,
+                                               C.POINTER(vfm_kv_pages_q8), C.c_void_p, C.c_int64, C.c_void_p,
+                                               C.c_size_t, C.c_void_p]
+        lib.vfm_workspace_size_q8.argtypes = lib.vfm_workspace_size_windowed.argtypes
+        lib.vfm_layer_forward_q8.argtypes = [C.POINTER(vfm_cfg), C.POINTER(vfm_layer_weights),
+                                             C.POINTER(vfm_lora_table), C.POINTER(vfm_batch), C.c_void_p,
+                                             C.POINTER(vfm_kv_pages_q8), C.c_int32, C.c_int32, C.c_void_p,
+                                             C.c_size_t, C.c_void_p]
         for name in EXPORTS:
             getattr(lib, name).restype = C.c_int if name != "vfm_status_string" else C.c_char_p
         _LIB = lib
@@ -627,6 +654,138 @@ def vfm_sample_tokens(batch, out, sampling, u, ids, logprob=None, stream=None):
                                          _operand(logprob, "logprob", torch.float32, n, dev)
                                          if logprob is not None else None, _stream(stream, dev))
     _check(st, "vfm_sample_tokens")
+
+
+class OutputAdjust:
+    """Penalties, biases and masks of a batch's requests (device tensors, original order, groups of them optional) as the
+    C struct vfm_adjust.  hist with hist_begin, hist_len (and n_prompt): the earlier tokens; bias with bias_id,
+    bias_begin, bias_len: the biases; mask [n_masks, mask_words] with mask_row: the masks."""
+    _TYPES = {"repetition": torch.float32, "presence": torch.float32, "frequency": torch.float32,
+              "hist": torch.int32, "hist_begin": torch.int64, "hist_len": torch.int32, "n_prompt": torch.int32,
+              "bias": torch.float32, "bias_id": torch.int32, "bias_begin": torch.int64, "bias_len": torch.int32,
+              "mask": torch.int32, "mask_row": torch.int32}
+
+    def __init__(self, **tensors):
+        unknown = set(tensors) - set(self._TYPES)
+        if unknown:
+            raise ValueError(f"{sorted(unknown)}: not among {list(self._TYPES)}")
+        self.tensors = t = {n: tensors.get(n) for n in self._TYPES}
+        for n, v in t.items():
+            if v is not None and (v.dtype != self._TYPES[n] or not v.is_contiguous()):
+                raise ValueError(f"{n}: a dense {self._TYPES[n]} tensor is expected")
+        for n, more in (("hist", ("hist_begin", "hist_len")), ("bias", ("bias_id", "bias_begin", "bias_len")),
+                        ("mask", ("mask_row",))):
+            if t[n] is not None and any(t[m] is None for m in more):
+                raise ValueError(f"{n} needs {', '.join(more)}")
+        if t["mask"] is not None and (t["mask"].dim() != 2 or t["mask"].shape[1] < 1):
+            raise ValueError("mask: a tensor [n_masks, mask_words] is expected")
+        if t["bias"] is not None and t["bias_id"].numel() < t["bias"].numel():
+            raise ValueError("bias_id: as many as biases are expected")
+        devices = {v.device for v in t.values() if v is not None}
+        if len(devices) > 1:
+            raise ValueError("the adjustment's tensors are on different devices")
+        self.device = devices.pop() if devices else None
+        per_request = [v.numel() for n, v in t.items() if v is not None and n not in ("hist", "bias", "bias_id", "mask")]
+        self.n = min(per_request, default=None)                              # requests they are enough for
+        size = lambda n: 0 if t[n] is None else t[n].numel()  # noqa: E731
+        shape = (0, 1) if t["mask"] is None else t["mask"].shape
+        # a tensor without elements has no address: an address that nothing is read from says that the group is there
+        at = lambda n: None if t[n] is None else t[n].data_ptr() or 16  # noqa: E731
+        self.c = vfm_adjust(at("repetition"), at("presence"), at("frequency"), at("hist"), size("hist"),
+                            at("hist_begin"), at("hist_len"), at("n_prompt"), at("bias"), at("bias_id"), size("bias"),
+                            at("bias_begin"), at("bias_len"), at("mask"), _i32(shape[0], "n_masks"),
+                            _i32(shape[1], "mask_words"), at("mask_row"))
+
+
+def vfm_adjust_outputs(batch, out, adjust, adjusted=None, stream=None):
+    """Head outputs under the penalties, biases and masks of an OutputAdjust; adjusted: where to (default: in place)."""
+    n, dev, total = batch.plan_host[0], out.device, batch.plan_host[6]
+    if adjust.n is not None and (adjust.n < n or adjust.device != dev):
+        raise ValueError(f"the adjustment is for {adjust.n} requests on {adjust.device}, the batch has {n} on {dev}")
+    src = _operand(out, "out", torch.float32, total, _same_device(dev))
+    dst = src if adjusted is None else _operand(adjusted, "adjusted", torch.float32, total, dev)
+    if dst != src and src < dst + 4 * total and dst < src + 4 * total:
+        raise ValueError("adjusted: out itself or memory apart from it is expected")
+    st = _lib_handle().vfm_adjust_outputs(C.byref(batch), src, C.byref(adjust.c), dst, _stream(stream, dev))
+    _check(st, "vfm_adjust_outputs")
+
+
+# ---- decoding over a cache held in 8 bits (include/vfm_kv8.h) ----------------
+class PagedKVQ8:
+    """One layer's paged K / V pool in 8 bits: codes k, v (device, torch.float8_e4m3fn or uint8, [n_kv_heads,
+    n_pages * page_size, head_dim]) and exponents exps (device uint8 [n_pages * page_size / 16, n_kv_heads, 2]), with a
+    page table (host int32 [n_req, max_pages], original request order), as the C struct vfm_kv_pages_q8."""
+
+    def __init__(self, k, v, exps, page_size, table, device="cuda"):
+        types = (torch.float8_e4m3fn, torch.uint8)
+        if k.dtype not in types or v.dtype not in types or exps.dtype != torch.uint8:
+            raise ValueError("k, v: 8-bit codes, exps: uint8 exponents are expected")
+        self.k, self.v, self.exps = k, v, exps
+        base = PagedKV(k.view(torch.uint8), v.view(torch.uint8), page_size, table, device)
+        self.table, self.table_dev = base.table, base.table_dev
+        self.c = vfm_kv_pages_q8(base.c, exps.data_ptr())
+        fits = base.layout is not None and exps.is_contiguous() and exps.device == k.device and \
+            tuple(exps.shape) == (k.shape[1] // 16, k.shape[0], 2)
+        self.layout = base.layout[1:] if fits else None
+
+
+def _cache_q8(kv, attn, device):
+    if not isinstance(kv, PagedKVQ8):
+        return kv
+    if kv.layout != (attn.n_kv_heads, attn.head_dim, device):
+        raise ValueError("the cache's pools, exponents and table are not dense [n_kv_heads, n_pages * page_size, head_dim] "
+                         "and [n_pages * page_size / 16, n_kv_heads, 2] on the rows' device")
+    return kv.c
+
+
+def vfm_kv_append_q8(attn, batch, qkv, q_out, kv, stream=None):
+    """As vfm_kv_append, to a PagedKVQ8 (or a vfm_kv_pages_q8)."""
+    hd, T, td, dev = attn.head_dim, batch.plan_host[2], _TORCH_DTYPE.get(attn.dtype), qkv.device
+    p, ld = _rows(qkv, "qkv", td, T, (attn.n_heads + 2 * attn.n_kv_heads) * hd, dev)
+    q, c = _operand(q_out, "q_out", td, T * attn.n_heads * hd, dev), _cache_q8(kv, attn, _same_device(dev))
+    st = _lib_handle().vfm_kv_append_q8(C.byref(attn), C.byref(batch), p, ld, q, C.byref(c), _stream(stream, dev))
+    _check(st, "vfm_kv_append_q8")
+
+
+def vfm_attention_workspace_q8(attn, batch) -> int:
+    n = C.c_size_t()
+    _check(_lib_handle().vfm_attention_workspace_q8(C.byref(attn), C.byref(batch), C.byref(n)),
+           "vfm_attention_workspace_q8")
+    return n.value
+
+
+def vfm_attention_paged_q8(attn, batch, q, kv, out, workspace=None, stream=None):
+    """As vfm_attention_paged, over a PagedKVQ8 (or a vfm_kv_pages_q8)."""
+    cols, T, td, dev = attn.n_heads * attn.head_dim, batch.plan_host[2], _TORCH_DTYPE.get(attn.dtype), q.device
+    pq, ldq = _rows(q, "q", td, T, cols, dev)
+    po, ldo = _rows(out, "out", td, T, cols, dev)
+    c = _cache_q8(kv, attn, _same_device(dev))
+    ws, nb = None, 0
+    if workspace is not None:
+        if workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace: a dense tensor on {dev} is expected")
+        ws, nb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    st = _lib_handle().vfm_attention_paged_q8(C.byref(attn), C.byref(batch), pq, ldq, C.byref(c), po, ldo, ws, nb,
+                                              _stream(stream, dev))
+    _check(st, "vfm_attention_paged_q8")
+
+
+def vfm_workspace_size_q8(cfg, batch, lora=None, window=0, n_sink=0) -> int:
+    n = C.c_size_t()
+    st = _lib_handle().vfm_workspace_size_q8(C.byref(cfg), C.byref(batch), C.byref(lora) if lora is not None else None,
+                                             _i32(window, "window"), _i32(n_sink, "n_sink"), C.byref(n))
+    _check(st, "vfm_workspace_size_q8")
+    return n.value
+
+
+def vfm_layer_forward_q8(cfg, weights, lora, batch, x, kv, window, n_sink, workspace, stream=None):
+    """kv: a PagedKVQ8, or a vfm_kv_pages_q8 struct built by the caller."""
+    kvc, window, n_sink = kv.c if isinstance(kv, PagedKVQ8) else kv, _i32(window, "window"), _i32(n_sink, "n_sink")
+    st = _lib_handle().vfm_layer_forward_q8(C.byref(cfg), C.byref(weights),
+                                            C.byref(lora) if lora is not None else None, C.byref(batch), _ptr(x),
+                                            C.byref(kvc), window, n_sink, workspace.data_ptr(),
+                                            workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "vfm_layer_forward_q8")
 
 
 # ---- KV page allocator (host, include/vfm_pages.h) --------------------------

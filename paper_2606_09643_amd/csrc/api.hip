@@ -326,9 +326,10 @@ int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, At
   return VFM_OK;
 }
 
+// exps: k and v are codes with these exponents (vfm_kv8.h), or NULL
 hipError_t run_attention(const vfm_attn& a, const Plan& pl, const AttnPlan& ap, const void* q, int64_t ldq, const void* k,
-                         const void* v, int64_t slots, const KvPages& kp, void* out, int64_t ldo, char* ws,
-                         hipStream_t s) {
+                         const void* v, const uint8_t* exps, int64_t slots, const KvPages& kp, void* out, int64_t ldo,
+                         char* ws, hipStream_t s) {
   PagedAttn p = {};
   p.H = a.n_heads; p.KH = a.n_kv_heads; p.G = a.n_heads / a.n_kv_heads;
   p.window = a.window; p.n_sink = a.window > 0 ? a.n_sink : 0;
@@ -343,6 +344,8 @@ hipError_t run_attention(const vfm_attn& a, const Plan& pl, const AttnPlan& ap, 
     p.rec_o = (float*)(ws + ap.table_bytes(pl));
     p.rec_ml = (float2*)((char*)p.rec_o + align_up((size_t)ap.recs * a.head_dim * 4));
   }
+  if (exps != nullptr)
+    return launch_attention8(a.dtype, a.head_dim, pl, p, exps, ap.few_blocks, ap.rows_blocks, ap.joins, ap.table, s);
   return launch_attention_paged(a.dtype, a.head_dim, pl, p, ap.few_blocks, ap.rows_blocks, ap.joins, ap.one,
                                 ap.table, s);
 }
@@ -385,11 +388,12 @@ int check_layer(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_t
   return VFM_OK;
 }
 
-// win: attention over the paged cache with a window and sinks (vfm_layer_forward_windowed), or NULL.
+// win: attention over the paged cache with a window and sinks (vfm_layer_forward_windowed), or NULL; exps: with it, the
+// cache is held in 8 bits under these exponents (vfm_layer_forward_q8).
 int layer_impl(const vfm_cfg& c, const vfm_layer_weights* w, const vfm_lora_table* lora,
                const vfm_batch* batch, const Plan& pl, float* x, void* k_cache, void* v_cache,
                int64_t kv_slots, const KvPages& kp, void* workspace, size_t ws_bytes, void* stream,
-               const vfm_attn* win = nullptr);
+               const vfm_attn* win = nullptr, uint8_t* exps = nullptr);
 
 }  // namespace
 
@@ -513,7 +517,7 @@ namespace {
 int layer_impl(const vfm_cfg& c, const vfm_layer_weights* w, const vfm_lora_table* lora,
                const vfm_batch* batch, const Plan& pl, float* x, void* k_cache, void* v_cache,
                int64_t kv_slots, const KvPages& kp, void* workspace, size_t ws_bytes, void* stream,
-               const vfm_attn* win) {
+               const vfm_attn* win, uint8_t* exps) {
   const int d = c.d_model, f = c.d_ff, T = pl.T;
   const int max_keys = max_keys_of(batch, pl);
   AttnPlan ap = {};
@@ -687,10 +691,17 @@ int layer_impl(const vfm_cfg& c, const vfm_layer_weights* w, const vfm_lora_tabl
   if (win) {
     // Rotation in place and cache write in one pass: a sequence that keeps a window of its past goes on to
     // positions at which an angle in fp32 is off (position 700: by up to 4e-5, position 10^6: by 0.06).
-    VFM_TIMED(VFM_PROF_OTHER, launch_kv_append(c.dtype, pl, c.n_heads, c.n_heads, c.head_dim, c.rope_theta, qkv,
-                                               3 * (int64_t)d, c.rope_theta > 0.f ? qkv : nullptr, 3 * (int64_t)d,
-                                               k_cache, v_cache, kv_slots, kp, s));
-    VFM_HIP(run_attention(*win, pl, ap, qkv, 3 * (int64_t)d, k_cache, v_cache, kv_slots, kp, attn, d, base + ws.aws, s));
+    void* const q_out = c.rope_theta > 0.f ? qkv : nullptr;
+    if (exps) {
+      const Pool8 pool = {(uint8_t*)k_cache, (uint8_t*)v_cache, exps, kv_slots};
+      VFM_TIMED(VFM_PROF_OTHER, launch_append8(c.dtype, pl, c.n_heads, c.n_heads, c.head_dim, c.rope_theta, qkv,
+                                               3 * (int64_t)d, q_out, 3 * (int64_t)d, pool, kp, s));
+    } else {
+      VFM_TIMED(VFM_PROF_OTHER, launch_kv_append(c.dtype, pl, c.n_heads, c.n_heads, c.head_dim, c.rope_theta, qkv,
+                                                 3 * (int64_t)d, q_out, 3 * (int64_t)d, k_cache, v_cache, kv_slots, kp, s));
+    }
+    VFM_HIP(run_attention(*win, pl, ap, qkv, 3 * (int64_t)d, k_cache, v_cache, exps, kv_slots, kp, attn, d,
+                          base + ws.aws, s));
   }
   bool chunked = false;                      // a prompt chunk after cached tokens
   if (!win && c.attn == VFM_ATTN_MIXED) {
@@ -805,9 +816,12 @@ extern "C" int vfm_workspace_size_windowed(const vfm_cfg* cfg, const vfm_batch* 
   return VFM_OK;
 }
 
-extern "C" int vfm_layer_forward_windowed(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_table* lora,
-                                          const vfm_batch* batch, float* x, const vfm_kv_pages* kv, int32_t window,
-                                          int32_t n_sink, void* workspace, size_t ws_bytes, void* stream) {
+namespace {
+
+// A layer over a paged cache, in 8 bits where exps is given.
+int layer_windowed(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_table* lora, const vfm_batch* batch,
+                   float* x, const vfm_kv_pages* kv, uint8_t* exps, int32_t window, int32_t n_sink, void* workspace,
+                   size_t ws_bytes, void* stream) {
   VFM_TRY(check_pool(kv));
   Plan pl;
   VFM_TRY(check_layer(cfg, w, lora, batch, x, true, &pl, true));
@@ -818,20 +832,57 @@ extern "C" int vfm_layer_forward_windowed(const vfm_cfg* cfg, const vfm_layer_we
   VFM_TRY(check_pages(a, batch, pl, kv, true));
   VFM_TRY(check_stream(stream));
   return layer_impl(*cfg, w, lora, batch, pl, x, kv->k, kv->v, kv->n_pages * kv->page_size, pages_of(kv), workspace,
-                    ws_bytes, stream, &a);
+                    ws_bytes, stream, &a, exps);
 }
 
-extern "C" int vfm_kv_append(const vfm_attn* attn, const vfm_batch* batch, const void* qkv, int64_t ld, void* q_out,
-                             const vfm_kv_pages* kv, void* stream) {
+// vfm_attention_paged and its form over 8 bits.
+int attend_paged(const vfm_attn* attn, const vfm_batch* batch, const void* q, int64_t ldq, const vfm_kv_pages* kv,
+                 const uint8_t* exps, void* out, int64_t ldo, void* workspace, size_t ws_bytes, void* stream) {
   VFM_TRY(check_attn(attn));
   VFM_TRY(check_pool(kv));
   Plan pl;
   VFM_TRY(check_batch(batch, &pl));
+  if (!q || !out || !aligned16(q) || !aligned16(out)) return VFM_ERR_ARG;
+  const int64_t cols = (int64_t)attn->n_heads * attn->head_dim;
+  if (ldq % 8 || ldo % 8 || ldq < cols || ldo < cols) return VFM_ERR_SHAPE;
+  VFM_TRY(check_pages(*attn, batch, pl, kv, true));
+  AttnPlan ap;
+  VFM_TRY(plan_attention(*attn, batch, pl, &ap));
+  if (ap.bytes > 0 && (!workspace || ws_bytes < (size_t)ap.bytes || ((uintptr_t)workspace % ALIGN)))
+    return VFM_ERR_WORKSPACE;
+  VFM_TRY(check_stream(stream));
+  VFM_HIP(run_attention(*attn, pl, ap, q, ldq, kv->k, kv->v, exps, kv->n_pages * kv->page_size, pages_of(kv), out, ldo,
+                        (char*)workspace, (hipStream_t)stream));
+  return VFM_OK;
+}
+
+// What the two appends check; the plan of the batch.
+int check_append(const vfm_attn* attn, const vfm_batch* batch, const void* qkv, int64_t ld, const void* q_out,
+                 const vfm_kv_pages* kv, void* stream, Plan* pl) {
+  VFM_TRY(check_attn(attn));
+  VFM_TRY(check_pool(kv));
+  VFM_TRY(check_batch(batch, pl));
   if (!qkv || !q_out || !aligned16(qkv) || !aligned16(q_out)) return VFM_ERR_ARG;
   if (ld % 8 || ld < (int64_t)(attn->n_heads + 2 * attn->n_kv_heads) * attn->head_dim) return VFM_ERR_SHAPE;
-  if ((int64_t)pl.T * APPEND_THREADS > kMaxThreads) return VFM_ERR_UNSUPPORTED;
-  VFM_TRY(check_pages(*attn, batch, pl, kv, false));
-  VFM_TRY(check_stream(stream));
+  if ((int64_t)pl->T * APPEND_THREADS > kMaxThreads) return VFM_ERR_UNSUPPORTED;
+  VFM_TRY(check_pages(*attn, batch, *pl, kv, false));
+  return check_stream(stream);
+}
+
+int check_exps(const vfm_kv_pages_q8* kv) { return kv && kv->exps && aligned16(kv->exps) ? VFM_OK : VFM_ERR_ARG; }
+
+}  // namespace
+
+extern "C" int vfm_layer_forward_windowed(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_table* lora,
+                                          const vfm_batch* batch, float* x, const vfm_kv_pages* kv, int32_t window,
+                                          int32_t n_sink, void* workspace, size_t ws_bytes, void* stream) {
+  return layer_windowed(cfg, w, lora, batch, x, kv, nullptr, window, n_sink, workspace, ws_bytes, stream);
+}
+
+extern "C" int vfm_kv_append(const vfm_attn* attn, const vfm_batch* batch, const void* qkv, int64_t ld, void* q_out,
+                             const vfm_kv_pages* kv, void* stream) {
+  Plan pl;
+  VFM_TRY(check_append(attn, batch, qkv, ld, q_out, kv, stream, &pl));
   hipStream_t s = (hipStream_t)stream;
   VFM_TIMED(VFM_PROF_OTHER, launch_kv_append(attn->dtype, pl, attn->n_heads, attn->n_kv_heads, attn->head_dim,
                                              attn->rope_theta, qkv, ld, q_out,
@@ -854,22 +905,7 @@ extern "C" int vfm_attention_workspace(const vfm_attn* attn, const vfm_batch* ba
 extern "C" int vfm_attention_paged(const vfm_attn* attn, const vfm_batch* batch, const void* q, int64_t ldq,
                                    const vfm_kv_pages* kv, void* out, int64_t ldo, void* workspace, size_t ws_bytes,
                                    void* stream) {
-  VFM_TRY(check_attn(attn));
-  VFM_TRY(check_pool(kv));
-  Plan pl;
-  VFM_TRY(check_batch(batch, &pl));
-  if (!q || !out || !aligned16(q) || !aligned16(out)) return VFM_ERR_ARG;
-  const int64_t cols = (int64_t)attn->n_heads * attn->head_dim;
-  if (ldq % 8 || ldo % 8 || ldq < cols || ldo < cols) return VFM_ERR_SHAPE;
-  VFM_TRY(check_pages(*attn, batch, pl, kv, true));
-  AttnPlan ap;
-  VFM_TRY(plan_attention(*attn, batch, pl, &ap));
-  if (ap.bytes > 0 && (!workspace || ws_bytes < (size_t)ap.bytes || ((uintptr_t)workspace % ALIGN)))
-    return VFM_ERR_WORKSPACE;
-  VFM_TRY(check_stream(stream));
-  VFM_HIP(run_attention(*attn, pl, ap, q, ldq, kv->k, kv->v, kv->n_pages * kv->page_size, pages_of(kv), out, ldo,
-                        (char*)workspace, (hipStream_t)stream));
-  return VFM_OK;
+  return attend_paged(attn, batch, q, ldq, kv, nullptr, out, ldo, workspace, ws_bytes, stream);
 }
 
 extern "C" int vfm_sample_tokens(const vfm_batch* batch, const float* out, const vfm_sampling* sampling, const float* u,
@@ -885,4 +921,66 @@ extern "C" int vfm_sample_tokens(const vfm_batch* batch, const float* out, const
   if ((int64_t)pl.n_req * sample_threads(most) > kMaxThreads) return VFM_ERR_UNSUPPORTED;
   VFM_TRY(check_stream(stream));
   return hip_status(launch_sample(pl, out, *sampling, u, ids, logprob, most, (hipStream_t)stream));
+}
+
+extern "C" int vfm_adjust_outputs(const vfm_batch* batch, const float* out, const vfm_adjust* adjust, float* adjusted,
+                                  void* stream) {
+  Plan pl;
+  VFM_TRY(check_batch(batch, &pl));
+  if (!out || !adjust || !adjusted || !aligned16(out) || !aligned16(adjusted)) return VFM_ERR_ARG;
+  const vfm_adjust& a = *adjust;
+  if (a.hist && (!a.hist_begin || !a.hist_len)) return VFM_ERR_ARG;
+  if (a.bias && (!a.bias_id || !a.bias_begin || !a.bias_len)) return VFM_ERR_ARG;
+  if (a.mask && !a.mask_row) return VFM_ERR_ARG;
+  if (a.n_hist < 0 || a.n_bias < 0 || (a.mask && (a.n_masks < 0 || a.mask_words < 1))) return VFM_ERR_SHAPE;
+  const PlanOffsets po = plan_offsets(pl.n_req, pl.n_tasks, pl.T);
+  const int32_t* off = host_arr(batch, po.out_off);
+  int most = 0;
+  for (int i = 0; i < pl.n_req; ++i) most = std::max(most, off[i + 1] - off[i]);
+  if (pl.n_req > 1 << 23 || adjust_blocks(pl.n_req, most) > kMaxThreads / ADJUST_THREADS) return VFM_ERR_UNSUPPORTED;
+  VFM_TRY(check_stream(stream));
+  if (most == 0) return VFM_OK;
+  hipStream_t s = (hipStream_t)stream;
+  VFM_TIMED(VFM_PROF_OTHER, launch_adjust(pl, out, adjusted, a, most, s));
+  return VFM_OK;
+}
+
+// ---- decoding over a cache held in 8 bits (vfm_kv8.h) --------------------------
+
+extern "C" int vfm_kv_append_q8(const vfm_attn* attn, const vfm_batch* batch, const void* qkv, int64_t ld, void* q_out,
+                                const vfm_kv_pages_q8* kv, void* stream) {
+  VFM_TRY(check_exps(kv));
+  const vfm_kv_pages& pages = kv->pages;
+  Plan pl;
+  VFM_TRY(check_append(attn, batch, qkv, ld, q_out, &pages, stream, &pl));
+  hipStream_t s = (hipStream_t)stream;
+  const Pool8 pool{(uint8_t*)pages.k, (uint8_t*)pages.v, (uint8_t*)kv->exps, pages.n_pages * pages.page_size};
+  VFM_TIMED(VFM_PROF_OTHER, launch_append8(attn->dtype, pl, attn->n_heads, attn->n_kv_heads, attn->head_dim,
+                                           attn->rope_theta, qkv, ld, q_out, (int64_t)attn->n_heads * attn->head_dim,
+                                           pool, pages_of(&pages), s));
+  return VFM_OK;
+}
+
+extern "C" int vfm_attention_workspace_q8(const vfm_attn* attn, const vfm_batch* batch, size_t* bytes) {
+  return vfm_attention_workspace(attn, batch, bytes);
+}
+
+extern "C" int vfm_attention_paged_q8(const vfm_attn* attn, const vfm_batch* batch, const void* q, int64_t ldq,
+                                      const vfm_kv_pages_q8* kv, void* out, int64_t ldo, void* workspace,
+                                      size_t ws_bytes, void* stream) {
+  VFM_TRY(check_exps(kv));
+  return attend_paged(attn, batch, q, ldq, &kv->pages, (const uint8_t*)kv->exps, out, ldo, workspace, ws_bytes, stream);
+}
+
+extern "C" int vfm_workspace_size_q8(const vfm_cfg* cfg, const vfm_batch* batch, const vfm_lora_table* lora,
+                                     int32_t window, int32_t n_sink, size_t* bytes) {
+  return vfm_workspace_size_windowed(cfg, batch, lora, window, n_sink, bytes);
+}
+
+extern "C" int vfm_layer_forward_q8(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_table* lora,
+                                    const vfm_batch* batch, float* x, const vfm_kv_pages_q8* kv, int32_t window,
+                                    int32_t n_sink, void* workspace, size_t ws_bytes, void* stream) {
+  VFM_TRY(check_exps(kv));
+  return layer_windowed(cfg, w, lora, batch, x, &kv->pages, (uint8_t*)kv->exps, window, n_sink, workspace, ws_bytes,
+                        stream);
 }

@@ -3,6 +3,7 @@
 
 #include "vfm_decode.h"
 #include "vfm_internal.h"
+#include "vfm_kv8.h"
 
 // One attention over a paged cache, as the kernels take it.
 struct PagedAttn {
@@ -124,7 +125,39 @@ hipError_t launch_kv_append(int dtype, const Plan& pl, int H, int KH, int head_d
 hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, int64_t few_blocks,
                                   int64_t rows_blocks, int64_t joins, bool one, bool table, hipStream_t s);
 
+// its parts: a.table written, and the chunks' records joined
+void launch_attention_table(int dtype, const Plan& pl, const PagedAttn& a, hipStream_t s);
+void launch_attention_joins(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, int joins, bool table, hipStream_t s);
+
+// ---- a cache held in 8 bits (k_kv8.hip) ----
+struct Pool8 {
+  uint8_t *k, *v;              // codes [n_kv_heads][slots][head_dim]
+  uint8_t* exps;               // [slots / 16][n_kv_heads][2]
+  int64_t slots;
+};
+// From this many rows on a block of the append takes the runs of 16 rows (a prompt's whole run), below of one.
+constexpr int APPEND8_GROUPED = 2048;
+// q_out, ldq: as launch_kv_append
+hipError_t launch_append8(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv, int64_t ld,
+                          void* q_out, int64_t ldq, const Pool8& pool, const KvPages& kp, hipStream_t s);
+// a.k, a.v: the pools' codes; the other arguments as launch_attention_paged's
+hipError_t launch_attention8(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, const uint8_t* exps, int64_t few_blocks,
+                             int64_t rows_blocks, int64_t joins, bool table, hipStream_t s);
+
 // max_out: the batch's longest row of head outputs; a block of that many threads per request
 inline int sample_threads(int max_out) { return max_out <= 1024 ? 256 : 1024; }
 hipError_t launch_sample(const Plan& pl, const float* out, const vfm_sampling& sp, const float* u, int32_t* ids,
                          float* logprob, int max_out, hipStream_t s);
+
+// ---- penalties, biases and masks on head outputs (k_adjust.hip) ----
+// Outputs that a block takes: where the larger slices give every CU a block, fewer blocks go through a request's
+// earlier tokens; below that the smaller ones spread a request over more CUs.
+constexpr int ADJUST_SLICE = 8192, ADJUST_THREADS = 512, ADJUST_SMALL = 1024, ADJUST_SMALL_THREADS = 256;
+// blocks of slice s begin at s * adjust_rows: a multiple of 8, so a request's blocks share their number mod 8, the XCD
+inline int adjust_rows(int n_req) { return (n_req + 7) & ~7; }
+inline int64_t adjust_slices(int max_out, int slice) { return ((int64_t)max_out + 3 + slice - 1) / slice; }
+inline int adjust_small(int n_req, int max_out) { return n_req * adjust_slices(max_out, ADJUST_SLICE) < 256 || max_out <= ADJUST_SMALL; }
+inline int64_t adjust_blocks(int n_req, int max_out) {
+  return adjust_rows(n_req) * adjust_slices(max_out, adjust_small(n_req, max_out) ? ADJUST_SMALL : ADJUST_SLICE);
+}
+hipError_t launch_adjust(const Plan& pl, const float* in, float* out, const vfm_adjust& a, int max_out, hipStream_t s);

@@ -1,0 +1,1086 @@
+// A paged KV cache held in 8 bits: appending rotated keys and values to it, and attention of new rows over it.
+//
+// K and V are e4m3 codes; the 16 positions of a run (an aligned 16 of a page) share one scale per key head, a power of two
+// 2^(e - 127) whose exponent byte e lies beside the other pool's: exps[run][key head][K, V].  A power of two, because a run
+// fills up over several steps: when a later row needs a larger scale, the codes that are there move by their exponents
+// and keep their mantissas (all but those that become subnormal), where a scale of any size would round them anew.
+// It also is what gfx950's conversions multiply by for nothing: v_cvt_scalef32_pk_{bf16,f32}_fp8 give code 2^(e - 127)
+// exactly, as e4m3 has 4 significant bits and bf16 8.
+#include "paged_device.h"
+
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// what the scale's exponent byte stands for, as the conversions take it (they look at the exponent field alone)
+__device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
+
+// 8 codes times their scale
+__device__ __forceinline__ bf16x8 decode8(uint32_t lo, uint32_t hi, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  const bf16x4 l = __builtin_shufflevector(a, b, 0, 1, 2, 3), h = __builtin_shufflevector(c, d, 0, 1, 2, 3);
+  return __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// 4 codes times their scale
+__device__ __forceinline__ f32x4 decode4(uint32_t w, float scale) {
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, true);
+  return f32x4{a[0], a[1], b[0], b[1]};
+}
+// 4 values of at most 448 as codes, ties to even
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// ---------------------------------------------------------------------------
+// Append.  A block takes the runs that begin in its group of rows (a run of new rows: those of one request in one aligned
+// 16 positions), all of their heads or, with gridDim.y, some; a wave takes a head of the whole run, so the run's largest
+// magnitude is found by lane exchanges and the codes are written from the registers that hold the rotated values.
+// A single row (decode) leaves most of such a wave idle: there it takes 64 / (DH / 16) heads at once.
+//
+// Rotation in fp64, of operands that fp64 holds exactly: a code is one rounding of the rotated value, and scale and code
+// do not depend on how the angle's last bits came out.  The value goes through fp32 rounded to odd (cut, the last
+// bit set if anything was lost), after which rounding to 4 or 8 bits is as if from the fp64 value, and a comparison with a
+// number of few bits comes out the same.
+// ---------------------------------------------------------------------------
+constexpr float TOP8 = 3.19014718988379809e38f;          // 1.875 2^127: larger magnitudes would round to 2^128
+
+__device__ __forceinline__ float to_odd(double d) {
+  u32x2 w;
+  __builtin_memcpy(&w, &d, 8);
+  w[0] = (w[0] & 0xE0000000u) | ((w[0] & 0x1FFFFFFFu) ? 0x20000000u : 0u);
+  double r;
+  __builtin_memcpy(&r, &w, 8);
+  return (float)r;
+}
+__device__ __forceinline__ bool finite(double d) { return (__double2hiint(d) & 0x7FF00000) != 0x7FF00000; }
+
+template <typename T> struct Half8;                       // 8 elements of a row
+template <> struct Half8<bf16> {
+  bf16x8 v;
+  __device__ __forceinline__ float get(int i) const { return (float)v[i]; }
+  __device__ __forceinline__ void put(int i, float f) { v[i] = (bf16)f; }
+};
+template <> struct Half8<float> {
+  f32x4 v[2];
+  __device__ __forceinline__ float get(int i) const { return v[i >> 2][i & 3]; }
+  __device__ __forceinline__ void put(int i, float f) { v[i >> 2][i & 3] = f; }
+};
+
+struct Append8 {
+  int H, KH, rotate, group;    // group: rows whose runs a block takes
+  double log2_theta;
+  int64_t ld, ldq, slots;
+  uint8_t *k, *v, *exps;
+  KvPages kp;
+};
+
+// Heads `unit` * HPW .. of one run: nr rows from row r0 at position pos0, slot slot0.  ONE: nr is 1, and 64 / PER heads.
+template <typename T, int DH, bool ONE>
+__device__ __forceinline__ void append_heads(const Append8& a, const T* qkv, T* q_out, int unit,
+                                             int r0, int nr, int pos0, int64_t slot0, const double2* cs) {
+  constexpr int HALF = DH / 2, PER = HALF / 8;            // a lane holds pairs (i, i + HALF), 8 of them per item
+  constexpr int RPP = ONE ? 1 : 64 / PER;                 // rows of the wave's heads at a time
+  constexpr int NI = ONE ? 1 : 16 / RPP;                  // items of a lane
+  const int lane = threadIdx.x & 63;
+  const int head = ONE ? unit * (64 / PER) + lane / PER : unit;
+  const int ch = lane % PER, row0 = ONE ? 0 : lane / PER;
+  const int n_heads = a.H + 2 * a.KH;
+  if (ONE && head >= n_heads) return;                     // whole groups of PER lanes, which alone exchange values
+  const bool is_q = head < a.H, rot = a.rotate && head < a.H + a.KH;
+  if (is_q && q_out == nullptr) return;
+  Half8<T> x[NI], y[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int r = min(row0 + i * RPP, nr - 1);            // rows past the last: copies of it
+    const T* p = qkv + (int64_t)(r0 + r) * a.ld + (int64_t)head * DH + ch * 8;
+    x[i] = *reinterpret_cast<const Half8<T>*>(p);
+    y[i] = *reinterpret_cast<const Half8<T>*>(p + HALF);
+  }
+  float u[NI][16];                                        // the rotated pairs' first halves, then the second ones
+  float big = 0.f;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int r = min(row0 + i * RPP, nr - 1);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float f = x[i].get(j), g = y[i].get(j);
+      bool ff = true, gf = true;
+      if (rot) {
+        const double2 c = cs[(r * 8 + j) * PER + ch + r * PER];
+        const double p = f, q = g, s = fma(p, c.x, -(q * c.y)), t = fma(p, c.y, q * c.x);
+        const bool last = sizeof(T) == 4 && is_q;         // fp32 is where the value stays
+        f = last ? (float)s : to_odd(s);
+        g = last ? (float)t : to_odd(t);
+        ff = finite(s);
+        gf = finite(t);
+      } else if (!is_q) {
+        ff = fabsf(f) < INFINITY;
+        gf = fabsf(g) < INFINITY;
+      }
+      if (!is_q) {
+        f = ff ? fminf(fmaxf(f, -TOP8), TOP8) : NAN;
+        g = gf ? fminf(fmaxf(g, -TOP8), TOP8) : NAN;
+        big = fmaxf(big, fmaxf(fabsf(f), fabsf(g)));      // fmaxf passes over NaN
+      }
+      u[i][j] = f;
+      u[i][8 + j] = g;
+    }
+  }
+  if (is_q) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int r = row0 + i * RPP;
+      if (r >= nr) continue;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[i].put(j, u[i][j]);
+        y[i].put(j, u[i][8 + j]);
+      }
+      T* p = q_out + (int64_t)(r0 + r) * a.ldq + (int64_t)head * DH + ch * 8;
+      *reinterpret_cast<Half8<T>*>(p) = x[i];
+      *reinterpret_cast<Half8<T>*>(p + HALF) = y[i];
+    }
+    return;
+  }
+#pragma unroll
+  for (int m = 1; m < (ONE ? PER : 64); m <<= 1) big = fmaxf(big, __shfl_xor(big, m, 64));
+  // the least e >= 1 with big <= 448 2^(e - 127) = 1.75 2^(e - 119)
+  const uint32_t bits = __float_as_uint(big);
+  int e = (int)(bits >> 23) - 8 + ((bits & 0x7FFFFF) > 0x600000 ? 1 : 0);
+  e = big > 0.f && e > 1 ? e : 1;
+  const bool is_v = head >= a.H + a.KH;
+  const int kh = head - a.H - (is_v ? a.KH : 0);
+  uint8_t* pool = (is_v ? a.v : a.k) + ((int64_t)kh * a.slots + slot0) * DH;      // the run's first new row
+  uint8_t* ex = a.exps + (((slot0 >> 4) * a.KH + kh) << 1) + (is_v ? 1 : 0);
+  const int older = pos0 & 15;
+  if (older) {                                            // rows of earlier steps keep the run's scale at least as large
+    const int was = *ex;
+    if (was >= e) {
+      e = was;
+    } else {
+      // their codes times 2^(was - e), 16 bytes at a time; a shift of 2^-18 and less leaves zeros
+      const float down = scale_of(127 - min(e - was, 60));
+      constexpr int BPR = DH / 16;
+      for (int i = ONE ? ch : lane; i < older * BPR; i += ONE ? PER : 64) {
+        u32x4* p = reinterpret_cast<u32x4*>(pool - (int64_t)(older - i / BPR) * DH + (i % BPR) * 16);
+        u32x4 w = *p;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 f = decode4(w[j], 1.f) * down;
+          w[j] = encode4(f[0], f[1], f[2], f[3]);
+        }
+        *p = w;
+      }
+    }
+  }
+  // every lane of the head has read the byte: its loads are before the store in program order
+  if ((ONE ? ch : lane) == 0) *ex = (uint8_t)e;
+  const float inv = e < 254 ? scale_of(254 - e) : 1.f / scale_of(e);
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int r = row0 + i * RPP;
+    if (r >= nr) continue;
+    const float* w = u[i];
+    uint8_t* p = pool + (int64_t)r * DH + ch * 8;
+    *reinterpret_cast<u32x2*>(p) = u32x2{encode4(w[0] * inv, w[1] * inv, w[2] * inv, w[3] * inv),
+                                         encode4(w[4] * inv, w[5] * inv, w[6] * inv, w[7] * inv)};
+    *reinterpret_cast<u32x2*>(p + HALF) = u32x2{encode4(w[8] * inv, w[9] * inv, w[10] * inv, w[11] * inv),
+                                                encode4(w[12] * inv, w[13] * inv, w[14] * inv, w[15] * inv)};
+  }
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void append8_kernel(Plan pl, Append8 a, const T* qkv, T* q_out) {
+  constexpr int HALF = DH / 2, PER = HALF / 8;
+  // cosine and sine of row r, pair 8 ch + j at (r * 8 + j) * PER + ch + r * PER: lanes of a row read neighbours, rows
+  // differ in banks
+  __shared__ double2 cs[16 * 9 * PER];
+  const int first = blockIdx.x * a.group, end = min(first + a.group, pl.T);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int r0 = first, next; r0 < end; r0 = next) {
+    const int pos0 = uniform(pl.pos[r0]), p = uniform(pl.row_req[r0]);
+    const int begin = uniform(pl.cu_seqlens[p]), past = uniform(pl.cu_seqlens[p + 1]);
+    next = min(past, r0 + 16 - (pos0 & 15));
+    if (r0 != begin && (pos0 & 15)) continue;             // inside a run
+    const int nr = next - r0;
+    const int64_t slot0 = page_slot(row_of(a.kp, uniform(pl.order[p])), a.kp.log2_page, pos0);
+    if (a.rotate) {
+      if (r0 != first) __syncthreads();                   // block-uniform; the run before has been rotated
+      for (int i = threadIdx.x; i < nr * HALF; i += 256) {
+        const int r = i / HALF, k = i % HALF;
+        const double inv = exp2(-(2.0 * (double)k / (double)DH) * a.log2_theta) * 0.15915494309189535;
+        const double rev = (double)(pos0 + r) * inv;
+        double s, c;
+        sincospi(2.0 * (rev - rint(rev)), &s, &c);
+        cs[(r * 8 + (k & 7)) * PER + (k >> 3) + r * PER] = double2{c, s};
+      }
+      __syncthreads();
+    }
+    const int n_heads = a.H + 2 * a.KH, step = 4 * gridDim.y;
+    const int units = nr == 1 ? (n_heads + 64 / PER - 1) / (64 / PER) : n_heads;
+    for (int unit = blockIdx.y * 4 + wave; unit < units; unit += step) {
+      if (nr == 1) append_heads<T, DH, true>(a, qkv, q_out, unit, r0, nr, pos0, slot0, cs);
+      else append_heads<T, DH, false>(a, qkv, q_out, unit, r0, nr, pos0, slot0, cs);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Attention, bf16 queries: one block per 16 packed queries of one request and key head and chunk of its keys; each of the 4
+// waves streams every 4th 32-key tile of the chunk on its own and the waves' partial softmax sums are merged through
+// LDS at the end (as in the bf16 cache's few-row kernel, k_paged.hip).  Codes become bf16 in registers: K on the way to
+// the MFMA, V on the way to a wave-private LDS tile that the transposing LDS read turns into the V^T operand.
+// A lane's 16-byte load of a K row holds 16 consecutive head dims, two MFMA steps of 8; the queries' fragments take the
+// same dims, as a dot product does not mind their order.
+// ---------------------------------------------------------------------------
+// the exponent bytes of K (low) and V (high) of a run
+__device__ __forceinline__ uint32_t run_exps(const uint8_t* exps, int64_t slot, int KH, int h) {
+  return reinterpret_cast<const uint16_t*>(exps)[(slot >> 4) * KH + h];
+}
+
+__device__ __forceinline__ bool is_nan8(uint32_t code) { return (code & 0x7F) == 0x7F; }
+
+template <int DH, bool TABLE>
+__device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, const uint8_t* __restrict__ exps, int id, char* smem) {
+  constexpr int LPR = DH / 16;         // lanes per K / V row (16 bytes each)
+  constexpr int RPI = 64 / LPR;        // rows per wave-wide load
+  constexpr int VI = 32 / RPI;         // V loads per lane and tile
+  constexpr int KL = DH / 64;          // K loads per lane and 16 keys
+  constexpr int KS = DH / 32;          // MFMA steps over the head dims
+  constexpr int ND = DH / 16;          // output tiles
+  __shared__ float sm[4][16], sl[4][16];
+
+  Work w;
+  if constexpr (TABLE) {
+    w.p = request_at(table_of(pl, a, TAB_FEW), pl.n_req, id);
+  } else {
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % a.few_chunks; id /= a.few_chunks;
+    w.qt = id % a.qtiles;
+    w.p = id / a.qtiles;
+  }
+  const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
+  const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide
+  if (!few_rows(VFM_BF16, m, a.G)) return;              // block-uniform, as every exit below
+  const int qn = m * a.G;
+  if (!TABLE && w.qt * 16 >= qn) return;
+  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink);
+  if constexpr (TABLE) {
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % ck.n;
+    w.qt = id / ck.n;
+  } else if (w.c >= ck.n) {
+    return;
+  }
+  const Vis vis = visible_runs<4>(ctx, ctx + m - 1, a.window, a.n_sink);
+  const int t0 = w.c * ck.tiles, t1 = min(t0 + ck.tiles, (vis.n + 1) / 2);
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int x = lane & 15, g = lane >> 4;
+  const int qi = min(w.qt * 16 + x, qn - 1);
+  const int jq = ctx + qi / a.G;
+  const int j0 = ctx + w.qt * 16 / a.G, j1 = ctx + min(w.qt * 16 + 15, qn - 1) / a.G;
+  int head;
+  const int64_t row = out_row(a, R0, w.h, qi, head);
+  bf16x8 qf[KS];
+  {
+    const bf16* qr = (const bf16*)a.q + row * a.ldq + head * DH + 16 * g;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + 64 * (s >> 1) + 8 * (s & 1));
+  }
+  const page_row prow = row_of(a.kp, request);
+  const int lp = a.kp.log2_page;
+  const uint8_t* kh = (const uint8_t*)a.k + (int64_t)w.h * a.slots * DH;
+  const uint8_t* vh = (const uint8_t*)a.v + (int64_t)w.h * a.slots * DH;
+  bf16* Vs = reinterpret_cast<bf16*>(smem) + wave * 32 * DH;
+
+  // a tile's two runs (one page each, as a page holds a multiple of 16 positions); runs past the last re-read it, unseen
+  auto run_pos = [&](int t, int e) { return 16 * vis.run(min(2 * t + e, vis.n - 1)); };
+  u32x4 kf[2][2][KL], vf[2][VI];
+  uint32_t ex[2][2];
+  int slot[2];
+  auto look_up = [&](int t) {
+    slot[0] = page_slot(prow, lp, run_pos(t, 0));
+    slot[1] = page_slot(prow, lp, run_pos(t, 1));
+  };
+  // keys of sub-tile e in rows x: 8 (x / 4) + x % 4 + 4 e, so that after the MFMA
+  // a lane holds the 8 consecutive keys 8 g .. 8 g + 7 over both sub-tiles
+  const int key0 = 8 * (x >> 2) + (x & 3);
+  auto load = [&](int b) {
+    const int64_t ks = (int64_t)(x < 8 ? slot[0] : slot[1]) + (key0 & 15);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) ex[b][e] = run_exps(exps, slot[e], a.KH, w.h);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int s = 0; s < KL; ++s)
+        kf[b][e][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kh + (ks + 4 * e) * DH + 16 * g + 64 * s));
+#pragma unroll
+    for (int i = 0; i < VI; ++i) {
+      const int64_t vs = (int64_t)slot[(RPI * i) >> 4] + ((RPI * i) & 15) + lane / LPR;
+      vf[b][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vh + vs * DH + 16 * (lane % LPR)));
+    }
+  };
+
+  f32x4 o[ND];
+#pragma unroll
+  for (int i = 0; i < ND; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = LOWEST, l_run = 0.f;
+
+  const int vst_seg = lane % LPR, vst_row = lane / LPR;
+  const int vrow = 8 * g + (x >> 2);
+  const int vbase = vrow * DH * 2 + (vswz<DH>(vrow) << 5) + (x & 3) * 8;
+
+  auto compute = [&](int b, int t) {
+    const int p0 = run_pos(t, 0);
+    const int p1 = 2 * t + 1 < vis.n ? run_pos(t, 1) : INT32_MAX - 64;   // no second run: unseen
+    const bool full = p1 == p0 + 16 && seen_by_all(j0, j1, p0, p0 + 31, a.window, a.n_sink);
+    bool poison = false;
+    // V to LDS
+#pragma unroll
+    for (int i = 0; i < VI; ++i) {
+      const int r = RPI * i + vst_row;
+      const float scale = scale_of(ex[b][(RPI * i) >> 4] >> 8);
+      bf16x8 v[2] = {decode8(vf[b][i][0], vf[b][i][1], scale), decode8(vf[b][i][2], vf[b][i][3], scale)};
+      if (!full) {
+        const int k = (((RPI * i) >> 4) ? p1 : p0) + (r & 15);
+        if (!seen_by_any(j0, j1, k, a.window, a.n_sink)) {
+          v[0] = v[1] = bf16x8{};
+        } else if (j0 != j1 && !seen_by_all(j0, j1, k, k, a.window, a.n_sink)) {
+          v[0] = drop_nonfinite(v[0], poison);
+          v[1] = drop_nonfinite(v[1], poison);
+        }
+      }
+      bf16x8* at = reinterpret_cast<bf16x8*>(Vs + r * DH + (vst_seg ^ vswz<DH>(r)) * 16);
+      at[0] = v[0];
+      at[1] = v[1];
+    }
+    wave_lds_order();
+    // S^T
+    const float kscale = scale_of((x < 8 ? ex[b][0] : ex[b][1]) & 0xFF);
+    float s[8];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < KS; ++st) {
+        const u32x4& c = kf[b][e][st >> 1];
+        acc = mfma16(decode8(c[2 * (st & 1)], c[2 * (st & 1) + 1], kscale), qf[st], acc);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[4 * e + i] = acc[i];
+    }
+    if (!full) {
+      const int kb = (g < 2 ? p0 : p1) + 8 * (g & 1);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] = sees(jq, kb + i, a.window, a.n_sink) ? s[i] : -INFINITY;
+    }
+    float mb = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+    mb = max_x32(max_x16(mb));
+    if (__any(mb > m_run)) {                              // elsewhere the factor is 1
+      const float m_new = fmaxf(m_run, mb);
+      const float alpha = fast_exp2((m_run - m_new) * a.scale_log2);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int i = 0; i < ND; ++i) o[i] *= alpha;
+    }
+    float e8[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      e8[i] = fast_exp2((s[i] - m_run) * a.scale_log2);
+      l_run += e8[i];
+    }
+    const bf16x8 pf = pack8(e8[0], e8[1], e8[2], e8[3], e8[4], e8[5], e8[6], e8[7]);
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      const char* vp = reinterpret_cast<const char*>(Vs) + (vbase ^ (d << 5));
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp + 4 * DH * 2));
+      bf16x8 f;
+      __builtin_memcpy(&f, &lo, 8);
+      __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
+      o[d] = mfma16(f, pf, o[d]);
+    }
+    wave_lds_order();
+    if (__any(poison)) {                                  // rare: re-read the tile's V rows from memory
+      for (int r = 0; r < 32; ++r) {
+        const int k = (r < 16 ? p0 : p1) + (r & 15);
+        if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
+        const uint8_t* vr = vh + (int64_t)page_slot(prow, lp, k) * DH + 4 * g;
+        const bool see = sees(jq, k, a.window, a.n_sink);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const uint32_t c = *reinterpret_cast<const uint32_t*>(vr + 16 * d);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (see && is_nan8(c >> (8 * i))) o[d][i] = NAN;
+          __builtin_amdgcn_sched_barrier(0);              // no registers for more loads in flight
+        }
+      }
+    }
+  };
+
+  // tiles t0 + wave, + 4, ...: a tile's loads in flight while the one before is computed, its page lookups a tile
+  // before that
+  int t = t0 + wave;
+  if (t < t1) {
+    look_up(t);
+    load(0);
+    if (t + 4 < t1) look_up(t + 4);
+    for (;;) {
+      if (t + 4 < t1) { load(1); if (t + 8 < t1) look_up(t + 8); }
+      compute(0, t);
+      t += 4;
+      if (t >= t1) break;
+      if (t + 4 < t1) { load(0); if (t + 8 < t1) look_up(t + 8); }
+      compute(1, t);
+      t += 4;
+      if (t >= t1) break;
+    }
+  }
+  l_run = sum_x32(sum_x16(l_run));
+
+  // merge the four waves
+  __syncthreads();
+  float* so = reinterpret_cast<float*>(smem);             // [4][16][DH]
+  if (lane < 16) { sm[wave][x] = m_run; sl[wave][x] = l_run; }
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+    *reinterpret_cast<f32x4*>(so + (wave * 16 + x) * DH + 16 * d + 4 * g) = o[d];
+  __syncthreads();
+  const int nq = min(16, qn - w.qt * 16);
+  for (int e = tid; e < nq * DH / 4; e += 256) {
+    const int q = e / (DH / 4), d = (e % (DH / 4)) * 4;
+    const float M = fmaxf(fmaxf(sm[0][q], sm[1][q]), fmaxf(sm[2][q], sm[3][q]));
+    float L = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float wt = fast_exp2((sm[i][q] - M) * a.scale_log2);
+      L += sl[i][q] * wt;
+      // a wave without any visible key has weight 0 and zeros
+      acc += *reinterpret_cast<const f32x4*>(so + (i * 16 + q) * DH + d) * wt;
+    }
+    int hd;
+    const int64_t r = out_row(a, R0, w.h, w.qt * 16 + q, hd);
+    if (ck.n == 1) {
+      const float inv = 1.f / L;
+      bf16x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = (bf16)(acc[i] * inv);
+      *reinterpret_cast<bf16x4*>((bf16*)a.out + r * a.ldo + hd * DH + d) = v;
+    } else {
+      const int64_t rec = record_of<TABLE>(pl, a, w.p, R0, ck.n, r, hd) + w.c;
+      *reinterpret_cast<f32x4*>(a.rec_o + rec * DH + d) = acc;
+      if (d == 0) a.rec_ml[rec] = make_float2(M, L);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows (prompts and chunks), bf16: one block per 128 packed queries of one request and key head (and chunk of the keys
+// where the request has few blocks), waves of 32 queries, 64-key tiles in two LDS stages by turns, as in the bf16 cache's
+// many-row kernel (k_paged.hip).  Codes go through registers: a thread loads 16 of a K and of a V row ahead and stores
+// them as bf16 a step later, so each is converted once per block.
+// ---------------------------------------------------------------------------
+template <int DH, bool TABLE>
+__device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, const uint8_t* __restrict__ exps, int id, bf16* stage0, bf16* stage1) {
+  constexpr int NW = 4;                  // waves
+  constexpr int LPR = DH / 16;           // lanes per row of codes (16 bytes each)
+  constexpr int CH = DH / 8;             // 16-byte chunks per row of a stage
+  constexpr int RPI = 64 / LPR;          // rows per wave-wide load
+  constexpr int NI = 64 / (NW * RPI);    // K (and V) loads per wave and tile
+  constexpr int KS = DH / 16;            // MFMA steps over the head dims
+  constexpr int ND = DH / 32;            // output tiles
+  // Stage j: K of a tile t with t mod 2 = j, then V of tile t - 1 (a step reads K a tile ahead of V).
+  constexpr int TE = 64 * DH;
+  auto stage = [&](auto b) -> bf16* {
+    if constexpr (b == 0) return stage0;
+    else return stage1;
+  };
+  __shared__ int s_poison;
+
+  const int rb = rows_per_block(a.G);
+  Work w;
+  if constexpr (TABLE) {
+    w.p = request_at(table_of(pl, a, TAB_ROWS), pl.n_req, id);
+  } else {
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % a.rows_chunks; id /= a.rows_chunks;
+    // request p's blocks start at cu[p] / rb + p: at least ceil(m / rb) before the next request's
+    int lo = 0, hi = pl.n_req - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (uniform(pl.cu_seqlens[mid]) / rb + mid <= id) lo = mid; else hi = mid - 1;
+    }
+    w.p = lo;
+  }
+  const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
+  const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide
+  // a request's last rows see the most keys: they come first
+  const int nb = (m + rb - 1) / rb;
+  int bi = id - (R0 / rb + w.p);
+  if (few_rows(VFM_BF16, m, a.G) || (!TABLE && bi >= nb)) return;   // block-uniform, as every exit below
+  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink);
+  if constexpr (TABLE) {
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % ck.n;
+    bi = id / ck.n;
+  } else if (w.c >= ck.n) {
+    return;
+  }
+  const int r0 = (nb - 1 - bi) * rb, nr = min(rb, m - r0);
+  const int j0 = ctx + r0, j1 = j0 + nr - 1, qn = nr * a.G;
+  const Vis vis = visible_runs<6>(j0, j1, a.window, a.n_sink);
+  const int tpc = (vis.n + ck.n - 1) / ck.n;
+  const int t0 = w.c * tpc, t1 = min(t0 + tpc, vis.n);    // may be empty: an empty record
+  const int lo_any = a.window > 0 ? max(0, j0 - a.window + 1) : 0;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int x = lane & 31, h2 = lane >> 5;
+  const int qi = min(wave * 32 + x, qn - 1);
+  const int jq = j0 + qi / a.G;
+  // the wave's rows
+  const int wj0 = j0 + min(wave * 32, qn - 1) / a.G, wj1 = j0 + min(wave * 32 + 31, qn - 1) / a.G;
+  int head;
+  const int64_t row = out_row(a, R0 + r0, w.h, qi, head);
+  bf16x8 qf[KS];
+  {
+    const bf16* qr = (const bf16*)a.q + row * a.ldq + head * DH + 8 * h2;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s);
+  }
+  const page_row prow = row_of(a.kp, request);
+  const int lp = a.kp.log2_page;
+  const uint8_t* kh = (const uint8_t*)a.k + (int64_t)w.h * a.slots * DH;
+  const uint8_t* vh = (const uint8_t*)a.v + (int64_t)w.h * a.slots * DH;
+  if (tid == 0) s_poison = -1;
+
+  f32x16 o[ND];
+#pragma unroll
+  for (int i = 0; i < ND; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+  float m_run = LOWEST, l_run = 0.f;
+
+  // A lane's load i of a tile: 16 codes of row RPI (NW i + wave) + lane / LPR, from dim 16 (lane % LPR).
+  const int lrow = RPI * wave + lane / LPR;               // mod 16: the row in its run
+  const uint32_t off = (lrow & 15) * DH + (lane % LPR) * 16;   // from the run's first row, which is a scalar
+  // Pages of the wave's runs of a tile (scalar loads, a step ahead of their use) and where the runs
+  // start in them.  A run that no row sees reads a seen one instead: its page may not exist.
+  int page[NI], in_page[NI];
+  auto look_up = [&](int t) {
+    const int kb = 64 * vis.run(min(t, vis.n - 1));
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      int k = min(kb + (RPI * (NW * i + wave) & ~15), j1 & ~15);
+      if (k + 15 < lo_any && k >= a.n_sink) k = lo_any & ~15;
+      page[i] = prow[k >> lp];
+      in_page[i] = k & ((1 << lp) - 1);
+    }
+  };
+  // Loads K of the tile looked up last and V of the one looked up before it; looks `next` up.  Past the last tile that one
+  // is loaded again, into stages that nothing reads any more: the loop needs no branch.
+  int64_t vslot[NI] = {};
+  u32x4 kr[NI], vr[NI];
+  uint32_t kx[NI] = {}, vx[NI] = {};
+  auto load = [&](int next) {
+    int64_t kslot[NI], pslot[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      kslot[i] = (int64_t)((page[i] << lp) + in_page[i]);
+      pslot[i] = vslot[i];
+      vslot[i] = kslot[i];
+    }
+    look_up(next);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      vx[i] = kx[i];
+      kx[i] = run_exps(exps, kslot[i], a.KH, w.h);
+      kr[i] = *reinterpret_cast<const u32x4*>(kh + kslot[i] * DH + off);
+      vr[i] = *reinterpret_cast<const u32x4*>(vh + pslot[i] * DH + off);
+    }
+  };
+  // what was loaded, as bf16 into stage b
+  auto store = [&](auto b, bool with_v) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int r = RPI * NW * i + lrow, c = 2 * (lane % LPR);
+      const float ks = scale_of(kx[i] & 0xFF), vs = scale_of(vx[i] >> 8);
+      bf16* kd = stage(b) + r * DH;
+      *reinterpret_cast<bf16x8*>(kd + rows_kswz<DH>(r, c) * 8) = decode8(kr[i][0], kr[i][1], ks);
+      *reinterpret_cast<bf16x8*>(kd + rows_kswz<DH>(r, c + 1) * 8) = decode8(kr[i][2], kr[i][3], ks);
+      if (with_v) {
+        bf16* vd = kd + TE;
+        *reinterpret_cast<bf16x8*>(vd + rows_vswz<DH>(r, c) * 8) = decode8(vr[i][0], vr[i][1], vs);
+        *reinterpret_cast<bf16x8*>(vd + rows_vswz<DH>(r, c + 1) * 8) = decode8(vr[i][2], vr[i][3], vs);
+      }
+    }
+  };
+  // every wave's LDS accesses have finished
+  auto meet = [&]() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // V rows of a tile that some row of the block does not see: zeros where none sees them, no
+  // infinities or NaN where some do
+  auto mend = [&](auto b, int t) {
+    const int kb = 64 * vis.run(t);
+#pragma unroll 1
+    for (int i = 0; i < NI; ++i) {
+      const int r = RPI * NW * i + lrow, k = kb + r;
+      bf16x8* at = reinterpret_cast<bf16x8*>(stage(b) + TE + r * DH);
+      const int c[2] = {rows_vswz<DH>(r, 2 * (lane % LPR)), rows_vswz<DH>(r, 2 * (lane % LPR) + 1)};
+      if (!seen_by_any(j0, j1, k, a.window, a.n_sink)) {
+        at[c[0]] = at[c[1]] = bf16x8{};
+      } else if (!seen_by_all(j0, j1, k, k, a.window, a.n_sink)) {
+        bool found = false;
+        const bf16x8 v[2] = {drop_nonfinite(at[c[0]], found), drop_nonfinite(at[c[1]], found)};
+        if (found) { at[c[0]] = v[0]; at[c[1]] = v[1]; s_poison = t; }
+      }
+    }
+  };
+
+  // fragment addresses (bytes): K row x of a 32-key half, chunk 2 s + h2;
+  // V: the transposing read takes 4 keys x 16 dims per 16 lanes, lane (x & 15)
+  // bringing key (x & 15) / 4, dims 4 (x & 3).  Its rows differ from the lane's
+  // first by multiples of 8, which leave the swizzle alone.
+  const int kq = x & 15, gq = x >> 4;
+  const int kaddr = x * DH * 2 + (rows_kswz<DH>(x, h2) << 4);
+  const int vaddr = (4 * h2 + (kq >> 2)) * DH * 2 + (rows_vswz<DH>(kq >> 2, 0) << 4) + gq * 32 + (kq & 3) * 8;
+
+  // S^T of a tile: two 32-key halves; lane half h2, register i: key 8 (i / 4) + 4 h2 + i % 4
+  auto scores = [&](auto b, f32x16 (&st)[2]) {
+    const char* kp = reinterpret_cast<const char*>(stage(b));
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      f32x16 acc;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) acc[j] = 0.f;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const bf16x8 f = *reinterpret_cast<const bf16x8*>(kp + kt * 32 * DH * 2 + (kaddr ^ (s << 5)));
+        acc = mfma32(f, qf[s], acc);
+      }
+      st[kt] = acc;
+    }
+  };
+  auto mask = [&](int t, f32x16 (&st)[2]) {
+    const int kb = 64 * vis.run(t);
+    if (seen_by_all(wj0, wj1, kb, kb + 63, a.window, a.n_sink)) return;
+    // made anew in each masked tile: held over the loop, the compares' lane masks would fill the scalar registers
+    int d0 = jq - kb - 4 * h2, n0 = a.n_sink - kb - 4 * h2;     // of the lane's key 0
+    asm volatile("" : "+v"(d0), "+v"(n0));
+    const int win = a.window > 0 ? a.window : INT32_MAX;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int k = 32 * kt + 8 * (i >> 2) + (i & 3);
+        const bool see = (d0 >= k) & ((d0 - k < win) | (k < n0));
+        st[kt][i] = see ? st[kt][i] : -INFINITY;
+      }
+  };
+  // largest score of the lane's query
+  auto largest = [&](const f32x16 (&st)[2]) {
+    float mb = st[0][0];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mb = fmaxf(mb, st[kt][i]);
+    return max_x32(mb);
+  };
+  // The running maximum follows the scores only where one passes it by 8 (a factor of 256, which
+  // neither fp32 sums nor bf16 weights mind): with 32 queries a wave, some maximum grows in most
+  // tiles, and the products would be rescaled that often.
+  auto follow = [&](float mb) {
+    if (__any((mb - m_run) * a.scale_log2 > 8.f)) {
+      const float m_new = fmaxf(m_run, mb);
+      const float alpha = fast_exp2((m_run - m_new) * a.scale_log2);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int i = 0; i < ND; ++i) o[i] *= alpha;
+    }
+  };
+  // A weight is one fma here, 2^(s scale - m scale): the rest that m scale's rounding leaves is a factor common
+  // to all of a query's weights, below 2^(1/16) while |m scale| < 2^20.  Beyond (m at its start, too) the
+  // tile's scores are made differences from m first.  (Differences throughout: 579 us for the 564 of 4 chunks.)
+  float neg_m = 0.f;
+  auto settle = [&](f32x16 (&st)[2]) {
+    neg_m = -m_run * a.scale_log2;
+    if (__any(!(fabsf(neg_m) < 1048576.f))) {
+      neg_m = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[kt][i] -= m_run;
+    }
+  };
+  // P^T of 16 keys u of a tile, 8 of them in this lane
+  auto weights = [&](const f32x16 (&st)[2], int u, bf16x8 (&pf)[4]) {
+    float e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = fast_exp2(fmaf(st[u >> 1][8 * (u & 1) + i], a.scale_log2, neg_m));
+    pf[u] = pack8(e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]);
+  };
+  // Their sum, of the weights rounded to bf16 that the products use (two to an instruction; and what rounding
+  // adds to all weights of a row divides out), and the products
+  auto products = [&](auto b, const bf16x8 (&pf)[4]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        l_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[u][2 * i], pf[u][2 * i + 1]}, bf16x2{(bf16)1.f, (bf16)1.f}, l_run, false);
+    const char* vp = reinterpret_cast<const char*>(stage(b) + TE);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const char* q = vp + (vaddr ^ (d << 6)) + u * 16 * DH * 2;
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q + 8 * DH * 2));
+        bf16x8 f;
+        __builtin_memcpy(&f, &lo, 8);
+        __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
+        o[d] = mfma32(f, pf[u], o[d]);
+      }
+  };
+  // the NaN that `mend` took out of tile t
+  auto add_nonfinite = [&](int t) {
+    const int kb = 64 * vis.run(t);
+#pragma unroll 1
+    for (int r = 0; r < 64; ++r) {
+      const int k = kb + r;
+      if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
+      const uint8_t* vrow = vh + (int64_t)(page_slot(prow, lp, k)) * DH + 4 * h2;
+      if (sees(jq, k, a.window, a.n_sink)) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t c = *reinterpret_cast<const uint32_t*>(vrow + 32 * d + 8 * j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (is_nan8(c >> (8 * i))) o[d][4 * j + i] = NAN;
+            __builtin_amdgcn_sched_barrier(0);            // rare: no registers for loads in flight
+          }
+      }
+    }
+  };
+
+  // While the weights of tile t are computed (vector ALU), the matrix cores already take the scores
+  // of tile t + 1; while they take the products of t, its largest scores are found.  K of tile t + 1
+  // and V of tile t were stored a step ago from what had been loaded in the step before;
+  // the barrier makes every wave's part visible, and frees K of tile t and V of tile t - 1.
+  if (t0 < t1) {
+    f32x16 sa[2], sb[2];
+    look_up(t0);
+    load(t0 + 1);
+    store(std::integral_constant<int, 0>{}, false);
+    load(t0 + 2);
+    store(std::integral_constant<int, 1>{}, true);
+    load(t0 + 3);
+    meet();
+    scores(std::integral_constant<int, 0>{}, sa);
+    mask(t0, sa);
+    follow(largest(sa));
+    settle(sa);
+    // tile t, t mod 2 = j: its scores st, the next one's sn (behind the last tile: of what the stage
+    // holds, and not used)
+    auto step = [&](auto j, int t, f32x16 (&st)[2], f32x16 (&sn)[2]) {
+      constexpr auto jn = std::integral_constant<int, 1 - j>{};   // holds K of tile t + 1, V of tile t
+      meet();
+      const int kb = 64 * vis.run(t);
+      if (!seen_by_all(j0, j1, kb, kb + 63, a.window, a.n_sink)) {
+        mend(jn, t);
+        meet();
+      }
+      bf16x8 pf[4];
+      __builtin_amdgcn_sched_barrier(0);
+      // scores of t + 1 (2 KS MFMAs) beside the first half of t's weights
+      store(j, true);
+      load(t + 4);
+      scores(jn, sn);
+      weights(st, 0, pf);
+      weights(st, 1, pf);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(pf[u]));   // not put off behind the mask
+      __builtin_amdgcn_sched_barrier(0);
+      if (t + 1 < t1) mask(t + 1, sn);
+      __builtin_amdgcn_sched_barrier(0);
+      // products of t (4 ND MFMAs) beside the second half of its weights and the largest scores of t + 1
+      weights(st, 2, pf);
+      weights(st, 3, pf);
+      products(jn, pf);
+      const float mb = largest(sn);
+      __builtin_amdgcn_sched_barrier(0);
+      if (s_poison == t) add_nonfinite(t);
+      if (t + 1 >= t1) return false;
+      follow(mb);
+      settle(sn);
+      return true;
+    };
+    for (int t = t0;; t += 2) {
+      if (!step(std::integral_constant<int, 0>{}, t, sa, sb)) break;
+      if (!step(std::integral_constant<int, 1>{}, t + 1, sb, sa)) break;
+    }
+  }
+  l_run = sum_x32(l_run);
+  if (wave * 32 + x >= qn) return;
+  if (ck.n == 1) {
+    const float inv = 1.f / l_run;
+    bf16* orow = (bf16*)a.out + row * a.ldo + head * DH + 4 * h2;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bf16x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (bf16)(o[d][4 * j + i] * inv);
+        *reinterpret_cast<bf16x4*>(orow + 32 * d + 8 * j) = v;
+      }
+  } else {
+    const int64_t rec = record_of<TABLE>(pl, a, w.p, R0, ck.n, row, head) + w.c;
+    float* ro = a.rec_o + rec * DH + 4 * h2;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(ro + 32 * d + 8 * j) =
+            f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+    if (h2 == 0) a.rec_ml[rec] = make_float2(m_run, l_run);
+  }
+}
+
+// ROWS / FEW as in the bf16 cache's kernel (k_paged.hip): the blocks of a step's many-row requests, then those of its few-row
+// ones, in one launch.
+template <int DH, bool ROWS, bool FEW, bool TABLE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn8_bf16_kernel(
+    Plan pl, PagedAttn a, const uint8_t* __restrict__ exps, int rows_blocks) {
+  __shared__ __attribute__((aligned(16))) bf16 stage0[128 * DH], stage1[ROWS ? 128 * DH : 8];
+  if constexpr (FEW)
+    if ((int)blockIdx.x >= rows_blocks) {
+      few_block8<DH, TABLE>(pl, a, exps, (int)blockIdx.x - rows_blocks, reinterpret_cast<char*>(stage0));
+      return;
+    }
+  if constexpr (ROWS) rows_block8<DH, TABLE>(pl, a, exps, blockIdx.x, stage0, stage1);
+}
+
+// ---------------------------------------------------------------------------
+// fp32 queries, any number of rows: as the fp32 cache's kernel (k_paged.hip), the codes made fp32 in registers.  A lane
+// loads 16 consecutive head dims of its key's K row (its queries' registers hold the same ones), and DH / 16 consecutive
+// ones of V rows, which give as many MFMAs a row each.
+// ---------------------------------------------------------------------------
+template <int DH, bool TABLE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attn8_f32_kernel(
+    Plan pl, PagedAttn a, const uint8_t* __restrict__ exps) {
+  constexpr int NC = DH / 16, KL = DH / 64, NV = DH / 16;
+  __shared__ float sm[4][16], sl[4][16];
+  __shared__ __attribute__((aligned(16))) float so[4][16][DH];
+  auto mfma = [](float p, float q, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(p, q, c, 0, 0, 0); };
+  Work w;
+  int id = blockIdx.x;
+  if constexpr (TABLE) {
+    w.p = request_at(table_of(pl, a, TAB_FEW), pl.n_req, id);
+  } else {
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % a.few_chunks; id /= a.few_chunks;
+    // request p's query tiles start at cu[p] G / 16 + p
+    int lo = 0, hi = pl.n_req - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if ((int64_t)uniform(pl.cu_seqlens[mid]) * a.G / 16 + mid <= id) lo = mid; else hi = mid - 1;
+    }
+    w.p = lo;
+    w.qt = id - (int)((int64_t)uniform(pl.cu_seqlens[lo]) * a.G / 16 + lo);
+  }
+  const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
+  const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide
+  const int qn = m * a.G;
+  if (!TABLE && w.qt * 16 >= qn) return;      // block-uniform, as every exit below
+  const Chunks ck = request_chunks(VFM_F32, m, ctx, a.G, a.KH, a.window, a.n_sink);
+  if constexpr (TABLE) {
+    w.h = id % a.KH; id /= a.KH;
+    w.c = id % ck.n;
+    w.qt = id / ck.n;
+  } else if (w.c >= ck.n) {
+    return;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int x = lane & 15, g = lane >> 4;
+  const int qi = min(w.qt * 16 + x, qn - 1);
+  const int jq = ctx + qi / a.G;
+  const int j0 = ctx + w.qt * 16 / a.G, j1 = ctx + min(w.qt * 16 + 15, qn - 1) / a.G;
+  // the tile's own runs, dealt over the request's chunks
+  const Vis vis = visible_runs<4>(j0, j1, a.window, a.n_sink);
+  const int rpc = (vis.n + ck.n - 1) / ck.n;
+  const int t0 = w.c * rpc, t1 = min(t0 + rpc, vis.n);
+  int head;
+  const int64_t row = out_row(a, R0, w.h, qi, head);
+  const page_row prow = row_of(a.kp, request);
+  const int lp = a.kp.log2_page;
+  const uint8_t* kh = (const uint8_t*)a.k + (int64_t)w.h * a.slots * DH;
+  const uint8_t* vh = (const uint8_t*)a.v + (int64_t)w.h * a.slots * DH;
+  f32x4 q[NC], o[NV];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    q[c] = *reinterpret_cast<const f32x4*>((const float*)a.q + row * a.ldq + head * DH + 64 * (c >> 2) + 16 * g + 4 * (c & 3));
+#pragma unroll
+  for (int c = 0; c < NV; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = LOWEST, l_run = 0.f;
+  for (int t = t0 + wave; t < t1; t += 4) {
+    const int p0 = 16 * vis.run(t);
+    const int64_t slot = page_slot(prow, lp, p0);
+    const bool full = seen_by_all(j0, j1, p0, p0 + 15, a.window, a.n_sink);
+    const uint32_t ex = run_exps(exps, slot, a.KH, w.h);
+    u32x4 kc[KL];
+    uint32_t vc[4][NV / 4];
+#pragma unroll
+    for (int c = 0; c < KL; ++c) kc[c] = *reinterpret_cast<const u32x4*>(kh + (slot + x) * DH + 64 * c + 16 * g);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) __builtin_memcpy(vc[j], __builtin_assume_aligned(vh + (slot + 4 * g + j) * DH + NV * x, NV), NV);
+    const float kscale = scale_of(ex & 0xFF), vscale = scale_of(ex >> 8);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const f32x4 kf = decode4(kc[c >> 2][c & 3], kscale);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = mfma(kf[e], q[c][e], s);
+    }
+    f32x4 vf[4][NV / 4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int c = 0; c < NV / 4; ++c) vf[j][c] = decode4(vc[j][c], vscale);
+    bool poison = false;
+    if (!full) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = p0 + 4 * g + j;
+        s[j] = sees(jq, k, a.window, a.n_sink) ? s[j] : -INFINITY;
+        const bool any = seen_by_any(j0, j1, k, a.window, a.n_sink);
+        const bool some = any && !seen_by_all(j0, j1, k, k, a.window, a.n_sink);
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+          const bool bad = some && nonfinite(vf[j][c >> 2][c & 3]);
+          poison = poison || bad;
+          vf[j][c >> 2][c & 3] = !any || bad ? 0.f : vf[j][c >> 2][c & 3];
+        }
+      }
+    }
+    float mb = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    mb = max_x32(max_x16(mb));
+    const float m_new = fmaxf(m_run, mb);
+    const float alpha = exp2f((m_run - m_new) * a.scale_log2);
+    m_run = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) o[c] *= alpha;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float e = exp2f((s[j] - m_run) * a.scale_log2);
+      l_run += e;
+#pragma unroll
+      for (int c = 0; c < NV; ++c) o[c] = mfma(vf[j][c >> 2][c & 3], e, o[c]);
+    }
+    if (__any(poison)) {                                  // rare: see the bf16 kernel
+      for (int r = 0; r < 16; ++r) {
+        const int k = p0 + r;
+        if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
+        const bool see = sees(jq, k, a.window, a.n_sink);
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (see && is_nan8(vh[(slot + r) * DH + NV * (4 * g + i) + c])) o[c][i] = NAN;
+      }
+    }
+  }
+  l_run = sum_x32(sum_x16(l_run));
+  if (lane < 16) { sm[wave][x] = m_run; sl[wave][x] = l_run; }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int c = 0; c < NV; c += 4)
+      *reinterpret_cast<f32x4*>(&so[wave][x][NV * (4 * g + i) + c]) = f32x4{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
+  __syncthreads();
+  const int nq = min(16, qn - w.qt * 16);
+  for (int e = tid; e < nq * DH / 4; e += 256) {
+    const int qq = e / (DH / 4), d = (e % (DH / 4)) * 4;
+    const float M = fmaxf(fmaxf(sm[0][qq], sm[1][qq]), fmaxf(sm[2][qq], sm[3][qq]));
+    float L = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float wt = exp2f((sm[i][qq] - M) * a.scale_log2);
+      L += sl[i][qq] * wt;
+      acc += *reinterpret_cast<const f32x4*>(&so[i][qq][d]) * wt;
+    }
+    int hd;
+    const int64_t r = out_row(a, R0, w.h, w.qt * 16 + qq, hd);
+    if (ck.n == 1) {
+      *reinterpret_cast<f32x4*>((float*)a.out + r * a.ldo + hd * DH + d) = acc / L;
+    } else {
+      const int64_t rec = record_of<TABLE>(pl, a, w.p, R0, ck.n, r, hd) + w.c;
+      *reinterpret_cast<f32x4*>(a.rec_o + rec * DH + d) = acc;
+      if (d == 0) a.rec_ml[rec] = make_float2(M, L);
+    }
+  }
+}
+
+template <int DH, bool TABLE>
+void launch_blocks8(int dtype, const Plan& pl, const PagedAttn& a, const uint8_t* exps, unsigned nf, unsigned nr, hipStream_t s) {
+  const dim3 block(256), grid(nf + nr);
+  if (dtype != VFM_BF16) hipLaunchKernelGGL((attn8_f32_kernel<DH, TABLE>), grid, block, 0, s, pl, a, exps);
+#define BF16(R_, F_) hipLaunchKernelGGL((attn8_bf16_kernel<DH, R_, F_, TABLE>), grid, block, 0, s, pl, a, exps, (int)nr)
+  else if (nr && nf) BF16(true, true);
+  else if (nr) BF16(true, false);
+  else BF16(false, true);
+#undef BF16
+}
+
+}  // namespace
+
+hipError_t launch_append8(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv, int64_t ld,
+                          void* q_out, int64_t ldq, const Pool8& pool, const KvPages& kp, hipStream_t s) {
+  Append8 a = {};
+  a.H = H; a.KH = KH; a.rotate = theta > 0.f; a.log2_theta = theta > 0.f ? log2((double)theta) : 0.0;
+  a.ld = ld; a.ldq = ldq; a.slots = pool.slots; a.k = pool.k; a.v = pool.v; a.exps = pool.exps; a.kp = kp;
+  a.group = pl.T >= APPEND8_GROUPED ? 16 : 1;
+  const int blocks = (pl.T + a.group - 1) / a.group;
+  const int units = a.group > 1 ? H + 2 * KH : (H + 2 * KH + 1024 / head_dim - 1) / (1024 / head_dim);
+  const int most = (units + 3) / 4;
+  int split = (512 + blocks - 1) / blocks;
+  split = split < 1 ? 1 : split > most ? most : split;
+#define APPEND(T_, D_)                                                                                             \
+  hipLaunchKernelGGL((append8_kernel<T_, D_>), dim3((unsigned)blocks, (unsigned)split), dim3(256), 0, s, pl, a, (const T_*)qkv, (T_*)q_out)
+  if (dtype == VFM_BF16) { if (head_dim == 64) APPEND(bf16, 64); else APPEND(bf16, 128); }
+  else { if (head_dim == 64) APPEND(float, 64); else APPEND(float, 128); }
+#undef APPEND
+  return hipGetLastError();
+}
+
+hipError_t launch_attention8(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, const uint8_t* exps, int64_t few_blocks,
+                             int64_t rows_blocks, int64_t joins, bool table, hipStream_t s) {
+  if (table) launch_attention_table(dtype, pl, a, s);
+  const int pi = prof_begin(VFM_PROF_ATTN, s);
+  const unsigned nf = (unsigned)few_blocks, nr = (unsigned)rows_blocks;
+  if (head_dim == 64) {
+    if (table) launch_blocks8<64, true>(dtype, pl, a, exps, nf, nr, s);
+    else launch_blocks8<64, false>(dtype, pl, a, exps, nf, nr, s);
+  } else if (table) {
+    launch_blocks8<128, true>(dtype, pl, a, exps, nf, nr, s);
+  } else {
+    launch_blocks8<128, false>(dtype, pl, a, exps, nf, nr, s);
+  }
+  prof_end(pi, s);
+  if (joins) launch_attention_joins(dtype, head_dim, pl, a, (int)joins, table, s);
+  return hipGetLastError();
+}

@@ -1077,27 +1077,33 @@ void launch_attention_join(int dtype, const Plan& pl, const PagedAttn& a, int jo
 
 }  // namespace
 
-hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, int64_t few_blocks,
-                                  int64_t rows_blocks, int64_t joins, bool one, bool table, hipStream_t s) {
+void launch_attention_table(int dtype, const Plan& pl, const PagedAttn& a, hipStream_t s) {
+  const int pi = prof_begin(VFM_PROF_OTHER, s);
+  hipLaunchKernelGGL(attn_table_kernel, dim3(1), dim3(256), 0, s, pl, a, dtype, const_cast<int32_t*>(a.table));
+  prof_end(pi, s);
+}
+
 #define BY(F_, ...)                                                                       \
   do {                                                                                    \
     if (table) { if (head_dim == 64) F_<64, true>(__VA_ARGS__); else F_<128, true>(__VA_ARGS__); } \
     else if (head_dim == 64) F_<64, false>(__VA_ARGS__);                                  \
     else F_<128, false>(__VA_ARGS__);                                                     \
   } while (0)
-  if (table) {
-    const int pi = prof_begin(VFM_PROF_OTHER, s);
-    hipLaunchKernelGGL(attn_table_kernel, dim3(1), dim3(256), 0, s, pl, a, dtype, const_cast<int32_t*>(a.table));
-    prof_end(pi, s);
-  }
-  int pi = prof_begin(VFM_PROF_ATTN, s);
+
+void launch_attention_joins(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, int joins, bool table, hipStream_t s) {
+  const int pi = prof_begin(VFM_PROF_OTHER, s);
+  BY(launch_attention_join, dtype, pl, a, joins, s);
+  prof_end(pi, s);
+}
+
+hipError_t launch_attention_paged(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, int64_t few_blocks,
+                                  int64_t rows_blocks, int64_t joins, bool one, bool table, hipStream_t s) {
+  if (table) launch_attention_table(dtype, pl, a, s);
+  const int pi = prof_begin(VFM_PROF_ATTN, s);
   BY(launch_attention_blocks, dtype, pl, a, (unsigned)few_blocks, (unsigned)rows_blocks, one, s);
   prof_end(pi, s);
-  if (joins) {
-    pi = prof_begin(VFM_PROF_OTHER, s);
-    BY(launch_attention_join, dtype, pl, a, (int)joins, s);
-    prof_end(pi, s);
-  }
-#undef BY
+  if (joins) launch_attention_joins(dtype, head_dim, pl, a, (int)joins, table, s);
   return hipGetLastError();
 }
+
+#undef BY
