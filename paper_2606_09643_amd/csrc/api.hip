@@ -272,7 +272,9 @@ struct AttnPlan {
   bool table;                // blocks and records where each request's own begin, not in rectangles
   int64_t few_blocks, rows_blocks, recs, joins;
   int64_t bytes;             // workspace
+  int64_t few_own, few_tiles;    // few-row blocks with work, and the 32-key tiles of all of them
   int nchunk() const { return std::max(few_chunks, rows_chunks); }
+  bool deep() const { return few_blocks <= 512 || few_tiles >= 64 * few_own; }
   size_t table_bytes(const Plan& pl) const { return table ? align_up((size_t)4 * (pl.n_req + 1) * sizeof(int32_t)) : 0; }
 };
 
@@ -293,6 +295,8 @@ int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, At
     for (int i = 0; i < 4; ++i) own[i] += c.v[i];
     if (few_rows(a.dtype, m, G)) {
       ap.one = ap.one && n * ck.tiles <= 4;
+      ap.few_own += c.v[TAB_FEW];
+      ap.few_tiles += c.v[TAB_FEW] * ck.tiles;
       ap.few_chunks = std::max(ap.few_chunks, n);
       if (a.dtype == VFM_BF16) ap.qtiles = std::max(ap.qtiles, (int)few_qtiles(m, G));
     } else {
@@ -345,7 +349,7 @@ hipError_t run_attention(const vfm_attn& a, const Plan& pl, const AttnPlan& ap, 
     p.rec_ml = (float2*)((char*)p.rec_o + align_up((size_t)ap.recs * a.head_dim * 4));
   }
   if (exps != nullptr)
-    return launch_attention8(a.dtype, a.head_dim, pl, p, exps, ap.few_blocks, ap.rows_blocks, ap.joins, ap.table, s);
+    return launch_attention8(a.dtype, a.head_dim, pl, p, exps, ap.few_blocks, ap.rows_blocks, ap.joins, ap.deep(), ap.table, s);
   return launch_attention_paged(a.dtype, a.head_dim, pl, p, ap.few_blocks, ap.rows_blocks, ap.joins, ap.one,
                                 ap.table, s);
 }

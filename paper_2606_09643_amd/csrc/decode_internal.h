@@ -140,9 +140,10 @@ constexpr int APPEND8_GROUPED = 2048;
 // q_out, ldq: as launch_kv_append
 hipError_t launch_append8(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv, int64_t ld,
                           void* q_out, int64_t ldq, const Pool8& pool, const KvPages& kp, hipStream_t s);
-// a.k, a.v: the pools' codes; the other arguments as launch_attention_paged's
+// a.k, a.v: the pools' codes; deep: few blocks, or long ones (AttnPlan::deep); the other arguments as
+// launch_attention_paged's
 hipError_t launch_attention8(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, const uint8_t* exps, int64_t few_blocks,
-                             int64_t rows_blocks, int64_t joins, bool table, hipStream_t s);
+                             int64_t rows_blocks, int64_t joins, bool deep, bool table, hipStream_t s);
 
 // max_out: the batch's longest row of head outputs; a block of that many threads per request
 inline int sample_threads(int max_out) { return max_out <= 1024 ? 256 : 1024; }

@@ -50,6 +50,9 @@ template <int SLICE, int THREADS, bool BIAS>
 __global__ __launch_bounds__(THREADS) void adjust_kernel(Plan pl, const float* in, float* out, vfm_adjust a, int padded) {
   __shared__ __attribute__((aligned(16))) uint32_t count[SLICE];   // generated so many times, IN_PROMPT
   __shared__ __attribute__((aligned(16))) uint32_t last[BIAS ? SLICE : 4];   // 1 + place of its last bias
+  constexpr int G = SLICE / (4 * THREADS);                // groups of 4 outputs of a thread
+  constexpr int WORDS = SLICE / 32 + 2;
+  __shared__ uint32_t allow[WORDS];
   const int r = blockIdx.x % padded, slice = blockIdx.x / padded;
   if (r >= pl.n_req) return;                              // block-uniform, as every exit below
   const int tid = threadIdx.x;
@@ -70,36 +73,56 @@ __global__ __launch_bounds__(THREADS) void adjust_kernel(Plan pl, const float* i
   const bool same = in == out;
   if (same && !hist && !biases && !masked) return;
 
+  const float* src = in + base + lo;
+  f32x4 v[G];
+  auto fetch = [&](int g) {
+    const int i = 4 * (tid + g * THREADS);
+    const int64_t id = lo + i;
+    if (id >= 0 && id + 4 <= n) v[g] = *reinterpret_cast<const f32x4*>(src + i);
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (id + e >= 0 && id + e < n) v[g][e] = src[i + e];
+  };
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    v[g] = f32x4{};
+    if (!same) fetch(g);                                  // all of them, on their way while the tokens are counted
+  }
+
   for (int i = 4 * tid; i < SLICE; i += 4 * THREADS) {
     *reinterpret_cast<u32x4*>(count + i) = u32x4{};
     if constexpr (BIAS) *reinterpret_cast<u32x4*>(last + i) = u32x4{};
   }
+  // the request's outputs of the slice: span of them from output `from`, which is place `skip` of it
+  const uint32_t from = lo > 0 ? (uint32_t)lo : 0u, skip = (uint32_t)(from - lo);
+  const uint32_t span = (uint32_t)min((int64_t)n - from, (int64_t)SLICE - skip);
   __syncthreads();
   if (hist) {
     const int prompt = a.n_prompt ? a.n_prompt[r] : 0;
     each<THREADS>(a.hist + hb, hist, [&](int i, int32_t id) {
-      const int64_t k = id - lo;
-      if (id >= 0 && id < n && k >= 0 && k < SLICE) {
-        if (i < prompt) atomicOr(&count[k], IN_PROMPT);
-        else atomicAdd(&count[k], 1u);
+      const uint32_t k = (uint32_t)id - from;
+      if (k < span) {
+        if (i < prompt) atomicOr(&count[k + skip], IN_PROMPT);
+        else atomicAdd(&count[k + skip], 1u);
       }
     });
   }
   if constexpr (BIAS)
     for (int i = tid; i < biases; i += THREADS) {
-      const int32_t id = a.bias_id[bb + i];
-      const int64_t k = id - lo;
-      if (id >= 0 && id < n && k >= 0 && k < SLICE) atomicMax(&last[k], (uint32_t)i + 1);
+      const uint32_t k = (uint32_t)a.bias_id[bb + i] - from;
+      if (k < span) atomicMax(&last[k + skip], (uint32_t)i + 1);
     }
-  const uint32_t* mask = masked ? a.mask + (int64_t)row * a.mask_words : nullptr;
+  // the slice's words of the request's mask, bits past the request's outputs cleared
+  const int first = lo > 0 ? (int)lo : 0, w0 = first >> 5;
   bool none = false;                                      // the mask allows no output of the request
   if (masked) {
+    const uint32_t* mask = a.mask + (int64_t)row * a.mask_words;
     const int words = min(a.mask_words, (n + 31) >> 5);
     const uint32_t rest = (n & 31) ? (1u << (n & 31)) - 1 : ~0u;     // of word n / 32
-    auto left = [&](int w) { return mask[w] & (w == n >> 5 ? rest : ~0u); };
-    const int w0 = (int)(lo > 0 ? lo >> 5 : 0), w1 = (int)min((int64_t)words, (lo + SLICE + 31) >> 5);
+    auto left = [&](int w) { return w < words ? mask[w] & (w == n >> 5 ? rest : ~0u) : 0u; };
     bool any = false;
-    for (int w = w0 + tid; w < w1; w += THREADS) any = any || left(w) != 0;
+    for (int w = tid; w < WORDS; w += THREADS) any = (allow[w] = left(w0 + w)) != 0 || any;
     if (!__syncthreads_or(any)) {
       for (int w = tid; w < words; w += THREADS) any = any || left(w) != 0;
       none = !__syncthreads_or(any);
@@ -107,57 +130,55 @@ __global__ __launch_bounds__(THREADS) void adjust_kernel(Plan pl, const float* i
   }
   __syncthreads();
 
-  const float* src = in + base + lo;
   float* dst = out + base + lo;
-  for (int i = 4 * tid; i < SLICE; i += 4 * THREADS) {
-    const int64_t id = lo + i;                            // of the first of 4
-    if (id >= n) break;
-    const u32x4 c = *reinterpret_cast<const u32x4*>(count + i);
-    u32x4 b = {};
-    if constexpr (BIAS) b = *reinterpret_cast<const u32x4*>(last + i);
-    uint32_t ok = 15;
+  u32x4 c[G], b[G];
+  uint32_t ok[G];
+  bool load[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int i = 4 * (tid + g * THREADS);
+    c[g] = *reinterpret_cast<const u32x4*>(count + i);
+    b[g] = u32x4{};
+    if constexpr (BIAS) b[g] = *reinterpret_cast<const u32x4*>(last + i);
+    ok[g] = 15;
     if (masked) {
-      ok = 0;
+      // bits of outputs lo + i .. + 3, those before the request's first as if after it
+      const int64_t bit = lo + i - 32 * w0;
+      const int w = bit < 0 ? 0 : (int)(bit >> 5), at = (int)(bit - 32 * w);
+      const uint64_t two = allow[w] | (uint64_t)allow[w + 1] << 32;
+      ok[g] = (uint32_t)(at < 0 ? two << -at : two >> at) & 15;
+    }
+  }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int64_t w = (id + e) >> 5;
-        if (id + e >= 0 && w < a.mask_words && id + e < n) ok |= ((mask[w] >> ((id + e) & 31)) & 1) << e;
+  for (int g = 0; g < G; ++g) {
+    const int i = 4 * (tid + g * THREADS);
+    const bool some = (c[g][0] | c[g][1] | c[g][2] | c[g][3] | b[g][0] | b[g][1] | b[g][2] | b[g][3]) != 0;
+    load[g] = lo + i < n && (!same || some || ok[g] != 15);       // otherwise these 4 stay as they are
+    if (same && load[g]) fetch(g);
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int i = 4 * (tid + g * THREADS);
+    if (!load[g]) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      double l = (double)v[g][e];
+      if (c[g][e]) {
+        l *= v[g][e] > 0.f ? inv : rep;
+        const uint32_t times = c[g][e] & ~IN_PROMPT;
+        if (times) l -= fma((double)times, freq, pres);
       }
+      if constexpr (BIAS)
+        if (b[g][e]) l += (double)a.bias[bb + b[g][e] - 1];
+      if (c[g][e] | b[g][e]) v[g][e] = (float)l;
+      if (masked) v[g][e] = none ? NAN : (ok[g] >> e & 1) ? v[g][e] : -INFINITY;
     }
-    const bool whole = id >= 0 && id + 4 <= n;
-    const uint32_t some = c[0] | c[1] | c[2] | c[3] | b[0] | b[1] | b[2] | b[3];
-    if (same && !some && ok == 15) continue;
-    f32x4 v = {};
-    if (!(masked && ok == 0)) {
-      if (whole) v = *reinterpret_cast<const f32x4*>(src + i);
-      else
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (id + e >= 0 && id + e < n) v[e] = src[i + e];
-    }
-    if (some) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        double l = (double)v[e];
-        if (c[e]) {
-          l *= v[e] > 0.f ? inv : rep;
-          const uint32_t times = c[e] & ~IN_PROMPT;
-          if (times) l -= fma((double)times, freq, pres);
-        }
-        if constexpr (BIAS)
-          if (b[e]) l += (double)a.bias[bb + b[e] - 1];
-        if (c[e] | b[e]) v[e] = (float)l;
-      }
-    }
-    if (masked) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = none ? NAN : (ok >> e & 1) ? v[e] : -INFINITY;
-    }
-    if (whole) *reinterpret_cast<f32x4*>(dst + i) = v;
+    const int64_t id = lo + i;
+    if (id >= 0 && id + 4 <= n) *reinterpret_cast<f32x4*>(dst + i) = v[g];
     else
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (id + e >= 0 && id + e < n) dst[i + e] = v[e];
+        if (id + e >= 0 && id + e < n) dst[i + e] = v[g][e];
   }
 }
 

@@ -235,14 +235,31 @@ __global__ __launch_bounds__(256) void append8_kernel(Plan pl, Append8 a, const 
 // A lane's 16-byte load of a K row holds 16 consecutive head dims, two MFMA steps of 8; the queries' fragments take the
 // same dims, as a dot product does not mind their order.
 // ---------------------------------------------------------------------------
-// the exponent bytes of K (low) and V (high) of a run
-__device__ __forceinline__ uint32_t run_exps(const uint8_t* exps, int64_t slot, int KH, int h) {
+// The exponent bytes of K (low) and V (high) of two runs, even lanes the first's and odd lanes the second's.  (A load from
+// the same address in every lane would be made a scalar at once, and waited for before anything after it is issued.)
+__device__ __forceinline__ uint32_t runs_exps(const uint8_t* exps, int64_t slot0, int64_t slot1, int KH, int h) {
+  const int64_t slot = threadIdx.x & 1 ? slot1 : slot0;
   return reinterpret_cast<const uint16_t*>(exps)[(slot >> 4) * KH + h];
 }
+__device__ __forceinline__ float k_scale(uint32_t ex, int run) { return scale_of(__builtin_amdgcn_readlane(ex, run) & 0xFF); }
+__device__ __forceinline__ float v_scale(uint32_t ex, int run) { return scale_of(__builtin_amdgcn_readlane(ex, run) >> 8); }
 
 __device__ __forceinline__ bool is_nan8(uint32_t code) { return (code & 0x7F) == 0x7F; }
 
-template <int DH, bool TABLE>
+// A lane converts 16 consecutive head dims of a V (or K) row, two 16-byte chunks of bf16.  In LDS the rows' first chunks lie
+// beside each other, then the second ones, so that the lanes of a store fill whole runs of banks: logical chunk c holds
+// head dims from here on.  Odd rows of 128 bytes have the two halves swapped, as two of them make such a run.
+template <int DH>
+__device__ __forceinline__ constexpr int dims_of(int c) { return 16 * (c % (DH / 16)) + 8 * (c / (DH / 16)); }
+template <int DH>
+__device__ __forceinline__ int odd_rows(int r) { return DH == 64 ? (r & 1) << 2 : 0; }   // to a chunk's number by xor
+
+// Swizzle of the 32-byte segments of a V row in a few-row tile: the 8 rows that a half of a transposing read touches, one
+// segment each, lie in different banks.
+template <int DH>
+__device__ __forceinline__ int few_vswz(int r) { return DH == 128 ? r & 7 : (r >> 1) & 3; }
+
+template <int DH, int NB, bool TABLE>
 __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, const uint8_t* __restrict__ exps, int id, char* smem) {
   constexpr int LPR = DH / 16;         // lanes per K / V row (16 bytes each)
   constexpr int RPI = 64 / LPR;        // rows per wave-wide load
@@ -298,30 +315,37 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
 
   // a tile's two runs (one page each, as a page holds a multiple of 16 positions); runs past the last re-read it, unseen
   auto run_pos = [&](int t, int e) { return 16 * vis.run(min(2 * t + e, vis.n - 1)); };
-  u32x4 kf[2][2][KL], vf[2][VI];
-  uint32_t ex[2][2];
-  int slot[2];
+  u32x4 kf[NB][2][KL], vf[NB][VI];
+  uint32_t ex[NB];
+  int page[2], in_page[2];
   auto look_up = [&](int t) {
-    slot[0] = page_slot(prow, lp, run_pos(t, 0));
-    slot[1] = page_slot(prow, lp, run_pos(t, 1));
-  };
-  // keys of sub-tile e in rows x: 8 (x / 4) + x % 4 + 4 e, so that after the MFMA
-  // a lane holds the 8 consecutive keys 8 g .. 8 g + 7 over both sub-tiles
-  const int key0 = 8 * (x >> 2) + (x & 3);
-  auto load = [&](int b) {
-    const int64_t ks = (int64_t)(x < 8 ? slot[0] : slot[1]) + (key0 & 15);
 #pragma unroll
-    for (int e = 0; e < 2; ++e) ex[b][e] = run_exps(exps, slot[e], a.KH, w.h);
+    for (int e = 0; e < 2; ++e) {
+      const int k = run_pos(t, e);
+      page[e] = prow[k >> lp];
+      in_page[e] = k & ((1 << lp) - 1);
+    }
+  };
+  // The tile's runs are the two sub-tiles of keys, so that a load's run, and with it its base and scale, is the wave's.
+  const uint32_t koff = x * DH + 16 * g, voff = (lane / LPR & 15) * DH + 16 * (lane % LPR);
+  auto load = [&](int b) {
+    const uint8_t *kr[2], *vr[2];
+    int slot[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      slot[e] = (page[e] << lp) + in_page[e];
+      kr[e] = kh + (int64_t)slot[e] * DH;
+      vr[e] = vh + (int64_t)slot[e] * DH;
+    }
+    ex[b] = runs_exps(exps, slot[0], slot[1], a.KH, w.h);
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int s = 0; s < KL; ++s)
-        kf[b][e][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kh + (ks + 4 * e) * DH + 16 * g + 64 * s));
+        kf[b][e][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kr[e] + (koff + 64 * s)));
 #pragma unroll
-    for (int i = 0; i < VI; ++i) {
-      const int64_t vs = (int64_t)slot[(RPI * i) >> 4] + ((RPI * i) & 15) + lane / LPR;
-      vf[b][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vh + vs * DH + 16 * (lane % LPR)));
-    }
+    for (int i = 0; i < VI; ++i)
+      vf[b][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vr[(RPI * i) >> 4] + (voff + ((RPI * i) & 15) * DH)));
   };
 
   f32x4 o[ND];
@@ -329,9 +353,14 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
   for (int i = 0; i < ND; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = LOWEST, l_run = 0.f;
 
-  const int vst_seg = lane % LPR, vst_row = lane / LPR;
-  const int vrow = 8 * g + (x >> 2);
-  const int vbase = vrow * DH * 2 + (vswz<DH>(vrow) << 5) + (x & 3) * 8;
+  // where a lane's two chunks of row RPI i + vst_row go, for i = 0 (the swizzle is the same for all of them)
+  const int vst_row = lane / LPR, vst_swz = few_vswz<DH>(vst_row) << 1 ^ odd_rows<DH>(vst_row);
+  char* const vst[2] = {reinterpret_cast<char*>(Vs + vst_row * DH) + 16 * ((lane % LPR) ^ vst_swz),
+                        reinterpret_cast<char*>(Vs + vst_row * DH) + 16 * ((lane % LPR + LPR) ^ vst_swz)};
+  const int vrow = 4 * g + (x >> 2);
+  const int vbase = vrow * DH * 2 + ((few_vswz<DH>(vrow) << 5) ^ (odd_rows<DH>(vrow) << 4)) + (x & 3) * 8;
+  // head dims of the lane's outputs of tile d: chunk 2 d + g / 2, from 4 (g % 2) on
+  auto out_dims = [&](int d) { return dims_of<DH>(2 * d + (g >> 1)) + 4 * (g & 1); };
 
   auto compute = [&](int b, int t) {
     const int p0 = run_pos(t, 0);
@@ -342,7 +371,7 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
 #pragma unroll
     for (int i = 0; i < VI; ++i) {
       const int r = RPI * i + vst_row;
-      const float scale = scale_of(ex[b][(RPI * i) >> 4] >> 8);
+      const float scale = v_scale(ex[b], (RPI * i) >> 4);
       bf16x8 v[2] = {decode8(vf[b][i][0], vf[b][i][1], scale), decode8(vf[b][i][2], vf[b][i][3], scale)};
       if (!full) {
         const int k = (((RPI * i) >> 4) ? p1 : p0) + (r & 15);
@@ -353,16 +382,15 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
           v[1] = drop_nonfinite(v[1], poison);
         }
       }
-      bf16x8* at = reinterpret_cast<bf16x8*>(Vs + r * DH + (vst_seg ^ vswz<DH>(r)) * 16);
-      at[0] = v[0];
-      at[1] = v[1];
+      *reinterpret_cast<bf16x8*>(vst[0] + RPI * i * DH * 2) = v[0];
+      *reinterpret_cast<bf16x8*>(vst[1] + RPI * i * DH * 2) = v[1];
     }
     wave_lds_order();
     // S^T
-    const float kscale = scale_of((x < 8 ? ex[b][0] : ex[b][1]) & 0xFF);
     float s[8];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
+      const float kscale = k_scale(ex[b], e);
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
@@ -373,9 +401,9 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
       for (int i = 0; i < 4; ++i) s[4 * e + i] = acc[i];
     }
     if (!full) {
-      const int kb = (g < 2 ? p0 : p1) + 8 * (g & 1);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] = sees(jq, kb + i, a.window, a.n_sink) ? s[i] : -INFINITY;
+      for (int i = 0; i < 8; ++i)
+        s[i] = sees(jq, (i < 4 ? p0 : p1) + 4 * g + (i & 3), a.window, a.n_sink) ? s[i] : -INFINITY;
     }
     float mb = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
     mb = max_x32(max_x16(mb));
@@ -394,12 +422,14 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
       l_run += e8[i];
     }
     const bf16x8 pf = pack8(e8[0], e8[1], e8[2], e8[3], e8[4], e8[5], e8[6], e8[7]);
+    int vb = vbase;
+    asm volatile("" : "+v"(vb));                          // the ND addresses made here, not held over the loop
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
-      const char* vp = reinterpret_cast<const char*>(Vs) + (vbase ^ (d << 5));
+      const char* vp = reinterpret_cast<const char*>(Vs) + (vb ^ (d << 5));
       typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp + 4 * DH * 2));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp + 16 * DH * 2));
       bf16x8 f;
       __builtin_memcpy(&f, &lo, 8);
       __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
@@ -410,11 +440,11 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
       for (int r = 0; r < 32; ++r) {
         const int k = (r < 16 ? p0 : p1) + (r & 15);
         if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
-        const uint8_t* vr = vh + (int64_t)page_slot(prow, lp, k) * DH + 4 * g;
+        const uint8_t* vr = vh + (int64_t)page_slot(prow, lp, k) * DH;
         const bool see = sees(jq, k, a.window, a.n_sink);
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-          const uint32_t c = *reinterpret_cast<const uint32_t*>(vr + 16 * d);
+          const uint32_t c = *reinterpret_cast<const uint32_t*>(vr + out_dims(d));
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (see && is_nan8(c >> (8 * i))) o[d][i] = NAN;
@@ -424,23 +454,23 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
     }
   };
 
-  // tiles t0 + wave, + 4, ...: a tile's loads in flight while the one before is computed, its page lookups a tile
-  // before that
+  // tiles t0 + wave, + 4, ...: the loads of NB - 1 tiles in flight while one is computed, page lookups a tile ahead of them
   int t = t0 + wave;
   if (t < t1) {
+    constexpr int AHEAD = 4 * (NB - 1);
     look_up(t);
-    load(0);
-    if (t + 4 < t1) look_up(t + 4);
-    for (;;) {
-      if (t + 4 < t1) { load(1); if (t + 8 < t1) look_up(t + 8); }
-      compute(0, t);
+#pragma unroll
+    for (int b = 0; b < NB - 1; ++b)
+      if (t + 4 * b < t1) { load(b); if (t + 4 * b + 4 < t1) look_up(t + 4 * b + 4); }
+    auto step = [&](int b) {
+      if (t + AHEAD < t1) { load((b + NB - 1) % NB); if (t + AHEAD + 4 < t1) look_up(t + AHEAD + 4); }
+      compute(b, t);
       t += 4;
-      if (t >= t1) break;
-      if (t + 4 < t1) { load(0); if (t + 8 < t1) look_up(t + 8); }
-      compute(1, t);
-      t += 4;
-      if (t >= t1) break;
-    }
+      return t < t1;
+    };
+    if constexpr (NB == 1) while (step(0)) {}
+    else if constexpr (NB == 2) while (step(0) && step(1)) {}
+    else while (step(0) && step(1) && step(2)) {}
   }
   l_run = sum_x32(sum_x16(l_run));
 
@@ -450,7 +480,7 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
   if (lane < 16) { sm[wave][x] = m_run; sl[wave][x] = l_run; }
 #pragma unroll
   for (int d = 0; d < ND; ++d)
-    *reinterpret_cast<f32x4*>(so + (wave * 16 + x) * DH + 16 * d + 4 * g) = o[d];
+    *reinterpret_cast<f32x4*>(so + (wave * 16 + x) * DH + (out_dims(d) ^ (x << 2))) = o[d];   // queries in different banks
   __syncthreads();
   const int nq = min(16, qn - w.qt * 16);
   for (int e = tid; e < nq * DH / 4; e += 256) {
@@ -463,7 +493,7 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
       const float wt = fast_exp2((sm[i][q] - M) * a.scale_log2);
       L += sl[i][q] * wt;
       // a wave without any visible key has weight 0 and zeros
-      acc += *reinterpret_cast<const f32x4*>(so + (i * 16 + q) * DH + d) * wt;
+      acc += *reinterpret_cast<const f32x4*>(so + (i * 16 + q) * DH + (d ^ (q << 2))) * wt;
     }
     int hd;
     const int64_t r = out_row(a, R0, w.h, w.qt * 16 + q, hd);
@@ -550,9 +580,9 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
   const int64_t row = out_row(a, R0 + r0, w.h, qi, head);
   bf16x8 qf[KS];
   {
-    const bf16* qr = (const bf16*)a.q + row * a.ldq + head * DH + 8 * h2;
+    const bf16* qr = (const bf16*)a.q + row * a.ldq + head * DH;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s);
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + dims_of<DH>(2 * s + h2));
   }
   const page_row prow = row_of(a.kp, request);
   const int lp = a.kp.log2_page;
@@ -585,39 +615,39 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
   };
   // Loads K of the tile looked up last and V of the one looked up before it; looks `next` up.  Past the last tile that one
   // is loaded again, into stages that nothing reads any more: the loop needs no branch.
-  int64_t vslot[NI] = {};
+  int vslot[NI] = {};
   u32x4 kr[NI], vr[NI];
-  uint32_t kx[NI] = {}, vx[NI] = {};
+  uint32_t kx = 0, vx = 0;
   auto load = [&](int next) {
-    int64_t kslot[NI], pslot[NI];
+    int kslot[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) kslot[i] = (page[i] << lp) + in_page[i];
+    look_up(next);
+    vx = kx;
+    kx = runs_exps(exps, kslot[0], kslot[NI - 1], a.KH, w.h);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      kslot[i] = (int64_t)((page[i] << lp) + in_page[i]);
-      pslot[i] = vslot[i];
+      kr[i] = *reinterpret_cast<const u32x4*>(kh + (int64_t)kslot[i] * DH + off);
+      vr[i] = *reinterpret_cast<const u32x4*>(vh + (int64_t)vslot[i] * DH + off);
       vslot[i] = kslot[i];
     }
-    look_up(next);
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      vx[i] = kx[i];
-      kx[i] = run_exps(exps, kslot[i], a.KH, w.h);
-      kr[i] = *reinterpret_cast<const u32x4*>(kh + kslot[i] * DH + off);
-      vr[i] = *reinterpret_cast<const u32x4*>(vh + pslot[i] * DH + off);
-    }
   };
+  // where the two chunks that a lane's codes become go in a stage's K and V, for i = 0: row RPI NW i + lrow has the same
+  // swizzle for every i
+  const int seg = lane % LPR, flip = odd_rows<DH>(lrow), row_at = lrow * DH;
+  const int k_at[2] = {row_at + 8 * rows_kswz<DH>(lrow, seg ^ flip), row_at + 8 * rows_kswz<DH>(lrow, (seg + LPR) ^ flip)};
+  const int v_at[2] = {row_at + 8 * rows_vswz<DH>(lrow, seg ^ flip), row_at + 8 * rows_vswz<DH>(lrow, (seg + LPR) ^ flip)};
   // what was loaded, as bf16 into stage b
   auto store = [&](auto b, bool with_v) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int r = RPI * NW * i + lrow, c = 2 * (lane % LPR);
-      const float ks = scale_of(kx[i] & 0xFF), vs = scale_of(vx[i] >> 8);
-      bf16* kd = stage(b) + r * DH;
-      *reinterpret_cast<bf16x8*>(kd + rows_kswz<DH>(r, c) * 8) = decode8(kr[i][0], kr[i][1], ks);
-      *reinterpret_cast<bf16x8*>(kd + rows_kswz<DH>(r, c + 1) * 8) = decode8(kr[i][2], kr[i][3], ks);
+      const float ks = k_scale(kx, i), vs = v_scale(vx, i);
+      bf16* to = stage(b) + RPI * NW * i * DH;
+      *reinterpret_cast<bf16x8*>(to + k_at[0]) = decode8(kr[i][0], kr[i][1], ks);
+      *reinterpret_cast<bf16x8*>(to + k_at[1]) = decode8(kr[i][2], kr[i][3], ks);
       if (with_v) {
-        bf16* vd = kd + TE;
-        *reinterpret_cast<bf16x8*>(vd + rows_vswz<DH>(r, c) * 8) = decode8(vr[i][0], vr[i][1], vs);
-        *reinterpret_cast<bf16x8*>(vd + rows_vswz<DH>(r, c + 1) * 8) = decode8(vr[i][2], vr[i][3], vs);
+        *reinterpret_cast<bf16x8*>(to + TE + v_at[0]) = decode8(vr[i][0], vr[i][1], vs);
+        *reinterpret_cast<bf16x8*>(to + TE + v_at[1]) = decode8(vr[i][2], vr[i][3], vs);
       }
     }
   };
@@ -633,15 +663,15 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
     const int kb = 64 * vis.run(t);
 #pragma unroll 1
     for (int i = 0; i < NI; ++i) {
-      const int r = RPI * NW * i + lrow, k = kb + r;
-      bf16x8* at = reinterpret_cast<bf16x8*>(stage(b) + TE + r * DH);
-      const int c[2] = {rows_vswz<DH>(r, 2 * (lane % LPR)), rows_vswz<DH>(r, 2 * (lane % LPR) + 1)};
+      const int k = kb + RPI * NW * i + lrow;
+      bf16* v = stage(b) + TE + RPI * NW * i * DH;
+      bf16x8 *lo = reinterpret_cast<bf16x8*>(v + v_at[0]), *hi = reinterpret_cast<bf16x8*>(v + v_at[1]);
       if (!seen_by_any(j0, j1, k, a.window, a.n_sink)) {
-        at[c[0]] = at[c[1]] = bf16x8{};
+        *lo = *hi = bf16x8{};
       } else if (!seen_by_all(j0, j1, k, k, a.window, a.n_sink)) {
         bool found = false;
-        const bf16x8 v[2] = {drop_nonfinite(at[c[0]], found), drop_nonfinite(at[c[1]], found)};
-        if (found) { at[c[0]] = v[0]; at[c[1]] = v[1]; s_poison = t; }
+        const bf16x8 l = drop_nonfinite(*lo, found), h = drop_nonfinite(*hi, found);
+        if (found) { *lo = l; *hi = h; s_poison = t; }
       }
     }
   };
@@ -651,8 +681,10 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
   // bringing key (x & 15) / 4, dims 4 (x & 3).  Its rows differ from the lane's
   // first by multiples of 8, which leave the swizzle alone.
   const int kq = x & 15, gq = x >> 4;
-  const int kaddr = x * DH * 2 + (rows_kswz<DH>(x, h2) << 4);
-  const int vaddr = (4 * h2 + (kq >> 2)) * DH * 2 + (rows_vswz<DH>(kq >> 2, 0) << 4) + gq * 32 + (kq & 3) * 8;
+  const int kaddr = x * DH * 2 + (rows_kswz<DH>(x, h2 ^ odd_rows<DH>(x)) << 4);
+  const int vaddr = (4 * h2 + (kq >> 2)) * DH * 2 + (rows_vswz<DH>(kq >> 2, odd_rows<DH>(kq >> 2)) << 4) + gq * 32 + (kq & 3) * 8;
+  // head dims of the lane's outputs 4 j .. of tile d: chunk 4 d + j, from 4 h2 on
+  auto out_dims = [&](int d, int j) { return dims_of<DH>(4 * d + j) + 4 * h2; };
 
   // S^T of a tile: two 32-key halves; lane half h2, register i: key 8 (i / 4) + 4 h2 + i % 4
   auto scores = [&](auto b, f32x16 (&st)[2]) {
@@ -759,13 +791,13 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
     for (int r = 0; r < 64; ++r) {
       const int k = kb + r;
       if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
-      const uint8_t* vrow = vh + (int64_t)(page_slot(prow, lp, k)) * DH + 4 * h2;
+      const uint8_t* vrow = vh + (int64_t)(page_slot(prow, lp, k)) * DH;
       if (sees(jq, k, a.window, a.n_sink)) {
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const uint32_t c = *reinterpret_cast<const uint32_t*>(vrow + 32 * d + 8 * j);
+            const uint32_t c = *reinterpret_cast<const uint32_t*>(vrow + out_dims(d, j));
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (is_nan8(c >> (8 * i))) o[d][4 * j + i] = NAN;
@@ -804,12 +836,22 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
       }
       bf16x8 pf[4];
       __builtin_amdgcn_sched_barrier(0);
-      // scores of t + 1 (2 KS MFMAs) beside the first half of t's weights
+      // Scores of t + 1 (2 KS MFMAs) beside the first half of t's weights, the conversion of what was loaded and the next
+      // loads; a fragment is read four ahead of its MFMA.
       store(j, true);
       load(t + 4);
       scores(jn, sn);
       weights(st, 0, pf);
       weights(st, 1, pf);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int s = 0; s < 2 * KS; ++s) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 96 / (2 * KS), 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        if (s % 2) __builtin_amdgcn_sched_group_barrier(0x200, 4 * NI * 2 / (2 * KS), 0);
+        if (s % (2 * KS / 8) == 1) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+      }
 #pragma unroll
       for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(pf[u]));   // not put off behind the mask
       __builtin_amdgcn_sched_barrier(0);
@@ -820,6 +862,13 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
       weights(st, 3, pf);
       products(jn, pf);
       const float mb = largest(sn);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int s = 0; s < 4 * ND; ++s) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 96 / (4 * ND), 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
       __builtin_amdgcn_sched_barrier(0);
       if (s_poison == t) add_nonfinite(t);
       if (t + 1 >= t1) return false;
@@ -836,7 +885,7 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
   if (wave * 32 + x >= qn) return;
   if (ck.n == 1) {
     const float inv = 1.f / l_run;
-    bf16* orow = (bf16*)a.out + row * a.ldo + head * DH + 4 * h2;
+    bf16* orow = (bf16*)a.out + row * a.ldo + head * DH;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -844,16 +893,16 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
         bf16x4 v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = (bf16)(o[d][4 * j + i] * inv);
-        *reinterpret_cast<bf16x4*>(orow + 32 * d + 8 * j) = v;
+        *reinterpret_cast<bf16x4*>(orow + out_dims(d, j)) = v;
       }
   } else {
     const int64_t rec = record_of<TABLE>(pl, a, w.p, R0, ck.n, row, head) + w.c;
-    float* ro = a.rec_o + rec * DH + 4 * h2;
+    float* ro = a.rec_o + rec * DH;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<f32x4*>(ro + 32 * d + 8 * j) =
+        *reinterpret_cast<f32x4*>(ro + out_dims(d, j)) =
             f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
     if (h2 == 0) a.rec_ml[rec] = make_float2(m_run, l_run);
   }
@@ -861,13 +910,13 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
 
 // ROWS / FEW as in the bf16 cache's kernel (k_paged.hip): the blocks of a step's many-row requests, then those of its few-row
 // ones, in one launch.
-template <int DH, bool ROWS, bool FEW, bool TABLE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn8_bf16_kernel(
+template <int DH, bool ROWS, int NB, int WAVES, bool TABLE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) void attn8_bf16_kernel(
     Plan pl, PagedAttn a, const uint8_t* __restrict__ exps, int rows_blocks) {
   __shared__ __attribute__((aligned(16))) bf16 stage0[128 * DH], stage1[ROWS ? 128 * DH : 8];
-  if constexpr (FEW)
+  if constexpr (NB > 0)
     if ((int)blockIdx.x >= rows_blocks) {
-      few_block8<DH, TABLE>(pl, a, exps, (int)blockIdx.x - rows_blocks, reinterpret_cast<char*>(stage0));
+      few_block8<DH, NB, TABLE>(pl, a, exps, (int)blockIdx.x - rows_blocks, reinterpret_cast<char*>(stage0));
       return;
     }
   if constexpr (ROWS) rows_block8<DH, TABLE>(pl, a, exps, blockIdx.x, stage0, stage1);
@@ -939,14 +988,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
     const int p0 = 16 * vis.run(t);
     const int64_t slot = page_slot(prow, lp, p0);
     const bool full = seen_by_all(j0, j1, p0, p0 + 15, a.window, a.n_sink);
-    const uint32_t ex = run_exps(exps, slot, a.KH, w.h);
+    const uint32_t ex = runs_exps(exps, slot, slot, a.KH, w.h);
     u32x4 kc[KL];
     uint32_t vc[4][NV / 4];
 #pragma unroll
     for (int c = 0; c < KL; ++c) kc[c] = *reinterpret_cast<const u32x4*>(kh + (slot + x) * DH + 64 * c + 16 * g);
 #pragma unroll
     for (int j = 0; j < 4; ++j) __builtin_memcpy(vc[j], __builtin_assume_aligned(vh + (slot + 4 * g + j) * DH + NV * x, NV), NV);
-    const float kscale = scale_of(ex & 0xFF), vscale = scale_of(ex >> 8);
+    const float kscale = k_scale(ex, 0), vscale = v_scale(ex, 0);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -1036,13 +1085,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
 }
 
 template <int DH, bool TABLE>
-void launch_blocks8(int dtype, const Plan& pl, const PagedAttn& a, const uint8_t* exps, unsigned nf, unsigned nr, hipStream_t s) {
+void launch_blocks8(int dtype, const Plan& pl, const PagedAttn& a, const uint8_t* exps, unsigned nf, unsigned nr, bool deep, hipStream_t s) {
   const dim3 block(256), grid(nf + nr);
   if (dtype != VFM_BF16) hipLaunchKernelGGL((attn8_f32_kernel<DH, TABLE>), grid, block, 0, s, pl, a, exps);
-#define BF16(R_, F_) hipLaunchKernelGGL((attn8_bf16_kernel<DH, R_, F_, TABLE>), grid, block, 0, s, pl, a, exps, (int)nr)
-  else if (nr && nf) BF16(true, true);
-  else if (nr) BF16(true, false);
-  else BF16(false, true);
+#define BF16(R_, N_, W_) hipLaunchKernelGGL((attn8_bf16_kernel<DH, R_, N_, W_, TABLE>), grid, block, 0, s, pl, a, exps, (int)nr)
+  else if (nr && nf) BF16(true, 2, 2);
+  else if (nr) BF16(true, 0, 2);
+  else if (deep) BF16(false, (DH == 64 ? 2 : 3), (DH == 64 ? 3 : 2));
+  else BF16(false, 1, (DH == 64 ? 5 : 4));
 #undef BF16
 }
 
@@ -1056,8 +1106,11 @@ hipError_t launch_append8(int dtype, const Plan& pl, int H, int KH, int head_dim
   a.group = pl.T >= APPEND8_GROUPED ? 16 : 1;
   const int blocks = (pl.T + a.group - 1) / a.group;
   const int units = a.group > 1 ? H + 2 * KH : (H + 2 * KH + 1024 / head_dim - 1) / (1024 / head_dim);
+  // A wave takes 6 heads of a run, so that the blocks come to several rounds over the chip and the last one is short; where
+  // blocks are few, less.  (Each split takes the run's angles anew.)
   const int most = (units + 3) / 4;
-  int split = (512 + blocks - 1) / blocks;
+  int split = (units + 23) / 24;
+  if ((int64_t)blocks * split < 512) split = (512 + blocks - 1) / blocks;
   split = split < 1 ? 1 : split > most ? most : split;
 #define APPEND(T_, D_)                                                                                             \
   hipLaunchKernelGGL((append8_kernel<T_, D_>), dim3((unsigned)blocks, (unsigned)split), dim3(256), 0, s, pl, a, (const T_*)qkv, (T_*)q_out)
@@ -1068,17 +1121,17 @@ hipError_t launch_append8(int dtype, const Plan& pl, int H, int KH, int head_dim
 }
 
 hipError_t launch_attention8(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, const uint8_t* exps, int64_t few_blocks,
-                             int64_t rows_blocks, int64_t joins, bool table, hipStream_t s) {
+                             int64_t rows_blocks, int64_t joins, bool deep, bool table, hipStream_t s) {
   if (table) launch_attention_table(dtype, pl, a, s);
   const int pi = prof_begin(VFM_PROF_ATTN, s);
   const unsigned nf = (unsigned)few_blocks, nr = (unsigned)rows_blocks;
   if (head_dim == 64) {
-    if (table) launch_blocks8<64, true>(dtype, pl, a, exps, nf, nr, s);
-    else launch_blocks8<64, false>(dtype, pl, a, exps, nf, nr, s);
+    if (table) launch_blocks8<64, true>(dtype, pl, a, exps, nf, nr, deep, s);
+    else launch_blocks8<64, false>(dtype, pl, a, exps, nf, nr, deep, s);
   } else if (table) {
-    launch_blocks8<128, true>(dtype, pl, a, exps, nf, nr, s);
+    launch_blocks8<128, true>(dtype, pl, a, exps, nf, nr, deep, s);
   } else {
-    launch_blocks8<128, false>(dtype, pl, a, exps, nf, nr, s);
+    launch_blocks8<128, false>(dtype, pl, a, exps, nf, nr, deep, s);
   }
   prof_end(pi, s);
   if (joins) launch_attention_joins(dtype, head_dim, pl, a, (int)joins, table, s);
