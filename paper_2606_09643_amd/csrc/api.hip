@@ -941,7 +941,7 @@ extern "C" int vfm_adjust_outputs(const vfm_batch* batch, const float* out, cons
   const int32_t* off = host_arr(batch, po.out_off);
   int most = 0;
   for (int i = 0; i < pl.n_req; ++i) most = std::max(most, off[i + 1] - off[i]);
-  if (pl.n_req > 1 << 23 || adjust_blocks(pl.n_req, most) > kMaxThreads / ADJUST_THREADS) return VFM_ERR_UNSUPPORTED;
+  if (pl.n_req > 1 << 23 || adjust_blocks(pl.n_req, most) > kMaxThreads / adjust_threads(adjust_slice(pl.n_req, most))) return VFM_ERR_UNSUPPORTED;
   VFM_TRY(check_stream(stream));
   if (most == 0) return VFM_OK;
   hipStream_t s = (hipStream_t)stream;

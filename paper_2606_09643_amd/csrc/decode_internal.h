@@ -1,6 +1,8 @@
 // Declarations of the bounded-cache decoding kernels (k_paged.hip, k_sample.hip).
 #pragma once
 
+#include <initializer_list>
+
 #include "vfm_decode.h"
 #include "vfm_internal.h"
 #include "vfm_kv8.h"
@@ -151,14 +153,19 @@ hipError_t launch_sample(const Plan& pl, const float* out, const vfm_sampling& s
                          float* logprob, int max_out, hipStream_t s);
 
 // ---- penalties, biases and masks on head outputs (k_adjust.hip) ----
-// Outputs that a block takes: where the larger slices give every CU a block, fewer blocks go through a request's
-// earlier tokens; below that the smaller ones spread a request over more CUs.
-constexpr int ADJUST_SLICE = 8192, ADJUST_THREADS = 512, ADJUST_SMALL = 1024, ADJUST_SMALL_THREADS = 256;
+// Outputs that a block takes, 16 a thread (4 with the small ones): the largest with which there is a block for every CU, as
+// each goes through all of a request's earlier tokens.
+constexpr int ADJUST_LARGE = 16384, ADJUST_MIDDLE = 8192, ADJUST_SMALL = 1024;
+constexpr int adjust_threads(int slice) { return slice == ADJUST_SMALL ? 256 : slice / 16; }
 // blocks of slice s begin at s * adjust_rows: a multiple of 8, so a request's blocks share their number mod 8, the XCD
 inline int adjust_rows(int n_req) { return (n_req + 7) & ~7; }
 inline int64_t adjust_slices(int max_out, int slice) { return ((int64_t)max_out + 3 + slice - 1) / slice; }
-inline int adjust_small(int n_req, int max_out) { return n_req * adjust_slices(max_out, ADJUST_SLICE) < 256 || max_out <= ADJUST_SMALL; }
+inline int adjust_slice(int n_req, int max_out) {
+  for (int slice : {ADJUST_LARGE, ADJUST_MIDDLE})
+    if (max_out > ADJUST_SMALL && n_req * adjust_slices(max_out, slice) >= 256) return slice;
+  return ADJUST_SMALL;
+}
 inline int64_t adjust_blocks(int n_req, int max_out) {
-  return adjust_rows(n_req) * adjust_slices(max_out, adjust_small(n_req, max_out) ? ADJUST_SMALL : ADJUST_SLICE);
+  return adjust_rows(n_req) * adjust_slices(max_out, adjust_slice(n_req, max_out));
 }
 hipError_t launch_adjust(const Plan& pl, const float* in, float* out, const vfm_adjust& a, int max_out, hipStream_t s);

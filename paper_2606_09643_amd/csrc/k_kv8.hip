@@ -6,6 +6,8 @@
 // and keep their mantissas (all but those that become subnormal), where a scale of any size would round them anew.
 // It also is what gfx950's conversions multiply by for nothing: v_cvt_scalef32_pk_{bf16,f32}_fp8 give code 2^(e - 127)
 // exactly, as e4m3 has 4 significant bits and bf16 8.
+#include <type_traits>
+
 #include "paged_device.h"
 
 namespace {
@@ -69,35 +71,49 @@ template <> struct Half8<float> {
 };
 
 struct Append8 {
-  int H, KH, rotate, group;    // group: rows whose runs a block takes
+  int H, KH, rotate, group, split;   // rows whose runs a block takes, blocks that share them
   double log2_theta;
   int64_t ld, ldq, slots;
   uint8_t *k, *v, *exps;
   KvPages kp;
 };
 
-// Heads `unit` * HPW .. of one run: nr rows from row r0 at position pos0, slot slot0.  ONE: nr is 1, and 64 / PER heads.
+// How a wave holds rows of a run's head(s), a lane pairs (i, i + DH/2) of 8 of the dims: one head of up to 16 rows, or with
+// ONE a single row of 64 / PER heads.
 template <typename T, int DH, bool ONE>
-__device__ __forceinline__ void append_heads(const Append8& a, const T* qkv, T* q_out, int unit,
+struct Held {
+  static constexpr int HALF = DH / 2, PER = HALF / 8;     // lanes of a row
+  static constexpr int RPP = ONE ? 1 : 64 / PER;          // rows at a time
+  static constexpr int NI = ONE ? 1 : 16 / RPP;
+  Half8<T> x[NI], y[NI];
+  __device__ __forceinline__ static int head_of(int unit) {
+    return ONE ? unit * (64 / PER) + (int)(threadIdx.x & 63) / PER : unit;
+  }
+  __device__ __forceinline__ static int row0() { return ONE ? 0 : (int)(threadIdx.x & 63) / PER; }
+  __device__ __forceinline__ void load(const T* qkv, int64_t ld, int n_heads, int unit, int r0, int nr) {
+    const int head = min(head_of(unit), n_heads - 1), ch = (threadIdx.x & 63) % PER;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int r = min(row0() + i * RPP, nr - 1);        // rows past the last: copies of it
+      const T* p = qkv + (int64_t)(r0 + r) * ld + (int64_t)head * DH + ch * 8;
+      x[i] = *reinterpret_cast<const Half8<T>*>(p);
+      y[i] = *reinterpret_cast<const Half8<T>*>(p + HALF);
+    }
+  }
+};
+
+// The run's nr rows from row r0 at position pos0, slot slot0.
+template <typename T, int DH, bool ONE>
+__device__ __forceinline__ void append_heads(const Append8& a, Held<T, DH, ONE>& in, T* q_out, int unit,
                                              int r0, int nr, int pos0, int64_t slot0, const double2* cs) {
-  constexpr int HALF = DH / 2, PER = HALF / 8;            // a lane holds pairs (i, i + HALF), 8 of them per item
-  constexpr int RPP = ONE ? 1 : 64 / PER;                 // rows of the wave's heads at a time
-  constexpr int NI = ONE ? 1 : 16 / RPP;                  // items of a lane
-  const int lane = threadIdx.x & 63;
-  const int head = ONE ? unit * (64 / PER) + lane / PER : unit;
-  const int ch = lane % PER, row0 = ONE ? 0 : lane / PER;
+  constexpr int HALF = DH / 2, PER = HALF / 8, RPP = Held<T, DH, ONE>::RPP, NI = Held<T, DH, ONE>::NI;
+  Half8<T>(&x)[NI] = in.x;
+  Half8<T>(&y)[NI] = in.y;
+  const int lane = threadIdx.x & 63, ch = lane % PER, row0 = in.row0(), head = in.head_of(unit);
   const int n_heads = a.H + 2 * a.KH;
   if (ONE && head >= n_heads) return;                     // whole groups of PER lanes, which alone exchange values
   const bool is_q = head < a.H, rot = a.rotate && head < a.H + a.KH;
   if (is_q && q_out == nullptr) return;
-  Half8<T> x[NI], y[NI];
-#pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int r = min(row0 + i * RPP, nr - 1);            // rows past the last: copies of it
-    const T* p = qkv + (int64_t)(r0 + r) * a.ld + (int64_t)head * DH + ch * 8;
-    x[i] = *reinterpret_cast<const Half8<T>*>(p);
-    y[i] = *reinterpret_cast<const Half8<T>*>(p + HALF);
-  }
   float u[NI][16];                                        // the rotated pairs' first halves, then the second ones
   float big = 0.f;
 #pragma unroll
@@ -192,13 +208,25 @@ __device__ __forceinline__ void append_heads(const Append8& a, const T* qkv, T* 
 }
 
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void append8_kernel(Plan pl, Append8 a, const T* qkv, T* q_out) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) void append8_kernel(Plan pl, Append8 a, const T* qkv, T* q_out) {
   constexpr int HALF = DH / 2, PER = HALF / 8;
   // cosine and sine of row r, pair 8 ch + j at (r * 8 + j) * PER + ch + r * PER: lanes of a row read neighbours, rows
   // differ in banks
   __shared__ double2 cs[16 * 9 * PER];
-  const int first = blockIdx.x * a.group, end = min(first + a.group, pl.T);
+  const int split = a.split, share = (int)blockIdx.x % split, first = (int)blockIdx.x / split * a.group;
+  const int end = min(first + a.group, pl.T);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // revolutions per position of the pair whose angles this thread takes
+  const int pair = threadIdx.x % HALF;
+  const double inv = a.rotate ? exp2(-(2.0 * (double)pair / (double)DH) * a.log2_theta) * 0.15915494309189535 : 0.0;
+  const int n_heads = a.H + 2 * a.KH, step = 4 * split, unit0 = share * 4 + wave;
+  auto heads = [&](auto one, int units, int r0, int nr, int pos0, int64_t slot0) {
+    for (int unit = unit0; unit < units; unit += step) {
+      Held<T, DH, decltype(one)::value> rows;
+      rows.load(qkv, a.ld, n_heads, unit, r0, nr);
+      append_heads<T, DH, decltype(one)::value>(a, rows, q_out, unit, r0, nr, pos0, slot0, cs);
+    }
+  };
   for (int r0 = first, next; r0 < end; r0 = next) {
     const int pos0 = uniform(pl.pos[r0]), p = uniform(pl.row_req[r0]);
     const int begin = uniform(pl.cu_seqlens[p]), past = uniform(pl.cu_seqlens[p + 1]);
@@ -208,22 +236,16 @@ __global__ __launch_bounds__(256) void append8_kernel(Plan pl, Append8 a, const 
     const int64_t slot0 = page_slot(row_of(a.kp, uniform(pl.order[p])), a.kp.log2_page, pos0);
     if (a.rotate) {
       if (r0 != first) __syncthreads();                   // block-uniform; the run before has been rotated
-      for (int i = threadIdx.x; i < nr * HALF; i += 256) {
-        const int r = i / HALF, k = i % HALF;
-        const double inv = exp2(-(2.0 * (double)k / (double)DH) * a.log2_theta) * 0.15915494309189535;
+      for (int r = threadIdx.x / HALF; r < nr; r += 256 / HALF) {
         const double rev = (double)(pos0 + r) * inv;
-        double s, c;
-        sincospi(2.0 * (rev - rint(rev)), &s, &c);
-        cs[(r * 8 + (k & 7)) * PER + (k >> 3) + r * PER] = double2{c, s};
+        double sine, cosine;
+        sincospi(2.0 * (rev - rint(rev)), &sine, &cosine);
+        cs[(r * 8 + (pair & 7)) * PER + (pair >> 3) + r * PER] = double2{cosine, sine};
       }
       __syncthreads();
     }
-    const int n_heads = a.H + 2 * a.KH, step = 4 * gridDim.y;
-    const int units = nr == 1 ? (n_heads + 64 / PER - 1) / (64 / PER) : n_heads;
-    for (int unit = blockIdx.y * 4 + wave; unit < units; unit += step) {
-      if (nr == 1) append_heads<T, DH, true>(a, qkv, q_out, unit, r0, nr, pos0, slot0, cs);
-      else append_heads<T, DH, false>(a, qkv, q_out, unit, r0, nr, pos0, slot0, cs);
-    }
+    if (nr == 1) heads(std::true_type{}, (n_heads + 64 / PER - 1) / (64 / PER), r0, nr, pos0, slot0);
+    else heads(std::false_type{}, n_heads, r0, nr, pos0, slot0);
   }
 }
 
@@ -1109,11 +1131,11 @@ hipError_t launch_append8(int dtype, const Plan& pl, int H, int KH, int head_dim
   // A wave takes 6 heads of a run, so that the blocks come to several rounds over the chip and the last one is short; where
   // blocks are few, less.  (Each split takes the run's angles anew.)
   const int most = (units + 3) / 4;
-  int split = (units + 23) / 24;
+  int split = (units + 15) / 16;
   if ((int64_t)blocks * split < 512) split = (512 + blocks - 1) / blocks;
-  split = split < 1 ? 1 : split > most ? most : split;
+  a.split = split < 1 ? 1 : split > most ? most : split;
 #define APPEND(T_, D_)                                                                                             \
-  hipLaunchKernelGGL((append8_kernel<T_, D_>), dim3((unsigned)blocks, (unsigned)split), dim3(256), 0, s, pl, a, (const T_*)qkv, (T_*)q_out)
+  hipLaunchKernelGGL((append8_kernel<T_, D_>), dim3((unsigned)(blocks * a.split)), dim3(256), 0, s, pl, a, (const T_*)qkv, (T_*)q_out)
   if (dtype == VFM_BF16) { if (head_dim == 64) APPEND(bf16, 64); else APPEND(bf16, 128); }
   else { if (head_dim == 64) APPEND(float, 64); else APPEND(float, 128); }
 #undef APPEND
