@@ -27,45 +27,41 @@ constexpr uint32_t IN_PROMPT = 1u << 31;                  // the token was seen 
 // lets twice as many share a CU; with WIDE, one each.
 constexpr int BIAS_AT = 16, BIAS_MOST = (1 << 15) - 1, COUNT_MOST = (1 << 16) - 1;
 
-// The tokens p[0 .. n), taken by all threads of a block, 16 bytes a load where they are aligned.  The first load is made
-// apart from the rest: it is on its way while something else is done.
+// The tokens p[0 .. n), taken by all threads of a block, 16 bytes a load where they are aligned, three loads ahead of their
+// use; the first three are on their way while LDS is cleared.
 template <int THREADS>
 struct Tokens {
-  const int32_t* p;
-  int n, head, quads, tail;    // tokens before the quads, quads, the first token behind them
-  i32x4 first;
-  int32_t edge;                // of the thread: one before or behind the quads (3 and 3 at most)
-  __device__ __forceinline__ Tokens(const int32_t* p_, int n_) : p(p_), n(n_), first{}, edge(0) {
-    head = min(n, (int)((4 - (((uintptr_t)p >> 2) & 3)) & 3));
+  const i32x4* quad;
+  int quads;
+  int32_t edge;                // of the thread: one before or behind the quads (3 and 3 at most), or none
+  bool has_edge;
+  i32x4 q[3];
+  __device__ __forceinline__ Tokens(const int32_t* p, int n) {
+    const int tid = threadIdx.x;
+    const int head = min(n, (int)((4 - (((uintptr_t)p >> 2) & 3)) & 3));
     quads = (n - head) >> 2;
-    tail = head + 4 * quads;
-    const int tid = threadIdx.x;
-    if (tid < quads) first = quad()[tid];
-    if (tid < head) edge = p[tid];
-    else if (tid >= 4 && tid - 4 < n - tail) edge = p[tail + tid - 4];
-  }
-  __device__ __forceinline__ const i32x4* quad() const { return reinterpret_cast<const i32x4*>(p + head); }
-  template <typename F>
-  __device__ __forceinline__ void each(F f) const {
-    const int tid = threadIdx.x;
-    if (tid < head || (tid >= 4 && tid - 4 < n - tail)) f(edge);
-    if (tid < quads)
+    quad = reinterpret_cast<const i32x4*>(p + head);
+    const int at = tid < 4 ? tid : head + 4 * quads + tid - 4;
+    has_edge = tid < 4 ? tid < head : tid < 8 && at < n;
+    edge = has_edge ? p[at] : 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f(first[e]);
-    int i = tid + THREADS;
-    for (; i + 3 * THREADS < quads; i += 4 * THREADS) {
-      i32x4 v[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = quad()[i + k * THREADS];
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f(v[k][e]);
+    for (int k = 0; k < 3; ++k) {
+      q[k] = i32x4{};
+      if (tid + k * THREADS < quads) q[k] = quad[tid + k * THREADS];
     }
-    for (; i < quads; i += THREADS) {
-      const i32x4 v = quad()[i];
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F f) {
+    if (has_edge) f(edge);
+#pragma unroll 1
+    for (int i = threadIdx.x; i < quads; i += THREADS) {
+      i32x4 next = {};
+      if (i + 3 * THREADS < quads) next = quad[i + 3 * THREADS];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f(v[e]);
+      for (int e = 0; e < 4; ++e) f(q[0][e]);
+      q[0] = q[1];
+      q[1] = q[2];
+      q[2] = next;
     }
   }
 };
@@ -118,7 +114,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(8, 8)))
     float* dst = out + base + at;
     const int skip = at < 0 ? -at : 0, past = min(n - at, SIZE);   // its outputs are places skip .. past - 1
     const uint32_t from = (uint32_t)(at + skip), span = (uint32_t)(past - skip);
-    const Tokens<THREADS> before(a.hist + hb, prompt), generated(a.hist + hb + prompt, hist - prompt);
+    Tokens<THREADS> before(a.hist + hb, prompt), generated(a.hist + hb + prompt, hist - prompt);
     const int32_t bias0 = tid < biases ? a.bias_id[bb + tid] : -1;
 #pragma unroll
     for (int g = 0; g < SLICE / (4 * THREADS); ++g) *reinterpret_cast<u32x4*>(known + 4 * (tid + g * THREADS)) = u32x4{};
