@@ -858,6 +858,7 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
       }
       bf16x8 pf[4];
       __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
       // Scores of t + 1 (2 KS MFMAs) beside the first half of t's weights, the conversion of what was loaded and the next
       // loads; a fragment is read four ahead of its MFMA.
       store(j, true);
@@ -877,6 +878,7 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
 #pragma unroll
       for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(pf[u]));   // not put off behind the mask
       __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(0);
       if (t + 1 < t1) mask(t + 1, sn);
       __builtin_amdgcn_sched_barrier(0);
       // products of t (4 ND MFMAs) beside the second half of its weights and the largest scores of t + 1
@@ -1006,18 +1008,32 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
 #pragma unroll
   for (int c = 0; c < NV; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = LOWEST, l_run = 0.f;
+  // a run's codes, loaded while the one before is computed
+  struct Run {
+    int slot;
+    uint32_t ex, vc[4][NV / 4];
+    u32x4 kc[KL];
+  } next;
+  auto load = [&](int t) {
+    const int slot = page_slot(prow, lp, 16 * vis.run(t));
+    next.slot = slot;
+    next.ex = runs_exps(exps, slot, slot, a.KH, w.h);
+    const uint8_t *kr = kh + (int64_t)slot * DH, *vr = vh + (int64_t)slot * DH;
+#pragma unroll
+    for (int c = 0; c < KL; ++c) next.kc[c] = *reinterpret_cast<const u32x4*>(kr + (x * DH + 64 * c + 16 * g));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) __builtin_memcpy(next.vc[j], __builtin_assume_aligned(vr + ((4 * g + j) * DH + NV * x), NV), NV);
+  };
+  if (t0 + wave < t1) load(t0 + wave);
   for (int t = t0 + wave; t < t1; t += 4) {
     const int p0 = 16 * vis.run(t);
-    const int64_t slot = page_slot(prow, lp, p0);
     const bool full = seen_by_all(j0, j1, p0, p0 + 15, a.window, a.n_sink);
-    const uint32_t ex = runs_exps(exps, slot, slot, a.KH, w.h);
-    u32x4 kc[KL];
-    uint32_t vc[4][NV / 4];
-#pragma unroll
-    for (int c = 0; c < KL; ++c) kc[c] = *reinterpret_cast<const u32x4*>(kh + (slot + x) * DH + 64 * c + 16 * g);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) __builtin_memcpy(vc[j], __builtin_assume_aligned(vh + (slot + 4 * g + j) * DH + NV * x, NV), NV);
-    const float kscale = k_scale(ex, 0), vscale = v_scale(ex, 0);
+    const Run now = next;
+    if (t + 4 < t1) load(t + 4);
+    const int64_t slot = now.slot;
+    const u32x4(&kc)[KL] = now.kc;
+    const uint32_t(&vc)[4][NV / 4] = now.vc;
+    const float kscale = k_scale(now.ex, 0), vscale = v_scale(now.ex, 0);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
