@@ -231,8 +231,9 @@ def loop_bench(args):
     (or by BFQ with --admission bfq) up to 8192 tokens per step.  Timed from the first step to the last request
     finishing, host scheduling and the per-step token read-back included.
     --window W: every row sees the last W positions and the first --sinks (a
-    ring of pages per sequence); --draw: tokens drawn at temperature 0.8 from
-    the 40 largest outputs, of those from 0.95 of the weight."""
+    ring of pages per sequence); --kv8: the cache held in 8 bits; --draw: tokens
+    drawn at temperature 0.8 from the 40 largest outputs, of those from 0.95 of
+    the weight; --penalize: repetition 1.2, presence 0.3, frequency 0.1."""
     import torch
     from paper_2606_09643_amd import binding as B
     from paper_2606_09643_amd import runner as R
@@ -256,10 +257,11 @@ def loop_bench(args):
             bfq = B.BFQ(np.ones(w.n_tasks), [0.0] + [1.0 + 0.25 * b for b in range(1, 17)], b_max=16)
         cb = R.ContinuousBatcher(model, emb, page_size=page, n_pages=n_pages, max_seqs=max_seqs,
                                  max_step_tokens=8192, max_pages=(512 + 128 + page - 1) // page, bfq=bfq,
-                                 token_time=1.0 / max_seqs, window=args.window or None, n_sink=args.sinks)
+                                 token_time=1.0 / max_seqs, window=args.window or None, n_sink=args.sinks, kv8=args.kv8)
         for i in range(n):
             cb.submit(i, int(tasks[i]), rng.integers(0, w.vocab, size=int(plen[i])), int(new[i]),
-                      sampling=R.SamplingParams(0.8, top_k=40, top_p=0.95, seed=i) if args.draw else None)
+                      sampling=R.SamplingParams(0.8, top_k=40, top_p=0.95, seed=i) if args.draw else None,
+                      adjust=R.AdjustParams(1.2, 0.3, 0.1) if args.penalize else None)
         return cb
     warm = make()                                      # warm-up run (kernels, allocator caches)
     for _ in range(3):
@@ -284,6 +286,10 @@ def loop_bench(args):
         out["config"].update(window=args.window, sinks=args.sinks)
     if args.draw:
         out["config"]["draw"] = "temperature 0.8, top-k 40, top-p 0.95"
+    if args.kv8:
+        out["config"]["kv_cache"] = "e4m3, a scale per 16 positions and head"
+    if args.penalize:
+        out["config"]["penalties"] = "repetition 1.2, presence 0.3, frequency 0.1"
     print(json.dumps(out), flush=True)
 
 
@@ -358,6 +364,8 @@ def main():
                     help="--loop: admit prompts FIFO or by BFQ (16-request batches, decode tokens charged)")
     ap.add_argument("--window", type=int, default=0, help="--loop: attend to this many last positions (0: all)")
     ap.add_argument("--sinks", type=int, default=0, help="--loop --window: and to this many first ones")
+    ap.add_argument("--kv8", action="store_true", help="--loop: hold the KV cache in 8 bits")
+    ap.add_argument("--penalize", action="store_true", help="--loop: penalize repeated tokens")
     ap.add_argument("--draw", action="store_true", help="--loop: draw the tokens instead of taking the largest output")
     ap.add_argument("--paged", type=int, default=0,
                     help="decode workloads: read the KV cache through pages of this many slots "

@@ -209,10 +209,37 @@ class SamplingParams:
         self.seed = seed
 
 
-class _Seq:
-    __slots__ = ("rid", "task", "prompt", "max_new", "slot", "cached", "generated", "budget", "row", "sampling", "rng")
+class AdjustParams:
+    """What is done to a request's head outputs before its token is picked or
+    drawn (vfm_adjust_outputs): penalties for tokens of its prompt and of its
+    answer so far (repetition divides or multiplies the output, frequency is
+    subtracted per occurrence in the answer, presence once), `bias`
+    {output: value to add}, and `allowed`: a bool array over the outputs, or a
+    function of the list of tokens generated so far that gives one (a grammar;
+    the step then waits for the step before it, whose tokens it reads back).
+    Where `allowed` leaves nothing, the token is -1."""
 
-    def __init__(self, rid, task, prompt, max_new, page_size, sampling=None):
+    def __init__(self, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None):
+        self.repetition, self.presence, self.frequency = float(repetition), float(presence), float(frequency)
+        if not (0 < self.repetition < float("inf") and np.isfinite(self.presence) and np.isfinite(self.frequency)):
+            raise ValueError("repetition is positive, all penalties are finite")
+        bias = dict(bias or {})
+        self.bias_id = np.array(list(bias), np.int64)
+        self.bias = np.array(list(bias.values()), np.float32)
+        if len(bias) and (self.bias_id.min() < 0 or np.isnan(self.bias).any()):
+            raise ValueError("bias: outputs from 0 on, values that are numbers")
+        self.allowed = allowed if allowed is None or callable(allowed) else np.array(allowed, bool)
+
+    @property
+    def penalizes(self):
+        return self.repetition != 1.0 or self.presence != 0.0 or self.frequency != 0.0
+
+
+class _Seq:
+    __slots__ = ("rid", "task", "prompt", "max_new", "slot", "cached", "generated", "budget", "row", "sampling", "rng",
+                 "adjust", "answer", "hist")
+
+    def __init__(self, rid, task, prompt, max_new, page_size, sampling=None, adjust=None):
         self.rid, self.task = rid, int(task)
         self.prompt = np.asarray(prompt, np.int32)
         self.max_new = int(max_new)
@@ -224,6 +251,9 @@ class _Seq:
         self.budget = -(-(len(self.prompt) + self.max_new - 1) // page_size)
         self.sampling = sampling        # None: greedy
         self.rng = np.random.default_rng(sampling.seed) if sampling is not None else None
+        self.adjust = adjust            # None: the head outputs as they are
+        self.answer = []                # the generated tokens, kept on the host where a mask depends on them
+        self.hist = -1                  # where its tokens begin on the device, where they are penalized
 
 
 class ContinuousBatcher:
@@ -253,25 +283,34 @@ class ContinuousBatcher:
     as many as the window and one step's new rows can touch, used again in
     turn.  A prompt then takes at most `max_chunk` rows of a step (default:
     the window, but no less than a page), in fp32 too.  Requests submitted
-    with a SamplingParams have their tokens drawn by vfm_sample_tokens."""
+    with a SamplingParams have their tokens drawn by vfm_sample_tokens, those
+    with an AdjustParams from outputs that vfm_adjust_outputs has changed.
+
+    With `kv8` the cache is held in 8 bits (vfm_layer_forward_q8): the same
+    pages take half a bf16 cache's memory, with or without a window, and
+    prompts may come in chunks in fp32 too."""
 
     def __init__(self, model: Model, emb, page_size=64, n_pages=1024, max_seqs=256, max_step_tokens=8192,
                  max_pages=None, bfq=None, token_time=1.0, chunk_prompts=None, record=False, device="cuda",
-                 window=None, n_sink=0, max_chunk=None):
+                 window=None, n_sink=0, max_chunk=None, kv8=False):
         w = model.w
         self.m, self.emb, self.device = model, emb, device
         self.page_size, self.n_pages = int(page_size), int(n_pages)
         self.max_seqs, self.max_step_tokens = int(max_seqs), int(max_step_tokens)
         self.max_pages = int(max_pages) if max_pages is not None else self.n_pages
         self.alloc = B.PageAllocator(self.n_pages, self.page_size, self.max_seqs, self.max_pages)
-        shape = (w.n_heads, self.n_pages * self.page_size, w.head_dim)
-        self.k = [torch.zeros(shape, dtype=w.torch_dtype, device=device) for _ in range(model.n_layers)]
-        self.v = [torch.zeros(shape, dtype=w.torch_dtype, device=device) for _ in range(model.n_layers)]
+        self.kv8 = bool(kv8)
+        slots = self.n_pages * self.page_size
+        shape, kind = (w.n_heads, slots, w.head_dim), torch.uint8 if self.kv8 else w.torch_dtype
+        self.k = [torch.zeros(shape, dtype=kind, device=device) for _ in range(model.n_layers)]
+        self.v = [torch.zeros(shape, dtype=kind, device=device) for _ in range(model.n_layers)]
+        self.exps = [torch.zeros((slots // 16, w.n_heads, 2), dtype=torch.uint8, device=device)
+                     for _ in range(model.n_layers)] if self.kv8 else None
         self.cfg = B.vfm_cfg.from_buffer_copy(model.cfg)
         self.cfg.attn = B.VFM_ATTN_MIXED
         self.bfq, self.record, self.token_time = bfq, record, float(token_time)
-        # prompt chunks after cached tokens run on the bf16 path only, under a window in fp32 too
-        self.chunk = (w.dtype == "bf16" or window is not None) if chunk_prompts is None else bool(chunk_prompts)
+        # prompt chunks after cached tokens run on the bf16 path only, under a window or in 8 bits in fp32 too
+        self.chunk = (w.dtype == "bf16" or window is not None or self.kv8) if chunk_prompts is None else bool(chunk_prompts)
         if window is not None and not (1 <= window <= 2 ** 30 and 0 <= n_sink <= 2 ** 30
                                        and window == int(window) and n_sink == int(n_sink)):
             raise ValueError("window: 1 .. 2^30 positions, n_sink: 0 .. 2^30")
@@ -287,9 +326,11 @@ class ContinuousBatcher:
         self.committed = 0              # pages the running sequences hold or may still take
         self.ws = torch.empty(0, dtype=torch.uint8, device=device)
         self.steps = 0
-        self.trace = []                 # per step: [(rid, logits)] when record is set
+        self.trace = []                 # per step: [(rid, head outputs as the head gave them)] when record is set
         self._picks, self._prev_nxt, self._keep = [], None, None
         self._ready = []                # taken from BFQ, not yet admitted (in its order)
+        self._hist = torch.empty(0, dtype=torch.int32, device=device)    # tokens of the penalized sequences, a part each
+        self._hist_free = []            # parts that finished sequences have left: (length, begin)
 
     def _ring(self, s):
         """(pages of the sinks, pages of the ring behind them) of a windowed
@@ -299,8 +340,14 @@ class ContinuousBatcher:
         n = min(len(s.prompt), self.max_chunk) if self.chunk else len(s.prompt)
         return -(-self.n_sink // self.page_size), -(-(self.window - 2 + n) // self.page_size) + 1
 
-    def submit(self, rid, task, prompt, max_new, now=0.0, sampling=None):
-        s = _Seq(rid, task, prompt, max_new, self.page_size, sampling)
+    def submit(self, rid, task, prompt, max_new, now=0.0, sampling=None, adjust=None):
+        s = _Seq(rid, task, prompt, max_new, self.page_size, sampling, adjust)
+        if adjust is not None:
+            n_out = int(self.m.heads.n_out[s.task])
+            if len(adjust.bias_id) and adjust.bias_id.max() >= n_out:
+                raise ValueError(f"request {rid}: a bias of an output that its head of {n_out} does not have")
+            if isinstance(adjust.allowed, np.ndarray) and adjust.allowed.shape != (n_out,):
+                raise ValueError(f"request {rid}: a mask of its head's {n_out} outputs is expected")
         if self.window is not None:
             s.budget = min(s.budget, sum(self._ring(s)))
         if s.budget > self.max_pages or len(s.prompt) < 1 or s.max_new < 1:
@@ -397,10 +444,90 @@ class ContinuousBatcher:
         sp = B.Sampling(dev[0], dev[1].view(torch.int32), dev[2], dev[3])
         B.vfm_sample_tokens(pb.c, out, sp, dev[4], nxt)
 
+    def _place_history(self, s):
+        """Room on the device for the tokens of s, its prompt written there (in stream order)."""
+        need = len(s.prompt) + s.max_new
+        fit = min((f for f in self._hist_free if f[0] >= need), default=None)
+        if fit is None:
+            begin = self._hist.numel()
+            fit = (max(need, begin), begin)                # the buffer doubles
+            grown = torch.empty(begin + fit[0], dtype=torch.int32, device=self.device)
+            grown[:begin] = self._hist
+            self._hist = grown
+        else:
+            self._hist_free.remove(fit)
+        s.hist = fit[1]
+        if fit[0] > need:
+            self._hist_free.append((fit[0] - need, fit[1] + need))
+        self._hist[s.hist:s.hist + len(s.prompt)] = self._h2d(s.prompt)
+
+    def _read_answers(self, dec):
+        """The last step's tokens of the sequences whose masks depend on them (waits for that step)."""
+        who = [s for s in dec if s.adjust is not None and callable(s.adjust.allowed)]
+        if who:
+            last = self._prev_nxt.cpu().numpy()
+            for s in who:
+                s.answer.append(int(last[s.row]))
+
+    def _adjust(self, pb, batch, emits, out):
+        """Penalties, biases and masks of the requests that pick a token, in place on their head outputs."""
+        who = [(i, s) for i, s in enumerate(batch) if emits[i] and s.adjust is not None]
+        if not who:
+            return
+        n = len(batch)
+        t = {}
+        pen = [(i, s) for i, s in who if s.adjust.penalizes]
+        if pen:
+            par, where = np.zeros((3, n), np.float32), np.zeros((2, n), np.int32)
+            par[0] = 1.0
+            begin = np.zeros(n, np.int64)
+            for i, s in pen:
+                if s.hist < 0:
+                    self._place_history(s)
+                par[:, i] = s.adjust.repetition, s.adjust.presence, s.adjust.frequency
+                begin[i], where[:, i] = s.hist, (len(s.prompt) + len(s.generated), len(s.prompt))
+            par, where = self._h2d(par), self._h2d(where)
+            t.update(repetition=par[0], presence=par[1], frequency=par[2], hist=self._hist, hist_begin=self._h2d(begin),
+                     hist_len=where[0], n_prompt=where[1])
+        if any(len(s.adjust.bias) for _, s in who):
+            count = np.zeros(n, np.int32)
+            for i, s in who:
+                count[i] = len(s.adjust.bias)
+            begin = np.concatenate([[0], np.cumsum(count)[:-1]]).astype(np.int64)
+            t.update(bias=self._h2d(np.concatenate([s.adjust.bias for _, s in who])),
+                     bias_id=self._h2d(np.concatenate([s.adjust.bias_id for _, s in who]).astype(np.int32)),
+                     bias_begin=self._h2d(begin), bias_len=self._h2d(count))
+        masks = []
+        row = np.full(n, -1, np.int32)
+        for i, s in who:
+            allowed = s.adjust.allowed
+            if allowed is None:
+                continue
+            if callable(allowed):
+                allowed = np.asarray(allowed(list(s.answer)), bool)
+                if allowed.shape != (int(self.m.heads.n_out[s.task]),):
+                    raise ValueError(f"request {s.rid}: its mask is not one of its head's outputs")
+            row[i] = len(masks)
+            masks.append(np.packbits(allowed, bitorder="little"))
+        if masks:
+            words = np.zeros((len(masks), -(-max(len(b) for b in masks) // 4) * 4), np.uint8)
+            for w, b in zip(words, masks):
+                w[:len(b)] = b
+            t.update(mask=self._h2d(words.view(np.int32)), mask_row=self._h2d(row))
+        B.vfm_adjust_outputs(pb.c, out, B.OutputAdjust(**t))
+
+    def _keep_tokens(self, batch, emits, nxt):
+        """The picked tokens of the penalized sequences, behind those that they have."""
+        who = [(i, s.hist + len(s.prompt) + len(s.generated)) for i, s in enumerate(batch) if emits[i] and s.hist >= 0]
+        if who:
+            at = self._h2d(np.array(who, np.int64).T)
+            self._hist[at[1]] = nxt[at[0]]
+
     def step(self, now=0.0):
         """One continuous-batching step; returns the ids of the requests that finished.
 
-        Nothing here waits for the GPU (unless `record` is set): a decode
+        Nothing here waits for the GPU (unless `record` is set, or a
+        request's mask depends on its tokens): a decode
         row's input token is gathered on the device from the previous step's
         picks, the host copies go through pinned memory, and a
         sequence finishes by its token count, so the host plans step n + 1
@@ -413,6 +540,7 @@ class ContinuousBatcher:
         # next chunk of the step's token budget (the whole rest of the prompt
         # when prompts are not chunked)
         dec = [s for s in old if s.cached >= len(s.prompt)]
+        self._read_answers(dec)
         budget = self.max_step_tokens - len(dec)
         chunks = []
         for s in [s for s in old if s.cached < len(s.prompt)] + new:
@@ -432,7 +560,11 @@ class ContinuousBatcher:
         table_dev = self._h2d(table)
         pb = B.Batch(task, lens, w.n_tasks, ctx_len=ctx, n_out=self.m.heads.n_out, device=self.device,
                      non_blocking=True)
-        if self.window is None:
+        window = self.window or 0
+        if self.kv8:
+            need = max(B.vfm_workspace_size_q8(self.cfg, pb.c, self.m.lora_c(i), window, self.n_sink)
+                       for i in range(self.m.n_layers))
+        elif self.window is None:
             need = max(B.vfm_workspace_size(self.cfg, pb.c, self.m.lora_c(i)) for i in range(self.m.n_layers))
         else:
             need = max(B.vfm_workspace_size_windowed(self.cfg, pb.c, self.m.lora_c(i), self.window, self.n_sink)
@@ -454,7 +586,10 @@ class ContinuousBatcher:
         for li in range(self.m.n_layers):
             kv = B.vfm_kv_pages(self.k[li].data_ptr(), self.v[li].data_ptr(), self.n_pages, self.page_size,
                                 table.shape[1], tp, table_dev.data_ptr())
-            if self.window is None:
+            if self.kv8:
+                B.vfm_layer_forward_q8(self.cfg, self.m.c_layers[li], self.m.lora_c(li), pb.c, x,
+                                       B.vfm_kv_pages_q8(kv, self.exps[li].data_ptr()), window, self.n_sink, self.ws)
+            elif self.window is None:
                 B.vfm_layer_forward_paged(self.cfg, self.m.c_layers[li], self.m.lora_c(li), pb.c, x, kv, self.ws)
             else:
                 B.vfm_layer_forward_windowed(self.cfg, self.m.c_layers[li], self.m.lora_c(li), pb.c, x, kv,
@@ -464,10 +599,13 @@ class ContinuousBatcher:
         B.vfm_head_forward(self.cfg, fn["w"], fn.get("b"), self.m.head_tab.c, pb.c, x, out, self.ws)
         nxt = torch.empty(len(batch), dtype=torch.int32, device=self.device)
         emits = [s.cached + int(n) >= len(s.prompt) for s, n in zip(batch, lens)]
+        o = out.cpu().numpy() if self.record else None
+        self._adjust(pb, batch, emits, out)
         if any(s.sampling is not None for s in batch):
             self._sample(pb, batch, emits, out, nxt)
         else:
             B.vfm_greedy_tokens(pb.c, out, nxt)
+        self._keep_tokens(batch, emits, nxt)
         self._prev_nxt = nxt
         self._picks.append(nxt)
         self._keep = (pb, table, table_dev)            # host arrays the stream may still read
@@ -475,7 +613,6 @@ class ContinuousBatcher:
             per_task = np.bincount(task[:n_dec], minlength=w.n_tasks)
             for t in np.nonzero(per_task)[0]:
                 self.bfq.charge(int(t), float(per_task[t]) * self.token_time)
-        o = out.cpu().numpy() if self.record else None
         off = pb.out_off() if self.record else None
         rec, finished = [], []
         for i, s in enumerate(batch):
@@ -488,6 +625,8 @@ class ContinuousBatcher:
                 rec.append((s.rid, o[off[i]:off[i + 1]].copy()))
             if len(s.generated) == s.max_new:
                 self.alloc.release(s.slot)
+                if s.hist >= 0:
+                    self._hist_free.append((len(s.prompt) + s.max_new, s.hist))
                 self.free_slots.append(s.slot)
                 self.committed -= s.budget
                 self.running.remove(s)

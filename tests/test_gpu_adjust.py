@@ -232,3 +232,21 @@ def test_adjust_replayed_graph_and_other_stream():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(to[:-5].nan_to_num(7.0), want[:-5].nan_to_num(7.0)), i
+
+
+@pytest.mark.parametrize("n,n_req", [(50000, 1), (3000, 3), (20000, 260)])
+def test_adjust_lists_past_16_bits(n, n_req):
+    """One request of more tokens than 16 bits count, of one output mostly, and one of more biases than 15 bits count,
+    several for the same output; beside requests with short lists."""
+    rng = np.random.default_rng(n)
+    rows = [rng.standard_normal(n) * 4 for _ in range(n_req)]
+    par = [_par(rng, n, 50, allow=0.5) for _ in rows]
+    hist = np.full(200000, n - 2, np.int64)
+    hist[::100] = rng.integers(0, n, 2000)
+    par[0].update(hist=hist, n_prompt=1000, f=0.01, p=0.1, r=1.3)
+    par[-1]["bias"] = [(int(j), float(v)) for j, v in zip(rng.integers(0, n, 70000), rng.standard_normal(70000).round(2))]
+    if n_req > 1:
+        par[1].update(hist=np.full(65536, 5, np.int64), n_prompt=0, f=0.001, r=1.0)
+    b = Rows(rows, par)
+    for place in (True, False):
+        b.check(b.run(place))

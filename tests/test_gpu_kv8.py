@@ -427,3 +427,166 @@ def test_attention_replayed_graph_and_other_stream(dtype):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager), i
+
+
+@pytest.mark.parametrize("dtype,H,KH,dh,window,lens,ctx", [
+    ("bf16", 8, 1, 128, 0, [1] * 130, [20, 30000] + [40] * 127 + [9000]),
+    ("bf16", 32, 8, 64, 0, [700, 1, 2, 40], [0, 20000, 100, 9000]),
+    ("bf16", 32, 8, 128, 0, [5, 600, 1, 1], [30000, 10, 700, 12000]),
+    ("bf16", 16, 16, 64, 6000, [1] * 600 + [33], [90] * 599 + [20000, 9000]),
+    ("f32", 4, 2, 64, 0, [900, 1, 30], [0, 15000, 6000]), ("f32", 16, 2, 128, 0, [300, 2], [10, 12000])])
+def test_attention_long_contexts_beside_others(dtype, H, KH, dh, window, lens, ctx):
+    """Steps whose blocks and records are the requests' own by a table: every request has the bits that it has alone, the
+    long ones the 64-bit form's values; replayed from a graph the same."""
+    log(f"long beside others, 8 bits {dtype} H {H} KH {KH} dh {dh} {len(lens)} requests")
+    sinks = 2 if window else 0
+    c = Cache8(lens, ctx, KH, dh, 64, window, sinks, seed=13)
+    code, td, _ = DT[dtype]
+    q = _queries(lens, H, dh, dtype, 14, std=1.0)
+    n = len(lens)
+    task = _tasks(n, 5)
+    attn = B.make_attn(code, H, KH, dh, window=window, n_sink=sinks)
+    pb = B.Batch(task, c.lens, 5, ctx_len=c.ctx)
+    got = _attend(c, task, H, KH, dh, window, sinks, dtype, q)
+    order = np.argsort(ctx)
+    some = sorted({0, 1, min(2, n - 1), n - 2, n - 1, int(order[-1]), int(order[-2]), int(np.argmax(lens))})
+    for i in some:
+        assert np.array_equal(_attend(c, task, H, KH, dh, window, sinks, dtype, q, only=[i], ws_fill=0)[i], got[i]), i
+    few = {i: got[i] for i in some if lens[i] <= 5 or ctx[i] > 1000}
+    log(f"  {_check(c, few, q, window, sinks, dtype, dh ** -0.5):.3f} of the tolerance")
+    by = np.argsort(task, kind="stable")
+    qd = torch.from_numpy(np.concatenate([q[o].reshape(-1, H * dh) for o in by])).to(td).cuda()
+    eager, out = torch.empty_like(qd), torch.zeros_like(qd)
+    ws = torch.full((B.vfm_attention_workspace_q8(attn, pb.c),), 255, dtype=torch.uint8, device="cuda")
+    B.vfm_attention_paged_q8(attn, pb.c, qd, c.kv, eager, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.vfm_attention_paged_q8(attn, pb.c, qd, c.kv, out, ws)
+    for i in range(3):
+        out.fill_(float(i))
+        ws.fill_(170 + i)
+        (qd.float() @ qd[:1].float().T).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager), i
+
+
+@pytest.mark.parametrize("dtype,lens", [("bf16", [1, 1]), ("bf16", [1, 70]), ("f32", [1, 9])])
+def test_pages_past_32_bit_offsets_and_shared_by_requests(dtype, lens):
+    """A pool whose later codes lie past 2^32 bytes: the step's pages are the pool's last ones, and both requests' tables
+    begin with the same pages (a prefix that they share)."""
+    code, td, u = DT[dtype]
+    H, KH, dh, page = 4, 2, 128, 64
+    n_pages = (1 << 19) + 64                               # 2^25 slots and more of 128 bytes per head
+    lens, ctx = np.array(lens, np.int32), np.array([150, 200], np.int32)
+    last = n_pages - 1
+    table = np.array([[last, last - 3, last - 1, 0, 0], [last, last - 3, last - 2, last - 5, last - 4]], np.int32)
+    kp, vp = [torch.empty(KH, n_pages * page, dh, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    exps = torch.empty(n_pages * page // 16, KH, 2, dtype=torch.uint8, device="cuda")
+    rng = np.random.default_rng(17)
+    for t in (kp, vp):                                     # the last pages alone are written
+        t[:, -8 * page:] = torch.from_numpy(K.to_codes(rng.standard_normal((KH, 8 * page, dh)) * 80)).cuda()
+    exps[-8 * page // 16:] = torch.from_numpy(rng.integers(118, 121, (8 * page // 16, KH, 2)).astype(np.uint8)).cuda()
+    attn = B.make_attn(code, H, KH, dh)
+    pb = B.Batch(np.zeros(2, np.int32), lens, 1, ctx_len=ctx)
+    qkv = torch.from_numpy(rng.standard_normal((pb.T, (H + 2 * KH) * dh))).to(td).cuda()
+    kv = B.PagedKVQ8(kp, vp, exps, page, table)
+    q, out = [torch.empty(pb.T, H * dh, dtype=td, device="cuda") for _ in range(2)]
+    ws = torch.empty(max(1, B.vfm_attention_workspace_q8(attn, pb.c)), dtype=torch.uint8, device="cuda")
+    log(f"far pages, 8 bits {dtype} {lens}")
+    B.vfm_kv_append_q8(attn, pb.c, qkv, q, kv)
+    B.vfm_attention_paged_q8(attn, pb.c, q, kv, out, ws)
+    torch.cuda.synchronize()
+    rows, o, at = np64(qkv), np64(out), 0
+    assert np.array_equal(np64(q), rows[:, :H * dh])       # no rotation: as they were
+    for i, (m, c) in enumerate(zip(lens, ctx)):
+        pos = np.arange(int(c + m))
+        slots = table[i, pos // page].astype(np.int64) * page + pos % page
+        sd = torch.from_numpy(slots).cuda()
+        e = exps[sd // 16].cpu().numpy()
+        k, v = [K.VALUES[t[:, sd].cpu().numpy()].transpose(1, 0, 2) * 2.0 ** (e[..., n] - 127.0)[..., None]
+                for n, t in enumerate((kp, vp))]
+        r = rows[at:at + m].reshape(m, H + 2 * KH, dh)
+        for got, want, n in ((k[c:], r[:, H:H + KH], 0), (v[c:], r[:, H + KH:], 1)):
+            half = np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** (e[c:, :, n] - 137.0)[..., None])   # half an e4m3 step
+            assert np.all(np.abs(got - want) <= half)
+        ref, a, n = D.attention(r[:, :H], k, v, int(c), 0, 0, dh ** -0.5)
+        dot = D.score_sizes(r[:, :H], k, dh ** -0.5)[:, :, None]
+        lim = ((u if dtype == "bf16" else 0.0) + (n[:, None, None] + 16) * 2.0 ** -24) * (a + np.abs(ref)) \
+            + a * 2 * ((dh + 2) * 2.0 ** -24 * dot + 2.0 ** -22)
+        assert np.all(np.abs(o[at:at + m].reshape(m, H, dh) - ref) <= lim)
+        at += m
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shift", [-100, -20, 12, 18, 40])
+def test_attention_scales_of_any_size(dtype, shift):
+    """Keys under scales of 2^-110 to 2^30: scores from nothing to 2^33 and more, where the largest takes the whole weight;
+    values under the same scales come out times 2^shift.  Few rows and many."""
+    H, KH, dh = 2, 1, 64
+    lens, ctx = [1, 40], [200, 100]
+    c = Cache8(lens, ctx, KH, dh, 32, 0, 0, seed=2)
+    q = _queries(lens, H, dh, dtype, 1)
+    task = np.zeros(2, np.int32)
+    base = _attend(c, task, H, KH, dh, 0, 0, dtype, q)
+    seen = c.exps != 255
+    c.exps[..., 1] += (seen[..., 1] * shift).to(torch.uint8)        # wraps for negative shifts
+    got = _attend(c, task, H, KH, dh, 0, 0, dtype, q)
+    for i in range(2):
+        assert np.array_equal(got[i], base[i] * 2.0 ** shift)
+    c.v = [v * 2.0 ** shift for v in c.v]
+    c.exps[..., 0] += (seen[..., 0] * shift).to(torch.uint8)
+    c.k = [k * 2.0 ** shift for k in c.k]
+    got = _attend(c, task, H, KH, dh, 0, 0, dtype, q)
+    if shift > 0:                                          # rows whose two largest scores lie apart by more than rounding
+        for i in range(2):
+            for r in range(lens[i]):
+                for h in range(H):
+                    s = c.k[i][:ctx[i] + r + 1, 0] @ q[i][r, h] * dh ** -0.5
+                    top = np.argsort(s)
+                    size = np.abs(c.k[i][:ctx[i] + r + 1, 0]).max() * np.abs(q[i][r, h]).max() * dh ** 0.5
+                    if s[top[-1]] - s[top[-2]] > 40 + (dh + 2) * 2.0 ** -23 * size:
+                        v = c.v[i][top[-1], 0]
+                        assert np.all(np.abs(got[i][r, h] - v) <= 2.0 ** -8 * np.abs(v) + 2.0 ** -20 * np.abs(c.v[i]).max())
+    else:
+        log(f"  {_check(c, got, q, 0, 0, dtype, dh ** -0.5):.3f} of the tolerance")
+
+
+def test_attention_rows_of_a_wider_matrix():
+    """Queries as the first columns of [T, 3 d] rows, as a layer keeps them."""
+    H = KH = 2
+    dh = 64
+    c = Cache8([3, 40], [20, 0], KH, dh, 16, 10, 1, seed=3)
+    q = _queries([3, 40], H, dh, "bf16", 2, std=1.0)
+    ref = _attend(c, np.zeros(2, np.int32), H, KH, dh, 10, 1, "bf16", q)
+    pb = B.Batch(np.zeros(2, np.int32), c.lens, 1, ctx_len=c.ctx)
+    wide = torch.full((43, 3 * H * dh), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide[:, :H * dh] = torch.from_numpy(np.concatenate([x.reshape(-1, H * dh) for x in q])).to(torch.bfloat16).cuda()
+    out = torch.zeros(43, H * dh, dtype=torch.bfloat16, device="cuda")
+    attn = B.make_attn(B.VFM_BF16, H, KH, dh, window=10, n_sink=1)
+    B.vfm_attention_paged_q8(attn, pb.c, wide, c.kv, out)
+    assert np.array_equal(np64(out).reshape(-1, H, dh), np.concatenate([ref[0], ref[1]]))
+
+
+def test_prompt_in_chunks_and_at_once():
+    """A prompt appended in chunks that end on runs leaves the bits of one appended at once; in chunks that cut runs its
+    numbers are within a rounding to the run's last scale."""
+    H, KH, dh, n = 2, 2, 64, 100
+    rng = np.random.default_rng(4)
+    x = torch.from_numpy(rng.standard_normal((n, H + 2 * KH, dh)) * 2.0 ** rng.integers(-2, 3, (n, 1, 1))).to(torch.bfloat16)
+    pools = []
+    for cuts in ([0, 100], [0, 16, 64, 96, 100], [0, 5, 17, 18, 47, 50, 99, 100]):
+        pool = Pool8([0], [n], KH, dh, 16, 3)
+        for a, b in zip(cuts, cuts[1:]):
+            _step(pool, np.zeros(1, np.int32), [b - a], [a], H, KH, dh, "bf16", 10000.0, x[a:b])
+        pools.append(pool)
+    s = pools[0].slots(0, np.arange(n))
+    e = pools[0].ep.cpu().numpy()[s // 16]
+    for p in pools[1:]:
+        assert np.array_equal(p.ep.cpu().numpy()[s // 16], e)
+    for n_, t in enumerate(("kp", "vp")):
+        one, same, cut = (getattr(p, t).cpu().numpy()[:, s] for p in pools)
+        assert np.array_equal(one, same)
+        a, b = K.VALUES[one], K.VALUES[cut]
+        assert np.all(np.abs(a - b) <= 2.0 ** -9)          # e4m3's smallest number: what turns subnormal is rounded twice

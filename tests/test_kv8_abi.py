@@ -228,3 +228,54 @@ def test_plain_forms():
     assert np.isnan(K.adjust([1.0, 2.0], allowed=np.zeros(2, bool))).all()
     assert K.mask_words(np.arange(40) % 2 == 1, 2).view(np.uint32).tolist() == [0xAAAAAAAA, 0xAA]
     assert A.PTR == PTR
+
+
+class _Model:
+    """Just what the batcher reads before a step runs."""
+
+    def __init__(self):
+        from paper_2606_09643_amd import runner as R
+        from paper_2606_09643_amd import workloads as wl
+        self.w = wl.WORKLOADS[5].replace(n_layers=1, d=256, n_heads=2, head_dim=128, d_ff=512, n_tasks=3)
+        self.n_layers, self.cfg = 1, R.cfg_for(self.w)
+        self.heads = wl.Heads(np.array([7, 100, 33], np.int32), [], [])
+
+
+def test_adjust_parameters_are_refused():
+    from paper_2606_09643_amd import runner as R
+    for kw in (dict(repetition=0.0), dict(repetition=-1.0), dict(repetition=float("nan")), dict(repetition=float("inf")),
+               dict(presence=float("nan")), dict(frequency=float("inf")), dict(bias={-1: 1.0}), dict(bias={2: float("nan")})):
+        with pytest.raises(ValueError):
+            R.AdjustParams(**kw)
+    cb = R.ContinuousBatcher(_Model(), emb=None, page_size=16, n_pages=12, max_seqs=3, max_step_tokens=64, max_pages=6,
+                             device="cpu", kv8=True)
+    assert cb.k[0].dtype == torch.uint8 and cb.exps[0].shape == (12, 2, 2)
+    for task, a in ((0, R.AdjustParams(bias={7: 1.0})), (1, R.AdjustParams(allowed=np.ones(99))),
+                    (2, R.AdjustParams(allowed=np.ones((1, 33))))):
+        with pytest.raises(ValueError):
+            cb.submit(0, task, np.zeros(3, np.int32), 2, adjust=a)
+    cb.submit(0, 1, np.zeros(3, np.int32), 2, adjust=R.AdjustParams(bias={99: -np.inf}, allowed=np.ones(100)))
+    assert cb.waiting[0].adjust.penalizes is False
+
+
+def test_histories_have_their_own_room():
+    """Parts of the device's token buffer: none overlap while their sequences run, those of finished ones are used again."""
+    from paper_2606_09643_amd import runner as R
+    cb = R.ContinuousBatcher(_Model(), emb=None, page_size=16, n_pages=40, max_seqs=8, max_step_tokens=64, max_pages=6,
+                             device="cpu", kv8=True)
+    cb._h2d = lambda a: torch.from_numpy(np.ascontiguousarray(a))
+    rng = np.random.default_rng(0)
+    live, total = [], 0
+    for rid in range(200):
+        s = R._Seq(rid, 0, rng.integers(0, 9, rng.integers(1, 40)), int(rng.integers(1, 30)), 16)
+        cb._place_history(s)
+        live.append(s)
+        total = max(total, sum(len(x.prompt) + x.max_new for x in live))
+        if len(live) > 7:
+            gone = live.pop(int(rng.integers(0, len(live))))
+            cb._hist_free.append((len(gone.prompt) + gone.max_new, gone.hist))
+        spans = sorted((x.hist, x.hist + len(x.prompt) + x.max_new) for x in live)
+        assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])) and spans[-1][1] <= cb._hist.numel()
+        for x in live:
+            assert np.array_equal(cb._hist[x.hist:x.hist + len(x.prompt)].numpy(), x.prompt)
+    assert cb._hist.numel() <= 16 * total
