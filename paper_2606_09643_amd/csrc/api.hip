@@ -278,7 +278,9 @@ struct AttnPlan {
   size_t table_bytes(const Plan& pl) const { return table ? align_up((size_t)4 * (pl.n_req + 1) * sizeof(int32_t)) : 0; }
 };
 
-int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, AttnPlan* out) {
+// kv8: over a cache in 8 bits
+int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, bool kv8, AttnPlan* out) {
+  const int few_min = few_min_tiles(a.dtype, kv8);
   AttnPlan ap = {};
   ap.few_chunks = ap.rows_chunks = ap.qtiles = 1;
   ap.one = true;
@@ -289,7 +291,7 @@ int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, At
   for (int p = 0; p < pl.n_req; ++p) {
     const int m = cu[p + 1] - cu[p];
     if (ctx[p] < 0 || (int64_t)ctx[p] + m > kMaxPos) return VFM_ERR_SHAPE;
-    const Chunks ck = request_chunks(a.dtype, m, ctx[p], G, a.n_kv_heads, a.window, a.n_sink);
+    const Chunks ck = request_chunks(a.dtype, m, ctx[p], G, a.n_kv_heads, a.window, a.n_sink, few_min);
     const int n = ck.n;
     const AttnCounts c = request_counts(a.dtype, m, a.n_heads, a.n_kv_heads, n);
     for (int i = 0; i < 4; ++i) own[i] += c.v[i];
@@ -335,7 +337,8 @@ hipError_t run_attention(const vfm_attn& a, const Plan& pl, const AttnPlan& ap, 
                          const void* v, const uint8_t* exps, int64_t slots, const KvPages& kp, void* out, int64_t ldo,
                          char* ws, hipStream_t s) {
   PagedAttn p = {};
-  p.H = a.n_heads; p.KH = a.n_kv_heads; p.G = a.n_heads / a.n_kv_heads;
+  p.H = (int16_t)a.n_heads; p.KH = (int16_t)a.n_kv_heads; p.G = a.n_heads / a.n_kv_heads;
+  p.few_min = few_min_tiles(a.dtype, exps != nullptr);
   p.window = a.window; p.n_sink = a.window > 0 ? a.n_sink : 0;
   p.scale_log2 = (a.scale > 0.f ? a.scale : 1.f / sqrtf((float)a.head_dim)) * 1.4426950408889634f;
   p.q = q; p.ldq = ldq; p.k = k; p.v = v; p.slots = slots; p.kp = kp; p.out = out; p.ldo = ldo;
@@ -525,7 +528,7 @@ int layer_impl(const vfm_cfg& c, const vfm_layer_weights* w, const vfm_lora_tabl
   const int d = c.d_model, f = c.d_ff, T = pl.T;
   const int max_keys = max_keys_of(batch, pl);
   AttnPlan ap = {};
-  if (win) VFM_TRY(plan_attention(*win, batch, pl, &ap));
+  if (win) VFM_TRY(plan_attention(*win, batch, pl, exps != nullptr, &ap));
   const LayerWs ws = win ? layer_ws(c, pl, lora, 0, ap.bytes) : layer_ws(c, pl, lora, max_keys);
   if (!workspace || ws_bytes < ws.total || ((uintptr_t)workspace % ALIGN)) return VFM_ERR_WORKSPACE;
 
@@ -805,8 +808,10 @@ extern "C" int vfm_greedy_tokens(const vfm_batch* batch, const float* out, int32
 
 // ---- decoding over a bounded cache (vfm_decode.h) ----------------------------
 
-extern "C" int vfm_workspace_size_windowed(const vfm_cfg* cfg, const vfm_batch* batch, const vfm_lora_table* lora,
-                                           int32_t window, int32_t n_sink, size_t* bytes) {
+namespace {
+
+int workspace_windowed(const vfm_cfg* cfg, const vfm_batch* batch, const vfm_lora_table* lora, int32_t window,
+                       int32_t n_sink, bool kv8, size_t* bytes) {
   if (!bytes) return VFM_ERR_ARG;
   VFM_TRY(check_cfg(cfg));
   const vfm_attn a = attn_of_layer(*cfg, window, n_sink);
@@ -815,9 +820,27 @@ extern "C" int vfm_workspace_size_windowed(const vfm_cfg* cfg, const vfm_batch* 
   VFM_TRY(check_batch(batch, &pl));
   VFM_TRY(check_lora(lora, pl));
   AttnPlan ap;
-  VFM_TRY(plan_attention(a, batch, pl, &ap));
+  VFM_TRY(plan_attention(a, batch, pl, kv8, &ap));
   *bytes = std::max(layer_ws(*cfg, pl, lora, 0, ap.bytes).total, head_ws(*cfg, pl));
   return VFM_OK;
+}
+
+int workspace_attention(const vfm_attn* attn, const vfm_batch* batch, bool kv8, size_t* bytes) {
+  if (!bytes) return VFM_ERR_ARG;
+  VFM_TRY(check_attn(attn));
+  Plan pl;
+  VFM_TRY(check_batch(batch, &pl));
+  AttnPlan ap;
+  VFM_TRY(plan_attention(*attn, batch, pl, kv8, &ap));
+  *bytes = (size_t)ap.bytes;
+  return VFM_OK;
+}
+
+}  // namespace
+
+extern "C" int vfm_workspace_size_windowed(const vfm_cfg* cfg, const vfm_batch* batch, const vfm_lora_table* lora,
+                                           int32_t window, int32_t n_sink, size_t* bytes) {
+  return workspace_windowed(cfg, batch, lora, window, n_sink, false, bytes);
 }
 
 namespace {
@@ -851,7 +874,7 @@ int attend_paged(const vfm_attn* attn, const vfm_batch* batch, const void* q, in
   if (ldq % 8 || ldo % 8 || ldq < cols || ldo < cols) return VFM_ERR_SHAPE;
   VFM_TRY(check_pages(*attn, batch, pl, kv, true));
   AttnPlan ap;
-  VFM_TRY(plan_attention(*attn, batch, pl, &ap));
+  VFM_TRY(plan_attention(*attn, batch, pl, exps != nullptr, &ap));
   if (ap.bytes > 0 && (!workspace || ws_bytes < (size_t)ap.bytes || ((uintptr_t)workspace % ALIGN)))
     return VFM_ERR_WORKSPACE;
   VFM_TRY(check_stream(stream));
@@ -896,14 +919,7 @@ extern "C" int vfm_kv_append(const vfm_attn* attn, const vfm_batch* batch, const
 }
 
 extern "C" int vfm_attention_workspace(const vfm_attn* attn, const vfm_batch* batch, size_t* bytes) {
-  if (!bytes) return VFM_ERR_ARG;
-  VFM_TRY(check_attn(attn));
-  Plan pl;
-  VFM_TRY(check_batch(batch, &pl));
-  AttnPlan ap;
-  VFM_TRY(plan_attention(*attn, batch, pl, &ap));
-  *bytes = (size_t)ap.bytes;
-  return VFM_OK;
+  return workspace_attention(attn, batch, false, bytes);
 }
 
 extern "C" int vfm_attention_paged(const vfm_attn* attn, const vfm_batch* batch, const void* q, int64_t ldq,
@@ -966,7 +982,7 @@ extern "C" int vfm_kv_append_q8(const vfm_attn* attn, const vfm_batch* batch, co
 }
 
 extern "C" int vfm_attention_workspace_q8(const vfm_attn* attn, const vfm_batch* batch, size_t* bytes) {
-  return vfm_attention_workspace(attn, batch, bytes);
+  return workspace_attention(attn, batch, true, bytes);
 }
 
 extern "C" int vfm_attention_paged_q8(const vfm_attn* attn, const vfm_batch* batch, const void* q, int64_t ldq,
@@ -978,7 +994,7 @@ extern "C" int vfm_attention_paged_q8(const vfm_attn* attn, const vfm_batch* bat
 
 extern "C" int vfm_workspace_size_q8(const vfm_cfg* cfg, const vfm_batch* batch, const vfm_lora_table* lora,
                                      int32_t window, int32_t n_sink, size_t* bytes) {
-  return vfm_workspace_size_windowed(cfg, batch, lora, window, n_sink, bytes);
+  return workspace_windowed(cfg, batch, lora, window, n_sink, true, bytes);
 }
 
 extern "C" int vfm_layer_forward_q8(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_table* lora,

@@ -9,7 +9,9 @@
 
 // One attention over a paged cache, as the kernels take it.
 struct PagedAttn {
-  int H, KH, G;                // query heads, key heads, query heads per key head
+  int16_t H, KH;               // query heads, key heads (at most 1024)
+  int G;                       // query heads per key head
+  int few_min;                 // fewest tiles of a few-row request's chunk
   int window, n_sink;          // window 0: none
   float scale_log2;            // scale * log2(e)
   const void* q; int64_t ldq;
@@ -80,6 +82,11 @@ constexpr int FEW_QUERIES = 32;      // packed queries (rows x group) up to whic
 // after 1500 keys take 26.3 us with 8 and 32.3 with 16; 512 rows after none 21.2 with 8 and 30.6 with 4.
 constexpr int FEW_MIN_TILES = 12;
 constexpr int ROWS_MIN_TILES = 8;
+// bf16 over a cache in 8 bits, whose tiles are read in half the time: 256 rows under a window of 1024, 32 heads of 128 on 32,
+// take 321 us with 12 and 305 with 18 (uncut), 128 rows after 1000 keys, 64 heads of 64 on 8, 32 and 24; one row after 1500 takes
+// 14.2 and 15.9.
+constexpr int FEW_MIN_TILES8 = 18;
+inline int few_min_tiles(int dtype, bool kv8) { return kv8 && dtype == VFM_BF16 ? FEW_MIN_TILES8 : FEW_MIN_TILES; }
 
 // few-row kernel (bf16; fp32: every request): 16 packed queries per block
 __host__ __device__ inline bool few_rows(int dtype, int m, int G) { return dtype != VFM_BF16 || (int64_t)m * G <= FEW_QUERIES; }
@@ -88,12 +95,13 @@ __host__ __device__ inline int64_t few_qtiles(int m, int G) { return ((int64_t)m
 __host__ __device__ inline int rows_per_block(int G) { return 128 / G; }
 
 // chunks of the request with m rows after ctx cached tokens
-__host__ __device__ inline Chunks request_chunks(int dtype, int m, int ctx, int G, int KH, int window, int n_sink) {
+__host__ __device__ inline Chunks request_chunks(int dtype, int m, int ctx, int G, int KH, int window, int n_sink,
+                                                 int few_min = FEW_MIN_TILES) {
   if (few_rows(dtype, m, G)) {
     const int tiles = (visible_runs<4>(ctx, ctx + m - 1, window, n_sink).n + 1) / 2;
     const int64_t qt = few_qtiles(m, G);
     const int par = KH * (qt > 256 ? 256 : (int)qt);
-    return key_chunks(tiles, par > 256 ? 256 : par, FEW_MIN_TILES);
+    return key_chunks(tiles, par > 256 ? 256 : par, few_min);
   }
   const int rb = rows_per_block(G);
   const int64_t par = (int64_t)KH * ((m + rb - 1) / rb);

@@ -305,7 +305,7 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
   if (!few_rows(VFM_BF16, m, a.G)) return;              // block-uniform, as every exit below
   const int qn = m * a.G;
   if (!TABLE && w.qt * 16 >= qn) return;
-  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink);
+  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink, FEW_MIN_TILES8);
   if constexpr (TABLE) {
     w.h = id % a.KH; id /= a.KH;
     w.c = id % ck.n;
@@ -577,7 +577,7 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
   const int nb = (m + rb - 1) / rb;
   int bi = id - (R0 / rb + w.p);
   if (few_rows(VFM_BF16, m, a.G) || (!TABLE && bi >= nb)) return;   // block-uniform, as every exit below
-  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink);
+  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink, FEW_MIN_TILES8);
   if constexpr (TABLE) {
     w.h = id % a.KH; id /= a.KH;
     w.c = id % ck.n;
