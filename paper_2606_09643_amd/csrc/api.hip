@@ -973,6 +973,7 @@ extern "C" int vfm_kv_append_q8(const vfm_attn* attn, const vfm_batch* batch, co
   const vfm_kv_pages& pages = kv->pages;
   Plan pl;
   VFM_TRY(check_append(attn, batch, qkv, ld, q_out, &pages, stream, &pl));
+  if (pl.n_req > APPEND8_MAX_BLOCKS - (pl.T + 15) / 16) return VFM_ERR_UNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   const Pool8 pool{(uint8_t*)pages.k, (uint8_t*)pages.v, (uint8_t*)kv->exps, pages.n_pages * pages.page_size};
   VFM_TIMED(VFM_PROF_OTHER, launch_append8(attn->dtype, pl, attn->n_heads, attn->n_kv_heads, attn->head_dim,

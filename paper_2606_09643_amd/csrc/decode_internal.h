@@ -145,8 +145,7 @@ struct Pool8 {
   uint8_t* exps;               // [slots / 16][n_kv_heads][2]
   int64_t slots;
 };
-// From this many rows on a block of the append takes the runs of 16 rows (a prompt's whole run), below of one.
-constexpr int APPEND8_GROUPED = 2048;
+constexpr int APPEND8_MAX_BLOCKS = (1 << 24) - 1;   // of 256 threads; requests and 16th rows together are at most as many
 // q_out, ldq: as launch_kv_append
 hipError_t launch_append8(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv, int64_t ld,
                           void* q_out, int64_t ldq, const Pool8& pool, const KvPages& kp, hipStream_t s);

@@ -36,15 +36,23 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) 
 }
 
 // ---------------------------------------------------------------------------
-// Append.  A block takes the runs that begin in its group of rows (a run of new rows: those of one request in one aligned
-// 16 positions), all of their heads or, with gridDim.y, some; a wave takes a head of the whole run, so the run's largest
-// magnitude is found by lane exchanges and the codes are written from the registers that hold the rotated values.
-// A single row (decode) leaves most of such a wave idle: there it takes 64 / (DH / 16) heads at once.
+// Append.  A block takes a run of new rows (those of one request in one aligned 16 positions) and some of its heads: the
+// launch's first blocks each request's first run, the others the further runs that begin in 16 rows of the batch.  A wave
+// takes a head of the whole run, so the run's largest magnitude is found by lane exchanges and the codes are written from
+// the registers that hold the rotated values.  A single row (decode) leaves most of such a wave idle: there it takes
+// 64 / (DH / 16) heads at once; with head dim 128 up to 8 rows are half a run's work (200 requests of 2 to 4 rows: 27 us,
+// 38 as whole runs).
 //
 // Rotation in fp64, of operands that fp64 holds exactly: a code is one rounding of the rotated value, and scale and code
 // do not depend on how the angle's last bits came out.  The value goes through fp32 rounded to odd (cut, the last
 // bit set if anything was lost), after which rounding to 4 or 8 bits is as if from the fp64 value, and a comparison with a
 // number of few bits comes out the same.
+//
+// Bound by its bytes: 32 prompts of 128 to 1024 tokens, 32 heads of 128 on 32, take 161 us, 4.8 TB/s (a copy of 2 GiB runs
+// at 4.95).  The blocks that share a run's heads are neighbours in the launch, so its rows are read at once: 191 us with
+// them far apart.  4 heads a wave; 6 take 164, 12 190 (a long last round), and loading a head ahead 205 for 191 (3
+// waves on a SIMD in place of 4).  One row: 4.4 us, all latency.  A block per row, most of which find no run, took 42 us for 40
+// requests of 40 to 60 rows, 20 now, and a block for all runs of 16 rows 100 for 3000 single rows, 31 now.
 // ---------------------------------------------------------------------------
 constexpr float TOP8 = 3.19014718988379809e38f;          // 1.875 2^127: larger magnitudes would round to 2^128
 
@@ -71,20 +79,21 @@ template <> struct Half8<float> {
 };
 
 struct Append8 {
-  int H, KH, rotate, group, split;   // rows whose runs a block takes, blocks that share them
+  int H, KH, rotate, split;          // blocks that share the heads of a run
   double log2_theta;
   int64_t ld, ldq, slots;
   uint8_t *k, *v, *exps;
   KvPages kp;
 };
 
-// How a wave holds rows of a run's head(s), a lane pairs (i, i + DH/2) of 8 of the dims: one head of up to 16 rows, or with
-// ONE a single row of 64 / PER heads.
-template <typename T, int DH, bool ONE>
+// How a wave holds rows of a run's head(s), a lane pairs (i, i + DH/2) of 8 of the dims: one head of up to ROWS rows, or
+// with ROWS = 1 a single row of 64 / PER heads.
+template <typename T, int DH, int ROWS>
 struct Held {
   static constexpr int HALF = DH / 2, PER = HALF / 8;     // lanes of a row
+  static constexpr bool ONE = ROWS == 1;
   static constexpr int RPP = ONE ? 1 : 64 / PER;          // rows at a time
-  static constexpr int NI = ONE ? 1 : 16 / RPP;
+  static constexpr int NI = ONE ? 1 : ROWS / RPP;
   Half8<T> x[NI], y[NI];
   __device__ __forceinline__ static int head_of(int unit) {
     return ONE ? unit * (64 / PER) + (int)(threadIdx.x & 63) / PER : unit;
@@ -103,10 +112,12 @@ struct Held {
 };
 
 // The run's nr rows from row r0 at position pos0, slot slot0.
-template <typename T, int DH, bool ONE>
-__device__ __forceinline__ void append_heads(const Append8& a, Held<T, DH, ONE>& in, T* q_out, int unit,
+template <typename T, int DH, int ROWS>
+__device__ __forceinline__ void append_heads(const Append8& a, Held<T, DH, ROWS>& in, T* q_out, int unit,
                                              int r0, int nr, int pos0, int64_t slot0, const double2* cs) {
-  constexpr int HALF = DH / 2, PER = HALF / 8, RPP = Held<T, DH, ONE>::RPP, NI = Held<T, DH, ONE>::NI;
+  using In = Held<T, DH, ROWS>;
+  constexpr int HALF = In::HALF, PER = In::PER, RPP = In::RPP, NI = In::NI;
+  constexpr bool ONE = In::ONE;
   Half8<T>(&x)[NI] = in.x;
   Half8<T>(&y)[NI] = in.y;
   const int lane = threadIdx.x & 63, ch = lane % PER, row0 = in.row0(), head = in.head_of(unit);
@@ -213,25 +224,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
   // cosine and sine of row r, pair 8 ch + j at (r * 8 + j) * PER + ch + r * PER: lanes of a row read neighbours, rows
   // differ in banks
   __shared__ double2 cs[16 * 9 * PER];
-  const int split = a.split, share = (int)blockIdx.x % split, first = (int)blockIdx.x / split * a.group;
-  const int end = min(first + a.group, pl.T);
+  const int split = a.split, share = (int)blockIdx.x % split, i = (int)blockIdx.x / split;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // revolutions per position of the pair whose angles this thread takes
   const int pair = threadIdx.x % HALF;
   const double inv = a.rotate ? exp2(-(2.0 * (double)pair / (double)DH) * a.log2_theta) * 0.15915494309189535 : 0.0;
   const int n_heads = a.H + 2 * a.KH, step = 4 * split, unit0 = share * 4 + wave;
-  auto heads = [&](auto one, int units, int r0, int nr, int pos0, int64_t slot0) {
+  auto heads = [&](auto most, int units, int r0, int nr, int pos0, int64_t slot0) {
     for (int unit = unit0; unit < units; unit += step) {
-      Held<T, DH, decltype(one)::value> rows;
+      Held<T, DH, decltype(most)::value> rows;
       rows.load(qkv, a.ld, n_heads, unit, r0, nr);
-      append_heads<T, DH, decltype(one)::value>(a, rows, q_out, unit, r0, nr, pos0, slot0, cs);
+      append_heads(a, rows, q_out, unit, r0, nr, pos0, slot0, cs);
     }
   };
+  const int first = i < pl.n_req ? uniform(pl.cu_seqlens[i]) : (i - pl.n_req) * 16;
+  const int end = i < pl.n_req ? first + 1 : min(first + 16, pl.T);
   for (int r0 = first, next; r0 < end; r0 = next) {
-    const int pos0 = uniform(pl.pos[r0]), p = uniform(pl.row_req[r0]);
+    const int pos0 = uniform(pl.pos[r0]), p = i < pl.n_req ? i : uniform(pl.row_req[r0]);
     const int begin = uniform(pl.cu_seqlens[p]), past = uniform(pl.cu_seqlens[p + 1]);
     next = min(past, r0 + 16 - (pos0 & 15));
-    if (r0 != begin && (pos0 & 15)) continue;             // inside a run
+    if (i >= pl.n_req && (r0 == begin || (pos0 & 15))) continue;   // a request's first run, or inside one
     const int nr = next - r0;
     const int64_t slot0 = page_slot(row_of(a.kp, uniform(pl.order[p])), a.kp.log2_page, pos0);
     if (a.rotate) {
@@ -244,8 +256,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
       }
       __syncthreads();
     }
-    if (nr == 1) heads(std::true_type{}, (n_heads + 64 / PER - 1) / (64 / PER), r0, nr, pos0, slot0);
-    else heads(std::false_type{}, n_heads, r0, nr, pos0, slot0);
+    if (nr == 1) heads(std::integral_constant<int, 1>{}, (n_heads + 64 / PER - 1) / (64 / PER), r0, nr, pos0, slot0);
+    else if (64 / PER < 16 && nr <= 64 / PER) heads(std::integral_constant<int, 64 / PER>{}, n_heads, r0, nr, pos0, slot0);
+    else heads(std::integral_constant<int, 16>{}, n_heads, r0, nr, pos0, slot0);
   }
 }
 
@@ -256,6 +269,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
 // the MFMA, V on the way to a wave-private LDS tile that the transposing LDS read turns into the V^T operand.
 // A lane's 16-byte load of a K row holds 16 consecutive head dims, two MFMA steps of 8; the queries' fragments take the
 // same dims, as a dot product does not mind their order.
+// Memory bound: 256 requests with up to 1028 visible keys, 32 heads of 128 on 32: 305 us, 6.2 TB/s (at most 6.5 here); 8
+// requests of 32768 to 131072, 32 heads on 8: 205 us, 6.2 TB/s.  One row after 300 keys: 8 us, the latency of a few
+// dependent loads.
+// NB tiles' registers: with few blocks, or long ones, the loads of two tiles are in flight while one is computed (head dim
+// 128: 212 registers, two blocks on a CU; 64: one tile ahead and three).  Otherwise one tile at a time, and four blocks on a CU
+// (64: five) hide each other's loads and starts.  With head dim 128, one tile and three: 256 rows of 30 to 60 keys 39 us and
+// 64, of 256 to 2048 440 and 519, 8 of 32768 to 131072 216 and 205, one of 30000 21.2 and 19.4; with head dim 64, one and
+// two: 256 of 30 to 60 15.4 and 16.9, 256 of 200 to 2000 110 and 114, 16 of 130 to 400 8.3 and 7.6.
 // ---------------------------------------------------------------------------
 // The exponent bytes of K (low) and V (high) of two runs, even lanes the first's and odd lanes the second's.  (A load from
 // the same address in every lane would be made a scalar at once, and waited for before anything after it is issued.)
@@ -538,6 +559,11 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
 // where the request has few blocks), waves of 32 queries, 64-key tiles in two LDS stages by turns, as in the bf16 cache's
 // many-row kernel (k_paged.hip).  Codes go through registers: a thread loads 16 of a K and of a V row ahead and stores
 // them as bf16 a step later, so each is converted once per block.
+// 4 chunks of 1900 to 2048 rows after 3000 to 9000, window 4096, 32 heads of 128 on 8: 550 to 565 us by machine, 940 to 960
+// TFLOP/s of visible products, as over a bf16 cache (a large matrix product: 1370): the matrix cores are busy for 39% of the
+// cycles, the vector ALU for 39, LDS for 30.  Blocks of 8 waves, which halve the conversions per query, give 1%; V's
+// conversion beside the products in place of the scores loses 2.  The matrix cores' own 8-bit products (a query as the
+// sum of two codes) would need no conversion of K, but their sums hold 16 bits (1.6e-5 of random rows' products of 64).
 // ---------------------------------------------------------------------------
 template <int DH, bool TABLE>
 __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, const uint8_t* __restrict__ exps, int id, bf16* stage0, bf16* stage1) {
@@ -858,7 +884,7 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
       }
       bf16x8 pf[4];
       __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_setprio(1);
+      __builtin_amdgcn_s_setprio(1);                       // before the other wave of the SIMD: 1%
       // Scores of t + 1 (2 KS MFMAs) beside the first half of t's weights, the conversion of what was loaded and the next
       // loads; a fragment is read four ahead of its MFMA.
       store(j, true);
@@ -1141,15 +1167,17 @@ hipError_t launch_append8(int dtype, const Plan& pl, int H, int KH, int head_dim
   Append8 a = {};
   a.H = H; a.KH = KH; a.rotate = theta > 0.f; a.log2_theta = theta > 0.f ? log2((double)theta) : 0.0;
   a.ld = ld; a.ldq = ldq; a.slots = pool.slots; a.k = pool.k; a.v = pool.v; a.exps = pool.exps; a.kp = kp;
-  a.group = pl.T >= APPEND8_GROUPED ? 16 : 1;
-  const int blocks = (pl.T + a.group - 1) / a.group;
-  const int units = a.group > 1 ? H + 2 * KH : (H + 2 * KH + 1024 / head_dim - 1) / (1024 / head_dim);
-  // A wave takes 6 heads of a run, so that the blocks come to several rounds over the chip and the last one is short; where
-  // blocks are few, less.  (Each split takes the run's angles anew.)
+  // single rows: a wave has 64 / (head_dim / 16) heads at a time, otherwise one
+  const int n_heads = H + 2 * KH, units = pl.max_seqlen > 1 ? n_heads : (n_heads + 1024 / head_dim - 1) / (1024 / head_dim);
+  const int blocks = pl.n_req + (pl.max_seqlen > 1 ? (pl.T + 15) / 16 : 0);
+  // A wave takes 4 heads of a run, so that the blocks come to several rounds over the chip and the last one is short; where
+  // blocks are few, less: up to 1024 blocks are resident.  (Each share takes the run's angles anew.)
   const int most = (units + 3) / 4;
   int split = (units + 15) / 16;
-  if ((int64_t)blocks * split < 512) split = (512 + blocks - 1) / blocks;
-  a.split = split < 1 ? 1 : split > most ? most : split;
+  if ((int64_t)blocks * split < 1024) split = (1024 + blocks - 1) / blocks;
+  if (split > most) split = most;
+  if (split > APPEND8_MAX_BLOCKS / blocks) split = APPEND8_MAX_BLOCKS / blocks;
+  a.split = split;
 #define APPEND(T_, D_)                                                                                             \
   hipLaunchKernelGGL((append8_kernel<T_, D_>), dim3((unsigned)(blocks * a.split)), dim3(256), 0, s, pl, a, (const T_*)qkv, (T_*)q_out)
   if (dtype == VFM_BF16) { if (head_dim == 64) APPEND(bf16, 64); else APPEND(bf16, 128); }

@@ -193,7 +193,7 @@ def test_append(dtype, H, KH, dh, page, theta):
 
 @pytest.mark.parametrize("dtype,H,KH,dh", [("bf16", 3, 1, 128), ("f32", 2, 2, 64)])
 def test_append_of_a_step_with_many_rows(dtype, H, KH, dh):
-    """More rows than blocks of one run are taken for: prompts, a chunk, single rows, runs cut at either end."""
+    """Prompts, a chunk, single rows, runs cut at either end."""
     rng = np.random.default_rng(8)
     td, u = DT[dtype][1:]
     lens, ctx = [1500, 1, 777, 16, 15, 1, 33, 2], [0, 5, 100, 16, 1, 64, 47, 15]
@@ -202,6 +202,23 @@ def test_append_of_a_step_with_many_rows(dtype, H, KH, dh):
     T = sum(lens)
     x = torch.from_numpy(rng.standard_normal((T, H + 2 * KH, dh), dtype=np.float32)).to(td)
     q = _step(pool, task, lens, ctx, H, KH, dh, dtype, 10000.0, x, wide=0)
+    _follow(pool, task, lens, ctx, H, KH, 10000.0, x, q, u)
+    pool.check()
+
+
+@pytest.mark.parametrize("dtype,H,KH,dh", [("bf16", 2, 1, 128), ("bf16", 3, 3, 64), ("f32", 1, 1, 128)])
+@pytest.mark.parametrize("most", [2, 5, 20])
+def test_append_of_a_step_with_many_short_requests(dtype, H, KH, dh, most):
+    """Requests of a few rows each around the ends of runs: several runs begin in 16 rows of the batch."""
+    rng = np.random.default_rng(most)
+    td, u = DT[dtype][1:]
+    lens = [int(n) for n in rng.integers(1, most + 1, 70)]
+    ctx = [16 * int(c) + int(r) for c, r in zip(rng.integers(0, 30, 70), rng.integers(12, 18, 70))]
+    pool = Pool8(ctx, [a + b + 16 for a, b in zip(lens, ctx)], KH, dh, 16, most)
+    T = sum(lens)
+    x = torch.from_numpy(rng.standard_normal((T, H + 2 * KH, dh), dtype=np.float32)).to(td)
+    task = rng.integers(0, 5, 70).astype(np.int32)
+    q = _step(pool, task, lens, ctx, H, KH, dh, dtype, 10000.0, x)
     _follow(pool, task, lens, ctx, H, KH, 10000.0, x, q, u)
     pool.check()
 
