@@ -278,6 +278,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
 // 64, of 256 to 2048 440 and 519, 8 of 32768 to 131072 216 and 205, one of 30000 21.2 and 19.4; with head dim 64, one and
 // two: 256 of 30 to 60 15.4 and 16.9, 256 of 200 to 2000 110 and 114, 16 of 130 to 400 8.3 and 7.6.
 // ---------------------------------------------------------------------------
+// The last request whose blocks begin at id or before it (the first one's at 0), by whole waves: 64 places are looked at
+// at once, as each step of a search waits for its load.  5 prompts of 40 to 250 rows and 19 single ones after 64 to
+// 2000 keys, 16 heads of 64: 40.8 us, by halves 42.4.
+template <typename F>
+__device__ __forceinline__ int last_request(int n_req, int id, F begin) {
+  int lo = 0;
+  for (int n = n_req; n > 1;) {
+    const int step = (n + 63) >> 6, at = (int)(threadIdx.x & 63) * step;
+    const int k = __popcll(__ballot(at < n && begin(lo + min(at, n - 1)) <= id)) - 1;
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  return lo;
+}
+
 // The exponent bytes of K (low) and V (high) of two runs, even lanes the first's and odd lanes the second's.  (A load from
 // the same address in every lane would be made a scalar at once, and waited for before anything after it is issued.)
 __device__ __forceinline__ uint32_t runs_exps(const uint8_t* exps, int64_t slot0, int64_t slot1, int KH, int h) {
@@ -314,7 +329,9 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
 
   Work w;
   if constexpr (TABLE) {
-    w.p = request_at(table_of(pl, a, TAB_FEW), pl.n_req, id);
+    const table_t parts = table_of(pl, a, TAB_FEW);
+    w.p = last_request(pl.n_req, id, [&](int p) { return parts[p]; });
+    id -= parts[w.p];
   } else {
     w.h = id % a.KH; id /= a.KH;
     w.c = id % a.few_chunks; id /= a.few_chunks;
@@ -585,17 +602,14 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
   const int rb = rows_per_block(a.G);
   Work w;
   if constexpr (TABLE) {
-    w.p = request_at(table_of(pl, a, TAB_ROWS), pl.n_req, id);
+    const table_t parts = table_of(pl, a, TAB_ROWS);
+    w.p = last_request(pl.n_req, id, [&](int p) { return parts[p]; });
+    id -= parts[w.p];
   } else {
     w.h = id % a.KH; id /= a.KH;
     w.c = id % a.rows_chunks; id /= a.rows_chunks;
     // request p's blocks start at cu[p] / rb + p: at least ceil(m / rb) before the next request's
-    int lo = 0, hi = pl.n_req - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (uniform(pl.cu_seqlens[mid]) / rb + mid <= id) lo = mid; else hi = mid - 1;
-    }
-    w.p = lo;
+    w.p = last_request(pl.n_req, id, [&](int p) { return pl.cu_seqlens[p] / rb + p; });
   }
   const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
   const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide
@@ -987,18 +1001,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
   Work w;
   int id = blockIdx.x;
   if constexpr (TABLE) {
-    w.p = request_at(table_of(pl, a, TAB_FEW), pl.n_req, id);
+    const table_t parts = table_of(pl, a, TAB_FEW);
+    w.p = last_request(pl.n_req, id, [&](int p) { return parts[p]; });
+    id -= parts[w.p];
   } else {
     w.h = id % a.KH; id /= a.KH;
     w.c = id % a.few_chunks; id /= a.few_chunks;
     // request p's query tiles start at cu[p] G / 16 + p
-    int lo = 0, hi = pl.n_req - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if ((int64_t)uniform(pl.cu_seqlens[mid]) * a.G / 16 + mid <= id) lo = mid; else hi = mid - 1;
-    }
-    w.p = lo;
-    w.qt = id - (int)((int64_t)uniform(pl.cu_seqlens[lo]) * a.G / 16 + lo);
+    auto begin = [&](int p) { return (int)((int64_t)pl.cu_seqlens[p] * a.G / 16 + p); };
+    w.p = last_request(pl.n_req, id, begin);
+    w.qt = id - uniform(begin(w.p));
   }
   const int R0 = uniform(pl.cu_seqlens[w.p]), m = uniform(pl.cu_seqlens[w.p + 1]) - R0, ctx = uniform(pl.ctx[w.p]);
   const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide

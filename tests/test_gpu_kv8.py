@@ -404,6 +404,24 @@ def test_attention_rows_alone_and_among_many(dh, lo, hi):
         assert np.array_equal(_attend(c, task, 16, 16, dh, 0, 0, "bf16", q, only=[i], ws_fill=0)[i], got[i])
 
 
+@pytest.mark.parametrize("dtype,n,long", [("bf16", 65, 0), ("bf16", 200, 0), ("f32", 130, 0), ("bf16", 130, 30000), ("f32", 70, 30000)])
+def test_attention_of_many_requests(dtype, n, long):
+    """More requests than are looked at in one step of the search for a block's, prompts and single rows by turns; with one
+    long context among them blocks are found in the table."""
+    rng = np.random.default_rng(n)
+    lens, ctx = rng.choice([1, 1, 2, 33, 70], n).tolist(), rng.integers(0, 40, n).tolist()
+    if long:
+        ctx[n // 2], lens[n // 2] = long, 1
+    H, KH, dh = (4, 4, 64) if dtype == "bf16" else (2, 2, 64)
+    c = Cache8(lens, ctx, KH, dh, 16, 0, 0, seed=n)
+    q = _queries(lens, H, dh, dtype, 5)
+    task = _tasks(n, 7)
+    got = _attend(c, task, H, KH, dh, 0, 0, dtype, q)
+    _check(c, got, q, 0, 0, dtype, dh ** -0.5)
+    for i in (0, n // 2, n - 1):
+        assert np.array_equal(_attend(c, task, H, KH, dh, 0, 0, dtype, q, only=[i], ws_fill=0)[i], got[i])
+
+
 def test_attention_large_logits_and_scale():
     """Scores of hundreds (one key takes the whole weight) and a given scale."""
     for dtype in ("bf16", "f32"):
