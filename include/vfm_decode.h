@@ -139,7 +139,7 @@ typedef struct vfm_adjust {
   const int32_t* mask_row;
 } vfm_adjust;
 
-/* adjusted: device float32, as out (vfm_head_forward's layout), or out itself:
+/* adjusted: device float32, as out (vfm_head_forward's layout) and apart from it, or out itself:
  * then only the outputs that change are written.  For output j = l of request
  * i, in 64 bits with one rounding at the end:
  *   l > 0 ? l / r : l * r   if j is among the earlier tokens;
@@ -152,7 +152,7 @@ typedef struct vfm_adjust {
  * Errors: VFM_ERR_ARG for null pointers, out or adjusted not 16-byte aligned,
  * a list without its other arrays; VFM_ERR_SHAPE for negative sizes, a mask
  * without words; VFM_ERR_UNSUPPORTED for a batch of more blocks than a launch
- * holds (2^23 requests, or the longest row's outputs times requests 2^35). */
+ * holds (2^23 requests, or the longest row's outputs times requests 2^36). */
 int vfm_adjust_outputs(const vfm_batch* batch, const float* out, const vfm_adjust* adjust,
                        float* adjusted, void* stream);
 
