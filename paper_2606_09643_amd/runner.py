@@ -444,21 +444,32 @@ class ContinuousBatcher:
         sp = B.Sampling(dev[0], dev[1].view(torch.int32), dev[2], dev[3])
         B.vfm_sample_tokens(pb.c, out, sp, dev[4], nxt)
 
-    def _place_history(self, s):
-        """Room on the device for the tokens of s, its prompt written there (in stream order)."""
-        need = len(s.prompt) + s.max_new
+    def _take_history(self, need):
+        """Where a part of the device's tokens that holds `need` begins: the shortest free one, or the buffer doubles."""
         fit = min((f for f in self._hist_free if f[0] >= need), default=None)
         if fit is None:
             begin = self._hist.numel()
-            fit = (max(need, begin), begin)                # the buffer doubles
-            grown = torch.empty(begin + fit[0], dtype=torch.int32, device=self.device)
+            size = max(need, begin)
+            grown = torch.empty(begin + size, dtype=torch.int32, device=self.device)
             grown[:begin] = self._hist
             self._hist = grown
-        else:
-            self._hist_free.remove(fit)
-        s.hist = fit[1]
+            self._give_history(begin, size)
+            fit = max(self._hist_free)
+        self._hist_free.remove(fit)
         if fit[0] > need:
             self._hist_free.append((fit[0] - need, fit[1] + need))
+        return fit[1]
+
+    def _give_history(self, begin, n):
+        """A part is free again, one with the free parts that it touches."""
+        for f in [f for f in self._hist_free if f[1] + f[0] == begin or begin + n == f[1]]:
+            self._hist_free.remove(f)
+            begin, n = min(begin, f[1]), n + f[0]
+        self._hist_free.append((n, begin))
+
+    def _place_history(self, s):
+        """Room on the device for the tokens of s, its prompt written there (in stream order)."""
+        s.hist = self._take_history(len(s.prompt) + s.max_new)
         self._hist[s.hist:s.hist + len(s.prompt)] = self._h2d(s.prompt)
 
     def _read_answers(self, dec):
@@ -626,7 +637,7 @@ class ContinuousBatcher:
             if len(s.generated) == s.max_new:
                 self.alloc.release(s.slot)
                 if s.hist >= 0:
-                    self._hist_free.append((len(s.prompt) + s.max_new, s.hist))
+                    self._give_history(s.hist, len(s.prompt) + s.max_new)
                 self.free_slots.append(s.slot)
                 self.committed -= s.budget
                 self.running.remove(s)

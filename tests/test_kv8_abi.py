@@ -279,3 +279,24 @@ def test_histories_have_their_own_room():
         for x in live:
             assert np.array_equal(cb._hist[x.hist:x.hist + len(x.prompt)].numpy(), x.prompt)
     assert cb._hist.numel() <= 16 * total
+
+
+def test_loop_device_tokens_of_finished_sequences_are_used_again():
+    """Parts do not overlap while they are taken, free neighbours become one, and the buffer stays bounded."""
+    from paper_2606_09643_amd import runner as R
+    cb = R.ContinuousBatcher(_Model(), emb=None, page_size=16, n_pages=12, max_seqs=3, max_step_tokens=64, max_pages=6,
+                             device="cpu")
+    rng, live = np.random.default_rng(0), []
+    for i in range(4000):
+        if len(live) == 8 or (live and rng.random() < 0.4):
+            cb._give_history(*live.pop(int(rng.integers(len(live)))))
+        else:
+            n = int(rng.integers(1, 200))
+            live.append((cb._take_history(n), n))
+        parts = sorted([(b, n) for b, n in live] + [(b, n) for n, b in cb._hist_free])
+        assert parts[0][0] == 0 and all(a + n == b for (a, n), (b, _) in zip(parts, parts[1:]))
+        assert sum(parts[-1]) == cb._hist.numel()
+    assert cb._hist.numel() <= 4 * 8 * 200
+    for part in live:
+        cb._give_history(*part)
+    assert cb._hist_free == [(cb._hist.numel(), 0)]
