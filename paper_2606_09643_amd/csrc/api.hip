@@ -845,6 +845,11 @@ extern "C" int vfm_workspace_size_windowed(const vfm_cfg* cfg, const vfm_batch* 
 
 namespace {
 
+// A launch holds the append's blocks.
+int check_append8(const Plan& pl) {
+  return pl.n_req > APPEND8_MAX_BLOCKS - ((int64_t)pl.T + 15) / 16 ? VFM_ERR_UNSUPPORTED : VFM_OK;
+}
+
 // A layer over a paged cache, in 8 bits where exps is given.
 int layer_windowed(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lora_table* lora, const vfm_batch* batch,
                    float* x, const vfm_kv_pages* kv, uint8_t* exps, int32_t window, int32_t n_sink, void* workspace,
@@ -857,6 +862,7 @@ int layer_windowed(const vfm_cfg* cfg, const vfm_layer_weights* w, const vfm_lor
   VFM_TRY(check_attn(&a));
   if ((int64_t)pl.T * APPEND_THREADS > kMaxThreads) return VFM_ERR_UNSUPPORTED;
   VFM_TRY(check_pages(a, batch, pl, kv, true));
+  if (exps) VFM_TRY(check_append8(pl));
   VFM_TRY(check_stream(stream));
   return layer_impl(*cfg, w, lora, batch, pl, x, kv->k, kv->v, kv->n_pages * kv->page_size, pages_of(kv), workspace,
                     ws_bytes, stream, &a, exps);
@@ -973,7 +979,7 @@ extern "C" int vfm_kv_append_q8(const vfm_attn* attn, const vfm_batch* batch, co
   const vfm_kv_pages& pages = kv->pages;
   Plan pl;
   VFM_TRY(check_append(attn, batch, qkv, ld, q_out, &pages, stream, &pl));
-  if (pl.n_req > APPEND8_MAX_BLOCKS - (pl.T + 15) / 16) return VFM_ERR_UNSUPPORTED;
+  VFM_TRY(check_append8(pl));
   hipStream_t s = (hipStream_t)stream;
   const Pool8 pool{(uint8_t*)pages.k, (uint8_t*)pages.v, (uint8_t*)kv->exps, pages.n_pages * pages.page_size};
   VFM_TIMED(VFM_PROF_OTHER, launch_append8(attn->dtype, pl, attn->n_heads, attn->n_kv_heads, attn->head_dim,
