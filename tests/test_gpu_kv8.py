@@ -223,6 +223,28 @@ def test_append_of_a_step_with_many_short_requests(dtype, H, KH, dh, most):
     pool.check()
 
 
+def test_append_of_two_requests_to_one_run():
+    """Either's scale and codes of either are there, and nothing beside them is touched."""
+    H, KH, dh = 2, 2, 64
+    rng = np.random.default_rng(3)
+    lens, x = [5, 3], torch.from_numpy(rng.standard_normal((8, H + 2 * KH, dh)) * np.repeat([1.0, 100.0], [5, 3])[:, None, None]).to(torch.bfloat16)
+    pools = [Pool8([0, 0], [32, 32], KH, dh, 32, 4) for _ in range(3)]
+    both = pools[2]
+    table = both.table.copy()
+    table[1] = table[0]
+    both.kv = B.PagedKVQ8(both.kp, both.vp, both.ep, both.page, table)
+    _step(both, np.zeros(2, np.int32), lens, [0, 0], H, KH, dh, "bf16", 0.0, x)
+    for i, pool in enumerate(pools[:2]):                  # each alone on those pages
+        rows = np64(x)[:5] if i == 0 else np64(x)[5:]
+        _, k, v = K.rotated(rows, H, KH, np.arange(lens[i]), 0.0)
+        pool.append(0, 0, k, v)
+    for got, c in ((both.kp, 0), (both.vp, 1)):
+        got = got.cpu().numpy()
+        assert np.all((got == pools[0].codes[c]) | (got == pools[1].codes[c]))
+    got = both.ep.cpu().numpy()
+    assert np.all((got == pools[0].exps) | (got == pools[1].exps))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("theta", [0.0, 10000.0])
 def test_append_special_values(dtype, theta):
