@@ -269,6 +269,7 @@ constexpr int64_t TABLE_MIN_BYTES = 16 << 20;
 struct AttnPlan {
   int few_chunks, rows_chunks, qtiles;
   bool one;                  // no few-row request has more than 4 tiles of keys
+  bool single, other;        // requests of a single row (single_row), and others
   bool table;                // blocks and records where each request's own begin, not in rectangles
   int64_t few_blocks, rows_blocks, recs, joins;
   int64_t bytes;             // workspace
@@ -280,7 +281,6 @@ struct AttnPlan {
 
 // kv8: over a cache in 8 bits
 int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, bool kv8, AttnPlan* out) {
-  const int few_min = few_min_tiles(a.dtype, kv8);
   AttnPlan ap = {};
   ap.few_chunks = ap.rows_chunks = ap.qtiles = 1;
   ap.one = true;
@@ -291,10 +291,11 @@ int plan_attention(const vfm_attn& a, const vfm_batch* batch, const Plan& pl, bo
   for (int p = 0; p < pl.n_req; ++p) {
     const int m = cu[p + 1] - cu[p];
     if (ctx[p] < 0 || (int64_t)ctx[p] + m > kMaxPos) return VFM_ERR_SHAPE;
-    const Chunks ck = request_chunks(a.dtype, m, ctx[p], G, a.n_kv_heads, a.window, a.n_sink, few_min);
+    const Chunks ck = request_chunks(a.dtype, m, ctx[p], G, a.n_kv_heads, a.window, a.n_sink, kv8);
     const int n = ck.n;
     const AttnCounts c = request_counts(a.dtype, m, a.n_heads, a.n_kv_heads, n);
     for (int i = 0; i < 4; ++i) own[i] += c.v[i];
+    (single_row(m, G, visible_runs<4>(ctx[p], ctx[p] + m - 1, a.window, a.n_sink).n) ? ap.single : ap.other) = true;
     if (few_rows(a.dtype, m, G)) {
       ap.one = ap.one && n * ck.tiles <= 4;
       ap.few_own += c.v[TAB_FEW];
@@ -338,7 +339,7 @@ hipError_t run_attention(const vfm_attn& a, const Plan& pl, const AttnPlan& ap, 
                          char* ws, hipStream_t s) {
   PagedAttn p = {};
   p.H = (int16_t)a.n_heads; p.KH = (int16_t)a.n_kv_heads; p.G = a.n_heads / a.n_kv_heads;
-  p.few_min = few_min_tiles(a.dtype, exps != nullptr);
+  p.kv8 = exps != nullptr;
   p.window = a.window; p.n_sink = a.window > 0 ? a.n_sink : 0;
   p.scale_log2 = (a.scale > 0.f ? a.scale : 1.f / sqrtf((float)a.head_dim)) * 1.4426950408889634f;
   p.q = q; p.ldq = ldq; p.k = k; p.v = v; p.slots = slots; p.kp = kp; p.out = out; p.ldo = ldo;
@@ -352,7 +353,7 @@ hipError_t run_attention(const vfm_attn& a, const Plan& pl, const AttnPlan& ap, 
     p.rec_ml = (float2*)((char*)p.rec_o + align_up((size_t)ap.recs * a.head_dim * 4));
   }
   if (exps != nullptr)
-    return launch_attention8(a.dtype, a.head_dim, pl, p, exps, ap.few_blocks, ap.rows_blocks, ap.joins, ap.deep(), ap.table, s);
+    return launch_attention8(a.dtype, a.head_dim, pl, p, exps, ap.few_blocks, ap.rows_blocks, ap.joins, ap.deep(), ap.single, ap.other, ap.table, s);
   return launch_attention_paged(a.dtype, a.head_dim, pl, p, ap.few_blocks, ap.rows_blocks, ap.joins, ap.one,
                                 ap.table, s);
 }

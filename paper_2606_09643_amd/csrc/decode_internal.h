@@ -11,7 +11,7 @@
 struct PagedAttn {
   int16_t H, KH;               // query heads, key heads (at most 1024)
   int G;                       // query heads per key head
-  int few_min;                 // fewest tiles of a few-row request's chunk
+  int kv8;                     // the cache is held in 8 bits
   int window, n_sink;          // window 0: none
   float scale_log2;            // scale * log2(e)
   const void* q; int64_t ldq;
@@ -86,21 +86,28 @@ constexpr int ROWS_MIN_TILES = 8;
 // take 321 us with 12 and 305 with 18 (uncut), 128 rows after 1000 keys, 64 heads of 64 on 8, 32 and 24; one row after 1500 takes
 // 14.2 and 15.9.
 constexpr int FEW_MIN_TILES8 = 18;
-inline int few_min_tiles(int dtype, bool kv8) { return kv8 && dtype == VFM_BF16 ? FEW_MIN_TILES8 : FEW_MIN_TILES; }
+// fp32 over 8 bits where single_row holds: 64 rows after 2000 keys, 16 heads of 64, take 78 us with 12, 61 with 24 and 54 with 32
+// (uncut), one after 3000, 16 heads on 4, 11.6, 15.3 and 18.7.
+constexpr int SINGLE_MIN_TILES8 = 24;
 
 // few-row kernel (bf16; fp32: every request): 16 packed queries per block
 __host__ __device__ inline bool few_rows(int dtype, int m, int G) { return dtype != VFM_BF16 || (int64_t)m * G <= FEW_QUERIES; }
+// fp32 over a cache in 8 bits: one row of at most 4 queries on a key head, which sees more than 8 runs of 16 keys (256 rows of
+// 30 to 60, 8 heads of 64: 20.2 us with the single rows' kernel, 16.2 without; 4 of 176 to 322, 4 heads of 128: 11.5 and 12.1)
+__host__ __device__ inline bool single_row(int m, int G, int runs) { return m == 1 && G <= 4 && runs > 8; }
 __host__ __device__ inline int64_t few_qtiles(int m, int G) { return ((int64_t)m * G + 15) / 16; }
 // many-row kernel (bf16): blocks of 128 packed queries, 32 a wave
 __host__ __device__ inline int rows_per_block(int G) { return 128 / G; }
 
 // chunks of the request with m rows after ctx cached tokens
 __host__ __device__ inline Chunks request_chunks(int dtype, int m, int ctx, int G, int KH, int window, int n_sink,
-                                                 int few_min = FEW_MIN_TILES) {
+                                                 bool kv8 = false) {
   if (few_rows(dtype, m, G)) {
-    const int tiles = (visible_runs<4>(ctx, ctx + m - 1, window, n_sink).n + 1) / 2;
+    const int runs = visible_runs<4>(ctx, ctx + m - 1, window, n_sink).n, tiles = (runs + 1) / 2;
     const int64_t qt = few_qtiles(m, G);
     const int par = KH * (qt > 256 ? 256 : (int)qt);
+    const int few_min = !kv8 ? FEW_MIN_TILES : dtype == VFM_BF16 ? FEW_MIN_TILES8
+                        : single_row(m, G, runs) ? SINGLE_MIN_TILES8 : FEW_MIN_TILES;
     return key_chunks(tiles, par > 256 ? 256 : par, few_min);
   }
   const int rb = rows_per_block(G);
@@ -149,10 +156,11 @@ constexpr int APPEND8_MAX_BLOCKS = (1 << 24) - 1;   // of 256 threads; requests 
 // q_out, ldq: as launch_kv_append
 hipError_t launch_append8(int dtype, const Plan& pl, int H, int KH, int head_dim, float theta, const void* qkv, int64_t ld,
                           void* q_out, int64_t ldq, const Pool8& pool, const KvPages& kp, hipStream_t s);
-// a.k, a.v: the pools' codes; deep: few blocks, or long ones (AttnPlan::deep); the other arguments as
+// a.k, a.v: the pools' codes; deep: few blocks, or long ones (AttnPlan::deep); single, other: fp32 requests of a single row
+// (single_row) and others; the other arguments as
 // launch_attention_paged's
 hipError_t launch_attention8(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, const uint8_t* exps, int64_t few_blocks,
-                             int64_t rows_blocks, int64_t joins, bool deep, bool table, hipStream_t s);
+                             int64_t rows_blocks, int64_t joins, bool deep, bool single, bool other, bool table, hipStream_t s);
 
 // max_out: the batch's longest row of head outputs; a block of that many threads per request
 inline int sample_threads(int max_out) { return max_out <= 1024 ? 256 : 1024; }

@@ -343,7 +343,7 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
   if (!few_rows(VFM_BF16, m, a.G)) return;              // block-uniform, as every exit below
   const int qn = m * a.G;
   if (!TABLE && w.qt * 16 >= qn) return;
-  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink, FEW_MIN_TILES8);
+  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink, true);
   if constexpr (TABLE) {
     w.h = id % a.KH; id /= a.KH;
     w.c = id % ck.n;
@@ -617,7 +617,7 @@ __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, 
   const int nb = (m + rb - 1) / rb;
   int bi = id - (R0 / rb + w.p);
   if (few_rows(VFM_BF16, m, a.G) || (!TABLE && bi >= nb)) return;   // block-uniform, as every exit below
-  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink, FEW_MIN_TILES8);
+  const Chunks ck = request_chunks(VFM_BF16, m, ctx, a.G, a.KH, a.window, a.n_sink, true);
   if constexpr (TABLE) {
     w.h = id % a.KH; id /= a.KH;
     w.c = id % ck.n;
@@ -987,11 +987,151 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WAVES, WAVE
 }
 
 // ---------------------------------------------------------------------------
-// fp32 queries, any number of rows: as the fp32 cache's kernel (k_paged.hip), the codes made fp32 in registers.  A lane
-// loads 16 consecutive head dims of its key's K row (its queries' registers hold the same ones), and DH / 16 consecutive
-// ones of V rows, which give as many MFMAs a row each.
+// fp32 queries of one row on a key head, at most 4 of them (single_row).  The 4 x 4 MFMA takes 16 independent products at a time: lane
+// 4 b + i brings key i of the block's 4 (a wave's 64) and query i, and gets its query's scores with the 4 keys.  Those are
+// just what the product with V takes, a key of each block at a time, lane 4 b + i bringing a quarter of the head dims of its
+// V row; so each lane has a softmax of its own until the end, and nothing is exchanged before it.
+// K of the next tile is loaded once the scores have taken this one's, V once the products have.
+// 64 rows after 2000 keys, 16 heads of 64: 61 us, 4.3 TB/s (16 x 16 x 4 products, 15 of 16 of them for nothing: 100); of 128 123
+// and 182; 8 rows after 30000, 32 heads of 128 on 8, 122 and 166.  Bound by its products and conversions; with head dim 64 three
+// blocks share a CU, four of them spill (66).
 // ---------------------------------------------------------------------------
-template <int DH, bool TABLE>
+template <int DH>
+__device__ __forceinline__ void single_row8(const PagedAttn& a, const uint8_t* __restrict__ exps, page_row prow, const uint8_t* kh, const uint8_t* vh,
+                                            const float* q, int h, const Vis& vis, int t0, int t1, int jq, float* sq,
+                                            float (*sm)[16], float (*sl)[16], float (*so)[16][DH]) {
+  constexpr int NV = DH / 4, KL = DH / 16, VL = DH / 64, QS = DH + 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 3, lp = a.kp.log2_page;
+  auto mfma = [](float p, float q, const f32x4& c) { return __builtin_amdgcn_mfma_f32_4x4x1f32(p, q, c, 0, 0, 0); };
+  for (int i = tid; i < DH; i += 256) {                   // queries past the group's: copies of its last
+    const int r = i / (DH / 4), d = i % (DH / 4) * 4;
+    *reinterpret_cast<f32x4*>(sq + r * QS + d) = *reinterpret_cast<const f32x4*>(q + min(r, a.G - 1) * DH + d);
+  }
+  __syncthreads();
+  f32x4 o[NV];
+#pragma unroll
+  for (int c = 0; c < NV; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = LOWEST, l_run = 0.f;
+  // the slot of the lane's key of the 4 runs from run t on; runs past the last re-read it, unseen
+  auto slot_of = [&](int t) {
+    const int k = 16 * vis.run(min(t + (lane >> 4), t1 - 1));
+    return (prow[k >> lp] << lp) + (k & ((1 << lp) - 1)) + (lane & 15);
+  };
+  u32x4 kc[KL], vc[4][VL];
+  uint32_t ex;
+  auto load_k = [&](int slot) {
+    ex = reinterpret_cast<const uint16_t*>(exps)[(int64_t)(slot >> 4) * a.KH + h];
+    const uint8_t* r = kh + (int64_t)slot * DH;
+#pragma unroll
+    for (int c = 0; c < KL; ++c) kc[c] = *reinterpret_cast<const u32x4*>(r + 16 * c);
+  };
+  auto load_v = [&](int slot) {
+    const uint8_t* r = vh + (int64_t)(slot - j) * DH + j * (DH / 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < VL; ++c) vc[i][c] = *reinterpret_cast<const u32x4*>(r + i * DH + 16 * c);
+  };
+  int t = t0 + 4 * wave;
+  if (t < t1) {
+    int slot = slot_of(t);
+    load_k(slot);
+    load_v(slot);
+    slot = slot_of(t + 16);
+    for (; t < t1; t += 16) {
+      f32x4 s2[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      const float kscale = scale_of(ex & 0xFF);
+      float vscale = scale_of(ex >> 8);
+      int at = j * QS;
+      asm volatile("" : "+v"(at));                        // the queries are read anew, not held over the loop
+#pragma unroll
+      for (int c = 0; c < KL; ++c)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const f32x4 kf = decode4(kc[c][w], kscale), qf = *reinterpret_cast<const f32x4*>(sq + at + 16 * c + 4 * w);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s2[w & 1] = mfma(kf[e], qf[e], s2[w & 1]);
+        }
+      if (t + 16 < t1) load_k(slot);
+      f32x4 s = s2[0] + s2[1];
+      // the block's 4 keys
+      const int run = t + (lane >> 4), k0 = 16 * vis.run(min(run, t1 - 1)) + (lane & 12);
+      bool see[4], all = true, any = false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        see[i] = run < t1 && sees(jq, k0 + i, a.window, a.n_sink);
+        all = all && see[i];
+        any = any || see[i];
+      }
+      if (__any(!all)) {
+        if (!any) vscale = 1.f;                           // of a run that may have none
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[i] = see[i] ? s[i] : -INFINITY;
+#pragma unroll
+          for (int c = 0; c < VL; ++c) vc[i][c] = see[i] ? vc[i][c] : u32x4{};
+        }
+      }
+      const float mb = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+      if (__any(mb > m_run)) {
+        const float m_new = fmaxf(m_run, mb), alpha = exp2f((m_run - m_new) * a.scale_log2);
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) o[c] *= alpha;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = exp2f((s[i] - m_run) * a.scale_log2);
+        l_run += e;
+#pragma unroll
+        for (int c = 0; c < NV; c += 4) {
+          const f32x4 v = decode4(vc[i][c / 16][c / 4 % 4], vscale);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) o[c + d] = mfma(v[d], e, o[c + d]);
+        }
+      }
+      if (t + 16 < t1) { load_v(slot); slot = slot_of(t + 32); }
+    }
+  }
+  // the 16 blocks' softmaxes as one; of the outputs, each lane keeps half of what it and its partner hold
+  float M = m_run;
+#pragma unroll
+  for (int x = 4; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
+  const float wt = exp2f((m_run - M) * a.scale_log2);
+  l_run *= wt;
+#pragma unroll
+  for (int x = 4; x < 64; x <<= 1) l_run += __shfl_xor(l_run, x, 64);
+#pragma unroll
+  for (int c = 0; c < NV; ++c) o[c] *= wt;
+  int c0 = 0;
+#pragma unroll
+  for (int x = 32, n = NV / 2; x >= 4; x >>= 1, n >>= 1) {
+    const bool upper = lane & x;
+    c0 += upper ? n : 0;
+#pragma unroll
+    for (int c = 0; c < n; ++c) {
+      f32x4 mine = upper ? o[c + n] : o[c], other = upper ? o[c] : o[c + n];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mine[i] += __shfl_xor(other[i], x, 64);
+      o[c] = mine;
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < NV / 16; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) so[wave][j][NV * i + c0 + c] = o[c][i];
+  if (lane < 4) { sm[wave][j] = M; sl[wave][j] = l_run; }
+}
+
+// ---------------------------------------------------------------------------
+// Other fp32 queries, any number of rows: as the fp32 cache's kernel (k_paged.hip), the codes made fp32 in registers.  A lane
+// loads 16 consecutive head dims of its key's K row (its queries' registers hold the same ones), and DH / 16 consecutive
+// ones of V rows, which give as many MFMAs a row each.  Bound by these: 8 chunks of 512 rows after 1000, 16 heads of 64, 231 us, 91
+// TFLOP/s of visible products (a large matrix product: 154).
+// SINGLE, OTHER: which requests the step has.
+// ---------------------------------------------------------------------------
+template <int DH, bool SINGLE, bool OTHER, bool TABLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attn8_f32_kernel(
     Plan pl, PagedAttn a, const uint8_t* __restrict__ exps) {
   constexpr int NC = DH / 16, KL = DH / 64, NV = DH / 16;
@@ -1016,7 +1156,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
   const int request = uniform(pl.order[w.p]);            // with them, not behind what they decide
   const int qn = m * a.G;
   if (!TABLE && w.qt * 16 >= qn) return;      // block-uniform, as every exit below
-  const Chunks ck = request_chunks(VFM_F32, m, ctx, a.G, a.KH, a.window, a.n_sink);
+  const Chunks ck = request_chunks(VFM_F32, m, ctx, a.G, a.KH, a.window, a.n_sink, true);
   if constexpr (TABLE) {
     w.h = id % a.KH; id /= a.KH;
     w.c = id % ck.n;
@@ -1025,116 +1165,123 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
     return;
   }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int x = lane & 15, g = lane >> 4;
-  const int qi = min(w.qt * 16 + x, qn - 1);
-  const int jq = ctx + qi / a.G;
   const int j0 = ctx + w.qt * 16 / a.G, j1 = ctx + min(w.qt * 16 + 15, qn - 1) / a.G;
   // the tile's own runs, dealt over the request's chunks
   const Vis vis = visible_runs<4>(j0, j1, a.window, a.n_sink);
   const int rpc = (vis.n + ck.n - 1) / ck.n;
   const int t0 = w.c * rpc, t1 = min(t0 + rpc, vis.n);
-  int head;
-  const int64_t row = out_row(a, R0, w.h, qi, head);
   const page_row prow = row_of(a.kp, request);
   const int lp = a.kp.log2_page;
   const uint8_t* kh = (const uint8_t*)a.k + (int64_t)w.h * a.slots * DH;
   const uint8_t* vh = (const uint8_t*)a.v + (int64_t)w.h * a.slots * DH;
-  f32x4 q[NC], o[NV];
+  if (SINGLE && (!OTHER || single_row(m, a.G, vis.n))) {         // block-uniform
+    int head;
+    const int64_t row = out_row(a, R0, w.h, 0, head);
+    __shared__ __attribute__((aligned(16))) float sq[4 * (DH + 4)];
+    single_row8<DH>(a, exps, prow, kh, vh, (const float*)a.q + row * a.ldq + head * DH, w.h, vis, t0, t1, j0, sq, sm, sl, so);
+  } else if constexpr (OTHER) {
+    const int x = lane & 15, g = lane >> 4;
+    const int qi = min(w.qt * 16 + x, qn - 1);
+    const int jq = ctx + qi / a.G;
+    int head;
+    const int64_t row = out_row(a, R0, w.h, qi, head);
+    f32x4 q[NC], o[NV];
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
-    q[c] = *reinterpret_cast<const f32x4*>((const float*)a.q + row * a.ldq + head * DH + 64 * (c >> 2) + 16 * g + 4 * (c & 3));
+    for (int c = 0; c < NC; ++c)
+      q[c] = *reinterpret_cast<const f32x4*>((const float*)a.q + row * a.ldq + head * DH + 64 * (c >> 2) + 16 * g + 4 * (c & 3));
 #pragma unroll
-  for (int c = 0; c < NV; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_run = LOWEST, l_run = 0.f;
-  // a run's codes, loaded while the one before is computed
-  struct Run {
-    int slot;
-    uint32_t ex, vc[4][NV / 4];
-    u32x4 kc[KL];
-  } next;
-  auto load = [&](int t) {
-    const int slot = page_slot(prow, lp, 16 * vis.run(t));
-    next.slot = slot;
-    next.ex = runs_exps(exps, slot, slot, a.KH, w.h);
-    const uint8_t *kr = kh + (int64_t)slot * DH, *vr = vh + (int64_t)slot * DH;
+    for (int c = 0; c < NV; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m_run = LOWEST, l_run = 0.f;
+    // a run's codes, loaded while the one before is computed
+    struct Run {
+      int slot;
+      uint32_t ex, vc[4][NV / 4];
+      u32x4 kc[KL];
+    } next;
+    auto load = [&](int t) {
+      const int slot = page_slot(prow, lp, 16 * vis.run(t));
+      next.slot = slot;
+      next.ex = runs_exps(exps, slot, slot, a.KH, w.h);
+      const uint8_t *kr = kh + (int64_t)slot * DH, *vr = vh + (int64_t)slot * DH;
 #pragma unroll
-    for (int c = 0; c < KL; ++c) next.kc[c] = *reinterpret_cast<const u32x4*>(kr + (x * DH + 64 * c + 16 * g));
+      for (int c = 0; c < KL; ++c) next.kc[c] = *reinterpret_cast<const u32x4*>(kr + (x * DH + 64 * c + 16 * g));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) __builtin_memcpy(next.vc[j], __builtin_assume_aligned(vr + ((4 * g + j) * DH + NV * x), NV), NV);
-  };
-  if (t0 + wave < t1) load(t0 + wave);
-  for (int t = t0 + wave; t < t1; t += 4) {
-    const int p0 = 16 * vis.run(t);
-    const bool full = seen_by_all(j0, j1, p0, p0 + 15, a.window, a.n_sink);
-    const Run now = next;
-    if (t + 4 < t1) load(t + 4);
-    const int64_t slot = now.slot;
-    const u32x4(&kc)[KL] = now.kc;
-    const uint32_t(&vc)[4][NV / 4] = now.vc;
-    const float kscale = k_scale(now.ex, 0), vscale = v_scale(now.ex, 0);
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < 4; ++j) __builtin_memcpy(next.vc[j], __builtin_assume_aligned(vr + ((4 * g + j) * DH + NV * x), NV), NV);
+    };
+    if (t0 + wave < t1) load(t0 + wave);
+    for (int t = t0 + wave; t < t1; t += 4) {
+      const int p0 = 16 * vis.run(t);
+      const bool full = seen_by_all(j0, j1, p0, p0 + 15, a.window, a.n_sink);
+      const Run now = next;
+      if (t + 4 < t1) load(t + 4);
+      const int64_t slot = now.slot;
+      const u32x4(&kc)[KL] = now.kc;
+      const uint32_t(&vc)[4][NV / 4] = now.vc;
+      const float kscale = k_scale(now.ex, 0), vscale = v_scale(now.ex, 0);
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const f32x4 kf = decode4(kc[c >> 2][c & 3], kscale);
+      for (int c = 0; c < NC; ++c) {
+        const f32x4 kf = decode4(kc[c >> 2][c & 3], kscale);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s = mfma(kf[e], q[c][e], s);
-    }
-    f32x4 vf[4][NV / 4];
+        for (int e = 0; e < 4; ++e) s = mfma(kf[e], q[c][e], s);
+      }
+      f32x4 vf[4][NV / 4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int c = 0; c < NV / 4; ++c) vf[j][c] = decode4(vc[j][c], vscale);
-    bool poison = false;
-    if (!full) {
+        for (int c = 0; c < NV / 4; ++c) vf[j][c] = decode4(vc[j][c], vscale);
+      bool poison = false;
+      if (!full) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int k = p0 + 4 * g + j;
+          s[j] = sees(jq, k, a.window, a.n_sink) ? s[j] : -INFINITY;
+          const bool any = seen_by_any(j0, j1, k, a.window, a.n_sink);
+          const bool some = any && !seen_by_all(j0, j1, k, k, a.window, a.n_sink);
+#pragma unroll
+          for (int c = 0; c < NV; ++c) {
+            const bool bad = some && nonfinite(vf[j][c >> 2][c & 3]);
+            poison = poison || bad;
+            vf[j][c >> 2][c & 3] = !any || bad ? 0.f : vf[j][c >> 2][c & 3];
+          }
+        }
+      }
+      float mb = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+      mb = max_x32(max_x16(mb));
+      const float m_new = fmaxf(m_run, mb);
+      const float alpha = exp2f((m_run - m_new) * a.scale_log2);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int c = 0; c < NV; ++c) o[c] *= alpha;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int k = p0 + 4 * g + j;
-        s[j] = sees(jq, k, a.window, a.n_sink) ? s[j] : -INFINITY;
-        const bool any = seen_by_any(j0, j1, k, a.window, a.n_sink);
-        const bool some = any && !seen_by_all(j0, j1, k, k, a.window, a.n_sink);
+        const float e = exp2f((s[j] - m_run) * a.scale_log2);
+        l_run += e;
 #pragma unroll
-        for (int c = 0; c < NV; ++c) {
-          const bool bad = some && nonfinite(vf[j][c >> 2][c & 3]);
-          poison = poison || bad;
-          vf[j][c >> 2][c & 3] = !any || bad ? 0.f : vf[j][c >> 2][c & 3];
+        for (int c = 0; c < NV; ++c) o[c] = mfma(vf[j][c >> 2][c & 3], e, o[c]);
+      }
+      if (__any(poison)) {                                  // rare: see the bf16 kernel
+        for (int r = 0; r < 16; ++r) {
+          const int k = p0 + r;
+          if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
+          const bool see = sees(jq, k, a.window, a.n_sink);
+#pragma unroll
+          for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (see && is_nan8(vh[(slot + r) * DH + NV * (4 * g + i) + c])) o[c][i] = NAN;
         }
       }
     }
-    float mb = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-    mb = max_x32(max_x16(mb));
-    const float m_new = fmaxf(m_run, mb);
-    const float alpha = exp2f((m_run - m_new) * a.scale_log2);
-    m_run = m_new;
-    l_run *= alpha;
+    l_run = sum_x32(sum_x16(l_run));
+    if (lane < 16) { sm[wave][x] = m_run; sl[wave][x] = l_run; }
 #pragma unroll
-    for (int c = 0; c < NV; ++c) o[c] *= alpha;
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float e = exp2f((s[j] - m_run) * a.scale_log2);
-      l_run += e;
-#pragma unroll
-      for (int c = 0; c < NV; ++c) o[c] = mfma(vf[j][c >> 2][c & 3], e, o[c]);
-    }
-    if (__any(poison)) {                                  // rare: see the bf16 kernel
-      for (int r = 0; r < 16; ++r) {
-        const int k = p0 + r;
-        if (!seen_by_any(j0, j1, k, a.window, a.n_sink) || seen_by_all(j0, j1, k, k, a.window, a.n_sink)) continue;
-        const bool see = sees(jq, k, a.window, a.n_sink);
-#pragma unroll
-        for (int c = 0; c < NV; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (see && is_nan8(vh[(slot + r) * DH + NV * (4 * g + i) + c])) o[c][i] = NAN;
-      }
-    }
+      for (int c = 0; c < NV; c += 4)
+        *reinterpret_cast<f32x4*>(&so[wave][x][NV * (4 * g + i) + c]) = f32x4{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
   }
-  l_run = sum_x32(sum_x16(l_run));
-  if (lane < 16) { sm[wave][x] = m_run; sl[wave][x] = l_run; }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int c = 0; c < NV; c += 4)
-      *reinterpret_cast<f32x4*>(&so[wave][x][NV * (4 * g + i) + c]) = f32x4{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
   __syncthreads();
   const int nq = min(16, qn - w.qt * 16);
   for (int e = tid; e < nq * DH / 4; e += 256) {
@@ -1161,9 +1308,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
 }
 
 template <int DH, bool TABLE>
-void launch_blocks8(int dtype, const Plan& pl, const PagedAttn& a, const uint8_t* exps, unsigned nf, unsigned nr, bool deep, hipStream_t s) {
+void launch_blocks8(int dtype, const Plan& pl, const PagedAttn& a, const uint8_t* exps, unsigned nf, unsigned nr, bool deep, bool single, bool other, hipStream_t s) {
   const dim3 block(256), grid(nf + nr);
-  if (dtype != VFM_BF16) hipLaunchKernelGGL((attn8_f32_kernel<DH, TABLE>), grid, block, 0, s, pl, a, exps);
+#define F32(S_, O_) hipLaunchKernelGGL((attn8_f32_kernel<DH, S_, O_, TABLE>), grid, block, 0, s, pl, a, exps)
+  if (dtype != VFM_BF16) { if (!single) F32(false, true); else if (other) F32(true, true); else F32(true, false); }
+#undef F32
 #define BF16(R_, N_, W_) hipLaunchKernelGGL((attn8_bf16_kernel<DH, R_, N_, W_, TABLE>), grid, block, 0, s, pl, a, exps, (int)nr)
   else if (nr && nf) BF16(true, 2, 2);
   else if (nr) BF16(true, 0, 2);
@@ -1199,17 +1348,17 @@ hipError_t launch_append8(int dtype, const Plan& pl, int H, int KH, int head_dim
 }
 
 hipError_t launch_attention8(int dtype, int head_dim, const Plan& pl, const PagedAttn& a, const uint8_t* exps, int64_t few_blocks,
-                             int64_t rows_blocks, int64_t joins, bool deep, bool table, hipStream_t s) {
+                             int64_t rows_blocks, int64_t joins, bool deep, bool single, bool other, bool table, hipStream_t s) {
   if (table) launch_attention_table(dtype, pl, a, s);
   const int pi = prof_begin(VFM_PROF_ATTN, s);
   const unsigned nf = (unsigned)few_blocks, nr = (unsigned)rows_blocks;
   if (head_dim == 64) {
-    if (table) launch_blocks8<64, true>(dtype, pl, a, exps, nf, nr, deep, s);
-    else launch_blocks8<64, false>(dtype, pl, a, exps, nf, nr, deep, s);
+    if (table) launch_blocks8<64, true>(dtype, pl, a, exps, nf, nr, deep, single, other, s);
+    else launch_blocks8<64, false>(dtype, pl, a, exps, nf, nr, deep, single, other, s);
   } else if (table) {
-    launch_blocks8<128, true>(dtype, pl, a, exps, nf, nr, deep, s);
+    launch_blocks8<128, true>(dtype, pl, a, exps, nf, nr, deep, single, other, s);
   } else {
-    launch_blocks8<128, false>(dtype, pl, a, exps, nf, nr, deep, s);
+    launch_blocks8<128, false>(dtype, pl, a, exps, nf, nr, deep, single, other, s);
   }
   prof_end(pi, s);
   if (joins) launch_attention_joins(dtype, head_dim, pl, a, (int)joins, table, s);

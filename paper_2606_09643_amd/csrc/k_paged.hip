@@ -955,7 +955,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Plan pl, PagedAttn a, in
   }
   const int head = id % a.H;
   const int R0 = uniform(pl.cu_seqlens[p]), m = uniform(pl.cu_seqlens[p + 1]) - R0, ctx = uniform(pl.ctx[p]);
-  const int n = request_chunks(DT, m, ctx, a.G, a.KH, a.window, a.n_sink, a.few_min).n;
+  const int n = request_chunks(DT, m, ctx, a.G, a.KH, a.window, a.n_sink, a.kv8).n;
   if (n <= 1) return;
   const int64_t rec = record_of<TABLE>(pl, a, p, R0, n, r, head);
   const float2* ml = a.rec_ml + rec;
@@ -1010,7 +1010,7 @@ __global__ __launch_bounds__(256) void attn_table_kernel(Plan pl, PagedAttn a, i
     AttnCounts c = {};
     if (p < pl.n_req) {
       const int m = pl.cu_seqlens[p + 1] - pl.cu_seqlens[p];
-      c = request_counts(dtype, m, a.H, a.KH, request_chunks(dtype, m, pl.ctx[p], a.G, a.KH, a.window, a.n_sink, a.few_min).n);
+      c = request_counts(dtype, m, a.H, a.KH, request_chunks(dtype, m, pl.ctx[p], a.G, a.KH, a.window, a.n_sink, a.kv8).n);
     }
     int64_t sum[4];
 #pragma unroll

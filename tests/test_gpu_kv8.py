@@ -444,6 +444,25 @@ def test_attention_of_many_requests(dtype, n, long):
         assert np.array_equal(_attend(c, task, H, KH, dh, 0, 0, dtype, q, only=[i], ws_fill=0)[i], got[i])
 
 
+@pytest.mark.parametrize("H,KH,dh,page,window,sinks", [
+    (2, 2, 64, 16, 0, 0), (4, 2, 128, 64, 0, 0), (3, 1, 64, 32, 0, 0), (4, 1, 128, 16, 0, 0), (4, 4, 64, 16, 130, 3),
+    (4, 2, 64, 128, 199, 17), (2, 2, 128, 16, 513, 0), (4, 1, 64, 64, 1000, 70)])
+def test_attention_single_fp32_rows(H, KH, dh, page, window, sinks):
+    """Single rows of up to 4 queries on a key head, few and many keys, alone (where every request is one) and beside chunks."""
+    log(f"single8 H {H} KH {KH} dh {dh} page {page} window {window} sinks {sinks}")
+    ctx = [0, 1, 127, 128, 143, 144, 150, 191, 255, 256, 257, 700, 1023, 1024, 2500, 40, 300]
+    lens = [1] * 15 + [9, 40]
+    c = Cache8(lens, ctx, KH, dh, page, window, sinks, seed=dh + window)
+    q = _queries(lens, H, dh, "f32", 4)
+    task = _tasks(len(lens), 3)
+    got = _attend(c, task, H, KH, dh, window, sinks, "f32", q, ldo=H * dh + 8)
+    log(f"  {_check(c, got, q, window, sinks, 'f32', dh ** -0.5):.3f} of the tolerance")
+    for only in ([4], [5], [14], [9, 11, 13], [12, 16], list(range(15))):
+        alone = _attend(c, task, H, KH, dh, window, sinks, "f32", q, only=only, ws_fill=0)
+        for i in only:
+            assert np.array_equal(alone[i], got[i]), i
+
+
 def test_attention_large_logits_and_scale():
     """Scores of hundreds (one key takes the whole weight) and a given scale."""
     for dtype in ("bf16", "f32"):
