@@ -505,6 +505,40 @@ def test_attention_replayed_graph_and_other_stream(dtype):
         assert torch.equal(out, eager), i
 
 
+def test_calls_on_two_streams_at_once():
+    """Attention over one cache from two streams, each with its outputs and workspace, while an append fills another."""
+    H, KH, dh = 8, 2, 64
+    c = Cache8([1, 1, 150, 2], [9000, 10, 700, 500], KH, dh, 64, 0, 0, seed=6)
+    pb = B.Batch(np.zeros(4, np.int32), c.lens, 1, ctx_len=c.ctx)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    calls = []
+    for dtype in ("bf16", "f32"):
+        code, td, _ = DT[dtype]
+        attn = B.make_attn(code, H, KH, dh, rope_theta=10000.0)
+        q = torch.randn(pb.T, H * dh, generator=gen, device="cuda").to(td)
+        qkv = torch.randn(pb.T, (H + 2 * KH) * dh, generator=gen, device="cuda").to(td)
+        ws = torch.empty(max(1, B.vfm_attention_workspace_q8(attn, pb.c)), dtype=torch.uint8, device="cuda")
+        pool = Pool8(c.ctx, (c.lens + c.ctx).tolist(), KH, dh, 64, 9)
+        first = [t.clone() for t in (pool.kp, pool.vp, pool.ep)]
+        calls.append((attn, q, qkv, ws, pool, first, torch.empty_like(q), torch.empty_like(q)))
+
+    def both(streams):
+        for s, (attn, q, qkv, ws, pool, first, out, q_out) in zip(streams, calls):
+            with torch.cuda.stream(s):
+                for now, was in zip((pool.kp, pool.vp, pool.ep), first):
+                    now.copy_(was)
+                B.vfm_kv_append_q8(attn, pb.c, qkv, q_out, pool.kv)
+                B.vfm_attention_paged_q8(attn, pb.c, q, c.kv, out, ws)
+        torch.cuda.synchronize()
+        return [t.clone() for x in calls for t in (x[4].kp, x[4].vp, x[4].ep, x[6], x[7])]
+
+    torch.cuda.synchronize()
+    want = both([torch.cuda.current_stream()] * 2)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        assert all(torch.equal(x, y) for x, y in zip(both(streams), want))
+
+
 @pytest.mark.parametrize("dtype,H,KH,dh,window,lens,ctx", [
     ("bf16", 8, 1, 128, 0, [1] * 130, [20, 30000] + [40] * 127 + [9000]),
     ("bf16", 32, 8, 64, 0, [700, 1, 2, 40], [0, 20000, 100, 9000]),
