@@ -216,8 +216,9 @@ class AdjustParams:
     subtracted per occurrence in the answer, presence once), `bias`
     {output: value to add}, and `allowed`: a bool array over the outputs, or a
     function of the list of tokens generated so far that gives one (a grammar;
-    the step then waits for the step before it, whose tokens it reads back).
-    Where `allowed` leaves nothing, the token is -1."""
+    the step then waits for the step before it, whose tokens it reads back; an
+    error of the function reaches the caller of step(), which may be called
+    again).  Where `allowed` leaves nothing, the token is -1."""
 
     def __init__(self, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None):
         self.repetition, self.presence, self.frequency = float(repetition), float(presence), float(frequency)
@@ -473,8 +474,9 @@ class ContinuousBatcher:
         self._hist[s.hist:s.hist + len(s.prompt)] = self._h2d(s.prompt)
 
     def _read_answers(self, dec):
-        """The last step's tokens of the sequences whose masks depend on them (waits for that step)."""
-        who = [s for s in dec if s.adjust is not None and callable(s.adjust.allowed)]
+        """The last step's tokens of the sequences whose masks depend on them (waits for that step).  A step that an
+        error ended has read them already: each is taken once."""
+        who = [s for s in dec if s.adjust is not None and callable(s.adjust.allowed) and len(s.answer) < len(s.generated)]
         if who:
             last = self._prev_nxt.cpu().numpy()
             for s in who:
