@@ -218,7 +218,8 @@ class AdjustParams:
     function of the list of tokens generated so far that gives one (a grammar;
     the step then waits for the step before it, whose tokens it reads back; an
     error of the function reaches the caller of step(), which may be called
-    again).  Where `allowed` leaves nothing, the token is -1."""
+    again).  Where `allowed` leaves nothing, the token is -1 and the request
+    ends with it."""
 
     def __init__(self, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None):
         self.repetition, self.presence, self.frequency = float(repetition), float(presence), float(frequency)
@@ -483,10 +484,11 @@ class ContinuousBatcher:
                 s.answer.append(int(last[s.row]))
 
     def _adjust(self, pb, batch, emits, out):
-        """Penalties, biases and masks of the requests that pick a token, in place on their head outputs."""
+        """Penalties, biases and masks of the requests that pick a token, in place on their head outputs.  Answers the
+        sequences whose masks leave nothing: they end with this step's token, -1."""
         who = [(i, s) for i, s in enumerate(batch) if emits[i] and s.adjust is not None]
         if not who:
-            return
+            return []
         n = len(batch)
         t = {}
         pen = [(i, s) for i, s in who if s.adjust.penalizes]
@@ -510,7 +512,7 @@ class ContinuousBatcher:
             t.update(bias=self._h2d(np.concatenate([s.adjust.bias for _, s in who])),
                      bias_id=self._h2d(np.concatenate([s.adjust.bias_id for _, s in who]).astype(np.int32)),
                      bias_begin=self._h2d(begin), bias_len=self._h2d(count))
-        masks = []
+        masks, ended = [], []
         row = np.full(n, -1, np.int32)
         for i, s in who:
             allowed = s.adjust.allowed
@@ -520,6 +522,8 @@ class ContinuousBatcher:
                 allowed = np.asarray(allowed(list(s.answer)), bool)
                 if allowed.shape != (int(self.m.heads.n_out[s.task]),):
                     raise ValueError(f"request {s.rid}: its mask is not one of its head's outputs")
+            if not allowed.any():
+                ended.append(s)
             row[i] = len(masks)
             masks.append(np.packbits(allowed, bitorder="little"))
         if masks:
@@ -528,6 +532,7 @@ class ContinuousBatcher:
                 w[:len(b)] = b
             t.update(mask=self._h2d(words.view(np.int32)), mask_row=self._h2d(row))
         B.vfm_adjust_outputs(pb.c, out, B.OutputAdjust(**t))
+        return ended
 
     def _keep_tokens(self, batch, emits, nxt):
         """The picked tokens of the penalized sequences, behind those that they have."""
@@ -543,7 +548,7 @@ class ContinuousBatcher:
         request's mask depends on its tokens): a decode
         row's input token is gathered on the device from the previous step's
         picks, the host copies go through pinned memory, and a
-        sequence finishes by its token count, so the host plans step n + 1
+        sequence finishes by its token count (or its mask), so the host plans step n + 1
         while the GPU still runs step n.  Token values are read back by
         `tokens()`."""
         new = self._admit(now)
@@ -613,7 +618,7 @@ class ContinuousBatcher:
         nxt = torch.empty(len(batch), dtype=torch.int32, device=self.device)
         emits = [s.cached + int(n) >= len(s.prompt) for s, n in zip(batch, lens)]
         o = out.cpu().numpy() if self.record else None
-        self._adjust(pb, batch, emits, out)
+        ended = self._adjust(pb, batch, emits, out)
         if any(s.sampling is not None for s in batch):
             self._sample(pb, batch, emits, out, nxt)
         else:
@@ -636,7 +641,7 @@ class ContinuousBatcher:
             s.row = i
             if self.record:
                 rec.append((s.rid, o[off[i]:off[i + 1]].copy()))
-            if len(s.generated) == s.max_new:
+            if len(s.generated) == s.max_new or s in ended:
                 self.alloc.release(s.slot)
                 if s.hist >= 0:
                     self._give_history(s.hist, len(s.prompt) + s.max_new)

@@ -115,3 +115,36 @@ def test_a_step_whose_mask_failed_can_be_taken_again(loop, how, error):
     assert gram[0].lists == [plain[0][:j] for j in range(7)]
     # the second request's function answers anew in a step that is taken again, from the same list
     assert all(x == plain[1][:len(x)] for x in gram[1].lists)
+
+
+def test_a_request_whose_mask_leaves_nothing_ends(loop):
+    """Its last token is -1, no function is asked with that token in its list, its pages and slot are free again, and the
+    requests beside it go on as they do without it."""
+    def grammar(n, stop, lists):
+        def allowed(answer):
+            lists.append(list(answer))
+            ok = np.zeros(n, bool)
+            if len(answer) < stop:
+                ok[len(answer) * 3 % n] = True
+            return ok
+        return allowed
+
+    def run(stops):
+        cb, lists = loop(max_seqs=2), [[] for _ in stops]
+        for rid, stop in enumerate(stops):
+            cb.submit(rid, rid % 3, np.arange(20, dtype=np.int32), 30,
+                      adjust=R.AdjustParams(1.5, allowed=grammar(int(N_OUT[rid % 3]), stop, lists[rid])))
+        cb.submit(9, 1, np.arange(5, dtype=np.int32), 6)
+        cb.submit(10, 0, np.arange(5, dtype=np.int32), 6, adjust=R.AdjustParams(allowed=np.zeros(40, bool)))
+        done = cb.run()
+        assert cb.committed == 0 and cb.alloc.count(0)[1] == 30 and len(cb.free_slots) == 2
+        assert cb._hist_free == [(cb._hist.numel(), 0)]
+        return done, lists, cb.steps
+    stops = [4, 0, 100, 29, 30]
+    done, lists, steps = run(stops)
+    for rid, stop in enumerate(stops):
+        want = [j * 3 % int(N_OUT[rid % 3]) for j in range(min(stop, 30))] + [-1] * (stop < 30)
+        assert done[rid] == want, rid
+        assert lists[rid] == [want[:j] for j in range(len(want))]
+    assert done[10] == [-1] and done[9] == [int(_scores(100).argmax())] * 6
+    assert run([100] * 5)[0][9] == done[9]
