@@ -223,13 +223,18 @@ class AdjustParams:
 
     def __init__(self, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None):
         self.repetition, self.presence, self.frequency = float(repetition), float(presence), float(frequency)
-        if not (0 < self.repetition < float("inf") and np.isfinite(self.presence) and np.isfinite(self.frequency)):
-            raise ValueError("repetition is positive, all penalties are finite")
         bias = dict(bias or {})
+        if any(i != int(i) for i in bias):
+            raise ValueError("bias: outputs are whole numbers")
+        values = np.array(list(bias.values()), np.float64)
+        with np.errstate(over="ignore"):                 # as the device takes them
+            r, p, f = np.array([self.repetition, self.presence, self.frequency], np.float32)
+            self.bias = values.astype(np.float32)
+        if not (0 < r < float("inf") and np.isfinite(p) and np.isfinite(f)):
+            raise ValueError("repetition is positive, all penalties are finite, in fp32 too")
         self.bias_id = np.array(list(bias), np.int64)
-        self.bias = np.array(list(bias.values()), np.float32)
-        if len(bias) and (self.bias_id.min() < 0 or np.isnan(self.bias).any()):
-            raise ValueError("bias: outputs from 0 on, values that are numbers")
+        if len(bias) and (self.bias_id.min() < 0 or np.isnan(values).any() or np.any(np.isinf(self.bias) & np.isfinite(values))):
+            raise ValueError("bias: outputs from 0 on, values that are numbers, the finite ones in fp32 too")
         self.allowed = allowed if allowed is None or callable(allowed) else np.array(allowed, bool)
 
     @property

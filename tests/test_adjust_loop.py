@@ -148,3 +148,16 @@ def test_a_request_whose_mask_leaves_nothing_ends(loop):
         assert lists[rid] == [want[:j] for j in range(len(want))]
     assert done[10] == [-1] and done[9] == [int(_scores(100).argmax())] * 6
     assert run([100] * 5)[0][9] == done[9]
+
+
+def test_parameters_that_fp32_does_not_hold_are_refused():
+    """A penalty goes to the device as fp32: one that is infinite or zero there would be another penalty.  Outputs are whole
+    numbers."""
+    for kw in (dict(repetition=1e39), dict(repetition=1e-46), dict(presence=1e39), dict(frequency=-1e39),
+               dict(bias={1: 1e39}), dict(bias={1: 0.0, 2: -4e38}), dict(bias={1.5: 1.0}), dict(bias={"1": 1.0})):
+        with pytest.raises(ValueError):
+            R.AdjustParams(**kw)
+    top = float(np.finfo(np.float32).max)
+    a = R.AdjustParams(top, -top, top, bias={np.int64(3): top, 4: -np.inf, 2.0: np.inf, 5: 1e-50})
+    assert a.penalizes and a.bias_id.tolist() == [3, 4, 2, 5] and a.bias.tolist() == [top, -np.inf, np.inf, 0.0]
+    assert R.AdjustParams(1e-45).repetition == 1e-45 and R.AdjustParams(presence=1e-50).penalizes
