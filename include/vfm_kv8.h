@@ -44,8 +44,9 @@ typedef struct vfm_kv_pages_q8 {
  * 2^(old e - e), rounded the same way (only what becomes subnormal changes).
  * "Rows of the sequence" are the positions before ctx; slots behind the last
  * new row keep what they hold.  q_out gets the rotated queries, rounded once
- * to their type.  New rows of two requests that a page table sends to one run
- * leave either's scale and codes of either there.  Errors as vfm_kv_append. */
+ * to their type (bf16 ones below 2^-126 from a number up to 2^-149 off).  New
+ * rows of two requests that a page table sends to one run leave either's scale
+ * and codes of either there.  Errors as vfm_kv_append. */
 int vfm_kv_append_q8(const vfm_attn* attn, const vfm_batch* batch, const void* qkv, int64_t ld,
                      void* q_out, const vfm_kv_pages_q8* kv, void* stream);
 

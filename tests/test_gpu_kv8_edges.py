@@ -1,0 +1,57 @@
+"""GPU tests of the 8-bit cache's append at the types' ends.
+
+Tolerances.  Append: a code and a rotated query are one rounding of the 64-bit value, below the types' normal numbers too.
+The 64-bit form's angles differ by up to 64 2^-53 of the position, its values by far = that times the pair's size, and its
+own 4 roundings.  Rounding is monotone, so a query lies between the rounded want - far and want + far, which are one number
+unless a tie lies between them.  (An fp32 query at position 80000 is up to 2^18 steps of 2^-149, and far 2e-4 of a
+step: of 1.5 million some are that close to a tie.  A code's steps are 2^14 times as large.)  A bf16 query below 2^-126 is
+cut to 24 bits first (off by less than 2^-150) and rounded to a multiple of 2^-149 (by 2^-150 at most): 2^-149 beside far."""
+import numpy as np
+import pytest
+import torch
+
+from tests import kv8_common as K
+from tests.gpu_common import log
+from tests.helpers import np64
+from tests.test_gpu_decode import DT
+from tests.test_gpu_kv8 import Pool8, _step
+
+pytestmark = pytest.mark.gpu
+
+
+def _once(y, bits):
+    """y rounded once to that many significant bits, ties to even, under fp32's exponents (fewer bits below 2^-126)."""
+    unit = 2.0 ** (np.maximum(np.frexp(y)[1] - 1, -126) - (bits - 1))
+    return np.rint(y / unit) * unit
+
+
+@pytest.mark.parametrize("dtype,H,KH,dh", [("f32", 6, 6, 128), ("f32", 8, 8, 64), ("bf16", 8, 1, 128), ("bf16", 12, 2, 64)])
+@pytest.mark.parametrize("rows", [1, 2000])
+def test_append_below_the_normal_numbers(dtype, H, KH, dh, rows):
+    """Rotated values below 2^-126, where fp32 has fewer bits than the number's own 24: codes are rounded once."""
+    log(f"append8 subnormal {dtype} H {H} KH {KH} dh {dh} rows {rows}")
+    rng = np.random.default_rng(H + dh)
+    td = DT[dtype][1]
+    n = 2000
+    # whole multiples of the type's smallest number, up to 2^-131 (fp32) and 2^-126 (bf16)
+    step, most = (2.0 ** -149, 1 << 18) if dtype == "f32" else (2.0 ** -133, 1 << 7)
+    x = torch.from_numpy(rng.integers(-most, most + 1, (n, H + 2 * KH, dh)) * step).to(td)
+    lens = [n] if rows > 1 else [1] * n
+    ctx = [5] if rows > 1 else [16 * int(c) for c in rng.integers(1, 5000, n)]
+    task = np.zeros(len(lens), np.int32)
+    pool = Pool8(ctx, [a + b + 16 for a, b in zip(lens, ctx)], KH, dh, 16, 3)
+    q = _step(pool, task, lens, ctx, H, KH, dh, dtype, 10000.0, x)
+    at, either, host = 0, 0, np64(x)
+    for i, m in enumerate(lens):
+        want, k, v = K.rotated(host[at:at + m], H, KH, np.arange(ctx[i], ctx[i] + m), 10000.0)
+        pool.append(i, ctx[i], k, v)
+        size = np.abs(host[at:at + m, :H])
+        size = size + np.roll(size, dh // 2, axis=-1)
+        far = (64 * np.arange(ctx[i], ctx[i] + m)[:, None, None] + 4) * 2.0 ** -53 * size + (2.0 ** -149 if dtype == "bf16" else 0.0)
+        lo, hi = (_once(want + d, 24 if dtype == "f32" else 8) for d in (-far, far))
+        differ = (q[at:at + m] < lo) | (q[at:at + m] > hi)
+        assert not differ.any(), (i, int(differ.sum()))
+        either += int((lo != hi).sum())
+        at += m
+    assert either < 1e-3 * n * H * dh
+    pool.check()
