@@ -161,3 +161,23 @@ def test_parameters_that_fp32_does_not_hold_are_refused():
     a = R.AdjustParams(top, -top, top, bias={np.int64(3): top, 4: -np.inf, 2.0: np.inf, 5: 1e-50})
     assert a.penalizes and a.bias_id.tolist() == [3, 4, 2, 5] and a.bias.tolist() == [top, -np.inf, np.inf, 0.0]
     assert R.AdjustParams(1e-45).repetition == 1e-45 and R.AdjustParams(presence=1e-50).penalizes
+
+
+def test_histories_of_finished_sequences_are_given_back(loop):
+    """Prompts on the device stay as they are while their sequences run, beside sequences that come and go."""
+    cb, rng, live = loop(), np.random.default_rng(0), []
+    for rid in range(300):
+        s = R._Seq(rid, 0, rng.integers(0, 9, rng.integers(1, 40)), int(rng.integers(1, 30)), 16)
+        cb._place_history(s)
+        live.append(s)
+        if len(live) > 7:
+            gone = live.pop(int(rng.integers(0, len(live))))
+            cb._give_history(gone.hist, len(gone.prompt) + gone.max_new)
+        spans = sorted((x.hist, x.hist + len(x.prompt) + x.max_new) for x in live)
+        assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])) and spans[-1][1] <= cb._hist.numel()
+        for x in live:
+            assert np.array_equal(cb._hist[x.hist:x.hist + len(x.prompt)].numpy(), x.prompt)
+    assert cb._hist.numel() <= 4 * 8 * 69
+    for s in live:
+        cb._give_history(s.hist, len(s.prompt) + s.max_new)
+    assert cb._hist_free == [(cb._hist.numel(), 0)]

@@ -1,11 +1,14 @@
-"""GPU tests of the 8-bit cache's append at the types' ends.
+"""GPU tests of the 8-bit cache's append and attention at the types' ends.
 
 Tolerances.  Append: a code and a rotated query are one rounding of the 64-bit value, below the types' normal numbers too.
 The 64-bit form's angles differ by up to 64 2^-53 of the position, its values by far = that times the pair's size, and its
 own 4 roundings.  Rounding is monotone, so a query lies between the rounded want - far and want + far, which are one number
 unless a tie lies between them.  (An fp32 query at position 80000 is up to 2^18 steps of 2^-149, and far 2e-4 of a
 step: of 1.5 million some are that close to a tie.  A code's steps are 2^14 times as large.)  A bf16 query below 2^-126 is
-cut to 24 bits first (off by less than 2^-150) and rounded to a multiple of 2^-149 (by 2^-150 at most): 2^-149 beside far."""
+cut to 24 bits first (off by less than 2^-150) and rounded to a multiple of 2^-149 (by 2^-150 at most): 2^-149 beside far.
+Attention where the largest score takes the whole weight: the other weights are below e^-40 each, 2^-57,
+so the output is the value at that key up to n 2^-57 of the largest one, and a rounding of the result (2^-24 in fp32), two with
+the division."""
 import numpy as np
 import pytest
 import torch
@@ -14,7 +17,7 @@ from tests import kv8_common as K
 from tests.gpu_common import log
 from tests.helpers import np64
 from tests.test_gpu_decode import DT
-from tests.test_gpu_kv8 import Pool8, _step
+from tests.test_gpu_kv8 import Cache8, Pool8, _attend, _queries, _step
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +58,29 @@ def test_append_below_the_normal_numbers(dtype, H, KH, dh, rows):
         at += m
     assert either < 1e-3 * n * H * dh
     pool.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shift", [12, 18, 40])
+def test_attention_of_the_largest_score_alone(dtype, shift):
+    """Scores so far apart that the largest takes the whole weight, of few rows and many: the output is that key's value."""
+    log(f"attend8 {dtype} shift {shift}")
+    H, KH, dh = 2, 1, 64
+    lens, ctx = [1, 40], [200, 100]
+    c = Cache8(lens, ctx, KH, dh, 32, 0, 0, seed=2)
+    q = _queries(lens, H, dh, dtype, 1)
+    c.exps[..., 0] += ((c.exps[..., 0] != 255) * shift).to(torch.uint8)
+    got = _attend(c, np.zeros(2, np.int32), H, KH, dh, 0, 0, dtype, q)
+    u, checked = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23), [0, 0]
+    for i in range(2):
+        k, v = c.k[i][:, 0] * 2.0 ** shift, c.v[i][:, 0]
+        for r in range(lens[i]):
+            for h in range(H):
+                s = k[:ctx[i] + r + 1] @ q[i][r, h] * dh ** -0.5
+                top = np.argsort(s)
+                size = np.abs(k).max() * np.abs(q[i][r, h]).max() * dh ** 0.5
+                if s[top[-1]] - s[top[-2]] > 40 + (dh + 2) * 2.0 ** -23 * size:
+                    want = v[top[-1]]
+                    assert np.all(np.abs(got[i][r, h] - want) <= u * np.abs(want) + 2.0 ** -40 * np.abs(v).max()), (i, r, h)
+                    checked[i] += 1
+    assert checked[0] > 0 and checked[1] > 20, checked
