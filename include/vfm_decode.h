@@ -140,9 +140,10 @@ typedef struct vfm_adjust {
 } vfm_adjust;
 
 /* adjusted: device float32, as out (vfm_head_forward's layout) and apart from it, or out itself:
- * then of each aligned 16 bytes of which an output changes or is masked, the
- * request's outputs are read and written back, and no others are written.  For
- * output j = l of request i, in 64 bits with one rounding at the end:
+ * then of each aligned 16 bytes of which an output changes or is masked (under a
+ * mask, of those at the row's ends too) the request's outputs are read and
+ * written back, and no others are written.  For output j = l of request i, in
+ * 64 bits with one rounding at the end:
  *   l > 0 ? l / r : l * r   if j is among the earlier tokens;
  *   l - (f * n + p)         if n > 0 of the generated ones are j;
  *   l + bias                if j has one;

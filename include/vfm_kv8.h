@@ -54,7 +54,9 @@ int vfm_kv_append_q8(const vfm_attn* attn, const vfm_batch* batch, const void* q
  * outputs.  With VFM_BF16 the products are of bf16 numbers (which hold every
  * code times its scale exactly), with VFM_F32 of fp32 ones.  A NaN code counts
  * as a NaN; what unseen slots hold, and scales of runs that no row sees, does
- * not reach any output.  Errors as vfm_attention_paged, workspace as
+ * not reach any output.  The sums of weights times values are fp32 before they
+ * are divided: a row's largest |value| times its visible keys times 2^8 stays
+ * below 2^128.  Errors as vfm_attention_paged, workspace as
  * vfm_attention_workspace_q8 says. */
 int vfm_attention_workspace_q8(const vfm_attn* attn, const vfm_batch* batch, size_t* bytes);
 int vfm_attention_paged_q8(const vfm_attn* attn, const vfm_batch* batch, const void* q, int64_t ldq,

@@ -40,22 +40,23 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) 
 // launch's first blocks each request's first run, the others the further runs that begin in 16 rows of the batch.  A wave
 // takes a head of the whole run, so the run's largest magnitude is found by lane exchanges and the codes are written from
 // the registers that hold the rotated values.  A single row (decode) leaves most of such a wave idle: there it takes
-// 64 / (DH / 16) heads at once; with head dim 128 up to 8 rows are half a run's work (200 requests of 2 to 4 rows: 27 us,
+// 64 / (DH / 16) heads at once; with head dim 128 up to 8 rows are half a run's work (200 requests of 2 to 4 rows: 28 us,
 // 38 as whole runs).
 //
 // Rotation in fp64, of operands that fp64 holds exactly: a code is one rounding of the rotated value, and scale and code
 // do not depend on how the angle's last bits came out.  The value goes through fp32 rounded to odd (cut, the last
 // bit set if anything was lost), after which rounding to 4 or 8 bits is as if from the fp64 value, and a comparison with a
 // number of few bits comes out the same.  Below 2^-126 fp32 has fewer bits and rounds that to the nearest: bf16 queries
-// stay so (off by up to 2^-149 before their own rounding: 2^-150 cut, 2^-150 rounded); a code feels it where the run's scale is among the smallest 11, and
-// such a head is taken again with the last bit put where fp32 has it, behind the others and out of their way (40
-// requests of 40 to 60 rows 22.1 us, 21.7 without, 22.6 with the queries' smallest magnitude looked at too).
+// stay so (off by up to 2^-149 before their own rounding: 2^-150 cut, 2^-150 rounded); a code feels it where the run's
+// scale is among the smallest 11, and such a head is taken again with the last bit put where fp32 has it, behind the
+// others and out of their way (40 requests of 40 to 60 rows: 22.1 us, 21.7 without, 22.6 with the queries' smallest
+// magnitude looked at too).
 //
-// Bound by its bytes: 32 prompts of 128 to 1024 tokens, 32 heads of 128 on 32, take 161 us, 4.8 TB/s (a copy of 2 GiB runs
+// Bound by its bytes: 32 prompts of 128 to 1024 tokens, 32 heads of 128 on 32, take 162 us, 4.8 TB/s (a copy of 2 GiB runs
 // at 4.95).  The blocks that share a run's heads are neighbours in the launch, so its rows are read at once: 191 us with
 // them far apart.  4 heads a wave; 6 take 164, 12 190 (a long last round), and loading a head ahead 205 for 191 (3
 // waves on a SIMD in place of 4).  One row: 4.4 us, all latency.  A block per row, most of which find no run, took 42 us for 40
-// requests of 40 to 60 rows, 20 now, and a block for all runs of 16 rows 100 for 3000 single rows, 31 now.
+// requests of 40 to 60 rows, 22 now, and a block for all runs of 16 rows 100 for 3000 single rows, 31 now.
 // ---------------------------------------------------------------------------
 constexpr float TOP8 = 3.19014718988379809e38f;          // 1.875 2^127: larger magnitudes would round to 2^128
 
@@ -295,11 +296,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
 // the MFMA, V on the way to a wave-private LDS tile that the transposing LDS read turns into the V^T operand.
 // A lane's 16-byte load of a K row holds 16 consecutive head dims, two MFMA steps of 8; the queries' fragments take the
 // same dims, as a dot product does not mind their order.
+// Weights are rounded to bf16 for the product with V, which the matrix cores take at 16 times fp32's rate: by up to 2^-8 of
+// each, as the output is by its own rounding; their sum and maximum are fp32.  Against 64 bits the output is off by 1.0
+// to 1.1 times what the fp32 form rounded once is.
 // Memory bound: 256 requests with up to 1028 visible keys, 32 heads of 128 on 32: 305 us, 6.2 TB/s (at most 6.5 here); 8
 // requests of 32768 to 131072, 32 heads on 8: 205 us, 6.2 TB/s.  One row after 300 keys: 8 us, the latency of a few
 // dependent loads.
 // NB tiles' registers: with few blocks, or long ones, the loads of two tiles are in flight while one is computed (head dim
-// 128: 212 registers, two blocks on a CU; 64: one tile ahead and three).  Otherwise one tile at a time, and four blocks on a CU
+// 128: 204 registers, two blocks on a CU; 64: one tile ahead and three).  Otherwise one tile at a time, and four blocks on a CU
 // (64: five) hide each other's loads and starts.  With head dim 128, one tile and three: 256 rows of 30 to 60 keys 39 us and
 // 64, of 256 to 2048 440 and 519, 8 of 32768 to 131072 216 and 205, one of 30000 21.2 and 19.4; with head dim 64, one and
 // two: 256 of 30 to 60 15.4 and 16.9, 256 of 200 to 2000 110 and 114, 16 of 130 to 400 8.3 and 7.6.
@@ -607,6 +611,9 @@ __device__ __forceinline__ void few_block8(const Plan& pl, const PagedAttn& a, c
 // cycles, the vector ALU for 47, LDS for 36.  Blocks of 8 waves, which halve the conversions per query, give 1%; V's
 // conversion beside the products in place of the scores loses 2.  The matrix cores' own 8-bit products (a query as the
 // sum of two codes) would need no conversion of K, but their sums hold 16 bits (1.6e-5 of random rows' products of 64).
+// Weights are rounded to bf16 as above, and summed so: 1.28 times the error of the fp32 form rounded once.  With head dim 64 the
+// softmax weighs more: 8 prompts of 4096, window 1024, 16 heads on 4, 209 to 222 us, the vector ALU busy for 51% of the
+// cycles, the matrix cores for 28, 29% of the waves' time waiting.
 // ---------------------------------------------------------------------------
 template <int DH, bool TABLE>
 __device__ __forceinline__ void rows_block8(const Plan& pl, const PagedAttn& a, const uint8_t* __restrict__ exps, int id, bf16* stage0, bf16* stage1) {
@@ -1153,9 +1160,11 @@ __device__ __forceinline__ void single_row8(const PagedAttn& a, const uint8_t* _
 // ---------------------------------------------------------------------------
 // Other fp32 queries, any number of rows: as the fp32 cache's kernel (k_paged.hip), the codes made fp32 in registers.  A lane
 // loads 16 consecutive head dims of its key's K row (its queries' registers hold the same ones), and DH / 16 consecutive
-// ones of V rows, which give as many MFMAs a row each.  Bound by these: 8 chunks of 512 rows after 1000, 16 heads of 64, 231 us, 91
-// TFLOP/s of visible products (a large matrix product: 154).
-// SINGLE, OTHER: which requests the step has.
+// ones of V rows, which give as many MFMAs a row each.  8 chunks of 512 rows after 1000, 16 heads of 64, take 231 to 237 us,
+// 91 TFLOP/s of visible products (a large matrix product: 154): the matrix cores are busy for 60% of the cycles and the
+// vector ALU for 37, by turns (each wave converts its own K and V); of 128 439 us, 64 and 31.
+// SINGLE, OTHER: which requests the step has.  With both, all blocks have the single rows' registers (head dim 64: 134 for 85, 128:
+// 232 for 141): one single row beside those chunks makes 237 us 240 and 439 464.
 // ---------------------------------------------------------------------------
 template <int DH, bool SINGLE, bool OTHER, bool TABLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attn8_f32_kernel(
