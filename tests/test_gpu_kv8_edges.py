@@ -1,4 +1,4 @@
-"""GPU tests of the 8-bit cache's append and attention at the types' ends.
+"""GPU tests of the 8-bit cache's append and attention at the types' ends, and of the loop where masks fail or end.
 
 Tolerances.  Append: a code and a rotated query are one rounding of the 64-bit value, below the types' normal numbers too.
 The 64-bit form's angles differ by up to 64 2^-53 of the position, its values by far = that times the pair's size, and its
@@ -13,11 +13,13 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2606_09643_amd import runner as R
 from tests import kv8_common as K
 from tests.gpu_common import log
 from tests.helpers import np64
 from tests.test_gpu_decode import DT
 from tests.test_gpu_kv8 import Cache8, Pool8, _attend, _queries, _step
+from tests.test_gpu_windowed import REQUESTS, SAMPLING, _decoder, _model
 
 pytestmark = pytest.mark.gpu
 
@@ -84,3 +86,46 @@ def test_attention_of_the_largest_score_alone(dtype, shift):
                     assert np.all(np.abs(got[i][r, h] - want) <= u * np.abs(want) + 2.0 ** -40 * np.abs(v).max()), (i, r, h)
                     checked[i] += 1
     assert checked[0] > 0 and checked[1] > 20, checked
+
+
+@pytest.mark.parametrize("dtype,window", [("bf16", 40), ("f32", None)])
+def test_loop_goes_on_after_a_failed_mask_and_ends_at_an_empty_one(dtype, window):
+    """Steps that a mask function's error ended behind their layers are taken again: rows that were appended twice, penalties,
+    drawn and greedy tokens are those without the failure.  A mask that leaves nothing ends its request alone."""
+    w = _decoder(dtype, 64)
+    model, emb, prompts = _model(w)
+    n = int(model.heads.n_out[0])
+
+    def grammar(bad, last):
+        calls = []
+
+        def allowed(answer):
+            calls.append(len(answer))
+            if len(calls) in bad:
+                raise RuntimeError("the grammar's own")
+            ok = np.ones(n, bool) if len(answer) < last else np.zeros(n, bool)
+            ok[answer] = False
+            return ok
+        return allowed
+
+    def run(bad):
+        log(f"loop {dtype} window {window}, failing calls {bad}")
+        cb = R.ContinuousBatcher(model, emb, page_size=16, n_pages=24, max_seqs=3, max_step_tokens=48, max_pages=9,
+                                 kv8=True, window=window)
+        adjust = [R.AdjustParams(1.3, 0.2, 0.1, allowed=grammar(bad, 99)), R.AdjustParams(1.2, bias={5: 1.0}), None,
+                  R.AdjustParams(allowed=grammar((), 2)), R.AdjustParams(frequency=0.3, allowed=grammar(bad, 7))]
+        for rid, ((task, _, n_new), pr) in enumerate(zip(REQUESTS, prompts)):
+            cb.submit(rid, task, pr, n_new, sampling=SAMPLING[rid], adjust=adjust[rid])
+        failed = 0
+        while cb.waiting or cb.running:
+            try:
+                cb.step()
+            except RuntimeError:
+                failed += 1
+        assert cb.committed == 0 and cb.alloc.count(0)[1] == 24
+        return cb.tokens(), failed
+    plain, failed = run(())
+    assert failed == 0 and [len(plain[r]) for r in range(5)] == [40, 30, 70, 3, 8]
+    assert plain[3][2] == plain[4][7] == -1 and min(plain[0] + plain[3][:2] + plain[4][:7]) >= 0
+    assert len(set(plain[0])) == 40
+    assert run((1, 2, 5, 6)) == (plain, 8)
